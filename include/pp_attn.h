@@ -19,6 +19,8 @@
  *   pp_rope, pp_attn_fwd_rope, pp_attn_bwd_rope
  *                   rotary position embedding on the packed position IDs
  *                   (Sec. 3.2), alone or fused into attention
+ *   pp_cross_attn_fwd, pp_cross_attn_bwd
+ *                   attention of packed rows to an encoder's states
  *   pp_plan_create, pp_attn_fwd_planned, pp_attn_bwd_planned
  *                   the same attention on a plan built once per packed batch
  *                   and reused (e.g. by every layer of a model)
@@ -393,6 +395,47 @@ pp_status pp_dpo_loss(int32_t num_rows, int32_t max_resp, const int32_t* num_res
                       const float* logp_pol, const float* logp_ref, float beta, float* loss,
                       float* row_loss, float* dlogp_pol, void* ws, size_t ws_bytes,
                       void* hip_stream);
+
+/* Cross attention: every real token of a packed row looks at encoder states of
+ * the row (an image's, an audio clip's, a source text's), whose number is the
+ * row's own.
+ *
+ * The states of all rows lie on one axis of sumE = enc_start[B] entries: row b's
+ * are [enc_start[b], enc_start[b] + enc_len[b]), what follows up to
+ * enc_start[b+1] is padding, which is never read.  A row may have none. */
+typedef struct pp_enc_desc {
+  const int32_t* enc_start;  /* host [B+1], enc_start[0] = 0, non-decreasing */
+  const int32_t* enc_len;    /* host [B], 0 <= enc_len[b] <= enc_start[b+1] - enc_start[b] */
+} pp_enc_desc;
+
+/* Token t of row b sees the states [0, enc_len[b]) of its row, or with key_begin
+ * and key_end (dev int32 [sumT], both or neither; any values, clipped to that
+ * range) those in [key_begin[t], key_end[t]): the image ahead of it in a text of
+ * several, say.  With P the softmax of scale q k over them, o = P v and lse is
+ * the natural log of the softmax denominator; a token that sees nothing gets
+ * o = 0, lse = 0 and dq = 0, and so does padding.  Prompt and responses are
+ * alike here, and a row may be a single token (sampling).  q-head h reads
+ * kv-head h / (hq / hkv); scale <= 0 means 1/sqrt(head_dim).
+ *   q, o, dout, dq [sumT, hq, head_dim], k, v, dk, dv [sumE, hkv, head_dim],
+ *   lse float [hq, sumT]; head_dim 64 or 128, hq at most 4096.
+ * PP_BF16: the probabilities (and dS) are rounded to bf16 for the second product,
+ * sums are fp32.  PP_FP32: nothing is rounded below fp32 (unlike pp_attn_fwd).
+ * The backward takes the forward's o and lse, and writes all of dq, dk and dv
+ * (0 in the states' padding).  Results do not depend on scheduling (no atomics).
+ * Scores and values of every state of [0, enc_len[b]) enter tile-wise products:
+ * a state that is not finite may reach tokens whose range leaves it out.
+ * ws_bytes >= pp_cross_workspace_size's fwd or bwd (either output may be NULL);
+ * a batch of a few short rows needs none in the forward.
+ * Errors as pp_attn_fwd; PP_ERR_BAD_LAYOUT also for a broken enc. */
+pp_status pp_cross_workspace_size(const pp_pack_desc* desc, const pp_enc_desc* enc, pp_dtype dtype, int hq, int hkv,
+                                  int head_dim, size_t* fwd, size_t* bwd);
+pp_status pp_cross_attn_fwd(const pp_pack_desc* desc, const pp_enc_desc* enc, pp_dtype dtype, int hq, int hkv, int head_dim,
+                            float scale, const void* q, const void* k, const void* v, const int32_t* key_begin,
+                            const int32_t* key_end, void* o, float* lse, void* ws, size_t ws_bytes, void* hip_stream);
+pp_status pp_cross_attn_bwd(const pp_pack_desc* desc, const pp_enc_desc* enc, pp_dtype dtype, int hq, int hkv, int head_dim,
+                            float scale, const void* q, const void* k, const void* v, const int32_t* key_begin,
+                            const int32_t* key_end, const void* o, const float* lse, const void* dout, void* dq, void* dk,
+                            void* dv, void* ws, size_t ws_bytes, void* hip_stream);
 
 /* Host-only export of the planner's integer view of a batch (no GPU needed):
  *   position_ids[sumT]  prompt token t -> t, response token j -> P_b + j,

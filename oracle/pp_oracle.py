@@ -595,3 +595,60 @@ def useful_pairs(prompt_len, num_resp, resp_len) -> int:
             o += L
         total += int(row_mask(o, P, offs, lens).sum())
     return total
+
+
+# ---------------------------------------------------------------------------
+# Cross attention of packed rows to an encoder's states
+# ---------------------------------------------------------------------------
+
+
+def cross_visible(row_start, prompt_len, num_resp, resp_off, resp_len, enc_len, key_begin=None, key_end=None):
+    """Per row a boolean [T_b, E_b]: which of the row's states each of its tokens sees (padding sees nothing)."""
+    out = []
+    for b in range(len(prompt_len)):
+        t0, t1, E = int(row_start[b]), int(row_start[b + 1]), int(enc_len[b])
+        n = int(prompt_len[b]) + sum(int(resp_len[b][k]) for k in range(int(num_resp[b])))
+        vis = np.zeros((t1 - t0, E), bool)
+        for i in range(n):
+            lo = 0 if key_begin is None else max(0, int(key_begin[t0 + i]))
+            hi = E if key_end is None else min(E, int(key_end[t0 + i]))
+            if hi > lo:
+                vis[i, lo:hi] = True
+        out.append(vis)
+    return out
+
+
+def cross_attn(row_start, prompt_len, num_resp, resp_off, resp_len, enc_start, enc_len, q, k, v, dout=None, key_begin=None,
+               key_end=None, scale=None):
+    """(o, lse) of cross attention, or with dout (o, lse, dq, dk, dv); q [T, hq, d], k, v [E, hkv, d]."""
+    T, hq, d = q.shape
+    G = hq // k.shape[1]
+    tau = 1.0 / np.sqrt(d) if scale is None else scale
+    vis = cross_visible(row_start, prompt_len, num_resp, resp_off, resp_len, enc_len, key_begin, key_end)
+    o, lse = np.zeros((T, hq, d)), np.zeros((hq, T))
+    dq, dk, dv = np.zeros((T, hq, d)), np.zeros(k.shape), np.zeros(v.shape)
+    for b, see in enumerate(vis):
+        t0, e0, E = int(row_start[b]), int(enc_start[b]), int(enc_len[b])
+        some = see.any(axis=1)
+        rows = t0 + np.nonzero(some)[0]
+        see = see[some]
+        if len(rows) == 0:
+            continue
+        for h in range(hq):
+            g = h // G
+            kh, vh = k[e0:e0 + E, g], v[e0:e0 + E, g]
+            s = np.where(see, tau * (q[rows, h] @ kh.T), -np.inf)
+            m = s.max(axis=1, keepdims=True)
+            w = np.exp(s - m)
+            z = w.sum(axis=1, keepdims=True)
+            P = w / z
+            lse[h, rows] = (m + np.log(z))[:, 0]
+            o[rows, h] = P @ vh
+            if dout is not None:
+                g_o = dout[rows, h]
+                dP = g_o @ vh.T
+                dS = P * (dP - (P * dP).sum(axis=1, keepdims=True))
+                dq[rows, h] = tau * dS @ kh
+                dk[e0:e0 + E, g] += tau * dS.T @ q[rows, h]
+                dv[e0:e0 + E, g] += P.T @ g_o
+    return (o, lse) if dout is None else (o, lse, dq, dk, dv)

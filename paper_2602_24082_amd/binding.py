@@ -15,7 +15,7 @@ from typing import Optional
 import numpy as np
 import torch
 
-from .workload import Pack
+from .workload import Enc, Pack
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
 # PP_LIB_PATH selects another build of the library (e.g. a host-sanitized one)
@@ -36,6 +36,7 @@ EXPORTED = [
     "pp_plan_workspace_size", "pp_plan_create", "pp_plan_destroy", "pp_attn_fwd_planned", "pp_attn_bwd_planned",
     "pp_attn_fwd_noalloc", "pp_build_id", "pp_logprob_row_count", "pp_seq_logprob_bwd_rows",
     "pp_bwd_stored_ds_workspace_size",
+    "pp_cross_workspace_size", "pp_cross_attn_fwd", "pp_cross_attn_bwd",
 ]
 
 NOALLOC_SCRATCH_BYTES = 4 << 20  # PP_NOALLOC_SCRATCH_BYTES
@@ -66,6 +67,10 @@ class _Desc(ctypes.Structure):
         ("resp_off", ctypes.POINTER(ctypes.c_int32)),
         ("resp_len", ctypes.POINTER(ctypes.c_int32)),
     ]
+
+
+class _EncDesc(ctypes.Structure):
+    _fields_ = [("enc_start", ctypes.POINTER(ctypes.c_int32)), ("enc_len", ctypes.POINTER(ctypes.c_int32))]
 
 
 _lib = None
@@ -116,6 +121,10 @@ def lib() -> ctypes.CDLL:
     L.pp_rm_scores.argtypes = [D, i, i, P, P, ctypes.c_float, P, P, sz, P]
     L.pp_rm_scores_bwd.argtypes = [D, i, i, P, P, P, P, P, P, P, sz, P]
     L.pp_dpo_loss.argtypes = [i32, i32, P, P, P, ctypes.c_float, P, P, P, P, sz, P]
+    E = ctypes.POINTER(_EncDesc)
+    L.pp_cross_workspace_size.argtypes = [D, E, i, i, i, i, ctypes.POINTER(sz), ctypes.POINTER(sz)]
+    L.pp_cross_attn_fwd.argtypes = [D, E, i, i, i, i, f32, P, P, P, P, P, P, P, P, sz, P]
+    L.pp_cross_attn_bwd.argtypes = [D, E, i, i, i, i, f32, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]
     L.pp_pack_export.argtypes = [D, i, i, P, P, P, sz]
     L.pp_tile_class_len.argtypes = [D, i, i, ctypes.POINTER(sz)]
     L.pp_timing_enable.argtypes = [i]
@@ -573,6 +582,110 @@ def pp_pack_export(pack: Pack, block_q: int = 128, block_k: int = 64, tiles: boo
                                 ctypes.c_void_p(seg.ctypes.data),
                                 ctypes.c_void_p(tc.ctypes.data) if tiles else None, n.value))
     return pos, seg, tc
+
+
+# ---------------------------------------------------------------- cross attention
+
+
+class _EncHolder:
+    """Keeps the int32 arrays of an Enc alive while the C struct points at them."""
+
+    def __init__(self, enc: Enc):
+        c = lambda a: np.ascontiguousarray(a, dtype=np.int32)
+        self.arrays = [c(enc.enc_start), c(enc.enc_len)]
+        ptr = lambda a: a.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
+        self.desc = _EncDesc(*[ptr(a) for a in self.arrays])
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.desc)
+
+
+def _check_tensor(name: str, t: torch.Tensor, shape, dtype, device):
+    if not isinstance(t, torch.Tensor) or tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be a tensor of shape {tuple(shape)}, got "
+                         f"{tuple(t.shape) if isinstance(t, torch.Tensor) else type(t).__name__}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, expected {device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t
+
+
+def _on_gpu(t: torch.Tensor):
+    if t.device.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, got {t.device}")
+
+
+def _cross_args(pack: Pack, enc: Enc, q, k, v, key_begin, key_end):
+    """Checks the inputs of cross attention; (pack holder, enc holder, hq, hkv, d, dtype code)."""
+    if len(enc.enc_len) != pack.num_rows or len(enc.enc_start) != pack.num_rows + 1:
+        raise ValueError(f"enc describes {len(enc.enc_len)} rows, pack {pack.num_rows}")
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k must be [tokens, heads, head_dim]")
+    T, E = max(0, pack.total_tokens), max(0, enc.total_states)
+    hq, d, hkv = q.shape[1], q.shape[2], k.shape[1]
+    _check_tensor("q", q, (T, hq, d), q.dtype, q.device)
+    _check_tensor("k", k, (E, hkv, d), q.dtype, q.device)
+    _check_tensor("v", v, (E, hkv, d), q.dtype, q.device)
+    for name, t in (("key_begin", key_begin), ("key_end", key_end)):
+        if t is not None:
+            _check_tensor(name, t, (T,), torch.int32, q.device)
+    _on_gpu(q)
+    return _desc_of(pack), _EncHolder(enc), hq, hkv, d, _dtype_code(q)
+
+
+def pp_cross_workspace_size(pack: Pack, enc: Enc, hq: int, hkv: int, head_dim: int, dtype: int = PP_BF16):
+    """(fwd, bwd) workspace bytes of cross attention."""
+    f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(lib().pp_cross_workspace_size(_desc_of(pack).ref, _EncHolder(enc).ref, dtype, hq, hkv, head_dim,
+                                         ctypes.byref(f), ctypes.byref(b)))
+    return int(f.value), int(b.value)
+
+
+def pp_cross_attn_fwd(pack: Pack, enc: Enc, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float = 0.0,
+                      key_begin: Optional[torch.Tensor] = None, key_end: Optional[torch.Tensor] = None, out=None, lse=None,
+                      ws=None):
+    """Attention of the packed tokens to their rows' encoder states (those of
+    [key_begin, key_end) if given); returns (o [sumT,hq,d], lse [hq,sumT] fp32)."""
+    h, e, hq, hkv, d, dt = _cross_args(pack, enc, q, k, v, key_begin, key_end)
+    T, dev = q.shape[0], q.device
+    out = torch.empty_like(q) if out is None else _check_tensor("out", out, q.shape, q.dtype, dev)
+    lse = (torch.empty(hq, T, dtype=torch.float32, device=dev) if lse is None
+           else _check_tensor("lse", lse, (hq, T), torch.float32, dev))
+    if ws is None:
+        n = ctypes.c_size_t(0)
+        _check(lib().pp_cross_workspace_size(h.ref, e.ref, dt, hq, hkv, d, ctypes.byref(n), None))
+        ws = _workspace(n.value, dev)
+    with torch.cuda.device(dev):
+        _check(lib().pp_cross_attn_fwd(h.ref, e.ref, dt, hq, hkv, d, float(scale), _ptr(q), _ptr(k), _ptr(v),
+                                       _ptr(key_begin), _ptr(key_end), _ptr(out), _ptr(lse), _ptr(ws), ws.numel(),
+                                       _stream(dev)))
+    return out, lse
+
+
+def pp_cross_attn_bwd(pack: Pack, enc: Enc, q, k, v, o, lse, dout, scale: float = 0.0, key_begin=None, key_end=None,
+                      dq=None, dk=None, dv=None, ws=None):
+    """Backward of pp_cross_attn_fwd; returns (dq, dk, dv) in the input dtype."""
+    h, e, hq, hkv, d, dt = _cross_args(pack, enc, q, k, v, key_begin, key_end)
+    T, dev = q.shape[0], q.device
+    _check_tensor("o", o, q.shape, q.dtype, dev)
+    _check_tensor("dout", dout, q.shape, q.dtype, dev)
+    _check_tensor("lse", lse, (hq, T), torch.float32, dev)
+    dq = torch.empty_like(q) if dq is None else _check_tensor("dq", dq, q.shape, q.dtype, dev)
+    dk = torch.empty_like(k) if dk is None else _check_tensor("dk", dk, k.shape, q.dtype, dev)
+    dv = torch.empty_like(v) if dv is None else _check_tensor("dv", dv, v.shape, q.dtype, dev)
+    if ws is None:
+        n = ctypes.c_size_t(0)
+        _check(lib().pp_cross_workspace_size(h.ref, e.ref, dt, hq, hkv, d, None, ctypes.byref(n)))
+        ws = _workspace(n.value, dev)
+    with torch.cuda.device(dev):
+        _check(lib().pp_cross_attn_bwd(h.ref, e.ref, dt, hq, hkv, d, float(scale), _ptr(q), _ptr(k), _ptr(v),
+                                       _ptr(key_begin), _ptr(key_end), _ptr(o), _ptr(lse), _ptr(dout), _ptr(dq), _ptr(dk),
+                                       _ptr(dv), _ptr(ws), ws.numel(), _stream(dev)))
+    return dq, dk, dv
 
 
 # ---------------------------------------------------------------- timing

@@ -1,0 +1,1083 @@
+// Cross attention of packed rows to an encoder's states, forward and backward, on gfx950.
+//
+// Every real token of packed row b -- prompt and responses alike -- looks at the row's
+// encoder states: keys and values [0, E_b), or the part [begin_t, end_t) of them.  There
+// is no order among the two axes, so the tokens of a row and the G query heads of one
+// kv-head are one list of T_b G rows, row r = token r / G, head r % G:
+//
+//   S = Q K^T scale (visible keys),  P = softmax(S),  O = P V
+//   dV = P^T dO,  dS = P (dO V^T - delta),  delta = dO . O
+//   dQ = scale dS K,  dK = scale dS^T Q
+//
+// which is one matrix of rows against keys per (packed row, kv-head): one token of an
+// 8-fold group fills 8 rows of a tile that reads its keys once, and the shared heads'
+// dK and dV sum up in the accumulators.  Kernels:
+//
+//   cross_fwd      one workgroup = 128 rows (four waves of 32), walking tiles of keys
+//   cross_few      one workgroup = 32 rows, its waves walking different keys
+//   cross_combine  joins forwards whose keys were split over workgroups
+//   cross_dq       delta and -lse log2(e), then dQ, shaped as cross_fwd
+//   cross_dq_sum   adds dQ of split keys
+//   cross_dkdv     key-major: one workgroup = 128 keys, walking the rows
+//   cross_kv_sum   adds dK, dV of split rows
+//
+// No atomics: the sums' order depends on the batch's shape alone.  All matrix products
+// run on the 32 x 32 MFMAs with fp32 accumulation: bf16 inputs on v_mfma_f32_32x32x16_bf16
+// with P and dS rounded to bf16 (nearest even; half a step of 2^-8 relative each, as small
+// as the rounding of the results), fp32 inputs on v_mfma_f32_32x32x2_f32 with nothing
+// rounded below fp32.
+
+#include <hip/hip_runtime.h>
+
+#include "pp_device.h"
+#include "pp_launch.h"
+
+namespace pp {
+namespace {
+
+constexpr float kRescaleSlack = 8.0f;  // log2 units
+
+// What a kernel does with 8 elements along the contraction axis: lane l of a fragment
+// holds elements 8 (l / 32) + 0..7 of its row (see pp_device.h).
+template <typename T>
+struct Ops;
+
+template <>
+struct Ops<__bf16> {
+  using Frag = bf16x8;
+  template <int D>
+  static constexpr int kRowD = D;  // the row as 2-byte elements, for the DMA and its swizzle
+  static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, const f32x16& c) { return mfma32(a, b, c); }
+  static __device__ __forceinline__ Frag from_acc(const f32x16& acc, int s) { return acc_half_to_bf16(acc, s); }
+  template <int D>
+  static __device__ __forceinline__ Frag row8(const __bf16* tile, int r, int lc) {
+    return lds_row8<D>(tile, r, lc);
+  }
+  template <int D>
+  static __device__ __forceinline__ Frag tr8(const __bf16* tile, int row16, int col0, int lane) {
+    return lds_tr8<D>(tile, row16, col0, lane);
+  }
+};
+
+// fp32: the MFMA takes one element of the contraction axis from either half of the wave,
+// so a fragment's element e pairs contraction indices e and 8 + e, alike in both operands.
+template <>
+struct Ops<float> {
+  using Frag = f32x8;
+  template <int D>
+  static constexpr int kRowD = 2 * D;
+  static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ Frag from_acc(const f32x16& acc, int s) {
+    Frag f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = acc[8 * s + e];
+    return f;
+  }
+  template <int D>
+  static __device__ __forceinline__ Frag row8(const float* tile, int r, int lc) {
+    const int sw = swz<2 * D>(r);
+    const f32x4 a = *reinterpret_cast<const f32x4*>(tile + r * D + (((2 * lc) ^ sw) << 2));
+    const f32x4 b = *reinterpret_cast<const f32x4*>(tile + r * D + (((2 * lc + 1) ^ sw) << 2));
+    return Frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  }
+  // column col0 + l % 32 of the rows that from_acc's elements stand for
+  template <int D>
+  static __device__ __forceinline__ Frag tr8(const float* tile, int row16, int col0, int lane) {
+    const int c = col0 + (lane & 31), h = lane >> 5;
+    Frag f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int r = row16 + 8 * (e >> 2) + 4 * h + (e & 3);
+      f[e] = tile[r * D + (((c >> 2) ^ swz<2 * D>(r)) << 2) + (c & 3)];
+    }
+    return f;
+  }
+};
+
+// Wave-cooperative DMA of NR rows of D elements of T (see TileDma).
+template <typename T, int D, int NR>
+using RowDma = TileDma<Ops<T>::template kRowD<D>, NR>;
+template <int RD, int NR, typename T>
+__device__ __forceinline__ void dma_rows(const TileDma<RD, NR>& d, T* lds_tile, const T* src, int rows_valid) {
+  d.issue(reinterpret_cast<__bf16*>(lds_tile), reinterpret_cast<const __bf16*>(src), rows_valid);
+}
+
+template <typename T>
+struct CrossParams {
+  const T* q;
+  const T* k;
+  const T* v;
+  const T* dout;
+  const T* o_in;           // backward
+  T* o;                    // forward: o; dQ: dq
+  T* dk;
+  T* dv;
+  float* lse;              // forward: out
+  const float* lse_in;
+  const CrossItem* items;  // null: in inl
+  const CrossKvItem* kv_items;
+  const int32_t* kbeg;     // per token, or null
+  const int32_t* kend;
+  float* part;             // partial sums of split items
+  float* part_ml;          // forward: (maximum, sum) of the partial rows
+  float* ndelta;           // [hkv][sumT G]: -delta and -lse log2(e) of every row
+  float* nlse2;
+  CrossRange* ranges;      // per block of 32 rows: least and greatest begin and end
+  int hq, hkv, G, sumT;
+  uint32_t g_magic;
+  float scale;
+  float scale_log2;
+};
+
+// Few items ride in the launch's arguments, so that a small call needs no copy ahead of
+// its kernels.
+struct InlineItems {
+  CrossItem item[kCrossInline];
+};
+
+template <typename P>
+__device__ __forceinline__ CrossItem cross_item(const P& p, const InlineItems& inl, int idx) {
+  if (p.items) return load_uniform(p.items + idx);
+  return inl.item[idx];
+}
+
+// One lane's row of an item and what it sees.
+struct RowOf {
+  bool in_tile, live;
+  int tok, head;  // flat token, query head
+  int lo, hi;     // visible keys of the item's part
+};
+
+template <bool RANGES, typename P>
+__device__ __forceinline__ RowOf row_of(const P& p, const CrossItem& it, int g, int r) {
+  RowOf w;
+  w.in_tile = r < it.rows;
+  w.live = r < it.live;
+  const int i = (int)((unsigned)r / (unsigned)p.G);
+  w.tok = it.tok0 + i;
+  w.head = g * p.G + (r - i * p.G);
+  w.lo = it.k_begin;
+  w.hi = w.live ? it.k_end : it.k_begin;
+  if (RANGES && w.live) {
+    w.lo = max(w.lo, p.kbeg[w.tok]);
+    w.hi = min(w.hi, p.kend[w.tok]);
+  }
+  if (w.hi <= w.lo) w.lo = w.hi = it.k_begin;
+  return w;
+}
+
+__device__ __forceinline__ int wave_min_i(int x) {
+  for (int off = 32; off > 0; off >>= 1) x = min(x, __shfl_xor(x, off, 64));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int wave_max_i(int x) {
+  for (int off = 32; off > 0; off >>= 1) x = max(x, __shfl_xor(x, off, 64));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+
+// What a wave's 32 rows see of the keys, as wave-uniform bounds: no row sees a key
+// outside [any_lo, any_hi), every live row sees all of [all_lo, all_hi).
+struct WaveKeys {
+  int any_lo, any_hi, all_lo, all_hi;
+  __device__ __forceinline__ bool none(int k0, int k1) const { return k1 <= any_lo || k0 >= any_hi; }
+  __device__ __forceinline__ bool every(int k0, int k1) const { return k0 >= all_lo && k1 <= all_hi; }
+};
+
+template <bool RANGES>
+__device__ __forceinline__ WaveKeys wave_keys(const CrossItem& it, const RowOf& w, int wave_r0) {
+  if constexpr (!RANGES) {
+    const bool any = wave_r0 < it.live && it.k_end > it.k_begin;
+    return {it.k_begin, any ? it.k_end : it.k_begin, it.k_begin, it.k_end};
+  } else {
+    const bool some = w.hi > w.lo;
+    return {wave_min_i(some ? w.lo : 0x7fffffff), wave_max_i(some ? w.hi : 0), wave_max_i(w.live ? w.lo : 0),
+            wave_min_i(w.live ? w.hi : 0x7fffffff)};
+  }
+}
+
+// S^T of masked pairs becomes -inf: key k0 + 4 hf + off is seen iff lo <= it < hi.
+template <int KB>
+__device__ __forceinline__ void mask_keys(f32x16 (&s)[KB], int k0, int hf, int lo, int hi) {
+  static_assert(KB <= 2, "64 bits");
+  const uint64_t vis = bits_below64(hi - k0 - 4 * hf) & ~bits_below64(lo - k0 - 4 * hf);
+  const uint32_t w[2] = {(uint32_t)vis, (uint32_t)(vis >> 32)};
+#pragma unroll
+  for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[kb][r] = keep_or_neginf(s[kb][r], w[kb], 8 * (r >> 2) + (r & 3));
+}
+
+// A row's running softmax: reference maximum (scaled, log2 units), this lane's share of
+// the denominator, and O^T.  The reference is only raised when a tile exceeds it by more
+// than 2^8, so most tiles do not rescale.
+template <int D>
+struct RowState {
+  f32x16 o[D / 32];
+  float m_ref, l;
+
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m) o[m] = f32x16{};
+    m_ref = kNegInf;
+    l = 0.f;
+  }
+
+  // turns the block's scores into probabilities relative to the reference
+  template <int KB>
+  __device__ __forceinline__ void probabilities(f32x16 (&s)[KB], float c2) {
+    float mx = kNegInf;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kb][r]);
+    mx = half_swap_max(mx) * c2;
+    const bool raise = mx > m_ref + kRescaleSlack;
+    if (wave_any(raise)) {
+      const float m_new = raise ? mx : m_ref;
+      const float alpha = (m_ref == kNegInf) ? 0.f : fast_exp2(m_ref - m_new);  // nothing seen yet: O = l = 0
+      l *= alpha;
+#pragma unroll
+      for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[m][r] *= alpha;
+      m_ref = m_new;
+    }
+    const float mref = (m_ref == kNegInf) ? 0.f : m_ref;
+    float ps[2] = {0.f, 0.f};
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[kb][r] = fast_exp2(fmaf(s[kb][r], c2, -mref));
+        ps[r & 1] += s[kb][r];
+      }
+    l += ps[0] + ps[1];
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Forward
+// ---------------------------------------------------------------------------
+
+// Keys per tile and tiles in flight: 64 keys of bf16 (32 KB of K and V at head size 128),
+// 32 of fp32; two workgroups a compute unit.
+template <typename T>
+constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
+constexpr int kStages = 2;
+constexpr int kWaves = 4;
+static_assert(32 * kWaves == kCrossRows, "rows a workgroup");
+
+// The keys [t0, t1) that a workgroup of kWaves waves walks, from tile-aligned t0.
+template <bool RANGES, int BN>
+__device__ __forceinline__ void block_keys(const CrossItem& it, const WaveKeys& wk, int wave, int& t0, int& t1) {
+  t0 = it.k_begin;
+  t1 = it.k_end;
+  if constexpr (RANGES) {
+    __shared__ int s_lo[kWaves], s_hi[kWaves];
+    if ((threadIdx.x & 63) == 0) {
+      s_lo[wave] = wk.any_lo;
+      s_hi[wave] = wk.any_hi;
+    }
+    __syncthreads();
+    int lo = s_lo[0], hi = s_hi[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) {
+      lo = min(lo, s_lo[w]);
+      hi = max(hi, s_hi[w]);
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
+    t0 = hi > lo ? lo / BN * BN : 0;
+    t1 = hi > lo ? hi : 0;
+  }
+}
+
+template <int D, typename T, bool RANGES>
+__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void cross_fwd_kernel(CrossParams<T> p, InlineItems inl) {
+  using O = Ops<T>;
+  using Frag = typename O::Frag;
+  constexpr int BN = kKeys<T>, KB = BN / 32, RPW = BN / kWaves;
+  using Dma = RowDma<T, D, RPW>;
+  __shared__ __attribute__((aligned(1024))) T sKV[kStages][2][BN * D];
+
+  const int item_idx = blockIdx.x / p.hkv, g = blockIdx.x - item_idx * p.hkv;
+  const CrossItem it = cross_item(p, inl, item_idx);
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, ln = lane & 31, hf = lane >> 5;
+  const RowOf w = row_of<RANGES>(p, it, g, it.r0 + wave * 32 + ln);
+  const WaveKeys wk = wave_keys<RANGES>(it, w, it.r0 + wave * 32);
+  const int64_t qrow = ((int64_t)w.tok * p.hq + w.head) * D;
+  Frag qf[D / 16];
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c)
+    qf[c] = w.live ? *reinterpret_cast<const Frag*>(p.q + qrow + 16 * c + 8 * hf) : Frag{};
+
+  int key0, key1;
+  block_keys<RANGES, BN>(it, wk, wave, key0, key1);
+  const int n_tiles = (key1 - key0 + BN - 1) / BN;
+  const int64_t kv_stride = (int64_t)p.hkv * D;
+  const T* kbase = p.k + ((int64_t)it.e0 * p.hkv + g) * D;
+  const T* vbase = p.v + ((int64_t)it.e0 * p.hkv + g) * D;
+  Dma dma;
+  dma.init(wave * RPW, kv_stride * (sizeof(T) / 2), lane);
+  auto issue = [&](int t) {
+    const int k0 = key0 + t * BN;
+    const int rows = min(BN, it.elen - k0);
+    dma_rows(dma, sKV[t % kStages][0], kbase + k0 * kv_stride, rows);
+    dma_rows(dma, sKV[t % kStages][1], vbase + k0 * kv_stride, rows);
+  };
+#pragma unroll
+  for (int t = 0; t < kStages - 1; ++t)
+    if (t < n_tiles) issue(t);
+
+  RowState<D> st;
+  st.init();
+  const float c2 = p.scale_log2;
+  for (int t = 0; t < n_tiles; ++t) {
+    const int k0 = key0 + t * BN;
+    wait_tile<kStages, 2 * Dma::N>(t, n_tiles);
+    __syncthreads();  // tile t landed for every wave; the stage of tile t-1 is free
+    if (t + kStages - 1 < n_tiles) issue(t + kStages - 1);
+    if (wk.none(k0, k0 + BN)) continue;
+    const T* sK = sKV[t % kStages][0];
+    const T* sV = sKV[t % kStages][1];
+    // S^T = K Q^T: lane = row, registers = keys; K fragments read PD steps ahead
+    f32x16 s[KB];
+    {
+      constexpr int NC = D / 16, NI = KB * NC, PD = 3;
+      Frag a[PD + 1];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) s[kb] = f32x16{};
+#pragma unroll
+      for (int n = 0; n < PD; ++n) a[n] = O::template row8<D>(sK, (n / NC) * 32 + ln, 2 * (n % NC) + hf);
+#pragma unroll
+      for (int n = 0; n < NI; ++n) {
+        if (n + PD < NI)
+          a[(n + PD) % (PD + 1)] = O::template row8<D>(sK, ((n + PD) / NC) * 32 + ln, 2 * ((n + PD) % NC) + hf);
+        s[n / NC] = O::mma(a[n % (PD + 1)], qf[n % NC], s[n / NC]);
+      }
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int n = 0; n < PD; ++n) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+#pragma unroll
+        for (int n = 0; n < NI; ++n) {
+          if (n + PD < NI) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+        }
+      }
+    }
+    if (!wk.every(k0, k0 + BN)) mask_keys<KB>(s, k0, hf, w.lo, w.hi);
+    st.probabilities(s, c2);
+    // O^T += V^T P^T over 16-key chunks
+#pragma unroll
+    for (int ch = 0; ch < 2 * KB; ++ch) {
+      const Frag pb = O::from_acc(s[ch >> 1], ch & 1);
+#pragma unroll
+      for (int m = 0; m < D / 32; ++m) st.o[m] = O::mma(O::template tr8<D>(sV, 16 * ch, 32 * m, lane), pb, st.o[m]);
+    }
+  }
+
+  if (!w.in_tile) return;
+  const float l_tot = half_swap_sum(st.l);
+  if (it.slot >= 0) {
+    if (!w.live) return;
+    const int64_t prow = ((int64_t)it.slot * p.hkv + g) * kCrossRows + wave * 32 + ln;
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *reinterpret_cast<f32x4*>(p.part + prow * D + 32 * m + 8 * r4 + 4 * hf) =
+            f32x4{st.o[m][4 * r4], st.o[m][4 * r4 + 1], st.o[m][4 * r4 + 2], st.o[m][4 * r4 + 3]};
+    if (hf == 0) {
+      p.part_ml[2 * prow] = st.m_ref;
+      p.part_ml[2 * prow + 1] = l_tot;
+    }
+    return;
+  }
+  const bool seen = w.hi > w.lo;
+  const float inv = seen ? 1.f / l_tot : 0.f;
+#pragma unroll
+  for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      f32x4 v4 = f32x4{};
+      if (seen) v4 = f32x4{st.o[m][4 * r4] * inv, st.o[m][4 * r4 + 1] * inv, st.o[m][4 * r4 + 2] * inv,
+                           st.o[m][4 * r4 + 3] * inv};
+      store4<T>(p.o + qrow + 32 * m + 8 * r4 + 4 * hf, v4);
+    }
+  if (hf == 0) p.lse[(int64_t)w.head * p.sumT + w.tok] = seen ? (st.m_ref + __log2f(l_tot)) * (1.0f / kLog2e) : 0.f;
+}
+
+// Joins the parts of rows whose keys were split, in part order: a row is D / 4 lanes,
+// four parts' loads in flight.
+template <int D, typename T>
+__global__ __launch_bounds__(256) void cross_combine_kernel(CrossParams<T> p, const CrossSplit* splits, CrossSplitList inl,
+                                                            int bm) {
+  constexpr int LPR = D / 4, RPB = 256 / LPR;
+  const int si = blockIdx.x / p.hkv, g = blockIdx.x - si * p.hkv;
+  const CrossSplit sp = splits ? load_uniform(splits + si) : inl.split[si];
+  const int lr = blockIdx.y * RPB + threadIdx.x / LPR, c = (threadIdx.x % LPR) * 4;
+  const int r = sp.r0 + lr;
+  if (lr >= bm || r >= sp.rows) return;
+  const int i = (int)((unsigned)r / (unsigned)p.G);
+  const int tok = sp.tok0 + i, head = g * p.G + (r - i * p.G);
+  f32x4 acc = f32x4{};
+  float m = kNegInf, l = 0.f;
+  if (r < sp.live) {
+    constexpr int NP = 4;
+    const int64_t stride = (int64_t)p.hkv * bm;  // rows between slots
+    int64_t prow = ((int64_t)sp.slot0 * p.hkv + g) * bm + lr;
+    for (int n0 = 0; n0 < sp.parts; n0 += NP, prow += NP * stride) {
+      f32x4 x[NP];
+      float pm[NP], pl[NP];
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        const bool on = n0 + n < sp.parts;
+        const int64_t row = prow + (on ? n : 0) * stride;
+        x[n] = *reinterpret_cast<const f32x4*>(p.part + row * D + c);
+        pm[n] = p.part_ml[2 * row];
+        pl[n] = on ? p.part_ml[2 * row + 1] : 0.f;
+      }
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        if (pl[n] == 0.f) continue;  // a part without a visible key
+        const float mn = fmaxf(m, pm[n]);
+        const float a = m == kNegInf ? 0.f : fast_exp2(m - mn), b = fast_exp2(pm[n] - mn);
+        l = l * a + pl[n] * b;
+        acc = acc * a + x[n] * b;
+        m = mn;
+      }
+    }
+  }
+  const bool seen = l != 0.f;
+  const float inv = seen ? 1.f / l : 0.f;
+  store4<T>(p.o + ((int64_t)tok * p.hq + head) * D + c, seen ? acc * inv : f32x4{});
+  if (c == 0) p.lse[(int64_t)head * p.sumT + tok] = seen ? (m + __log2f(l)) * (1.0f / kLog2e) : 0.f;
+}
+
+// ---------------------------------------------------------------------------
+// dQ
+// ---------------------------------------------------------------------------
+
+template <int D, typename T, bool RANGES>
+__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void cross_dq_kernel(CrossParams<T> p) {
+  using O = Ops<T>;
+  using Frag = typename O::Frag;
+  constexpr int BN = kKeys<T>, KB = BN / 32, RPW = BN / kWaves;
+  using Dma = RowDma<T, D, RPW>;
+  __shared__ __attribute__((aligned(1024))) T sKV[kStages][2][BN * D];
+
+  const int item_idx = blockIdx.x / p.hkv, g = blockIdx.x - item_idx * p.hkv;
+  const CrossItem it = load_uniform(p.items + item_idx);
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, ln = lane & 31, hf = lane >> 5;
+  const int r = it.r0 + wave * 32 + ln;
+  const RowOf w = row_of<RANGES>(p, it, g, r);
+  const WaveKeys wk = wave_keys<RANGES>(it, w, it.r0 + wave * 32);
+  const int64_t qrow = ((int64_t)w.tok * p.hq + w.head) * D;
+  Frag qf[D / 16], df[D / 16];
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) {
+    qf[c] = w.live ? *reinterpret_cast<const Frag*>(p.q + qrow + 16 * c + 8 * hf) : Frag{};
+    df[c] = w.live ? *reinterpret_cast<const Frag*>(p.dout + qrow + 16 * c + 8 * hf) : Frag{};
+  }
+  // delta = dO . O and -lse log2(e) of the lane's row, kept for the dK/dV pass
+  float nlse2 = 0.f, dlt = 0.f;
+  {
+    float acc = 0.f;
+    if (w.live) {
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        const Frag b = *reinterpret_cast<const Frag*>(p.o_in + qrow + 16 * c + 8 * hf);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc += (float)df[c][e] * (float)b[e];
+      }
+      nlse2 = -p.lse_in[(int64_t)w.head * p.sumT + w.tok] * kLog2e;
+    }
+    dlt = half_swap_sum(acc);
+    if (it.k_begin == 0) {  // the first part, if the keys are split
+      if (w.live && hf == 0) {
+        const int64_t at = (int64_t)g * p.sumT * p.G + (int64_t)it.tok0 * p.G + r;
+        p.ndelta[at] = -dlt;
+        p.nlse2[at] = nlse2;
+      }
+    }
+  }
+  if constexpr (RANGES) {
+    if (it.k_begin == 0 && g == 0) {
+      int lo = 0, hi = 0;
+      if (w.live) {
+        lo = max(0, p.kbeg[w.tok]);
+        hi = min(it.elen, p.kend[w.tok]);
+        if (hi <= lo) lo = hi = 0;
+      }
+      const CrossRange rg = {wave_min_i(hi > lo ? lo : 0x7fffffff), wave_max_i(hi > lo ? hi : 0), wave_max_i(w.live ? lo : 0),
+                             wave_min_i(w.live ? hi : 0x7fffffff)};
+      if (lane == 0 && it.r0 + wave * 32 < it.live) p.ranges[it.blk0 + ((it.r0 + wave * 32) >> 5)] = rg;
+    }
+  }
+
+  int key0, key1;
+  block_keys<RANGES, BN>(it, wk, wave, key0, key1);
+  const int n_tiles = (key1 - key0 + BN - 1) / BN;
+  const int64_t kv_stride = (int64_t)p.hkv * D;
+  const T* kbase = p.k + ((int64_t)it.e0 * p.hkv + g) * D;
+  const T* vbase = p.v + ((int64_t)it.e0 * p.hkv + g) * D;
+  Dma dma;
+  dma.init(wave * RPW, kv_stride * (sizeof(T) / 2), lane);
+  auto issue = [&](int t) {
+    const int k0 = key0 + t * BN;
+    const int rows = min(BN, it.elen - k0);
+    dma_rows(dma, sKV[t % kStages][0], kbase + k0 * kv_stride, rows);
+    dma_rows(dma, sKV[t % kStages][1], vbase + k0 * kv_stride, rows);
+  };
+#pragma unroll
+  for (int t = 0; t < kStages - 1; ++t)
+    if (t < n_tiles) issue(t);
+
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int m = 0; m < D / 32; ++m) acc[m] = f32x16{};
+  for (int t = 0; t < n_tiles; ++t) {
+    const int k0 = key0 + t * BN;
+    wait_tile<kStages, 2 * Dma::N>(t, n_tiles);
+    __syncthreads();
+    if (t + kStages - 1 < n_tiles) issue(t + kStages - 1);
+    if (wk.none(k0, k0 + BN)) continue;
+    const T* sK = sKV[t % kStages][0];
+    const T* sV = sKV[t % kStages][1];
+    // S^T = K Q^T and dP^T = V dO^T, fragments read PD ahead
+    f32x16 s[KB], dp[KB];
+    {
+      constexpr int NC = D / 16, NI = 2 * KB * NC, PD = 3;
+      auto frag = [&](int n) {
+        return O::template row8<D>(((n / NC) & 1) ? sV : sK, (n / (2 * NC)) * 32 + ln, 2 * (n % NC) + hf);
+      };
+      Frag a[PD + 1];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        s[kb] = f32x16{};
+        dp[kb] = f32x16{};
+      }
+#pragma unroll
+      for (int n = 0; n < PD; ++n) a[n] = frag(n);
+#pragma unroll
+      for (int n = 0; n < NI; ++n) {
+        if (n + PD < NI) a[(n + PD) % (PD + 1)] = frag(n + PD);
+        const int kb = n / (2 * NC), c = n % NC;
+        if ((n / NC) & 1) dp[kb] = O::mma(a[n % (PD + 1)], df[c], dp[kb]);
+        else s[kb] = O::mma(a[n % (PD + 1)], qf[c], s[kb]);
+      }
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int n = 0; n < PD; ++n) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+#pragma unroll
+        for (int n = 0; n < NI; ++n) {
+          if (n + PD < NI) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+        }
+      }
+    }
+    if (!wk.every(k0, k0 + BN)) mask_keys<KB>(s, k0, hf, w.lo, w.hi);
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dp[kb][e] = fast_exp2(fmaf(s[kb][e], p.scale_log2, nlse2)) * (dp[kb][e] - dlt);
+    // dQ^T += K^T dS^T over 16-key chunks
+#pragma unroll
+    for (int ch = 0; ch < 2 * KB; ++ch) {
+      const Frag db = O::from_acc(dp[ch >> 1], ch & 1);
+#pragma unroll
+      for (int m = 0; m < D / 32; ++m) acc[m] = O::mma(O::template tr8<D>(sK, 16 * ch, 32 * m, lane), db, acc[m]);
+    }
+  }
+
+  if (!w.in_tile) return;
+  if (it.slot >= 0) {
+    if (!w.live) return;
+    float* row = p.part + (((int64_t)it.slot * p.hkv + g) * kCrossRows + wave * 32 + ln) * D;
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4)
+        *reinterpret_cast<f32x4*>(row + 32 * m + 8 * r4 + 4 * hf) =
+            f32x4{acc[m][4 * r4], acc[m][4 * r4 + 1], acc[m][4 * r4 + 2], acc[m][4 * r4 + 3]};
+    return;
+  }
+  const bool seen = w.hi > w.lo;
+#pragma unroll
+  for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      f32x4 v4 = f32x4{};
+      if (seen) v4 = f32x4{acc[m][4 * r4] * p.scale, acc[m][4 * r4 + 1] * p.scale, acc[m][4 * r4 + 2] * p.scale,
+                           acc[m][4 * r4 + 3] * p.scale};
+      store4<T>(p.o + qrow + 32 * m + 8 * r4 + 4 * hf, v4);
+    }
+}
+
+// Adds the parts of dQ rows whose keys were split, in part order.
+template <int D, typename T>
+__global__ __launch_bounds__(256) void cross_dq_sum_kernel(CrossParams<T> p, const CrossSplit* splits) {
+  constexpr int LPR = D / 4, RPB = 256 / LPR;
+  const int si = blockIdx.x / p.hkv, g = blockIdx.x - si * p.hkv;
+  const CrossSplit sp = load_uniform(splits + si);
+  const int lr = blockIdx.y * RPB + threadIdx.x / LPR, c = (threadIdx.x % LPR) * 4;
+  const int r = sp.r0 + lr;
+  if (lr >= kCrossRows || r >= sp.rows) return;
+  const int i = (int)((unsigned)r / (unsigned)p.G);
+  f32x4 acc = f32x4{};
+  if (r < sp.live) {
+    constexpr int NP = 4;
+    const int64_t stride = (int64_t)p.hkv * kCrossRows * D;
+    const float* src = p.part + (((int64_t)sp.slot0 * p.hkv + g) * kCrossRows + lr) * D + c;
+    for (int n0 = 0; n0 < sp.parts; n0 += NP, src += NP * stride) {
+      f32x4 x[NP];
+#pragma unroll
+      for (int n = 0; n < NP; ++n)
+        if (n0 + n < sp.parts) x[n] = *reinterpret_cast<const f32x4*>(src + n * stride);
+#pragma unroll
+      for (int n = 0; n < NP; ++n)
+        if (n0 + n < sp.parts) acc += x[n];
+    }
+  }
+  store4<T>(p.o + ((int64_t)(sp.tok0 + i) * p.hq + g * p.G + (r - i * p.G)) * D + c, acc * p.scale);
+}
+
+// ---------------------------------------------------------------------------
+// dK, dV: key-major
+// ---------------------------------------------------------------------------
+
+// bf16: eight waves; waves w and w + 4 own keys 32 (w % 4) .. +31 and take the two
+// 32-row halves of every 64-row step; K and V of the tile stay in LDS (head size 128) or
+// in registers (64).  fp32: four waves, 32-row steps, K and V in registers.
+template <int D, typename T>
+struct KvShape {
+  static constexpr int QB = sizeof(T) == 2 ? 2 : 1;   // row blocks a step
+  static constexpr int STEP = 32 * QB;
+  static constexpr int WAVES = 4 * QB;
+  static constexpr bool HOLD = sizeof(T) == 4 || D == 64;
+};
+
+template <int D, typename T>
+struct KvStage {
+  T q[KvShape<D, T>::STEP * D];
+  T dout[KvShape<D, T>::STEP * D];
+  float nlse2[64];   // a DMA fills all 64
+  float ndelta[64];
+  int lo[64], hi[64];
+};
+
+template <int D, typename T, bool HOLD>
+struct KvTiles {
+  T k[kCrossKeys * D], v[kCrossKeys * D];
+};
+template <int D, typename T>
+struct KvTiles<D, T, true> {};
+
+template <int D, typename T>
+struct KvSmem : KvTiles<D, T, KvShape<D, T>::HOLD> {
+  union {
+    KvStage<D, T> st[2];
+    float red[4][32 * D];
+  };
+};
+
+template <int D, typename T, bool RANGES>
+__global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), 1) void cross_dkdv_kernel(CrossParams<T> p) {
+  using O = Ops<T>;
+  using Frag = typename O::Frag;
+  using S = KvShape<D, T>;
+  constexpr int STEP = S::STEP, RD = O::template kRowD<D>;
+  constexpr int RPI = 1024 / (RD * 2), CPR = RD / 8;   // rows and 16-byte chunks of a DMA instruction
+  constexpr int RPW = STEP / S::WAVES, NI = RPW / RPI;
+  static_assert(RPW % RPI == 0, "whole DMA instructions");
+  __shared__ __attribute__((aligned(1024))) KvSmem<D, T> sm;
+
+  const int item_idx = blockIdx.x / p.hkv, g = blockIdx.x - item_idx * p.hkv;
+  const CrossKvItem it = load_uniform(p.kv_items + item_idx);
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, ln = lane & 31, hf = lane >> 5;
+  const int kb = wave & 3, qb = wave >> 2;
+  const int wk0 = it.k0 + kb * 32, wk1 = min(it.elen, wk0 + 32);
+  const bool wave_live = wk0 < wk1;
+  const int j = wk0 + ln;
+  const int k1 = min(it.elen, it.k0 + kCrossKeys);
+  const int64_t kv_stride = (int64_t)p.hkv * D;
+
+  // rows past the states repeat the last one
+  Frag kf[S::HOLD ? D / 16 : 1], vf[S::HOLD ? D / 16 : 1];
+  const bool any = it.n_begin < it.n_end;
+  if constexpr (S::HOLD) {
+    if (any) {
+      const int64_t row = ((int64_t)(it.e0 + min(j, it.elen - 1)) * p.hkv + g) * D;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) {
+        kf[c] = *reinterpret_cast<const Frag*>(p.k + row + 16 * c + 8 * hf);
+        vf[c] = *reinterpret_cast<const Frag*>(p.v + row + 16 * c + 8 * hf);
+      }
+    }
+  } else {
+    if (any) {
+      TileDma<RD, kCrossKeys / S::WAVES> kd;
+      kd.init(wave * (kCrossKeys / S::WAVES), kv_stride * (sizeof(T) / 2), lane);
+      const int64_t row = ((int64_t)(it.e0 + it.k0) * p.hkv + g) * D;
+      dma_rows(kd, sm.k, p.k + row, k1 - it.k0);
+      dma_rows(kd, sm.v, p.v + row, k1 - it.k0);
+    }
+  }
+
+  // RANGES: the next step from n on in which some row sees a key of the tile
+  const CrossRange* ranges = RANGES ? p.ranges + it.blk0 : nullptr;
+  auto next_step = [&](int n) {
+    if constexpr (RANGES) {
+      for (; n < it.n_end; ++n) {
+        bool hit = false;
+#pragma unroll
+        for (int b = 0; b < S::QB; ++b) {
+          const int blk = n * S::QB + b;
+          if (blk * 32 >= it.live) break;
+          hit |= scalar_load(&ranges[blk].any_lo) < k1 && scalar_load(&ranges[blk].any_hi) > it.k0;
+        }
+        if (hit) break;
+      }
+    }
+    return n;
+  };
+  // lane's row lr of the step from row r0 on, as the token past i0 and the head
+  auto split_row = [&](int x, int& il, int& h) {
+    il = p.G == 1 ? x : (int)__umulhi((unsigned)x, p.g_magic);
+    h = x - il * p.G;
+  };
+  auto issue = [&](int n, int buf) {
+    KvStage<D, T>& sg = sm.st[buf];
+    const int r0 = n * STEP;
+    const int rows = min(STEP, it.live - r0);
+    const int i0 = (int)((unsigned)r0 / (unsigned)p.G), h0 = r0 - i0 * p.G;
+    const int64_t t0 = (int64_t)it.tok0 + i0;
+    const char* qbase = reinterpret_cast<const char*>(p.q + (t0 * p.hq + g * p.G) * D);
+    const char* obase = reinterpret_cast<const char*>(p.dout + (t0 * p.hq + g * p.G) * D);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int first = wave * RPW + i * RPI, lr = first + lane / CPR;
+      int il, h;
+      split_row(h0 + min(lr, rows - 1), il, h);
+      const uint32_t off = ((uint32_t)il * (uint32_t)p.hq + (uint32_t)h) * (uint32_t)(RD * 2) +
+                           ((uint32_t)((lane % CPR) ^ swz<RD>(lr)) << 4);
+      lds_dma16(qbase + off, sg.q + first * D);
+      lds_dma16(obase + off, sg.dout + first * D);
+    }
+    const int lr = min(lane, rows - 1);
+    const int64_t at = (int64_t)g * p.sumT * p.G + (int64_t)it.tok0 * p.G + r0 + lr;
+    if (wave == 0) dma_dword(sg.nlse2, p.nlse2 + at);
+    else if (wave == 1) dma_dword(sg.ndelta, p.ndelta + at);
+    if constexpr (RANGES) {
+      if (wave == 2 || wave == 3) {
+        int il, h;
+        split_row(h0 + lr, il, h);
+        if (wave == 2) dma_dword(sg.lo, p.kbeg + t0 + il);
+        else dma_dword(sg.hi, p.kend + t0 + il);
+      }
+    }
+  };
+  int n = next_step(it.n_begin), buf = 0;
+  if (n < it.n_end) issue(n, 0);
+
+  f32x16 acc_dk[D / 32], acc_dv[D / 32];
+#pragma unroll
+  for (int m = 0; m < D / 32; ++m) {
+    acc_dk[m] = f32x16{};
+    acc_dv[m] = f32x16{};
+  }
+  while (n < it.n_end) {
+    const int nn = next_step(n + 1);
+    wait_vmem<0>();
+    __syncthreads();  // step n (and K, V) landed for every wave; the other stage is free
+    if (nn < it.n_end) issue(nn, buf ^ 1);
+    const KvStage<D, T>& sg = sm.st[buf];
+    const int rb0 = n * STEP + qb * 32;
+    n = nn;
+    buf ^= 1;
+    if (!wave_live || rb0 >= it.live) continue;
+    bool masked = false;
+    if constexpr (RANGES) {
+      const CrossRange rg = load_uniform(ranges + (rb0 >> 5));
+      if (rg.any_hi <= wk0 || rg.any_lo >= wk1) continue;
+      masked = !(rg.all_lo <= wk0 && rg.all_hi >= wk1);
+    }
+    // S = Q K^T and dP = dO V^T: lane = key, registers = rows
+    f32x16 s = f32x16{}, dp = f32x16{};
+    {
+      constexpr int NC = D / 16;
+      Frag fq[2], fk[2], fo[2], fv[2];
+      auto load = [&](int c, int b) {
+        fq[b] = O::template row8<D>(sg.q, qb * 32 + ln, 2 * c + hf);
+        if constexpr (!S::HOLD) fk[b] = O::template row8<D>(sm.k, kb * 32 + ln, 2 * c + hf);
+        fo[b] = O::template row8<D>(sg.dout, qb * 32 + ln, 2 * c + hf);
+        if constexpr (!S::HOLD) fv[b] = O::template row8<D>(sm.v, kb * 32 + ln, 2 * c + hf);
+      };
+      load(0, 0);
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        if (c + 1 < NC) load(c + 1, (c + 1) & 1);
+        if constexpr (S::HOLD) {
+          s = O::mma(fq[c & 1], kf[c], s);
+          dp = O::mma(fo[c & 1], vf[c], dp);
+        } else {
+          s = O::mma(fq[c & 1], fk[c & 1], s);
+          dp = O::mma(fo[c & 1], fv[c & 1], dp);
+        }
+      }
+      if constexpr (sizeof(T) == 2) {
+        constexpr int R = S::HOLD ? 1 : 2;  // reads ahead of each MFMA
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 2 * R, 0);
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          if (c + 1 < NC) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, R, 0);
+          __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+          if (c + 1 < NC) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, R, 0);
+          __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+        }
+      }
+    }
+    if (rb0 + 32 > it.live) {  // rows past the last repeat it: not to be counted again
+      const uint32_t vis = bits_below32(it.live - rb0 - 4 * hf);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[e] = keep_or_neginf(s[e], vis, 8 * (e >> 2) + (e & 3));
+    }
+    if constexpr (RANGES) {
+      if (masked) {
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const int il = qb * 32 + 8 * r4 + 4 * hf;
+          const i32x4 lo = *reinterpret_cast<const i32x4*>(&sg.lo[il]);
+          const i32x4 hi = *reinterpret_cast<const i32x4*>(&sg.hi[il]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * r4 + e] = j >= lo[e] && j < hi[e] ? s[4 * r4 + e] : kNegInf;
+        }
+      }
+    }
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) {
+      const int il = qb * 32 + 8 * r4 + 4 * hf;
+      const f32x4 l4 = *reinterpret_cast<const f32x4*>(&sg.nlse2[il]);
+      const f32x4 d4 = *reinterpret_cast<const f32x4*>(&sg.ndelta[il]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int x = 4 * r4 + e;
+        const float pr = fast_exp2(fmaf(s[x], p.scale_log2, l4[e]));
+        s[x] = pr;
+        dp[x] = pr * (dp[x] + d4[e]);
+      }
+    }
+    // dV^T += dO^T P and dK^T += Q^T dS over two 16-row chunks
+    const Frag pb0 = O::from_acc(s, 0), pb1 = O::from_acc(s, 1);
+    const Frag db0 = O::from_acc(dp, 0), db1 = O::from_acc(dp, 1);
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m) {
+      acc_dv[m] = O::mma(O::template tr8<D>(sg.dout, qb * 32, 32 * m, lane), pb0, acc_dv[m]);
+      acc_dk[m] = O::mma(O::template tr8<D>(sg.q, qb * 32, 32 * m, lane), db0, acc_dk[m]);
+      acc_dv[m] = O::mma(O::template tr8<D>(sg.dout, qb * 32 + 16, 32 * m, lane), pb1, acc_dv[m]);
+      acc_dk[m] = O::mma(O::template tr8<D>(sg.q, qb * 32 + 16, 32 * m, lane), db1, acc_dk[m]);
+    }
+  }
+
+  wait_vmem<0>();  // K and V of a tile that no row looks at are still on their way
+  const int64_t krow = ((int64_t)(it.e0 + j) * p.hkv + g) * D;
+#pragma unroll
+  for (int pass = 0; pass < 2; ++pass) {
+    f32x16(&row)[D / 32] = pass == 0 ? acc_dk : acc_dv;
+    if constexpr (S::QB == 2) {
+      float* red = sm.red[kb];
+      __syncthreads();  // the stages (pass 0) or the previous pass's buffer are free
+      if (qb == 1) {
+#pragma unroll
+        for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) red[(m * 16 + r) * 64 + lane] = row[m][r];
+      }
+      __syncthreads();
+      if (qb == 0) {
+#pragma unroll
+        for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) row[m][r] += red[(m * 16 + r) * 64 + lane];
+      }
+    }
+    if (qb != 0) continue;
+    if (it.slot >= 0) {
+      float* part = p.part + ((((int64_t)it.slot * p.hkv + g) * 2 + pass) * 4 + kb) * (32 * D);
+#pragma unroll
+      for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4)
+          *reinterpret_cast<f32x4*>(part + ((m * 4 + r4) * 64 + lane) * 4) =
+              f32x4{row[m][4 * r4], row[m][4 * r4 + 1], row[m][4 * r4 + 2], row[m][4 * r4 + 3]};
+    } else if (j < it.ecap) {
+      const float sc = pass == 0 ? p.scale : 1.f;
+      T* dst = (pass == 0 ? p.dk : p.dv) + krow;
+      const bool real = j < it.elen;
+#pragma unroll
+      for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          f32x4 v4 = f32x4{};
+          if (real) v4 = f32x4{row[m][4 * r4] * sc, row[m][4 * r4 + 1] * sc, row[m][4 * r4 + 2] * sc, row[m][4 * r4 + 3] * sc};
+          store4<T>(dst + 32 * m + 8 * r4 + 4 * hf, v4);
+        }
+    }
+  }
+}
+
+// Adds the parts of key tiles whose rows were split, in part order: a workgroup is four
+// consecutive accumulator registers of the tile's four key blocks, of one gradient.
+template <int D, typename T>
+__global__ __launch_bounds__(256) void cross_kv_sum_kernel(CrossParams<T> p, const CrossKvSplit* splits) {
+  int b = blockIdx.x;
+  const int ch = b % (D / 8);  // 4 m + r4
+  b /= D / 8;
+  const int g = b % p.hkv;
+  b /= p.hkv;
+  const int pass = b & 1;
+  const CrossKvSplit sp = load_uniform(splits + (b >> 1));
+  const int kb = threadIdx.x >> 6, lane = threadIdx.x & 63, hf = lane >> 5;
+  const int j = sp.k0 + kb * 32 + (lane & 31);
+  const int64_t stride = (int64_t)p.hkv * 2 * 4 * (32 * D);
+  const float* part = p.part + ((((int64_t)sp.slot0 * p.hkv + g) * 2 + pass) * 4 + kb) * (32 * D) + (ch * 64 + lane) * 4;
+  f32x4 acc = f32x4{};
+  constexpr int NP = 4;
+  for (int i = 0; i < sp.parts; i += NP, part += NP * stride) {
+    f32x4 x[NP];
+#pragma unroll
+    for (int n = 0; n < NP; ++n)
+      if (i + n < sp.parts) x[n] = *reinterpret_cast<const f32x4*>(part + n * stride);
+#pragma unroll
+    for (int n = 0; n < NP; ++n)
+      if (i + n < sp.parts) acc += x[n];
+  }
+  if (j >= sp.ecap) return;
+  acc *= pass == 0 ? p.scale : 1.f;
+  if (j >= sp.elen) acc = f32x4{};
+  T* dst = (pass == 0 ? p.dk : p.dv) + ((int64_t)(sp.e0 + j) * p.hkv + g) * D;
+  store4<T>(dst + 32 * (ch >> 2) + 8 * (ch & 3) + 4 * hf, acc);
+}
+
+template <typename T>
+CrossParams<T> params_of(const CrossLaunch& a) {
+  CrossParams<T> p{};
+  p.q = (const T*)a.q;
+  p.k = (const T*)a.k;
+  p.v = (const T*)a.v;
+  p.dout = (const T*)a.dout;
+  p.o_in = (const T*)a.o_in;
+  p.o = (T*)a.out;
+  p.dk = (T*)a.dk;
+  p.dv = (T*)a.dv;
+  p.lse = a.lse;
+  p.lse_in = a.lse_in;
+  p.items = a.items;
+  p.kv_items = a.kv_items;
+  p.kbeg = a.key_begin;
+  p.kend = a.key_end;
+  p.part = a.part;
+  p.part_ml = a.part_ml;
+  p.ndelta = a.ndelta;
+  p.nlse2 = a.nlse2;
+  p.ranges = a.ranges;
+  p.hq = a.hq;
+  p.hkv = a.hkv;
+  p.G = a.hq / a.hkv;
+  p.sumT = a.sumT;
+  p.g_magic = (uint32_t)(0xffffffffu / (uint32_t)p.G) + 1u;
+  p.scale = a.scale;
+  p.scale_log2 = a.scale * kLog2e;
+  return p;
+}
+
+void fill_inline(const CrossLaunch& a, InlineItems* inl, CrossSplitList* sl) {
+  if (!a.items)
+    for (int i = 0; i < a.n_items; ++i) inl->item[i] = a.host_items[i];
+  if (!a.splits)
+    for (int i = 0; i < a.n_splits; ++i) sl->split[i] = a.host_splits[i];
+}
+
+template <int D, typename T>
+hipError_t launch_fwd_t(const CrossLaunch& a, hipStream_t s) {
+  const CrossParams<T> p = params_of<T>(a);
+  InlineItems inl{};
+  CrossSplitList sl{};
+  fill_inline(a, &inl, &sl);
+  if (a.n_items > 0) {
+    TimingScope t("pp_cross_attn_fwd", s);
+    const dim3 grid((unsigned)((int64_t)a.n_items * a.hkv));
+    if (a.key_begin) hipLaunchKernelGGL((cross_fwd_kernel<D, T, true>), grid, dim3(kWaves * 64), 0, s, p, inl);
+    else hipLaunchKernelGGL((cross_fwd_kernel<D, T, false>), grid, dim3(kWaves * 64), 0, s, p, inl);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.n_splits > 0) {
+    TimingScope t("pp_cross_attn_combine", s);
+    constexpr int RPB = 256 / (D / 4);
+    const dim3 grid((unsigned)((int64_t)a.n_splits * a.hkv), (unsigned)((kCrossRows + RPB - 1) / RPB));
+    hipLaunchKernelGGL((cross_combine_kernel<D, T>), grid, dim3(256), 0, s, p, a.splits, sl, kCrossRows);
+    return hipGetLastError();
+  }
+  return hipSuccess;
+}
+
+template <int D, typename T>
+hipError_t launch_bwd_t(const CrossLaunch& a, hipStream_t s) {
+  CrossParams<T> p = params_of<T>(a);
+  hipError_t e = hipSuccess;
+  if (a.n_items > 0) {
+    TimingScope t("pp_cross_attn_dq", s);
+    const dim3 grid((unsigned)((int64_t)a.n_items * a.hkv));
+    if (a.key_begin) hipLaunchKernelGGL((cross_dq_kernel<D, T, true>), grid, dim3(kWaves * 64), 0, s, p);
+    else hipLaunchKernelGGL((cross_dq_kernel<D, T, false>), grid, dim3(kWaves * 64), 0, s, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (a.n_splits > 0) {
+    TimingScope t("pp_cross_attn_dq_sum", s);
+    constexpr int RPB = 256 / (D / 4);
+    const dim3 grid((unsigned)((int64_t)a.n_splits * a.hkv), (unsigned)((kCrossRows + RPB - 1) / RPB));
+    hipLaunchKernelGGL((cross_dq_sum_kernel<D, T>), grid, dim3(256), 0, s, p, a.splits);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (a.n_kv_items > 0) {
+    TimingScope t("pp_cross_attn_dkdv", s);
+    p.part = a.kv_part;
+    const dim3 grid((unsigned)((int64_t)a.n_kv_items * a.hkv)), block(KvShape<D, T>::WAVES * 64);
+    if (a.key_begin) hipLaunchKernelGGL((cross_dkdv_kernel<D, T, true>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((cross_dkdv_kernel<D, T, false>), grid, block, 0, s, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (a.n_kv_splits > 0) {
+    TimingScope t("pp_cross_attn_kv_sum", s);
+    const dim3 grid((unsigned)((int64_t)a.n_kv_splits * 2 * a.hkv * (D / 8)));
+    hipLaunchKernelGGL((cross_kv_sum_kernel<D, T>), grid, dim3(256), 0, s, p, a.kv_splits);
+    e = hipGetLastError();
+  }
+  return e;
+}
+
+}  // namespace
+
+hipError_t launch_cross_fwd(const CrossLaunch& a, hipStream_t s) {
+  if (a.dtype == kBF16) return a.head_dim == 128 ? launch_fwd_t<128, __bf16>(a, s) : launch_fwd_t<64, __bf16>(a, s);
+  return a.head_dim == 128 ? launch_fwd_t<128, float>(a, s) : launch_fwd_t<64, float>(a, s);
+}
+
+hipError_t launch_cross_bwd(const CrossLaunch& a, hipStream_t s) {
+  if (a.dtype == kBF16) return a.head_dim == 128 ? launch_bwd_t<128, __bf16>(a, s) : launch_bwd_t<64, __bf16>(a, s);
+  return a.head_dim == 128 ? launch_bwd_t<128, float>(a, s) : launch_bwd_t<64, float>(a, s);
+}
+
+}  // namespace pp

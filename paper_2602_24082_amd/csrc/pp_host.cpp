@@ -2164,3 +2164,354 @@ pp_status pp_timing_get(int idx, const char** name, double* total_ms, int64_t* l
 }
 
 }  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Cross attention of packed rows to an encoder's states
+// ---------------------------------------------------------------------------
+
+namespace pp {
+namespace {
+
+// The encoder axis: row b's states are [start, start + len) of it, its padding runs on to
+// start + cap.
+struct EncRow {
+  int32_t start, cap, len;
+};
+
+pp_status read_enc(const pp_enc_desc* enc, const Batch& bt, std::vector<EncRow>* out) {
+  if (!enc) return fail(PP_ERR_INVALID_ARGUMENT, "enc is NULL");
+  if (!enc->enc_start || !enc->enc_len) return fail(PP_ERR_INVALID_ARGUMENT, "enc_start and enc_len must be non-NULL");
+  if (enc->enc_start[0] != 0) return fail(PP_ERR_BAD_LAYOUT, "enc_start[0] must be 0");
+  out->resize(bt.B);
+  for (int b = 0; b < bt.B; ++b) {
+    const int64_t e0 = enc->enc_start[b], e1 = enc->enc_start[b + 1];
+    if (e1 < e0) return fail(PP_ERR_BAD_LAYOUT, "enc_start must be non-decreasing (row %d)", b);
+    if (enc->enc_len[b] < 0 || enc->enc_len[b] > e1 - e0)
+      return fail(PP_ERR_BAD_LAYOUT, "enc_len[%d] = %d outside [0, %lld]", b, enc->enc_len[b], (long long)(e1 - e0));
+    (*out)[b] = EncRow{(int32_t)e0, (int32_t)(e1 - e0), enc->enc_len[b]};
+  }
+  return PP_OK;
+}
+
+// Workgroups that fill the card twice over.  A pass whose tiles are fewer has the axis
+// that its workgroups walk split, down to kCrossLeast units of it.
+constexpr int64_t kCrossGroups = 2 * kComputeUnits;
+constexpr int64_t kCrossLeast = 4;
+
+// The longest part that a walk of `total` units (over tiles x kv-heads workgroups) is cut to.
+int64_t cross_part(int64_t tiles, int64_t total, int hkv) {
+  if (tiles * hkv >= kCrossGroups) return INT32_MAX;
+  return std::max(kCrossLeast, (total * hkv + kCrossGroups - 1) / kCrossGroups);
+}
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct CrossPlan {
+  std::vector<CrossItem> items;
+  std::vector<CrossSplit> splits;
+  std::vector<CrossKvItem> kv_items;
+  std::vector<CrossKvSplit> kv_splits;
+  int32_t slots = 0, kv_slots = 0, blocks = 0;
+  bool inline_items = false;
+  Layout lay;
+  size_t r_items = 0, r_splits = 0, r_kv_items = 0, r_kv_splits = 0, r_part = 0, r_ml = 0, r_ndelta = 0, r_nlse2 = 0,
+         r_ranges = 0;
+};
+
+// Row tiles against the states, most keys first.
+void build_cross_items(const Batch& bt, const std::vector<EncRow>& enc, int G, int hkv, CrossPlan* p) {
+  int64_t tiles = 0, total = 0;
+  for (int b = 0; b < bt.B; ++b) {
+    const int64_t live = (int64_t)bt.rows[b].valid * G;
+    const int64_t n = enc[b].len > 0 ? ceil_div(live, kCrossRows) : 0;
+    tiles += n;
+    total += n * ceil_div(enc[b].len, kCrossKeyUnit);
+  }
+  const int64_t most = cross_part(tiles, total, hkv);
+  int32_t blk0 = 0;
+  for (int b = 0; b < bt.B; ++b) {
+    const Row& r = bt.rows[b];
+    const int32_t rows = r.T * G, live = r.valid * G;
+    const int64_t units = ceil_div(enc[b].len, kCrossKeyUnit);
+    for (int32_t r0 = 0; r0 < rows; r0 += kCrossRows) {
+      CrossItem it{r.tok0, r0, rows, live, enc[b].start, enc[b].len, 0, r0 < live ? enc[b].len : 0, -1, blk0};
+      const int64_t parts = r0 < live && units > 0 ? ceil_div(units, most) : 1;
+      if (parts == 1) {
+        p->items.push_back(it);
+        continue;
+      }
+      p->splits.push_back(CrossSplit{r.tok0, r0, rows, live, p->slots, (int32_t)parts});
+      for (int64_t i = 0; i < parts; ++i) {
+        it.k_begin = (int32_t)(units * i / parts * kCrossKeyUnit);
+        it.k_end = (int32_t)std::min<int64_t>(enc[b].len, units * (i + 1) / parts * kCrossKeyUnit);
+        it.slot = p->slots++;
+        p->items.push_back(it);
+      }
+    }
+    blk0 += (int32_t)ceil_div(live, 32);
+  }
+  p->blocks = blk0;
+  std::stable_sort(p->items.begin(), p->items.end(),
+                   [](const CrossItem& a, const CrossItem& b) { return a.k_end - a.k_begin > b.k_end - b.k_begin; });
+}
+
+// Key tiles against the rows, most steps first.
+void build_cross_kv(const Batch& bt, const std::vector<EncRow>& enc, int G, int hkv, int step, CrossPlan* p) {
+  int64_t tiles = 0, total = 0;
+  for (int b = 0; b < bt.B; ++b) {
+    const int64_t live = (int64_t)bt.rows[b].valid * G;
+    const int64_t n = live > 0 ? ceil_div(enc[b].len, kCrossKeys) : 0;
+    tiles += n;
+    total += n * ceil_div(live, step);
+  }
+  const int64_t most = cross_part(tiles, total, hkv);
+  int32_t blk0 = 0;
+  for (int b = 0; b < bt.B; ++b) {
+    const Row& r = bt.rows[b];
+    const int32_t live = r.valid * G;
+    const int64_t steps = ceil_div(live, step);
+    for (int32_t k0 = 0; k0 < enc[b].cap; k0 += kCrossKeys) {
+      CrossKvItem it{r.tok0, live, enc[b].start, k0, enc[b].len, enc[b].cap, 0, k0 < enc[b].len ? (int32_t)steps : 0, -1, blk0};
+      const int64_t parts = it.n_end > 0 ? ceil_div(steps, most) : 1;
+      if (parts == 1) {
+        p->kv_items.push_back(it);
+        continue;
+      }
+      p->kv_splits.push_back(CrossKvSplit{enc[b].start, k0, enc[b].len, enc[b].cap, p->kv_slots, (int32_t)parts});
+      for (int64_t i = 0; i < parts; ++i) {
+        it.n_begin = (int32_t)(steps * i / parts);
+        it.n_end = (int32_t)(steps * (i + 1) / parts);
+        it.slot = p->kv_slots++;
+        p->kv_items.push_back(it);
+      }
+    }
+    blk0 += (int32_t)ceil_div(live, 32);
+  }
+  std::stable_sort(p->kv_items.begin(), p->kv_items.end(), [](const CrossKvItem& a, const CrossKvItem& b) {
+    return a.n_end - a.n_begin > b.n_end - b.n_begin;
+  });
+}
+
+void plan_cross_fwd(const Batch& bt, const std::vector<EncRow>& enc, int hq, int hkv, int d, CrossPlan* p) {
+  build_cross_items(bt, enc, hq / hkv, hkv, p);
+  p->inline_items = p->items.size() <= (size_t)kCrossInline;  // and at most half as many splits
+  if (!p->inline_items) {
+    p->r_items = p->lay.add(p->items.size() * sizeof(CrossItem));
+    p->r_splits = p->lay.add(p->splits.size() * sizeof(CrossSplit));
+  }
+  p->lay.meta_bytes = p->lay.total;
+  p->r_part = p->lay.add((size_t)p->slots * hkv * kCrossRows * d * 4);
+  p->r_ml = p->lay.add((size_t)p->slots * hkv * kCrossRows * 8);
+}
+
+void plan_cross_bwd(const Batch& bt, const std::vector<EncRow>& enc, pp_dtype dtype, int hq, int hkv, int d, CrossPlan* p) {
+  build_cross_items(bt, enc, hq / hkv, hkv, p);
+  build_cross_kv(bt, enc, hq / hkv, hkv, dtype == PP_FP32 ? 32 : 64, p);
+  p->r_items = p->lay.add(p->items.size() * sizeof(CrossItem));
+  p->r_splits = p->lay.add(p->splits.size() * sizeof(CrossSplit));
+  p->r_kv_items = p->lay.add(p->kv_items.size() * sizeof(CrossKvItem));
+  p->r_kv_splits = p->lay.add(p->kv_splits.size() * sizeof(CrossKvSplit));
+  p->lay.meta_bytes = p->lay.total;
+  p->r_ndelta = p->lay.add((size_t)bt.sumT * hq * 4);
+  p->r_nlse2 = p->lay.add((size_t)bt.sumT * hq * 4);
+  p->r_ranges = p->lay.add((size_t)p->blocks * sizeof(CrossRange));
+  // one pass's partial sums are joined before the next pass runs
+  p->r_part = p->lay.add(std::max((size_t)p->slots * hkv * kCrossRows * d * 4, (size_t)p->kv_slots * hkv * kCrossKeys * d * 8));
+}
+
+// What both directions check, and the row's limits: a packed row's rows are counted in
+// 32 bits, a launch's threads too.
+pp_status check_cross(const pp_pack_desc* desc, const pp_enc_desc* enc, pp_dtype dtype, int hq, int hkv, int head_dim, Batch* bt,
+                      std::vector<EncRow>* rows) {
+  pp_status st = read_desc(desc, bt);
+  if (st != PP_OK) return st;
+  if ((st = read_enc(enc, *bt, rows)) != PP_OK) return st;
+  if ((st = check_heads(hq, hkv, head_dim)) != PP_OK) return st;
+  if ((st = check_dtype(dtype)) != PP_OK) return st;
+  if (hq > 4096) return fail(PP_ERR_UNSUPPORTED, "cross attention takes at most 4096 query heads (got %d)", hq);
+  const int64_t G = hq / hkv;
+  int64_t groups = 0;
+  for (int b = 0; b < bt->B; ++b) {
+    if (bt->rows[b].T * G > INT32_MAX - kCrossRows)
+      return fail(PP_ERR_UNSUPPORTED, "row %d: %d tokens of %lld heads a kv-head exceed 2^31 rows", b, bt->rows[b].T, (long long)G);
+    if ((*rows)[b].cap > INT32_MAX - kCrossKeys) return fail(PP_ERR_UNSUPPORTED, "row %d has too many encoder states", b);
+    groups += ceil_div(bt->rows[b].T * G, kCrossRows) + ceil_div((*rows)[b].cap, kCrossKeys);
+  }
+  // a launch holds fewer than 2^32 threads, 512 a workgroup; splitting adds at most 4 * kCrossGroups workgroups
+  if (groups * hkv > 0xffffffffll / 512 - 4 * kCrossGroups)
+    return fail(PP_ERR_UNSUPPORTED, "the batch has too many tiles for one launch");
+  return PP_OK;
+}
+
+pp_status check_cross_ws(const Layout& lay, const void* ws, size_t ws_bytes) {
+  if (ws_bytes < lay.total)
+    return fail(PP_ERR_WORKSPACE_TOO_SMALL, "cross attention needs %zu workspace bytes, got %zu", lay.total, ws_bytes);
+  if (lay.total && !ws) return fail(PP_ERR_INVALID_ARGUMENT, "ws is NULL");
+  if (ws && !aligned256(ws)) return fail(PP_ERR_INVALID_ARGUMENT, "ws must be 256-byte aligned");
+  return PP_OK;
+}
+
+pp_status check_ranges(const int32_t* key_begin, const int32_t* key_end) {
+  if (!key_begin != !key_end) return fail(PP_ERR_INVALID_ARGUMENT, "key_begin and key_end must be given together");
+  if (!aligned4(key_begin) || !aligned4(key_end))
+    return fail(PP_ERR_INVALID_ARGUMENT, "key_begin and key_end must be 4-byte aligned");
+  return PP_OK;
+}
+
+inline float scale_or_default(float scale, int head_dim) {
+  return scale > 0.f ? scale : 1.0f / std::sqrt((float)head_dim);
+}
+
+// Runs a C entry's body: nothing is thrown through it.
+template <typename Body>
+pp_status guarded(Body&& body) {
+  try {
+    return body();
+  } catch (const std::bad_alloc&) {
+    return fail(PP_ERR_INVALID_ARGUMENT, "out of host memory for the batch's plan");
+  } catch (const std::exception& e) {
+    return fail(PP_ERR_INVALID_ARGUMENT, "%s", e.what());
+  }
+}
+
+}  // namespace
+}  // namespace pp
+
+extern "C" {
+
+pp_status pp_cross_workspace_size(const pp_pack_desc* desc, const pp_enc_desc* enc, pp_dtype dtype, int hq, int hkv,
+                                  int head_dim, size_t* fwd, size_t* bwd) {
+  return guarded([&]() -> pp_status {
+    Batch bt;
+    std::vector<EncRow> er;
+    const pp_status st = check_cross(desc, enc, dtype, hq, hkv, head_dim, &bt, &er);
+    if (st != PP_OK) return st;
+    if (fwd) {
+      CrossPlan p;
+      plan_cross_fwd(bt, er, hq, hkv, head_dim, &p);
+      *fwd = p.lay.total;
+    }
+    if (bwd) {
+      CrossPlan p;
+      plan_cross_bwd(bt, er, dtype, hq, hkv, head_dim, &p);
+      *bwd = p.lay.total;
+    }
+    return PP_OK;
+  });
+}
+
+pp_status pp_cross_attn_fwd(const pp_pack_desc* desc, const pp_enc_desc* enc, pp_dtype dtype, int hq, int hkv, int head_dim,
+                            float scale, const void* q, const void* k, const void* v, const int32_t* key_begin,
+                            const int32_t* key_end, void* o, float* lse, void* ws, size_t ws_bytes, void* hip_stream) {
+  return guarded([&]() -> pp_status {
+    Batch bt;
+    std::vector<EncRow> er;
+    pp_status st = check_cross(desc, enc, dtype, hq, hkv, head_dim, &bt, &er);
+    if (st != PP_OK) return st;
+    const int sumE = er.back().start + er.back().cap;
+    if (bt.sumT > 0 && (!q || !o || !lse)) return fail(PP_ERR_INVALID_ARGUMENT, "q, o and lse must be non-NULL");
+    if (sumE > 0 && (!k || !v)) return fail(PP_ERR_INVALID_ARGUMENT, "k and v must be non-NULL");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned4(lse))
+      return fail(PP_ERR_INVALID_ARGUMENT, "q, k, v and o must be 16-byte aligned, lse 4-byte aligned");
+    if ((st = check_ranges(key_begin, key_end)) != PP_OK) return st;
+    CrossPlan p;
+    plan_cross_fwd(bt, er, hq, hkv, head_dim, &p);
+    if ((st = check_cross_ws(p.lay, ws, ws_bytes)) != PP_OK) return st;
+    if (bt.sumT == 0) return PP_OK;
+    hipStream_t s = (hipStream_t)hip_stream;
+    CrossLaunch a{};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.out = o;
+    a.lse = lse;
+    a.key_begin = key_begin;
+    a.key_end = key_end;
+    a.host_items = p.items.data();
+    a.host_splits = p.splits.data();
+    a.n_items = (int)p.items.size();
+    a.n_splits = (int)p.splits.size();
+    a.part = (float*)at(ws, p.lay, p.r_part);
+    a.part_ml = (float*)at(ws, p.lay, p.r_ml);
+    a.hq = hq;
+    a.hkv = hkv;
+    a.head_dim = head_dim;
+    a.sumT = bt.sumT;
+    a.scale = scale_or_default(scale, head_dim);
+    a.dtype = dtype == PP_FP32 ? kFP32 : kBF16;
+    if (!p.inline_items) {
+      MetaImage img;
+      img.put(p.lay.regions[p.r_items], p.items.data(), p.items.size() * sizeof(CrossItem));
+      img.put(p.lay.regions[p.r_splits], p.splits.data(), p.splits.size() * sizeof(CrossSplit));
+      if ((st = stage_copy(ws, img.buf.data(), img.buf.size(), s)) != PP_OK) return st;
+      a.items = (const CrossItem*)at(ws, p.lay, p.r_items);
+      a.splits = (const CrossSplit*)at(ws, p.lay, p.r_splits);
+    }
+    const hipError_t e = launch_cross_fwd(a, s);
+    return e == hipSuccess ? PP_OK : hip_fail(e, "cross attention forward launch");
+  });
+}
+
+pp_status pp_cross_attn_bwd(const pp_pack_desc* desc, const pp_enc_desc* enc, pp_dtype dtype, int hq, int hkv, int head_dim,
+                            float scale, const void* q, const void* k, const void* v, const int32_t* key_begin,
+                            const int32_t* key_end, const void* o, const float* lse, const void* dout, void* dq, void* dk,
+                            void* dv, void* ws, size_t ws_bytes, void* hip_stream) {
+  return guarded([&]() -> pp_status {
+    Batch bt;
+    std::vector<EncRow> er;
+    pp_status st = check_cross(desc, enc, dtype, hq, hkv, head_dim, &bt, &er);
+    if (st != PP_OK) return st;
+    const int sumE = er.back().start + er.back().cap;
+    if (bt.sumT > 0 && (!q || !o || !lse || !dout || !dq))
+      return fail(PP_ERR_INVALID_ARGUMENT, "q, o, lse, dout and dq must be non-NULL");
+    if (sumE > 0 && (!k || !v || !dk || !dv)) return fail(PP_ERR_INVALID_ARGUMENT, "k, v, dk and dv must be non-NULL");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || !aligned16(dout) || !aligned16(dq) ||
+        !aligned16(dk) || !aligned16(dv) || !aligned4(lse))
+      return fail(PP_ERR_INVALID_ARGUMENT, "q, k, v, o, dout, dq, dk and dv must be 16-byte aligned, lse 4-byte aligned");
+    if ((st = check_ranges(key_begin, key_end)) != PP_OK) return st;
+    CrossPlan p;
+    plan_cross_bwd(bt, er, dtype, hq, hkv, head_dim, &p);
+    if ((st = check_cross_ws(p.lay, ws, ws_bytes)) != PP_OK) return st;
+    if (p.lay.total == 0) return PP_OK;
+    hipStream_t s = (hipStream_t)hip_stream;
+    MetaImage img;
+    img.put(p.lay.regions[p.r_items], p.items.data(), p.items.size() * sizeof(CrossItem));
+    img.put(p.lay.regions[p.r_splits], p.splits.data(), p.splits.size() * sizeof(CrossSplit));
+    img.put(p.lay.regions[p.r_kv_items], p.kv_items.data(), p.kv_items.size() * sizeof(CrossKvItem));
+    img.put(p.lay.regions[p.r_kv_splits], p.kv_splits.data(), p.kv_splits.size() * sizeof(CrossKvSplit));
+    if ((st = stage_copy(ws, img.buf.data(), img.buf.size(), s)) != PP_OK) return st;
+    CrossLaunch a{};
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.out = dq;
+    a.o_in = o;
+    a.lse_in = lse;
+    a.dout = dout;
+    a.dk = dk;
+    a.dv = dv;
+    a.key_begin = key_begin;
+    a.key_end = key_end;
+    a.items = (const CrossItem*)at(ws, p.lay, p.r_items);
+    a.splits = (const CrossSplit*)at(ws, p.lay, p.r_splits);
+    a.kv_items = (const CrossKvItem*)at(ws, p.lay, p.r_kv_items);
+    a.kv_splits = (const CrossKvSplit*)at(ws, p.lay, p.r_kv_splits);
+    a.n_items = (int)p.items.size();
+    a.n_splits = (int)p.splits.size();
+    a.n_kv_items = (int)p.kv_items.size();
+    a.n_kv_splits = (int)p.kv_splits.size();
+    a.part = a.kv_part = (float*)at(ws, p.lay, p.r_part);
+    a.ndelta = (float*)at(ws, p.lay, p.r_ndelta);
+    a.nlse2 = (float*)at(ws, p.lay, p.r_nlse2);
+    a.ranges = (CrossRange*)at(ws, p.lay, p.r_ranges);
+    a.hq = hq;
+    a.hkv = hkv;
+    a.head_dim = head_dim;
+    a.sumT = bt.sumT;
+    a.scale = scale_or_default(scale, head_dim);
+    a.dtype = dtype == PP_FP32 ? kFP32 : kBF16;
+    const hipError_t e = launch_cross_bwd(a, s);
+    return e == hipSuccess ? PP_OK : hip_fail(e, "cross attention backward launch");
+  });
+}
+
+}  // extern "C"

@@ -151,6 +151,43 @@ struct AttnBwdLaunch {
 };
 hipError_t launch_attn_bwd(const AttnBwdLaunch& a, hipStream_t s);
 
+// Cross attention; every tensor has dtype `dtype`.
+struct CrossLaunch {
+  const void* q;
+  const void* k;
+  const void* v;
+  void* out;                 // forward: o, backward: dq
+  float* lse;                // forward
+  const void* o_in = nullptr;
+  const float* lse_in = nullptr;
+  const void* dout = nullptr;
+  void* dk = nullptr;
+  void* dv = nullptr;
+  const int32_t* key_begin;  // [sumT] or null
+  const int32_t* key_end;
+  // device records, or null: the host records ride in the launch's arguments (forward)
+  const CrossItem* items;
+  const CrossSplit* splits;
+  const CrossItem* host_items;
+  const CrossSplit* host_splits;
+  int n_items, n_splits;
+  const CrossKvItem* kv_items = nullptr;
+  const CrossKvSplit* kv_splits = nullptr;
+  int n_kv_items = 0, n_kv_splits = 0;
+  float* part;               // partial rows of split items, [slot][hkv][kCrossRows][head_dim]
+  float* part_ml;            // forward: their maximum and sum
+  float* kv_part = nullptr;  // [slot][hkv][2][kCrossKeys * head_dim]
+  float* ndelta = nullptr;   // [hkv][sumT G]
+  float* nlse2 = nullptr;
+  CrossRange* ranges = nullptr;
+  int hq, hkv, head_dim;
+  int sumT;
+  float scale;
+  int dtype;
+};
+hipError_t launch_cross_fwd(const CrossLaunch& a, hipStream_t s);
+hipError_t launch_cross_bwd(const CrossLaunch& a, hipStream_t s);
+
 // y = rotation of x by each token's position ([sumT, heads, head_dim], dtype);
 // inverse rotates by the negative angle.  y may equal x.
 struct RopeLaunch {

@@ -172,4 +172,56 @@ struct RespItem {
   int32_t pad;
 };
 
+// ---- cross attention (pp_cross.hip): the tokens of a packed row and the heads of a
+// kv-head's group are one list of rows, row r = token r / G, head r % G
+
+constexpr int kCrossRows = 128;    // rows per forward and dQ workgroup
+constexpr int kCrossKeys = 128;    // keys per dK/dV workgroup
+constexpr int kCrossKeyUnit = 64;  // parts of a row's keys are multiples of this
+constexpr int kCrossInline = 64;   // forward items that fit into the launch's arguments
+
+// Rows [r0, min(r0 + tile, rows)) of a packed row against the keys [k_begin, k_end) of its states.
+struct CrossItem {
+  int32_t tok0;     // flat index of the packed row's first token
+  int32_t r0;
+  int32_t rows;     // rows of the packed row, padding included
+  int32_t live;     // rows of its real tokens
+  int32_t e0;       // flat index of its first state
+  int32_t elen;     // its states
+  int32_t k_begin;
+  int32_t k_end;
+  int32_t slot;     // where the partial sums go, or -1: this item has all the keys
+  int32_t blk0;     // index of the packed row's first block of 32 rows
+};
+
+// A tile of rows whose keys are split: its parts sit in consecutive slots.
+struct CrossSplit {
+  int32_t tok0, r0, rows, live;
+  int32_t slot0, parts;
+};
+struct CrossSplitList {
+  CrossSplit split[kCrossInline / 2];
+};
+
+// Keys [k0, k0 + kCrossKeys) of a packed row's states against the row steps [n_begin, n_end).
+struct CrossKvItem {
+  int32_t tok0, live;
+  int32_t e0, k0;
+  int32_t elen;     // states of the packed row
+  int32_t ecap;     // with their padding
+  int32_t n_begin, n_end;
+  int32_t slot;     // or -1
+  int32_t blk0;
+};
+struct CrossKvSplit {
+  int32_t e0, k0, elen, ecap;
+  int32_t slot0, parts;
+};
+
+// What a block of 32 rows sees: no row a key outside [any_lo, any_hi), every real row
+// all of [all_lo, all_hi).
+struct CrossRange {
+  int32_t any_lo, any_hi, all_lo, all_hi;
+};
+
 }  // namespace pp

@@ -92,6 +92,31 @@ def make_pack(prompt_lens: Sequence[int], resp_lens: Sequence[Sequence[int]],
     return Pack(row_start, prompt, num, off, ln)
 
 
+@dataclasses.dataclass
+class Enc:
+    """Host description of the encoder states that a packed batch's rows look at
+    (int32 numpy arrays): row b's are [enc_start[b], enc_start[b] + enc_len[b])
+    of one axis, padding after them."""
+
+    enc_start: np.ndarray  # [B+1]
+    enc_len: np.ndarray    # [B]
+
+    @property
+    def total_states(self) -> int:
+        return int(self.enc_start[-1])
+
+
+def make_enc(lens: Sequence[int], pad: Optional[Sequence[int]] = None) -> Enc:
+    """Lay out encoder states: lens[b] of row b, then pad[b] entries of padding."""
+    ln = np.asarray(lens, np.int32).reshape(-1)
+    cap = ln.astype(np.int64) + (0 if pad is None else np.asarray(pad, np.int64).reshape(-1))
+    start = np.zeros(ln.shape[0] + 1, np.int64)
+    np.cumsum(cap, out=start[1:])
+    if start[-1] > np.iinfo(np.int32).max:
+        raise ValueError("the encoder states of a batch must be fewer than 2^31")
+    return Enc(start.astype(np.int32), ln)
+
+
 # ----------------------------------------------------------------------------
 # The five synthetic configurations
 # ----------------------------------------------------------------------------
