@@ -19,6 +19,9 @@
  *   pp_rope, pp_attn_fwd_rope, pp_attn_bwd_rope
  *                   rotary position embedding on the packed position IDs
  *                   (Sec. 3.2), alone or fused into attention
+ *   pp_tok_logprob  log-probs and entropies token by token, and their gradient
+ *   pp_policy_loss  clipped policy loss over the K responses of each row, with a KL
+ *                   and an entropy term, and its gradient
  *   pp_cross_attn_fwd, pp_cross_attn_bwd
  *                   attention of packed rows to an encoder's states
  *   pp_plan_create, pp_attn_fwd_planned, pp_attn_bwd_planned
@@ -436,6 +439,84 @@ pp_status pp_cross_attn_bwd(const pp_pack_desc* desc, const pp_enc_desc* enc, pp
                             float scale, const void* q, const void* k, const void* v, const int32_t* key_begin,
                             const int32_t* key_end, const void* o, const float* lse, const void* dout, void* dq, void* dk,
                             void* dv, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Log-probs of the response tokens one by one, and the entropies of the
+ * distributions that predict them, over the packed layout (pp_seq_logprob's
+ * gathering, without its sums):
+ *   tok_logp[t]    = log softmax(row)[tokens[t]],  row the logits that predict t
+ *   tok_entropy[t] = -sum_v softmax(row)[v] log softmax(row)[v]
+ * for response tokens t, 0 elsewhere (dev float [sumT]; tok_entropy may be NULL).
+ * Every response's first token is predicted by the last prompt row.  Entries of
+ * -inf or of the type's lowest value are masked ones: they count nothing.  A
+ * label outside the vocabulary gives NaN (its entropy stands).
+ * ws_bytes >= pp_workspace_size's logprob, here and in the gradients. */
+pp_status pp_tok_logprob(const pp_pack_desc* desc, pp_dtype logits_dtype, int vocab, const void* logits, const int32_t* tokens,
+                         float* tok_logp, float* tok_entropy, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Gradient with respect to the logits of
+ *   sum_t dtok[t] tok_logp[t] + dentropy[t] tok_entropy[t]
+ * over the response tokens (dtok, dentropy dev float [sumT], read there only;
+ * dentropy may be NULL): all of [sumT, vocab] (0 on rows that predict nothing), or
+ * the predicting rows only, as pp_seq_logprob_bwd_rows lists them.  A label
+ * outside the vocabulary makes its row NaN.  At most 256 responses a row. */
+pp_status pp_tok_logprob_bwd(const pp_pack_desc* desc, pp_dtype logits_dtype, int vocab, const void* logits,
+                             const int32_t* tokens, const float* dtok, const float* dentropy, void* dlogits, void* ws,
+                             size_t ws_bytes, void* hip_stream);
+pp_status pp_tok_logprob_bwd_rows(const pp_pack_desc* desc, pp_dtype logits_dtype, int vocab, const void* logits,
+                                  const int32_t* tokens, const float* dtok, const float* dentropy, void* dlogits_rows,
+                                  int32_t* row_index, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Estimators of the KL term, of x = logp_ref - logp. */
+typedef enum pp_kl {
+  PP_KL_K1 = 0,  /* -x */
+  PP_KL_K2 = 1,  /* x^2 / 2 */
+  PP_KL_K3 = 2,  /* e^x - 1 - x */
+  PP_KL_RANGE_MIN_ = -0x7fffffff - 1,
+  PP_KL_RANGE_MAX_ = 0x7fffffff
+} pp_kl;
+
+/* Weight of a counted token in the loss. */
+typedef enum pp_reduction {
+  PP_REDUCE_TOKEN = 0,  /* 1 / counted tokens of the batch */
+  PP_REDUCE_SEQ = 1,    /* 1 / (responses with a counted token x the response's counted tokens) */
+  PP_REDUCE_SUM = 2,    /* 1 / norm */
+  PP_REDUCE_RANGE_MIN_ = -0x7fffffff - 1,
+  PP_REDUCE_RANGE_MAX_ = 0x7fffffff
+} pp_reduction;
+
+typedef struct pp_policy_config {
+  double clip_low;    /* in [0, 1]: ratios are clipped to [1 - clip_low, 1 + clip_high] */
+  double clip_high;   /* >= 0 */
+  double dual_clip;   /* 0: none; else > 1: with a negative advantage A the surrogate is no less than dual_clip A */
+  double kl_coef;     /* needs logp_ref if not 0 */
+  double ent_coef;    /* needs entropy if not 0 */
+  double norm;        /* PP_REDUCE_SUM only: > 0 */
+  pp_kl kl;
+  pp_reduction reduction;
+} pp_policy_config;
+
+/* Clipped policy loss of the responses' tokens, a row's K responses being a group
+ * sampled from its prompt.  For every counted token t (of a response, and with
+ * mask[t] != 0 if there is a mask), r = exp(logp - logp_old) and A its advantage:
+ *   *loss = sum_t w_t (-min(r A, clip(r) A) + kl_coef KL_t - ent_coef entropy_t)
+ * with the dual clip, KL estimator and weight w of cfg.
+ *   logp, logp_old, logp_ref, entropy   dev float [sumT] (pp_tok_logprob's outputs);
+ *     logp_old NULL: the responses were sampled from this very policy, r = 1 with
+ *     the gradient of r; logp_ref NULL: no KL; entropy NULL: none
+ *   adv    dev float [B * K_max], or [sumT] with adv_per_token
+ *   mask   dev uint8 [sumT] or NULL; what it leaves out is not looked at
+ *   stats  dev float [4] or NULL: sum_t w_t of -min(...), KL, entropy and r
+ *   counts dev int32 [2] or NULL: counted tokens, and those that a clip holds
+ *   dlogp, dentropy  dev float [sumT] or NULL: the loss's gradients, all of them
+ *     written (0 off the counted tokens); a clipped token's gradient is its KL's.
+ * Terms and sums are formed in 64 bits.  Without a counted token the loss is 0.
+ * ws_bytes >= pp_policy_workspace_size's bytes.  Float and int32 arrays must be
+ * 4-byte aligned. */
+pp_status pp_policy_workspace_size(const pp_pack_desc* desc, size_t* bytes);
+pp_status pp_policy_loss(const pp_pack_desc* desc, const pp_policy_config* cfg, const float* logp, const float* logp_old,
+                         const float* logp_ref, const float* entropy, const float* adv, int adv_per_token, const uint8_t* mask,
+                         float* loss, float* stats, int32_t* counts, float* dlogp, float* dentropy, void* ws, size_t ws_bytes,
+                         void* hip_stream);
 
 /* Host-only export of the planner's integer view of a batch (no GPU needed):
  *   position_ids[sumT]  prompt token t -> t, response token j -> P_b + j,

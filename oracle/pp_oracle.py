@@ -652,3 +652,100 @@ def cross_attn(row_start, prompt_len, num_resp, resp_off, resp_len, enc_start, e
                 dk[e0:e0 + E, g] += tau * dS.T @ q[rows, h]
                 dv[e0:e0 + E, g] += P.T @ g_o
     return (o, lse) if dout is None else (o, lse, dq, dk, dv)
+
+
+# ---------------------------------------------------------------------------
+# Policy optimisation: token log-probs with entropies, and the clipped policy loss
+# ---------------------------------------------------------------------------
+
+
+def response_tokens(row_start, prompt_len, num_resp, resp_off, resp_len):
+    """[(predicting flat row, flat position, row b, response k)] of every response token."""
+    out = []
+    for b in range(len(prompt_len)):
+        t0 = int(row_start[b])
+        for k in range(int(num_resp[b])):
+            o = t0 + int(resp_off[b][k])
+            for j in range(int(resp_len[b][k])):
+                out.append((t0 + int(prompt_len[b]) - 1 if j == 0 else o + j - 1, o + j, b, k))
+    return out
+
+
+def _row_softmax(x):
+    """(p, log p) of one logit row; masked entries (-inf) have p = 0 and log p = -inf."""
+    m = x.max()
+    z = np.exp(x - m).sum()
+    lp = (x - m) - np.log(z)
+    return np.exp(lp), lp
+
+
+def tok_logprob(row_start, prompt_len, num_resp, resp_off, resp_len, logits, tokens):
+    """(log-probs, entropies) of the response tokens, [T] each, 0 elsewhere."""
+    tok, ent = np.zeros(logits.shape[0]), np.zeros(logits.shape[0])
+    for r, t, _, _ in response_tokens(row_start, prompt_len, num_resp, resp_off, resp_len):
+        p, lp = _row_softmax(logits[r])
+        y = int(tokens[t])
+        tok[t] = lp[y] if 0 <= y < logits.shape[1] else np.nan
+        some = p > 0
+        ent[t] = -(p[some] * lp[some]).sum()
+    return tok, ent
+
+
+def tok_logprob_grad(row_start, prompt_len, num_resp, resp_off, resp_len, logits, tokens, dtok, dent=None):
+    """Gradient of sum_t dtok[t] tok[t] + dent[t] ent[t] with respect to the logits, term by term."""
+    out = np.zeros(logits.shape)
+    for r, t, _, _ in response_tokens(row_start, prompt_len, num_resp, resp_off, resp_len):
+        p, lp = _row_softmax(logits[r])
+        y = int(tokens[t])
+        if not 0 <= y < logits.shape[1]:
+            out[r] = np.nan
+            continue
+        out[r] -= dtok[t] * p
+        out[r, y] += dtok[t]
+        if dent is not None:
+            some = p > 0
+            H = -(p[some] * lp[some]).sum()
+            out[r, some] -= dent[t] * p[some] * (lp[some] + H)
+    return out
+
+
+def policy_loss(row_start, prompt_len, num_resp, resp_off, resp_len, logp, adv, old=None, ref=None, entropy=None, mask=None,
+                clip_low=0.2, clip_high=0.2, dual_clip=0.0, kl_coef=0.0, kl="k3", ent_coef=0.0, reduction="token", norm=1.0):
+    """(loss, stats [4], counts [2], dlogp [T], dentropy [T]) token by token; adv [B, K] or [T]."""
+    toks = [(t, b, k) for _, t, b, k in response_tokens(row_start, prompt_len, num_resp, resp_off, resp_len)
+            if mask is None or mask[t]]
+    per = {}
+    for _, b, k in toks:
+        per[b, k] = per.get((b, k), 0) + 1
+    T = len(logp)
+    dlogp, dent, stats, clipped = np.zeros(T), np.zeros(T), np.zeros(4), 0
+    loss = 0.0
+    for t, b, k in toks:
+        w = {"token": 1.0 / len(toks), "seq": 1.0 / (len(per) * per[b, k]), "sum": 1.0 / norm}[reduction]
+        A = float(adv[t] if np.ndim(adv) == 1 else adv[b][k])
+        r = np.exp(float(logp[t]) - float(old[t])) if old is not None else 1.0
+        options = {"ratio": r * A, "clip": min(max(r, 1 - clip_low), 1 + clip_high) * A}
+        which = "clip" if options["clip"] < options["ratio"] else "ratio"
+        surr = options[which]
+        if dual_clip and A < 0 and surr < dual_clip * A:
+            which, surr = "dual", dual_clip * A
+        g = -A * r if which == "ratio" else 0.0
+        clipped += which != "ratio"
+        term = div = 0.0
+        if ref is not None:
+            x = float(ref[t]) - float(logp[t])
+            div, dd = {"k1": (-x, 1.0), "k2": (x * x / 2, -x), "k3": (np.expm1(x) - x, -np.expm1(x))}[kl]
+            if kl_coef:
+                g += kl_coef * dd
+                term += kl_coef * div
+        if entropy is not None:
+            stats[2] += w * float(entropy[t])
+            if ent_coef:
+                term -= ent_coef * float(entropy[t])
+        dlogp[t] = w * g
+        dent[t] = -w * ent_coef
+        stats[0] -= w * surr
+        stats[1] += w * div
+        stats[3] += w * r
+        loss += w * (-surr + term)
+    return loss, stats, np.array([len(toks), clipped]), dlogp, dent

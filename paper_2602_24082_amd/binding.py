@@ -37,6 +37,7 @@ EXPORTED = [
     "pp_attn_fwd_noalloc", "pp_build_id", "pp_logprob_row_count", "pp_seq_logprob_bwd_rows",
     "pp_bwd_stored_ds_workspace_size",
     "pp_cross_workspace_size", "pp_cross_attn_fwd", "pp_cross_attn_bwd",
+    "pp_tok_logprob", "pp_tok_logprob_bwd", "pp_tok_logprob_bwd_rows", "pp_policy_workspace_size", "pp_policy_loss",
 ]
 
 NOALLOC_SCRATCH_BYTES = 4 << 20  # PP_NOALLOC_SCRATCH_BYTES
@@ -71,6 +72,11 @@ class _Desc(ctypes.Structure):
 
 class _EncDesc(ctypes.Structure):
     _fields_ = [("enc_start", ctypes.POINTER(ctypes.c_int32)), ("enc_len", ctypes.POINTER(ctypes.c_int32))]
+
+
+class _PolicyConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_double) for n in ("clip_low", "clip_high", "dual_clip", "kl_coef", "ent_coef", "norm")] + [
+        ("kl", ctypes.c_int), ("reduction", ctypes.c_int)]
 
 
 _lib = None
@@ -125,6 +131,11 @@ def lib() -> ctypes.CDLL:
     L.pp_cross_workspace_size.argtypes = [D, E, i, i, i, i, ctypes.POINTER(sz), ctypes.POINTER(sz)]
     L.pp_cross_attn_fwd.argtypes = [D, E, i, i, i, i, f32, P, P, P, P, P, P, P, P, sz, P]
     L.pp_cross_attn_bwd.argtypes = [D, E, i, i, i, i, f32, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]
+    L.pp_tok_logprob.argtypes = [D, i, i, P, P, P, P, P, sz, P]
+    L.pp_tok_logprob_bwd.argtypes = [D, i, i, P, P, P, P, P, P, sz, P]
+    L.pp_tok_logprob_bwd_rows.argtypes = [D, i, i, P, P, P, P, P, P, P, sz, P]
+    L.pp_policy_workspace_size.argtypes = [D, ctypes.POINTER(sz)]
+    L.pp_policy_loss.argtypes = [D, ctypes.POINTER(_PolicyConfig), P, P, P, P, P, i, P, P, P, P, P, P, P, sz, P]
     L.pp_pack_export.argtypes = [D, i, i, P, P, P, sz]
     L.pp_tile_class_len.argtypes = [D, i, i, ctypes.POINTER(sz)]
     L.pp_timing_enable.argtypes = [i]
@@ -686,6 +697,120 @@ def pp_cross_attn_bwd(pack: Pack, enc: Enc, q, k, v, o, lse, dout, scale: float 
                                        _ptr(key_begin), _ptr(key_end), _ptr(o), _ptr(lse), _ptr(dout), _ptr(dq), _ptr(dk),
                                        _ptr(dv), _ptr(ws), ws.numel(), _stream(dev)))
     return dq, dk, dv
+
+
+# ---------------------------------------------------------------- policy optimisation
+
+
+def _tok_args(pack: Pack, logits, tokens, **per_token):
+    """Checks the inputs of the per-token log-probs; (pack holder, dtype code, vocab)."""
+    T = max(0, pack.total_tokens)
+    if logits.dim() != 2:
+        raise ValueError("logits must be [sumT, vocab]")
+    _check_tensor("logits", logits, (T, logits.shape[1]), logits.dtype, logits.device)
+    _check_tensor("tokens", tokens, (T,), torch.int32, logits.device)
+    for name, t in per_token.items():
+        if t is not None:
+            _check_tensor(name, t, (T,), torch.float32, logits.device)
+    dt = _dtype_code(logits)
+    _on_gpu(logits)
+    return _desc_of(pack), dt, logits.shape[1]
+
+
+def pp_tok_logprob(pack: Pack, logits: torch.Tensor, tokens: torch.Tensor, want_entropy: bool = False, tok=None,
+                   entropy=None, ws=None):
+    """Log-probs of the response tokens and, if asked for (else None), the entropies
+    of their distributions: ([sumT], [sumT]) fp32, 0 off the responses."""
+    h, dt, V = _tok_args(pack, logits, tokens, tok=tok, entropy=entropy)
+    dev = logits.device
+    tok = torch.empty(logits.shape[0], dtype=torch.float32, device=dev) if tok is None else tok
+    if want_entropy and entropy is None:
+        entropy = torch.empty(logits.shape[0], dtype=torch.float32, device=dev)
+    if ws is None:
+        ws = _workspace(_workspace_sizes(h, vocab=V, logprob=True)[2], dev)
+    with torch.cuda.device(dev):
+        _check(lib().pp_tok_logprob(h.ref, dt, V, _ptr(logits), _ptr(tokens), _ptr(tok), _ptr(entropy), _ptr(ws), ws.numel(),
+                                    _stream(dev)))
+    return tok, entropy
+
+
+def pp_tok_logprob_bwd(pack: Pack, logits, tokens, dtok: torch.Tensor, dentropy: Optional[torch.Tensor] = None, dlogits=None,
+                       ws=None):
+    """Gradient of sum(dtok * tok_logp + dentropy * tok_entropy) w.r.t. the logits: [sumT, V] in their dtype."""
+    h, dt, V = _tok_args(pack, logits, tokens, dtok=dtok, dentropy=dentropy)
+    dev = logits.device
+    dlogits = (torch.empty_like(logits) if dlogits is None
+               else _check_tensor("dlogits", dlogits, logits.shape, logits.dtype, dev))
+    if ws is None:
+        ws = _workspace(_workspace_sizes(h, vocab=V, logprob=True)[2], dev)
+    with torch.cuda.device(dev):
+        _check(lib().pp_tok_logprob_bwd(h.ref, dt, V, _ptr(logits), _ptr(tokens), _ptr(dtok), _ptr(dentropy), _ptr(dlogits),
+                                        _ptr(ws), ws.numel(), _stream(dev)))
+    return dlogits
+
+
+def pp_tok_logprob_bwd_rows(pack: Pack, logits, tokens, dtok: torch.Tensor, dentropy: Optional[torch.Tensor] = None,
+                            dlogits_rows=None, row_index=None, ws=None):
+    """pp_tok_logprob_bwd on the predicting logit rows only: (dlogits_rows [n, V], row_index [n] int32)."""
+    h, dt, V = _tok_args(pack, logits, tokens, dtok=dtok, dentropy=dentropy)
+    dev, n = logits.device, _row_count(h)
+    dlogits_rows = (torch.empty(n, V, dtype=logits.dtype, device=dev) if dlogits_rows is None
+                    else _check_tensor("dlogits_rows", dlogits_rows, (n, V), logits.dtype, dev))
+    row_index = (torch.empty(n, dtype=torch.int32, device=dev) if row_index is None
+                 else _check_tensor("row_index", row_index, (n,), torch.int32, dev))
+    if ws is None:
+        ws = _workspace(_workspace_sizes(h, vocab=V, logprob=True)[2], dev)
+    with torch.cuda.device(dev):
+        _check(lib().pp_tok_logprob_bwd_rows(h.ref, dt, V, _ptr(logits), _ptr(tokens), _ptr(dtok), _ptr(dentropy),
+                                             _ptr(dlogits_rows), _ptr(row_index), _ptr(ws), ws.numel(), _stream(dev)))
+    return dlogits_rows, row_index
+
+
+KL_KINDS = {"k1": 0, "k2": 1, "k3": 2}
+REDUCTIONS = {"token": 0, "seq": 1, "sum": 2}
+
+
+def pp_policy_workspace_size(pack: Pack) -> int:
+    n = ctypes.c_size_t(0)
+    _check(lib().pp_policy_workspace_size(_desc_of(pack).ref, ctypes.byref(n)))
+    return n.value
+
+
+def pp_policy_loss(pack: Pack, logp: torch.Tensor, adv: torch.Tensor, logp_old: Optional[torch.Tensor] = None,
+                   logp_ref: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                   mask: Optional[torch.Tensor] = None, clip_low: float = 0.2, clip_high: float = 0.2, dual_clip: float = 0.0,
+                   kl_coef: float = 0.0, kl: str = "k3", ent_coef: float = 0.0, reduction: str = "token", norm: float = 1.0,
+                   want_grad: bool = True, ws=None):
+    """Clipped policy loss of the response tokens, with KL and entropy terms; adv is
+    [B, K_max] (one per response) or [sumT] (one per token), mask uint8 or bool [sumT].
+    Returns (loss [1], stats [4], counts [2] int32, dlogp [sumT] or None, dentropy
+    [sumT] or None)."""
+    if kl not in KL_KINDS or reduction not in REDUCTIONS:
+        raise ValueError(f"kl is one of {sorted(KL_KINDS)}, reduction one of {sorted(REDUCTIONS)}")
+    T, dev, f32 = max(0, pack.total_tokens), logp.device, torch.float32
+    for name, t in (("logp", logp), ("logp_old", logp_old), ("logp_ref", logp_ref), ("entropy", entropy)):
+        if t is not None or name == "logp":
+            _check_tensor(name, t, (T,), f32, dev)
+    per_token = adv.dim() == 1
+    _check_tensor("adv", adv, (T,) if per_token else (pack.num_rows, max(pack.max_resp, 1)), f32, dev)
+    if mask is not None:
+        mask = _check_tensor("mask", mask.view(torch.uint8) if mask.dtype == torch.bool else mask, (T,), torch.uint8, dev)
+    _on_gpu(logp)
+    h = _desc_of(pack)
+    cfg = _PolicyConfig(clip_low, clip_high, dual_clip, kl_coef, ent_coef, norm, KL_KINDS[kl], REDUCTIONS[reduction])
+    new = lambda n, dtype=f32: torch.empty(n, dtype=dtype, device=dev)
+    loss, stats, counts = new(1), new(4), new(2, torch.int32)
+    dlogp = new(T) if want_grad else None
+    dent = new(T) if want_grad and entropy is not None else None
+    if ws is None:
+        n = ctypes.c_size_t(0)
+        _check(lib().pp_policy_workspace_size(h.ref, ctypes.byref(n)))
+        ws = _workspace(n.value, dev)
+    with torch.cuda.device(dev):
+        _check(lib().pp_policy_loss(h.ref, ctypes.byref(cfg), _ptr(logp), _ptr(logp_old), _ptr(logp_ref), _ptr(entropy),
+                                    _ptr(adv), int(per_token), _ptr(mask), _ptr(loss), _ptr(stats), _ptr(counts), _ptr(dlogp),
+                                    _ptr(dent), _ptr(ws), ws.numel(), _stream(dev)))
+    return loss, stats, counts, dlogp, dent
 
 
 # ---------------------------------------------------------------- timing

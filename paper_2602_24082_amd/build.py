@@ -25,7 +25,7 @@ BUILD_DIR = os.path.join(PKG, "_build")
 ARCH = "gfx950"
 
 SOURCES = ["pp_host.cpp", "pp_attn_fwd.hip", "pp_attn_bwd.hip", "pp_cross.hip", "pp_logprob.hip", "pp_rm.hip", "pp_rope.hip", "pp_stage.hip",
-           "pp_noalloc.hip"]
+           "pp_noalloc.hip", "pp_policy.hip"]
 
 COMMON = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",

@@ -2515,3 +2515,260 @@ pp_status pp_cross_attn_bwd(const pp_pack_desc* desc, const pp_enc_desc* enc, pp
 }
 
 }  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Token log-probs with entropies
+// ---------------------------------------------------------------------------
+
+namespace pp {
+namespace {
+
+pp_status check_tok(const pp_pack_desc* desc, pp_dtype dtype, int vocab, Batch* bt) {
+  pp_status st = read_desc(desc, bt);
+  if (st != PP_OK) return st;
+  if ((st = check_dtype(dtype)) != PP_OK) return st;
+  if (vocab < 1) return fail(PP_ERR_INVALID_ARGUMENT, "vocab must be >= 1");
+  return check_logprob_layout(*bt);
+}
+
+pp_status check_logprob_ws(const LogprobPlan& p, const void* ws, size_t ws_bytes) {
+  if (ws_bytes < p.lay.total)
+    return fail(PP_ERR_WORKSPACE_TOO_SMALL, "logprob needs %zu workspace bytes, got %zu", p.lay.total, ws_bytes);
+  if (p.lay.total && !ws) return fail(PP_ERR_INVALID_ARGUMENT, "ws is NULL");
+  if (ws && !aligned256(ws)) return fail(PP_ERR_INVALID_ARGUMENT, "ws must be 256-byte aligned");
+  return PP_OK;
+}
+
+// The gather records and label positions; dense: each logit row's record too.
+void tok_image(const Batch& bt, const LogprobPlan& p, bool dense, MetaImage* img) {
+  const auto& reg = p.lay.regions;
+  if (dense) img->at(reg[p.r_row_item]);  // the image has its size before the places are taken
+  else img->at(reg[p.r_labels]);
+  fill_lplan(bt, (LogitRowItem*)img->at(reg[p.r_rows]), (int32_t*)img->at(reg[p.r_labels]), nullptr, nullptr,
+             dense ? (int32_t*)img->at(reg[p.r_row_item]) : nullptr);
+}
+
+pp_status tok_logprob_bwd_impl(const pp_pack_desc* desc, pp_dtype dtype, int vocab, const void* logits, const int32_t* tokens,
+                               const float* dtok, const float* dentropy, void* dlogits, bool gathered, int32_t* row_index,
+                               void* ws, size_t ws_bytes, void* hip_stream) {
+  Batch bt;
+  pp_status st = check_tok(desc, dtype, vocab, &bt);
+  if (st != PP_OK) return st;
+  if (bt.Kmax > kMaxRowLabels)
+    return fail(PP_ERR_UNSUPPORTED, "the log-prob backward takes at most %d responses per row (max_resp %d)", kMaxRowLabels,
+                bt.Kmax);
+  if (bt.sumT == 0) return PP_OK;
+  LogprobPlan p;
+  plan_logprob(bt, &p);
+  if (gathered && p.n.rows == 0) return PP_OK;
+  if (!logits || !tokens || !dtok || !dlogits)
+    return fail(PP_ERR_INVALID_ARGUMENT, "logits, tokens, dtok and dlogits must be non-NULL");
+  if ((st = check_logprob_ws(p, ws, ws_bytes)) != PP_OK) return st;
+  hipStream_t s = (hipStream_t)hip_stream;
+  MetaImage img;
+  tok_image(bt, p, !gathered, &img);
+  if ((st = stage_copy(ws, img.buf.data(), img.buf.size(), s)) != PP_OK) return st;
+  LogprobBwdLaunch a{};
+  a.logits = logits;
+  a.tokens = tokens;
+  a.dseq = dtok;
+  a.dent = dentropy;
+  a.dlogits = dlogits;
+  a.rows = (const LogitRowItem*)at(ws, p.lay, p.r_rows);
+  a.labels = (const int32_t*)at(ws, p.lay, p.r_labels);
+  a.label_out = a.labels;  // a label's gradient stands at its own position
+  a.row_item = (const int32_t*)at(ws, p.lay, p.r_row_item);
+  a.vocab = vocab;
+  a.sumT = bt.sumT;
+  a.dtype = dtype == PP_FP32 ? kFP32 : kBF16;
+  a.gathered = gathered;
+  a.n_rows = (int)p.n.rows;
+  a.row_index = row_index;
+  const hipError_t e = launch_logprob_bwd(a, s);
+  return e == hipSuccess ? PP_OK : hip_fail(e, "log-prob backward launch");
+}
+
+}  // namespace
+}  // namespace pp
+
+extern "C" {
+
+pp_status pp_tok_logprob(const pp_pack_desc* desc, pp_dtype logits_dtype, int vocab, const void* logits, const int32_t* tokens,
+                         float* tok_logp, float* tok_entropy, void* ws, size_t ws_bytes, void* hip_stream) {
+  return guarded([&]() -> pp_status {
+    Batch bt;
+    pp_status st = check_tok(desc, logits_dtype, vocab, &bt);
+    if (st != PP_OK) return st;
+    if (bt.sumT == 0) return PP_OK;
+    if (!logits || !tokens || !tok_logp) return fail(PP_ERR_INVALID_ARGUMENT, "logits, tokens and tok_logp must be non-NULL");
+    LogprobPlan p;
+    plan_logprob(bt, &p);
+    if ((st = check_logprob_ws(p, ws, ws_bytes)) != PP_OK) return st;
+    hipStream_t s = (hipStream_t)hip_stream;
+    MetaImage img;
+    tok_image(bt, p, false, &img);
+    LogprobLaunch a{};
+    a.logits = logits;
+    a.tokens = tokens;
+    a.tok = tok_logp;
+    a.ent = tok_entropy;
+    a.rows = (const LogitRowItem*)at(ws, p.lay, p.r_rows);
+    a.labels = (const int32_t*)at(ws, p.lay, p.r_labels);
+    a.n_rows = (int)p.n.rows;
+    a.vocab = vocab;
+    a.dtype = logits_dtype == PP_FP32 ? kFP32 : kBF16;
+    return stage_with(ws, img.buf.data(), img.buf.size(), s, [&](const void* dev_src) -> pp_status {
+      StageLaunch pre = stage_of(ws, dev_src, img.buf.size());
+      pre.zero = tok_logp;  // 0 off the responses
+      pre.zero2 = tok_entropy;
+      pre.n_zero = bt.sumT;
+      hipError_t e = launch_stage(pre, s);
+      if (e != hipSuccess) return hip_fail(e, "stage_kernel");
+      e = launch_logprob(a, s);
+      return e == hipSuccess ? PP_OK : hip_fail(e, "log-prob launch");
+    });
+  });
+}
+
+pp_status pp_tok_logprob_bwd(const pp_pack_desc* desc, pp_dtype logits_dtype, int vocab, const void* logits,
+                             const int32_t* tokens, const float* dtok, const float* dentropy, void* dlogits, void* ws,
+                             size_t ws_bytes, void* hip_stream) {
+  return guarded([&] {
+    return tok_logprob_bwd_impl(desc, logits_dtype, vocab, logits, tokens, dtok, dentropy, dlogits, false, nullptr, ws, ws_bytes,
+                                hip_stream);
+  });
+}
+
+pp_status pp_tok_logprob_bwd_rows(const pp_pack_desc* desc, pp_dtype logits_dtype, int vocab, const void* logits,
+                                  const int32_t* tokens, const float* dtok, const float* dentropy, void* dlogits_rows,
+                                  int32_t* row_index, void* ws, size_t ws_bytes, void* hip_stream) {
+  return guarded([&] {
+    return tok_logprob_bwd_impl(desc, logits_dtype, vocab, logits, tokens, dtok, dentropy, dlogits_rows, true, row_index, ws,
+                                ws_bytes, hip_stream);
+  });
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// Clipped policy loss
+// ---------------------------------------------------------------------------
+
+namespace pp {
+namespace {
+
+struct PolicyPlan {
+  std::vector<PolicySlot> slots;  // responses with tokens, in token order
+  int64_t tokens = 0;
+  bool inline_slots = false;
+  Layout lay;
+  size_t r_slots = 0, r_counts = 0, r_part = 0;
+};
+
+void plan_policy(const Batch& bt, PolicyPlan* p) {
+  for (int b = 0; b < bt.B; ++b) {
+    const Row& r = bt.rows[b];
+    for (int k = 0; k < r.K; ++k) {
+      if (r.len[k] == 0) continue;
+      p->slots.push_back(PolicySlot{r.tok0 + r.off[k], r.len[k], b * bt.Kmax + k});
+      p->tokens += r.len[k];
+    }
+  }
+  p->inline_slots = p->slots.size() <= (size_t)kPolicyInline;
+  if (!p->inline_slots) p->r_slots = p->lay.add(p->slots.size() * sizeof(PolicySlot));
+  p->lay.meta_bytes = p->lay.total;
+  p->r_counts = p->lay.add(p->slots.size() * 4);
+  p->r_part = p->lay.add((size_t)policy_blocks(bt.sumT) * sizeof(PolicyPartial));
+}
+
+}  // namespace
+}  // namespace pp
+
+extern "C" {
+
+pp_status pp_policy_workspace_size(const pp_pack_desc* desc, size_t* bytes) {
+  return guarded([&]() -> pp_status {
+    Batch bt;
+    const pp_status st = read_desc(desc, &bt);
+    if (st != PP_OK) return st;
+    if (!bytes) return fail(PP_ERR_INVALID_ARGUMENT, "bytes is NULL");
+    PolicyPlan p;
+    plan_policy(bt, &p);
+    *bytes = p.lay.total;
+    return PP_OK;
+  });
+}
+
+pp_status pp_policy_loss(const pp_pack_desc* desc, const pp_policy_config* cfg, const float* logp, const float* logp_old,
+                         const float* logp_ref, const float* entropy, const float* adv, int adv_per_token, const uint8_t* mask,
+                         float* loss, float* stats, int32_t* counts, float* dlogp, float* dentropy, void* ws, size_t ws_bytes,
+                         void* hip_stream) {
+  return guarded([&]() -> pp_status {
+    Batch bt;
+    pp_status st = read_desc(desc, &bt);
+    if (st != PP_OK) return st;
+    if (!cfg) return fail(PP_ERR_INVALID_ARGUMENT, "cfg is NULL");
+    if (!(cfg->clip_low >= 0 && cfg->clip_low <= 1) || !(cfg->clip_high >= 0) || !std::isfinite(cfg->clip_high))
+      return fail(PP_ERR_INVALID_ARGUMENT, "clip_low must be in [0, 1] and clip_high in [0, inf)");
+    if (!(cfg->dual_clip == 0 || (cfg->dual_clip > 1 && std::isfinite(cfg->dual_clip))))
+      return fail(PP_ERR_INVALID_ARGUMENT, "dual_clip must be 0 (off) or above 1");
+    if (!std::isfinite(cfg->kl_coef) || !std::isfinite(cfg->ent_coef))
+      return fail(PP_ERR_INVALID_ARGUMENT, "kl_coef and ent_coef must be finite");
+    if (cfg->kl < PP_KL_K1 || cfg->kl > PP_KL_K3) return fail(PP_ERR_INVALID_ARGUMENT, "unknown kl %d", (int)cfg->kl);
+    if (cfg->reduction < PP_REDUCE_TOKEN || cfg->reduction > PP_REDUCE_SUM)
+      return fail(PP_ERR_INVALID_ARGUMENT, "unknown reduction %d", (int)cfg->reduction);
+    if (cfg->reduction == PP_REDUCE_SUM && !(cfg->norm > 0 && std::isfinite(cfg->norm)))
+      return fail(PP_ERR_INVALID_ARGUMENT, "norm must be positive and finite");
+    if (bt.sumT > 0 && cfg->kl_coef != 0 && !logp_ref) return fail(PP_ERR_INVALID_ARGUMENT, "kl_coef without logp_ref");
+    if (bt.sumT > 0 && cfg->ent_coef != 0 && !entropy) return fail(PP_ERR_INVALID_ARGUMENT, "ent_coef without entropy");
+    if (bt.sumT > 0 && dentropy && !entropy) return fail(PP_ERR_INVALID_ARGUMENT, "dentropy without entropy");
+    if (!loss) return fail(PP_ERR_INVALID_ARGUMENT, "loss is NULL");
+    if (bt.sumT > 0 && (!logp || !adv)) return fail(PP_ERR_INVALID_ARGUMENT, "logp and adv must be non-NULL");
+    for (const void* ptr : {(const void*)logp, (const void*)logp_old, (const void*)logp_ref, (const void*)entropy,
+                            (const void*)adv, (const void*)loss, (const void*)stats, (const void*)counts, (const void*)dlogp,
+                            (const void*)dentropy})
+      if (!aligned4(ptr)) return fail(PP_ERR_INVALID_ARGUMENT, "float and int32 arguments must be 4-byte aligned");
+    PolicyPlan p;
+    plan_policy(bt, &p);
+    if (ws_bytes < p.lay.total)
+      return fail(PP_ERR_WORKSPACE_TOO_SMALL, "policy loss needs %zu workspace bytes, got %zu", p.lay.total, ws_bytes);
+    if (p.lay.total && !ws) return fail(PP_ERR_INVALID_ARGUMENT, "ws is NULL");
+    if (ws && !aligned256(ws)) return fail(PP_ERR_INVALID_ARGUMENT, "ws must be 256-byte aligned");
+    hipStream_t s = (hipStream_t)hip_stream;
+    PolicyLaunch a{};
+    a.logp = logp;
+    a.old = logp_old;
+    a.ref = logp_ref;
+    a.entropy = entropy;
+    a.adv = adv;
+    a.adv_per_token = adv_per_token != 0;
+    a.mask = mask;
+    a.loss = loss;
+    a.stats = stats;
+    a.counts = counts;
+    a.dlogp = dlogp;
+    a.dentropy = dentropy;
+    a.clip_low = cfg->clip_low;
+    a.clip_high = cfg->clip_high;
+    a.dual_clip = cfg->dual_clip;
+    a.kl_coef = cfg->kl_coef;
+    a.ent_coef = cfg->ent_coef;
+    a.norm = cfg->norm;
+    a.kl = cfg->kl;
+    a.reduction = cfg->reduction;
+    a.sumT = bt.sumT;
+    a.tokens = p.tokens;
+    a.n_slots = (int)p.slots.size();
+    a.host_slots = p.slots.data();
+    a.slot_counts = (int32_t*)at(ws, p.lay, p.r_counts);
+    a.part = (PolicyPartial*)at(ws, p.lay, p.r_part);
+    if (!p.inline_slots) {
+      if ((st = stage_copy(ws, p.slots.data(), p.slots.size() * sizeof(PolicySlot), s)) != PP_OK) return st;
+      a.slots = (const PolicySlot*)at(ws, p.lay, p.r_slots);
+    }
+    const hipError_t e = launch_policy(a, s);
+    return e == hipSuccess ? PP_OK : hip_fail(e, "policy loss launch");
+  });
+}
+
+}  // extern "C"

@@ -48,8 +48,9 @@ struct StageLaunch {
     void* dst = nullptr;
     int64_t n = 0;
   } cast[kStageCasts];
-  // n_zero floats set to 0
+  // n_zero floats set to 0, of one or two outputs
   float* zero = nullptr;
+  float* zero2 = nullptr;
   int64_t n_zero = 0;
 };
 hipError_t launch_stage(const StageLaunch& a, hipStream_t s);
@@ -205,6 +206,7 @@ struct LogprobLaunch {
   const void* logits;
   const int32_t* tokens;
   float* tok;                // [sumT]; response positions written
+  float* ent = nullptr;      // [sumT]: entropies beside them, or null
   float* seq;                // [B * K_max]
   const LogitRowItem* rows;
   const int32_t* labels;     // flat token positions
@@ -219,11 +221,12 @@ hipError_t launch_logprob(const LogprobLaunch& a, hipStream_t s);
 struct LogprobBwdLaunch {
   const void* logits;
   const int32_t* tokens;
-  const float* dseq;          // [B * K_max] dL/dseq
+  const float* dseq;          // dL/dseq [B * K_max] or dL/dtok [sumT], as label_out says
+  const float* dent = nullptr;  // gradients of the entropies, indexed alike, or null
   void* dlogits;              // [sumT, vocab], logits dtype
   const LogitRowItem* rows;
   const int32_t* labels;      // flat token positions
-  const int32_t* label_out;   // response slot of each label
+  const int32_t* label_out;   // where each label's gradient is: its response slot, or its flat position
   const int32_t* row_item;    // [sumT]: gather record of each logit row or -1
   int vocab;
   int sumT;
@@ -282,6 +285,46 @@ struct LossLaunch {
   int32_t nr_inline[kLossInlineRows];  // K_b when B <= kLossInlineRows
 };
 hipError_t launch_loss(const LossLaunch& a, hipStream_t s);
+
+// Clipped policy loss (pp_policy.hip).
+constexpr int kPolicyThreads = 256;
+constexpr int kPolicyInline = 256;  // responses that ride in the launches' arguments
+struct PolicySlot {
+  int32_t begin;  // flat position of the response's first token
+  int32_t len;    // >= 1
+  int32_t out;    // b * K_max + k
+};
+struct PolicyPartial {
+  double sum[4];  // -surrogate, KL, entropy, ratio, each weighted
+  int32_t counted, clipped;
+};
+// partial sums that a pass over the token axis may leave
+inline int64_t policy_blocks(int64_t sumT) { return (sumT + kPolicyThreads - 1) / kPolicyThreads; }
+struct PolicyParams {
+  const float* logp;      // [sumT]
+  const float* old;       // [sumT] or null: the ratio is 1
+  const float* ref;       // [sumT] or null
+  const float* entropy;   // [sumT] or null
+  const float* adv;       // [B * K_max] or [sumT]
+  const uint8_t* mask;    // [sumT] or null
+  float* loss;
+  float* stats;           // [4] or null
+  int32_t* counts;        // [2] or null
+  float* dlogp;           // [sumT] or null
+  float* dentropy;        // [sumT] or null
+  const PolicySlot* slots;  // in token order; null: in the launch's arguments
+  int32_t* slot_counts;   // scratch
+  PolicyPartial* part;    // scratch
+  double clip_low, clip_high, dual_clip, kl_coef, ent_coef, norm;
+  int64_t sumT, tokens;
+  int n_slots;
+  int kl, reduction;
+  bool adv_per_token;
+};
+struct PolicyLaunch : PolicyParams {
+  const PolicySlot* host_slots;
+};
+hipError_t launch_policy(const PolicyLaunch& a, hipStream_t s);
 
 // Records `message` (printf-style) as the calling thread's pp_last_error and
 // returns st; the HIP variant appends the runtime's error string.

@@ -202,7 +202,6 @@ struct RowLse {
   // Where m is so large that lse no longer holds ln s, differences to it are formed part
   // by part.
   __device__ __forceinline__ float log_prob(float x) const { return far() ? (x - m) - logf(s) : x - lse; }
-  __device__ __forceinline__ float far_softmax(float x) const { return fast_exp2(((x - m) - logf(s)) * kLog2e); }
 };
 
 // The workgroup's (max, sum)s combined in a fixed order, for every thread.  `work` is
@@ -272,6 +271,183 @@ __global__ __launch_bounds__(kLpThreads) void logprob_rows_kernel(
   }
 }
 
+// ---- log-probs with entropies
+//
+// H = -sum_v p_v ln p_v = ln s - t / s  with  s = sum e^(x - m),  t = sum e^(x - m) (x - m)
+// takes one more multiply-add an element, so a row is still read once.  In base 2,
+// relative to the rounded product m log2(e): both sums then carry the same factor and the
+// same shift, which H does not see, and sums of different maxima are joined by the
+// difference of their rounded products.
+
+// Exponents below this count as this: 2^-200 is 0 in fp32, and 0 times a masked entry's
+// -inf is not.
+constexpr float kLeastExp = -200.f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct MaxSumEnt {
+  float m, s, t;  // t in log2 units
+};
+
+// m log2(e) rounded, and nothing else: contracted into a multiply-add with the other
+// product, equal maxima would differ by the rounding.
+__device__ __forceinline__ float base2(float m) {
+#pragma clang fp contract(off)
+  return m * kLog2e;
+}
+
+// sums relative to a.m, taken relative to m: d = the difference of the two in log2 units
+__device__ __forceinline__ void shift_ent(const MaxSumEnt& a, float d, float& s, float& t) {
+  const float f = fast_exp2(d);
+  s = fmaf(a.s, f, s);
+  t = fmaf(fmaf(fmaxf(d, kLeastExp), a.s, a.t), f, t);
+}
+
+// FAR: maxima whose products with log2(e) may overflow are compared first.
+template <bool FAR>
+__device__ __forceinline__ MaxSumEnt combine_ent(const MaxSumEnt& a, const MaxSumEnt& b) {
+  const float m = max_or_nan(a.m, b.m);
+  if (m == kNegInf) return {kNegInf, 0.f, 0.f};
+  MaxSumEnt r = {m, 0.f, 0.f};
+  shift_ent(a, FAR ? (a.m - m) * kLog2e : base2(a.m) - base2(m), r.s, r.t);
+  shift_ent(b, FAR ? (b.m - m) * kLog2e : base2(b.m) - base2(m), r.s, r.t);
+  return r;
+}
+
+// One element's terms relative to ml = m log2(e).
+__device__ __forceinline__ void add_ent(float x, float ml, float& s, float& t) {
+  const float y = fmaf(x, kLog2e, -ml), e = fast_exp2(y);
+  s += e;
+  t = fmaf(e, fmaxf(y, kLeastExp), t);
+}
+
+__device__ __forceinline__ MaxSumEnt one_ent(float x) {
+  MaxSumEnt r = {x, 0.f, 0.f};
+  if (x != kNegInf) add_ent(x, base2(x), r.s, r.t);
+  return r;
+}
+
+// As stream_max_sum, any_max_sum and block_lse, with the entropy's sum.
+template <typename T, int THREADS>
+__device__ __forceinline__ MaxSumEnt stream_ent(const u32x4* __restrict__ xv, int first, int nvec) {
+  const int tid = threadIdx.x;
+  constexpr int N = Vec16<T>::N;
+  MaxSumEnt acc = {kNegInf, 0.f, 0.f};
+  for (int base = first; base < nvec; base += THREADS * kLpUnroll) {
+    u32x4 u[kLpUnroll];
+#pragma unroll
+    for (int j = 0; j < kLpUnroll; ++j) {
+      const int vi = base + j * THREADS + tid;
+      u[j] = vi < nvec ? __builtin_nontemporal_load(xv + vi) : u32x4{0, 0, 0, 0};
+    }
+    float f[kLpUnroll * N];
+#pragma unroll
+    for (int j = 0; j < kLpUnroll; ++j) Vec16<T>::unpack(u[j], f + j * N);
+    float m = acc.m;
+#pragma unroll
+    for (int j = 0; j < kLpUnroll; ++j) {
+      if (base + j * THREADS + tid < nvec) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) m = max_or_nan(m, f[j * N + e]);
+      }
+    }
+    if (m != kNegInf) {
+      const float ml = base2(m);
+      float s = 0.f, t = 0.f;
+      shift_ent(acc, base2(acc.m) - ml, s, t);
+#pragma unroll
+      for (int j = 0; j < kLpUnroll; ++j) {
+        if (base + j * THREADS + tid < nvec) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) add_ent(f[j * N + e], ml, s, t);
+        }
+      }
+      acc = {m, s, t};
+    }
+  }
+  return acc;
+}
+
+template <typename T, int THREADS>
+__device__ __forceinline__ MaxSumEnt any_ent(const u32x4* __restrict__ xv, int nvec) {
+  constexpr int N = Vec16<T>::N;
+  MaxSumEnt acc = {kNegInf, 0.f, 0.f};
+#pragma unroll 1
+  for (int vi = threadIdx.x; vi < nvec; vi += THREADS) {
+    float f[N];
+    Vec16<T>::unpack(xv[vi], f);
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc = combine_ent<true>(acc, MaxSumEnt{f[e], 1.f, 0.f});
+  }
+  return acc;
+}
+
+// A row's sums and what follows from them (see RowLse for the maxima that are far).
+struct RowEnt {
+  float m, s, t;
+  bool natural;  // summed by any_ent: log_prob from differences to m, not from rounded products
+  __device__ __forceinline__ bool redo() const {
+    return fabsf(m) < __builtin_huge_valf() && (fabsf(m) >= 1e38f || !(s < __builtin_huge_valf()));
+  }
+  __device__ __forceinline__ float log_prob(float x) const {
+    if (natural) return (x - m) - logf(s);
+    return (fmaf(x, kLog2e, -base2(m)) - log2f(s)) * kLn2;
+  }
+  __device__ __forceinline__ float entropy() const { return (log2f(s) - t / s) * kLn2; }
+};
+
+template <int THREADS, bool FAR, typename Work>
+__device__ __forceinline__ RowEnt block_ent(MaxSumEnt acc, Work&& work) {
+  for (int off = 32; off > 0; off >>= 1) {
+    MaxSumEnt o;
+    o.m = __shfl_xor(acc.m, off, 64);
+    o.s = __shfl_xor(acc.s, off, 64);
+    o.t = __shfl_xor(acc.t, off, 64);
+    acc = combine_ent<FAR>(acc, o);
+  }
+  __shared__ MaxSumEnt part[THREADS / 64];
+  __shared__ MaxSumEnt s_row;
+  const int tid = threadIdx.x;
+  if ((tid & 63) == 0) part[tid >> 6] = acc;
+  __syncthreads();
+  if (tid == 0) {
+    MaxSumEnt t = part[0];
+    for (int w = 1; w < THREADS / 64; ++w) t = combine_ent<FAR>(t, part[w]);
+    s_row = t;
+    work();
+  }
+  __syncthreads();
+  return {s_row.m, s_row.s, s_row.t, FAR};
+}
+
+// The log-prob pass with entropies: a label token gets the entropy of the distribution
+// that it was drawn from.  Bound by the one read of the rows, as logprob_rows.
+template <typename T, int THREADS>
+__global__ __launch_bounds__(THREADS) void logprob_ent_kernel(
+    const T* __restrict__ logits, const int32_t* __restrict__ tokens, const LogitRowItem* __restrict__ rows,
+    const int32_t* __restrict__ labels, float* __restrict__ tok, float* __restrict__ ent, int vocab) {
+  const LogitRowItem it = rows[blockIdx.x];
+  const T* x = logits + it.logit_row * (int64_t)vocab;
+  const int tid = threadIdx.x;
+  const RowSplit<T> rs(x, vocab);
+  const float xe = tid < rs.n_extra ? elem<T>(x, rs.extra(tid)) : kNegInf;
+  const u32x4* xv = reinterpret_cast<const u32x4*>(x + rs.head);
+  MaxSumEnt acc = stream_ent<T, THREADS>(xv, 0, rs.nvec);
+  if (tid < rs.n_extra) acc = combine_ent<false>(acc, one_ent(xe));
+  RowEnt r = block_ent<THREADS, false>(acc, [] {});
+  if (r.redo()) {
+    acc = any_ent<T, THREADS>(xv, rs.nvec);
+    if (tid < rs.n_extra) acc = combine_ent<true>(acc, MaxSumEnt{xe, 1.f, 0.f});
+    __syncthreads();
+    r = block_ent<THREADS, true>(acc, [] {});
+  }
+  for (int j = tid; j < it.label_cnt; j += THREADS) {
+    const int32_t pos = labels[it.label_off + j];
+    const int32_t y = tokens[pos];
+    tok[pos] = (y >= 0 && y < vocab) ? r.log_prob(elem<T>(x, y)) : __builtin_nanf("");
+    ent[pos] = r.entropy();
+  }
+}
+
 // Packs floats into one 16-byte vector of T (bf16: round to nearest even).
 template <typename T>
 struct Pack16;
@@ -336,7 +512,11 @@ __device__ __forceinline__ void opaque(u32x4 (&u)[R]) {
   for (int j = 0; j < R; ++j) asm volatile("" : "+v"(u[j]));
 }
 
-template <typename T, int THREADS, int R, bool EDGE, bool OVER>
+//
+// ENT: the rows' entropies have a gradient too.  With h the sum of the labels' entropy
+// gradients, dH/dx_v = -p_v (ln p_v + H) adds  -h p_v (ln p_v + H): one more multiply-add
+// an element in the sums (see logprob_ent) and one in the gradient.
+template <typename T, int THREADS, int R, bool EDGE, bool OVER, bool ENT>
 __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(LogprobBwdLaunch a) {
   constexpr int N = Vec16<T>::N;
   const int tid = threadIdx.x;
@@ -386,6 +566,8 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
   __shared__ int s_y[kMaxRowLabels];
   __shared__ float s_g[kMaxRowLabels];
   __shared__ float s_c;
+  __shared__ float s_e[ENT ? kMaxRowLabels : 1];
+  __shared__ float s_h;
   __shared__ int s_bad;
   const int cnt = it.label_cnt;
   if (tid == 0) s_bad = 0;
@@ -394,10 +576,25 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
     const int32_t y = a.tokens[a.labels[it.label_off + j]];
     s_y[j] = y;
     s_g[j] = a.dseq[a.label_out[it.label_off + j]];
+    if constexpr (ENT) s_e[j] = a.dent[a.label_out[it.label_off + j]];
     if (y < 0 || y >= vocab) s_bad = 1;
   }
+  auto sum_labels = [&] {
+    float c = 0.f;
+    for (int j = 0; j < cnt; ++j) c += s_g[j];
+    s_c = c;
+    if constexpr (ENT) {
+      float h = 0.f;
+      for (int j = 0; j < cnt; ++j) h += s_e[j];
+      s_h = h;
+    }
+  };
   MaxSum over = {kNegInf, 0.f};  // of the vectors past the registers
-  if constexpr (OVER) over = stream_max_sum<T, THREADS>(xv, R * THREADS, nvec, n_extra > 0);
+  MaxSumEnt over_ent = {kNegInf, 0.f, 0.f};
+  if constexpr (OVER) {
+    if constexpr (ENT) over_ent = stream_ent<T, THREADS>(xv, R * THREADS, nvec);
+    else over = stream_max_sum<T, THREADS>(xv, R * THREADS, nvec, n_extra > 0);
+  }
   // logsumexp of the row from the registers
   float m = kNegInf;
 #pragma unroll
@@ -412,34 +609,53 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
   // the packed vectors count as rewritten here, so each pass below unpacks
   // them again instead of keeping the whole row live as floats
   opaque(u);
-  float s = 0.f;
+  float s = 0.f, t = 0.f;
   if (m != kNegInf) {
-    const float ml = m * kLog2e;
+    const float ml = ENT ? base2(m) : m * kLog2e;
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       if (j * THREADS + tid < nvec) {
         float f[N];
         Vec16<T>::unpack(u[j], f);
 #pragma unroll
-        for (int e = 0; e < N; ++e) s += fast_exp2(fmaf(f[e], kLog2e, -ml));
+        for (int e = 0; e < N; ++e) {
+          if constexpr (ENT) add_ent(f[e], ml, s, t);
+          else s += fast_exp2(fmaf(f[e], kLog2e, -ml));
+        }
       }
     }
-    if constexpr (EDGE) s = exact_base(s, m, ml, n_extra > 0);
+    if constexpr (EDGE && !ENT) s = exact_base(s, m, ml, n_extra > 0);
   }
-  MaxSum acc = {m, s};
-  if constexpr (OVER) acc = combine(acc, over);
-  if (EDGE && tid < n_extra) acc = combine(acc, MaxSum{xe, 1.f});
-  RowLse lse = block_lse<THREADS>(acc, [&] {
-    float c = 0.f;
-    for (int j = 0; j < cnt; ++j) c += s_g[j];
-    s_c = c;
-  });
+  RowLse lse;
+  RowEnt row;
+  float lse2;
+  if constexpr (ENT) {
+    MaxSumEnt acc = {m, s, t};
+    if constexpr (OVER) acc = combine_ent<false>(acc, over_ent);
+    if (EDGE && tid < n_extra) acc = combine_ent<false>(acc, one_ent(xe));
+    row = block_ent<THREADS, false>(acc, sum_labels);
+    lse2 = base2(row.m) + log2f(row.s);
+  } else {
+    MaxSum acc = {m, s};
+    if constexpr (OVER) acc = combine(acc, over);
+    if (EDGE && tid < n_extra) acc = combine(acc, MaxSum{xe, 1.f});
+    lse = block_lse<THREADS>(acc, sum_labels);
+    lse2 = lse.lse * kLog2e;
+  }
   const float c = s_c;
-  const float lse2 = lse.lse * kLog2e;
   const bool bad = s_bad != 0;
-  auto finish = [&](int vi, float* f) {  // f: the softmax of vector vi
-#pragma unroll
-    for (int e = 0; e < N; ++e) f[e] *= -c;
+  // -(c + h (ln p + H)) = ent_a + ent_b log2 p
+  float ent_a = 0.f, ent_b = 0.f;
+  if constexpr (ENT) {
+    ent_a = -fmaf(s_h, row.entropy(), c);
+    ent_b = -s_h * kLn2;
+  }
+  // an element's gradient, its label's terms aside, from the exponent of its softmax
+  auto slope = [&](float y) {
+    if constexpr (ENT) return fast_exp2(y) * fmaf(ent_b, fmaxf(y, kLeastExp), ent_a);
+    else return -c * fast_exp2(y);
+  };
+  auto finish = [&](int vi, float* f) {  // f: the slopes of vector vi
     for (int l = 0; l < cnt; ++l) {
       const int d = s_y[l] - (head + vi * N);
       if ((unsigned)d < (unsigned)N) {
@@ -453,32 +669,45 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
     }
     store(vi, Pack16<T>::pack(f));
   };
-  auto finish_extra = [&](float softmax) {
-    float f = -c * softmax;
+  auto finish_extra = [&](float f) {
     for (int l = 0; l < cnt; ++l) f += s_y[l] == xi ? s_g[l] : 0.f;
     out[xi] = (T)(bad ? __builtin_nanf("") : f);
   };
-  if (__builtin_expect(__builtin_amdgcn_readfirstlane(lse.redo() ? 1 : 0), 0)) {
-    acc = any_max_sum<T, THREADS>(xv, nvec);
-    if (EDGE && tid < n_extra) acc = combine(acc, MaxSum{xe, 1.f});
+  const bool redo = ENT ? row.redo() : lse.redo();
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(redo ? 1 : 0), 0)) {
+    float far_m, far_ln;  // the row's exponents are ((x - far_m) - far_ln) log2(e)
     __syncthreads();
-    lse = block_lse<THREADS>(acc, [] {});
+    if constexpr (ENT) {
+      MaxSumEnt acc = any_ent<T, THREADS>(xv, nvec);
+      if (EDGE && tid < n_extra) acc = combine_ent<true>(acc, MaxSumEnt{xe, 1.f, 0.f});
+      row = block_ent<THREADS, true>(acc, [] {});
+      ent_a = -fmaf(s_h, row.entropy(), c);
+      far_m = row.m;
+      far_ln = logf(row.s);
+    } else {
+      MaxSum acc = any_max_sum<T, THREADS>(xv, nvec);
+      if (EDGE && tid < n_extra) acc = combine(acc, MaxSum{xe, 1.f});
+      lse = block_lse<THREADS>(acc, [] {});
+      far_m = lse.m;
+      far_ln = logf(lse.s);
+    }
+    auto far = [&](float x) { return slope(((x - far_m) - far_ln) * kLog2e); };
 #pragma unroll 1
     for (int vi = tid; vi < nvec; vi += THREADS) {
       float f[N];
       Vec16<T>::unpack(xv[vi], f);
 #pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = lse.far_softmax(f[e]);
+      for (int e = 0; e < N; ++e) f[e] = far(f[e]);
       finish(vi, f);
     }
-    if (EDGE && tid < n_extra) finish_extra(lse.far_softmax(xe));
+    if (EDGE && tid < n_extra) finish_extra(far(xe));
     return;
   }
   auto gradient = [&](int vi, const u32x4& x16) {
     float f[N];
     Vec16<T>::unpack(x16, f);
 #pragma unroll
-    for (int e = 0; e < N; ++e) f[e] = fast_exp2(fmaf(f[e], kLog2e, -lse2));
+    for (int e = 0; e < N; ++e) f[e] = slope(fmaf(f[e], kLog2e, -lse2));
     finish(vi, f);
   };
   if constexpr (OVER) {
@@ -500,7 +729,7 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
     const int vi = j * THREADS + tid;
     if (vi < nvec) gradient(vi, u[j]);
   }
-  if (EDGE && tid < n_extra) finish_extra(fast_exp2(fmaf(xe, kLog2e, -lse2)));
+  if (EDGE && tid < n_extra) finish_extra(slope(fmaf(xe, kLog2e, -lse2)));
 }
 
 // One wave per (row, response) slot; lane l sums tokens l, l+64, ... in order,
@@ -639,11 +868,25 @@ __global__ __launch_bounds__(256) void pair_loss_kernel(LossLaunch a) {
 
 }  // namespace
 
+namespace {
+
+void launch_logprob_ent(const LogprobLaunch& a, hipStream_t s) {
+  auto launch = [&](auto kernel, auto* x, int threads) {
+    hipLaunchKernelGGL(kernel, dim3(a.n_rows), dim3(threads), 0, s, x, a.tokens, a.rows, a.labels, a.tok, a.ent, a.vocab);
+  };
+  if (a.dtype == kBF16) launch(logprob_ent_kernel<__bf16, kLpThreads>, (const __bf16*)a.logits, kLpThreads);
+  else launch(logprob_ent_kernel<float, kLpThreads>, (const float*)a.logits, kLpThreads);
+}
+
+}  // namespace
+
 hipError_t launch_logprob(const LogprobLaunch& a, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (a.n_rows > 0) {
     TimingScope t("pp_logprob_rows", s);
-    if (a.dtype == kBF16)
+    if (a.ent)
+      launch_logprob_ent(a, s);
+    else if (a.dtype == kBF16)
       hipLaunchKernelGGL(logprob_rows_kernel<__bf16>, dim3(a.n_rows), dim3(kLpThreads), 0, s,
                          (const __bf16*)a.logits, a.tokens, a.rows, a.labels, a.tok, a.vocab);
     else
@@ -679,7 +922,7 @@ namespace {
 //      .3    178 / 188    204 / 200    273 / 274    336 / 319
 //      .5    198 / 249    231 / 248    303 / 349    370 / 396
 // Below 1700 vectors (12000 bf16) and on rows off the boundaries four are as good.
-template <typename T, bool EDGE>
+template <typename T, bool EDGE, bool ENT>
 void launch_logprob_bwd_rows(const LogprobBwdLaunch& a, int grid, int nvec, hipStream_t s) {
   constexpr int kMost = EDGE ? 18 : 19;
   constexpr unsigned kHalfLds = 96 << 10;  // more than half of a unit's 160 KB
@@ -688,10 +931,10 @@ void launch_logprob_bwd_rows(const LogprobBwdLaunch& a, int grid, int nvec, hipS
   auto launch = [&](auto kernel, int threads) {
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), few ? kHalfLds : 0u, s, a);
   };
-  if (nvec <= 512 * 8) launch(logprob_bwd_kernel<T, 512, 8, EDGE, false>, 512);
-  else if (nvec <= 1024 * 8) launch(logprob_bwd_kernel<T, 1024, 8, EDGE, false>, 1024);
-  else if (nvec <= 1024 * kMost) launch(logprob_bwd_kernel<T, 1024, kMost, EDGE, false>, 1024);
-  else launch(logprob_bwd_kernel<T, 1024, 16, EDGE, true>, 1024);
+  if (nvec <= 512 * 8) launch(logprob_bwd_kernel<T, 512, 8, EDGE, false, ENT>, 512);
+  else if (nvec <= 1024 * 8) launch(logprob_bwd_kernel<T, 1024, 8, EDGE, false, ENT>, 1024);
+  else if (nvec <= 1024 * kMost) launch(logprob_bwd_kernel<T, 1024, kMost, EDGE, false, ENT>, 1024);
+  else launch(logprob_bwd_kernel<T, 1024, 16, EDGE, true, ENT>, 1024);
 }
 
 }  // namespace
@@ -705,13 +948,18 @@ hipError_t launch_logprob_bwd(const LogprobBwdLaunch& a, hipStream_t s) {
   // every row of both matrices starts on a 16-byte boundary?
   const bool edge = a.vocab % per_vec != 0 || (reinterpret_cast<uintptr_t>(a.logits) & 15) != 0 ||
                     (reinterpret_cast<uintptr_t>(a.dlogits) & 15) != 0;
-  if (a.dtype == kBF16) {
-    if (edge) launch_logprob_bwd_rows<__bf16, true>(a, grid, nvec, s);
-    else launch_logprob_bwd_rows<__bf16, false>(a, grid, nvec, s);
-  } else {
-    if (edge) launch_logprob_bwd_rows<float, true>(a, grid, nvec, s);
-    else launch_logprob_bwd_rows<float, false>(a, grid, nvec, s);
-  }
+  auto launch = [&](auto elem) {
+    using T = decltype(elem);
+    if (a.dent) {
+      if (edge) launch_logprob_bwd_rows<T, true, true>(a, grid, nvec, s);
+      else launch_logprob_bwd_rows<T, false, true>(a, grid, nvec, s);
+    } else {
+      if (edge) launch_logprob_bwd_rows<T, true, false>(a, grid, nvec, s);
+      else launch_logprob_bwd_rows<T, false, false>(a, grid, nvec, s);
+    }
+  };
+  if (a.dtype == kBF16) launch((__bf16)0.f);
+  else launch(0.f);
   return hipGetLastError();
 }
 

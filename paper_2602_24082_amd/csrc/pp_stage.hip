@@ -54,7 +54,10 @@ __global__ __launch_bounds__(kThreads) void stage_kernel(StageLaunch a, StageBlo
     b -= nb.cast[c];
   }
   const int64_t i = (int64_t)b * kThreads + threadIdx.x;
-  if (i < a.n_zero) a.zero[i] = 0.f;
+  if (i < a.n_zero) {
+    a.zero[i] = 0.f;
+    if (a.zero2) a.zero2[i] = 0.f;
+  }
 }
 
 }  // namespace
