@@ -8,6 +8,7 @@ library's HIP kernels; there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -71,7 +72,7 @@ class _Desc(ctypes.Structure):
 
 
 class _EncDesc(ctypes.Structure):
-    _fields_ = [("enc_start", ctypes.POINTER(ctypes.c_int32)), ("enc_len", ctypes.POINTER(ctypes.c_int32))]
+    _fields_ = [("enc_start", ctypes.c_void_p), ("enc_len", ctypes.c_void_p)]
 
 
 class _PolicyConfig(ctypes.Structure):
@@ -602,17 +603,28 @@ class _EncHolder:
     """Keeps the int32 arrays of an Enc alive while the C struct points at them."""
 
     def __init__(self, enc: Enc):
-        c = lambda a: np.ascontiguousarray(a, dtype=np.int32)
-        self.arrays = [c(enc.enc_start), c(enc.enc_len)]
-        ptr = lambda a: a.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
-        self.desc = _EncDesc(*[ptr(a) for a in self.arrays])
+        self.arrays = [np.ascontiguousarray(a, dtype=np.int32) for a in (enc.enc_start, enc.enc_len)]
+        self.desc = _EncDesc(*[a.ctypes.data for a in self.arrays])
+        self.ref = ctypes.byref(self.desc)
 
-    @property
-    def ref(self):
-        return ctypes.byref(self.desc)
+
+def _enc_of(enc: Enc) -> _EncHolder:
+    """The C descriptor of an Enc, kept on it as a pack's is (see _desc_of)."""
+    key = (np.asarray(enc.enc_start).tobytes(), np.asarray(enc.enc_len).tobytes())
+    h = getattr(enc, "_pp_desc", None)
+    if h is None or h.key != key:
+        h = _EncHolder(enc)
+        h.key = key
+        try:
+            enc._pp_desc = h
+        except AttributeError:  # an Enc type that takes no new attributes: no caching
+            pass
+    return h
 
 
 def _check_tensor(name: str, t: torch.Tensor, shape, dtype, device):
+    if isinstance(t, torch.Tensor) and t.shape == shape and t.dtype == dtype and t.device == device and t.is_contiguous():
+        return t
     if not isinstance(t, torch.Tensor) or tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be a tensor of shape {tuple(shape)}, got "
                          f"{tuple(t.shape) if isinstance(t, torch.Tensor) else type(t).__name__}")
@@ -620,9 +632,15 @@ def _check_tensor(name: str, t: torch.Tensor, shape, dtype, device):
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.device != device:
         raise ValueError(f"{name} is on {t.device}, expected {device}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t
+    raise ValueError(f"{name} must be contiguous")
+
+
+_SAME_DEVICE = contextlib.nullcontext()
+
+
+def _device_of(dev: torch.device):
+    """Makes the tensors' device current for a call, if it is not already."""
+    return _SAME_DEVICE if dev.index == torch.cuda.current_device() else torch.cuda.device(dev)
 
 
 def _on_gpu(t: torch.Tensor):
@@ -645,13 +663,13 @@ def _cross_args(pack: Pack, enc: Enc, q, k, v, key_begin, key_end):
         if t is not None:
             _check_tensor(name, t, (T,), torch.int32, q.device)
     _on_gpu(q)
-    return _desc_of(pack), _EncHolder(enc), hq, hkv, d, _dtype_code(q)
+    return _desc_of(pack), _enc_of(enc), hq, hkv, d, _dtype_code(q)
 
 
 def pp_cross_workspace_size(pack: Pack, enc: Enc, hq: int, hkv: int, head_dim: int, dtype: int = PP_BF16):
     """(fwd, bwd) workspace bytes of cross attention."""
     f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
-    _check(lib().pp_cross_workspace_size(_desc_of(pack).ref, _EncHolder(enc).ref, dtype, hq, hkv, head_dim,
+    _check(lib().pp_cross_workspace_size(_desc_of(pack).ref, _enc_of(enc).ref, dtype, hq, hkv, head_dim,
                                          ctypes.byref(f), ctypes.byref(b)))
     return int(f.value), int(b.value)
 
@@ -670,7 +688,7 @@ def pp_cross_attn_fwd(pack: Pack, enc: Enc, q: torch.Tensor, k: torch.Tensor, v:
         n = ctypes.c_size_t(0)
         _check(lib().pp_cross_workspace_size(h.ref, e.ref, dt, hq, hkv, d, ctypes.byref(n), None))
         ws = _workspace(n.value, dev)
-    with torch.cuda.device(dev):
+    with _device_of(dev):
         _check(lib().pp_cross_attn_fwd(h.ref, e.ref, dt, hq, hkv, d, float(scale), _ptr(q), _ptr(k), _ptr(v),
                                        _ptr(key_begin), _ptr(key_end), _ptr(out), _ptr(lse), _ptr(ws), ws.numel(),
                                        _stream(dev)))
@@ -692,7 +710,7 @@ def pp_cross_attn_bwd(pack: Pack, enc: Enc, q, k, v, o, lse, dout, scale: float 
         n = ctypes.c_size_t(0)
         _check(lib().pp_cross_workspace_size(h.ref, e.ref, dt, hq, hkv, d, None, ctypes.byref(n)))
         ws = _workspace(n.value, dev)
-    with torch.cuda.device(dev):
+    with _device_of(dev):
         _check(lib().pp_cross_attn_bwd(h.ref, e.ref, dt, hq, hkv, d, float(scale), _ptr(q), _ptr(k), _ptr(v),
                                        _ptr(key_begin), _ptr(key_end), _ptr(o), _ptr(lse), _ptr(dout), _ptr(dq), _ptr(dk),
                                        _ptr(dv), _ptr(ws), ws.numel(), _stream(dev)))
@@ -728,7 +746,7 @@ def pp_tok_logprob(pack: Pack, logits: torch.Tensor, tokens: torch.Tensor, want_
         entropy = torch.empty(logits.shape[0], dtype=torch.float32, device=dev)
     if ws is None:
         ws = _workspace(_workspace_sizes(h, vocab=V, logprob=True)[2], dev)
-    with torch.cuda.device(dev):
+    with _device_of(dev):
         _check(lib().pp_tok_logprob(h.ref, dt, V, _ptr(logits), _ptr(tokens), _ptr(tok), _ptr(entropy), _ptr(ws), ws.numel(),
                                     _stream(dev)))
     return tok, entropy
@@ -743,7 +761,7 @@ def pp_tok_logprob_bwd(pack: Pack, logits, tokens, dtok: torch.Tensor, dentropy:
                else _check_tensor("dlogits", dlogits, logits.shape, logits.dtype, dev))
     if ws is None:
         ws = _workspace(_workspace_sizes(h, vocab=V, logprob=True)[2], dev)
-    with torch.cuda.device(dev):
+    with _device_of(dev):
         _check(lib().pp_tok_logprob_bwd(h.ref, dt, V, _ptr(logits), _ptr(tokens), _ptr(dtok), _ptr(dentropy), _ptr(dlogits),
                                         _ptr(ws), ws.numel(), _stream(dev)))
     return dlogits
@@ -760,7 +778,7 @@ def pp_tok_logprob_bwd_rows(pack: Pack, logits, tokens, dtok: torch.Tensor, dent
                  else _check_tensor("row_index", row_index, (n,), torch.int32, dev))
     if ws is None:
         ws = _workspace(_workspace_sizes(h, vocab=V, logprob=True)[2], dev)
-    with torch.cuda.device(dev):
+    with _device_of(dev):
         _check(lib().pp_tok_logprob_bwd_rows(h.ref, dt, V, _ptr(logits), _ptr(tokens), _ptr(dtok), _ptr(dentropy),
                                              _ptr(dlogits_rows), _ptr(row_index), _ptr(ws), ws.numel(), _stream(dev)))
     return dlogits_rows, row_index
@@ -806,7 +824,7 @@ def pp_policy_loss(pack: Pack, logp: torch.Tensor, adv: torch.Tensor, logp_old: 
         n = ctypes.c_size_t(0)
         _check(lib().pp_policy_workspace_size(h.ref, ctypes.byref(n)))
         ws = _workspace(n.value, dev)
-    with torch.cuda.device(dev):
+    with _device_of(dev):
         _check(lib().pp_policy_loss(h.ref, ctypes.byref(cfg), _ptr(logp), _ptr(logp_old), _ptr(logp_ref), _ptr(entropy),
                                     _ptr(adv), int(per_token), _ptr(mask), _ptr(loss), _ptr(stats), _ptr(counts), _ptr(dlogp),
                                     _ptr(dent), _ptr(ws), ws.numel(), _stream(dev)))

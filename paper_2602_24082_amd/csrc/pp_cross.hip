@@ -413,6 +413,133 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void cross_fwd
   if (hf == 0) p.lse[(int64_t)w.head * p.sumT + w.tok] = seen ? (st.m_ref + __log2f(l_tot)) * (1.0f / kLog2e) : 0.f;
 }
 
+// ---------------------------------------------------------------------------
+// Forward of a few rows: sampling, a token or a few of each packed row
+// ---------------------------------------------------------------------------
+
+// Up to 32 rows a packed row leave three of cross_fwd's waves without any, and its one
+// barrier a tile makes a stream of keys wait for the slowest.  Here all waves hold the
+// same 32 rows and walk 32-key blocks of their own, w, w + NW, ..., each through a ring in
+// its own part of LDS that nobody else touches: no barrier until the waves' softmaxes are
+// joined.  Bound by reading keys and values once: 64 KB of them a compute unit are in
+// flight while as much is worked on.
+template <int D, typename T>
+constexpr int kFewWaves = D * sizeof(T) > 256 ? 2 : 4;  // 128 KB of LDS at most
+
+template <int D, typename T, bool RANGES>
+__global__ __launch_bounds__((kFewWaves<D, T> * 64), 1) void cross_few_kernel(CrossParams<T> p, InlineItems inl) {
+  using O = Ops<T>;
+  using Frag = typename O::Frag;
+  constexpr int NW = kFewWaves<D, T>, NC = D / 16;
+  using Dma = RowDma<T, D, 32>;
+  struct Join {
+    f32x4 o[D / 8][64];
+  };
+  union Smem {
+    T kv[NW][2][2][32 * D];  // [wave][stage][K / V]
+    Join join[NW];
+  };
+  __shared__ __attribute__((aligned(1024))) Smem sm;
+  __shared__ float s_m[NW][32], s_l[NW][32];
+
+  const int item_idx = blockIdx.x / p.hkv, g = blockIdx.x - item_idx * p.hkv;
+  const CrossItem it = cross_item(p, inl, item_idx);
+  const int tid = threadIdx.x;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, ln = lane & 31, hf = lane >> 5;
+  const RowOf w = row_of<RANGES>(p, it, g, it.r0 + ln);
+  const WaveKeys wk = wave_keys<RANGES>(it, w, it.r0);
+  const int key0 = RANGES ? (wk.any_hi > 0 ? wk.any_lo / 32 * 32 : 0) : it.k_begin;
+  const int nb = (wk.any_hi - key0 + 31) / 32;
+  const int64_t kv_stride = (int64_t)p.hkv * D;
+  const T* kbase = p.k + ((int64_t)it.e0 * p.hkv + g) * D;
+  const T* vbase = p.v + ((int64_t)it.e0 * p.hkv + g) * D;
+  Dma dma;
+  dma.init(0, kv_stride * (sizeof(T) / 2), lane);
+  auto issue = [&](int b, int stage) {
+    const int k0 = key0 + b * 32, rows = min(32, it.elen - k0);
+    dma_rows(dma, sm.kv[wave][stage][0], kbase + k0 * kv_stride, rows);
+    dma_rows(dma, sm.kv[wave][stage][1], vbase + k0 * kv_stride, rows);
+  };
+  if (wave < nb) issue(wave, 0);
+  const int64_t qrow = ((int64_t)w.tok * p.hq + w.head) * D;
+  Frag qf[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c)
+    qf[c] = w.live ? *reinterpret_cast<const Frag*>(p.q + qrow + 16 * c + 8 * hf) : Frag{};
+  RowState<D> st;
+  st.init();
+  int stage = 0;
+  for (int b = wave; b < nb; b += NW, stage ^= 1) {
+    // the stage of the block before is free: its reads have returned
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (b + NW < nb) {
+      issue(b + NW, stage ^ 1);
+      wait_vmem<2 * Dma::N>();
+    } else {
+      wait_vmem<0>();
+    }
+    asm volatile("" ::: "memory");
+    const int k0 = key0 + b * 32;
+    const T* sK = sm.kv[wave][stage][0];
+    const T* sV = sm.kv[wave][stage][1];
+    f32x16 s[1] = {f32x16{}};
+#pragma unroll
+    for (int c = 0; c < NC; ++c) s[0] = O::mma(O::template row8<D>(sK, ln, 2 * c + hf), qf[c], s[0]);
+    if (!wk.every(k0, k0 + 32)) mask_keys<1>(s, k0, hf, w.lo, w.hi);
+    st.probabilities(s, p.scale_log2);
+#pragma unroll
+    for (int ch = 0; ch < 2; ++ch) {
+      const Frag pb = O::from_acc(s[0], ch);
+#pragma unroll
+      for (int m = 0; m < D / 32; ++m) st.o[m] = O::mma(O::template tr8<D>(sV, 16 * ch, 32 * m, lane), pb, st.o[m]);
+    }
+  }
+  // the waves' shares, in wave order; wave w finishes D / 8 / NW groups of four columns
+  const float l_own = half_swap_sum(st.l);
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < D / 8; ++q)
+    sm.join[wave].o[q][lane] = f32x4{st.o[q >> 2][4 * (q & 3)], st.o[q >> 2][4 * (q & 3) + 1], st.o[q >> 2][4 * (q & 3) + 2],
+                                     st.o[q >> 2][4 * (q & 3) + 3]};
+  if (hf == 0) {
+    s_m[wave][ln] = st.m_ref;
+    s_l[wave][ln] = l_own;
+  }
+  __syncthreads();
+  float m = kNegInf, l = 0.f, a[NW];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) m = fmaxf(m, s_m[i][ln]);
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    const float li = s_l[i][ln];
+    a[i] = li == 0.f ? 0.f : fast_exp2(s_m[i][ln] - (m == kNegInf ? 0.f : m));  // 0: the wave saw no key of the row
+    l = fmaf(li, a[i], l);
+  }
+  if (!w.in_tile) return;
+  const bool seen = w.hi > w.lo;
+  const float inv = it.slot >= 0 ? 1.f : seen ? 1.f / l : 0.f;
+  const int64_t prow = ((int64_t)it.slot * p.hkv + g) * 32 + ln;
+  if (it.slot >= 0 && !w.live) return;
+#pragma unroll
+  for (int i = 0; i < D / 8 / NW; ++i) {
+    const int q = wave * (D / 8 / NW) + i, col = 8 * q + 4 * hf;
+    f32x4 v = f32x4{};
+#pragma unroll
+    for (int j = 0; j < NW; ++j) v += sm.join[j].o[q][lane] * a[j];
+    v *= inv;
+    if (it.slot >= 0) *reinterpret_cast<f32x4*>(p.part + prow * D + col) = v;
+    else store4<T>(p.o + qrow + col, seen ? v : f32x4{});
+  }
+  if (wave != 0 || hf != 0) return;
+  if (it.slot >= 0) {
+    p.part_ml[2 * prow] = m;
+    p.part_ml[2 * prow + 1] = l;
+  } else {
+    p.lse[(int64_t)w.head * p.sumT + w.tok] = seen ? (m + __log2f(l)) * (1.0f / kLog2e) : 0.f;
+  }
+}
+
 // Joins the parts of rows whose keys were split, in part order: a row is D / 4 lanes,
 // four parts' loads in flight.
 template <int D, typename T>
@@ -1018,16 +1145,22 @@ hipError_t launch_fwd_t(const CrossLaunch& a, hipStream_t s) {
   if (a.n_items > 0) {
     TimingScope t("pp_cross_attn_fwd", s);
     const dim3 grid((unsigned)((int64_t)a.n_items * a.hkv));
-    if (a.key_begin) hipLaunchKernelGGL((cross_fwd_kernel<D, T, true>), grid, dim3(kWaves * 64), 0, s, p, inl);
-    else hipLaunchKernelGGL((cross_fwd_kernel<D, T, false>), grid, dim3(kWaves * 64), 0, s, p, inl);
+    auto launch = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, s, p, inl); };
+    if (a.tile_rows == kCrossFewRows) {
+      if (a.key_begin) launch(cross_few_kernel<D, T, true>, kFewWaves<D, T>);
+      else launch(cross_few_kernel<D, T, false>, kFewWaves<D, T>);
+    } else {
+      if (a.key_begin) launch(cross_fwd_kernel<D, T, true>, kWaves);
+      else launch(cross_fwd_kernel<D, T, false>, kWaves);
+    }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (a.n_splits > 0) {
     TimingScope t("pp_cross_attn_combine", s);
     constexpr int RPB = 256 / (D / 4);
-    const dim3 grid((unsigned)((int64_t)a.n_splits * a.hkv), (unsigned)((kCrossRows + RPB - 1) / RPB));
-    hipLaunchKernelGGL((cross_combine_kernel<D, T>), grid, dim3(256), 0, s, p, a.splits, sl, kCrossRows);
+    const dim3 grid((unsigned)((int64_t)a.n_splits * a.hkv), (unsigned)((a.tile_rows + RPB - 1) / RPB));
+    hipLaunchKernelGGL((cross_combine_kernel<D, T>), grid, dim3(256), 0, s, p, a.splits, sl, a.tile_rows);
     return hipGetLastError();
   }
   return hipSuccess;

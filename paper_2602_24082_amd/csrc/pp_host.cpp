@@ -2193,17 +2193,68 @@ pp_status read_enc(const pp_enc_desc* enc, const Batch& bt, std::vector<EncRow>*
   return PP_OK;
 }
 
-// Workgroups that fill the card twice over.  A pass whose tiles are fewer has the axis
-// that its workgroups walk split, down to kCrossLeast units of it.
-constexpr int64_t kCrossGroups = 2 * kComputeUnits;
-constexpr int64_t kCrossLeast = 4;
-
-// The longest part that a walk of `total` units (over tiles x kv-heads workgroups) is cut to.
-int64_t cross_part(int64_t tiles, int64_t total, int hkv) {
-  if (tiles * hkv >= kCrossGroups) return INT32_MAX;
-  return std::max(kCrossLeast, (total * hkv + kCrossGroups - 1) / kCrossGroups);
-}
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// What a pass of cross attention costs: its workgroups walk units (64 keys, or a step of
+// rows) of their packed row, `slots` of them at a time.
+struct CrossCost {
+  int64_t slots;      // workgroups that run at once
+  double full, half;  // us a unit takes with all slots taken, and with half of them
+  double join;        // us that joining split walks takes, and
+  double join_part;   // us more for every part
+};
+
+// One packed row's walks: `tiles` workgroups a kv-head, of `units` each.
+struct CrossWalk {
+  int64_t tiles, units;
+};
+
+// The longest walk, in units, that the pass's workgroups are cut to: none when uncut
+// walks keep the card busy, else a length that fills 1/2, 1, 2 or 3 rounds of its slots,
+// whichever is estimated fastest.
+int64_t cross_part(const std::vector<CrossWalk>& walks, int hkv, const CrossCost& c) {
+  int64_t longest = 0, tiles = 0, total = 0;
+  for (const CrossWalk& w : walks) {
+    if (w.tiles == 0 || w.units == 0) continue;
+    longest = std::max(longest, w.units);
+    tiles += w.tiles * hkv;
+    total += w.tiles * w.units * hkv;
+  }
+  if (tiles >= 4 * c.slots || longest <= 1) return INT32_MAX;
+  // full rounds, and what is left over, by itself or sharing units
+  auto time = [&](int64_t n, int64_t most) {
+    const double mean = (double)total / n, worst = (double)std::min(longest, most);
+    const int64_t rest = n % c.slots;
+    const double last = rest == 0 ? 0 : rest <= c.slots / 2 ? c.half : c.full;
+    const double one = n <= c.slots / 2 ? c.half : c.full;
+    return std::max((n / c.slots) * mean * c.full + mean * last, worst * one);
+  };
+  auto groups = [&](int64_t most) {
+    int64_t n = 0;
+    for (const CrossWalk& w : walks) n += w.units ? w.tiles * ceil_div(w.units, most) : 0;
+    return n * hkv;
+  };
+  int64_t best = INT32_MAX;
+  double best_t = time(tiles, longest);
+  for (int half_rounds : {1, 2, 4, 6}) {
+    const int64_t want = half_rounds * c.slots / 2;
+    if (want <= tiles) continue;
+    int64_t lo = 1, hi = longest;  // the shortest part that stays within `want` workgroups
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) / 2;
+      if (groups(mid) <= want) hi = mid;
+      else lo = mid + 1;
+    }
+    if (lo >= longest) continue;
+    const int64_t n = groups(lo);
+    const double t = time(n, lo) + c.join + c.join_part * n;
+    if (t < best_t) {
+      best_t = t;
+      best = lo;
+    }
+  }
+  return best;
+}
 
 struct CrossPlan {
   std::vector<CrossItem> items;
@@ -2211,6 +2262,7 @@ struct CrossPlan {
   std::vector<CrossKvItem> kv_items;
   std::vector<CrossKvSplit> kv_splits;
   int32_t slots = 0, kv_slots = 0, blocks = 0;
+  int tile_rows = kCrossRows;
   bool inline_items = false;
   Layout lay;
   size_t r_items = 0, r_splits = 0, r_kv_items = 0, r_kv_splits = 0, r_part = 0, r_ml = 0, r_ndelta = 0, r_nlse2 = 0,
@@ -2218,21 +2270,17 @@ struct CrossPlan {
 };
 
 // Row tiles against the states, most keys first.
-void build_cross_items(const Batch& bt, const std::vector<EncRow>& enc, int G, int hkv, CrossPlan* p) {
-  int64_t tiles = 0, total = 0;
-  for (int b = 0; b < bt.B; ++b) {
-    const int64_t live = (int64_t)bt.rows[b].valid * G;
-    const int64_t n = enc[b].len > 0 ? ceil_div(live, kCrossRows) : 0;
-    tiles += n;
-    total += n * ceil_div(enc[b].len, kCrossKeyUnit);
-  }
-  const int64_t most = cross_part(tiles, total, hkv);
+void build_cross_items(const Batch& bt, const std::vector<EncRow>& enc, int G, int hkv, const CrossCost& cost, CrossPlan* p) {
+  std::vector<CrossWalk> walks(bt.B);
+  for (int b = 0; b < bt.B; ++b)
+    walks[b] = CrossWalk{ceil_div((int64_t)bt.rows[b].valid * G, p->tile_rows), ceil_div(enc[b].len, kCrossKeyUnit)};
+  const int64_t most = cross_part(walks, hkv, cost);
   int32_t blk0 = 0;
   for (int b = 0; b < bt.B; ++b) {
     const Row& r = bt.rows[b];
     const int32_t rows = r.T * G, live = r.valid * G;
     const int64_t units = ceil_div(enc[b].len, kCrossKeyUnit);
-    for (int32_t r0 = 0; r0 < rows; r0 += kCrossRows) {
+    for (int32_t r0 = 0; r0 < rows; r0 += p->tile_rows) {
       CrossItem it{r.tok0, r0, rows, live, enc[b].start, enc[b].len, 0, r0 < live ? enc[b].len : 0, -1, blk0};
       const int64_t parts = r0 < live && units > 0 ? ceil_div(units, most) : 1;
       if (parts == 1) {
@@ -2255,15 +2303,12 @@ void build_cross_items(const Batch& bt, const std::vector<EncRow>& enc, int G, i
 }
 
 // Key tiles against the rows, most steps first.
-void build_cross_kv(const Batch& bt, const std::vector<EncRow>& enc, int G, int hkv, int step, CrossPlan* p) {
-  int64_t tiles = 0, total = 0;
-  for (int b = 0; b < bt.B; ++b) {
-    const int64_t live = (int64_t)bt.rows[b].valid * G;
-    const int64_t n = live > 0 ? ceil_div(enc[b].len, kCrossKeys) : 0;
-    tiles += n;
-    total += n * ceil_div(live, step);
-  }
-  const int64_t most = cross_part(tiles, total, hkv);
+void build_cross_kv(const Batch& bt, const std::vector<EncRow>& enc, int G, int hkv, int step, const CrossCost& cost,
+                    CrossPlan* p) {
+  std::vector<CrossWalk> walks(bt.B);
+  for (int b = 0; b < bt.B; ++b)
+    walks[b] = CrossWalk{ceil_div(enc[b].len, kCrossKeys), ceil_div((int64_t)bt.rows[b].valid * G, step)};
+  const int64_t most = cross_part(walks, hkv, cost);
   int32_t blk0 = 0;
   for (int b = 0; b < bt.B; ++b) {
     const Row& r = bt.rows[b];
@@ -2291,21 +2336,45 @@ void build_cross_kv(const Batch& bt, const std::vector<EncRow>& enc, int G, int 
   });
 }
 
-void plan_cross_fwd(const Batch& bt, const std::vector<EncRow>& enc, int hq, int hkv, int d, CrossPlan* p) {
-  build_cross_items(bt, enc, hq / hkv, hkv, p);
+// Rates measured on the passes (pp_cross.hip) at full and half load; fp32 products take
+// eight times as long and their kernels run one workgroup a compute unit.
+constexpr int64_t kUnits = kComputeUnits;
+CrossCost fwd_cost(pp_dtype dtype, int d, int hkv) {
+  const double part = 2e-5 * kCrossRows * d / 128;  // us: a part is written and read once
+  if (dtype == PP_FP32) return CrossCost{kUnits, d == 128 ? 10.0 : 5.0, d == 128 ? 10.0 : 5.0, 4.0, part};
+  return d == 128 ? CrossCost{2 * kUnits, 2.2, 1.4, 4.0, part} : CrossCost{2 * kUnits, 1.5, 1.0, 4.0, part};
+}
+
+void plan_cross_fwd(const Batch& bt, const std::vector<EncRow>& enc, pp_dtype dtype, int hq, int hkv, int d, CrossPlan* p) {
+  const int G = hq / hkv;
+  int64_t most = 0;
+  for (const Row& r : bt.rows) most = std::max(most, (int64_t)r.valid * G);
+  if (most <= kCrossFewRows) {
+    p->tile_rows = kCrossFewRows;
+    // a unit's keys and values come at 6 TB/s over all compute units, at 60 GB/s to one
+    const double bytes = (double)kCrossKeyUnit * d * (dtype == PP_FP32 ? 8 : 4);
+    build_cross_items(bt, enc, G, hkv, CrossCost{kUnits, bytes / 23e3, bytes / 46e3, 4.0, 2e-5 * 32 * d / 128}, p);
+  } else {
+    build_cross_items(bt, enc, G, hkv, fwd_cost(dtype, d, hkv), p);
+  }
   p->inline_items = p->items.size() <= (size_t)kCrossInline;  // and at most half as many splits
   if (!p->inline_items) {
     p->r_items = p->lay.add(p->items.size() * sizeof(CrossItem));
     p->r_splits = p->lay.add(p->splits.size() * sizeof(CrossSplit));
   }
   p->lay.meta_bytes = p->lay.total;
-  p->r_part = p->lay.add((size_t)p->slots * hkv * kCrossRows * d * 4);
-  p->r_ml = p->lay.add((size_t)p->slots * hkv * kCrossRows * 8);
+  p->r_part = p->lay.add((size_t)p->slots * hkv * p->tile_rows * d * 4);
+  p->r_ml = p->lay.add((size_t)p->slots * hkv * p->tile_rows * 8);
 }
 
 void plan_cross_bwd(const Batch& bt, const std::vector<EncRow>& enc, pp_dtype dtype, int hq, int hkv, int d, CrossPlan* p) {
-  build_cross_items(bt, enc, hq / hkv, hkv, p);
-  build_cross_kv(bt, enc, hq / hkv, hkv, dtype == PP_FP32 ? 32 : 64, p);
+  const int G = hq / hkv;
+  CrossCost dq = fwd_cost(dtype, d, hkv);
+  dq.full *= 1.3;
+  dq.half *= 1.3;
+  build_cross_items(bt, enc, G, hkv, dq, p);
+  const double step = dtype == PP_FP32 ? (d == 128 ? 10.0 : 5.0) : d == 128 ? 2.1 : 1.4;
+  build_cross_kv(bt, enc, G, hkv, dtype == PP_FP32 ? 32 : 64, CrossCost{kUnits, step, step, 4.0, 4e-5 * kCrossKeys * d / 128}, p);
   p->r_items = p->lay.add(p->items.size() * sizeof(CrossItem));
   p->r_splits = p->lay.add(p->splits.size() * sizeof(CrossSplit));
   p->r_kv_items = p->lay.add(p->kv_items.size() * sizeof(CrossKvItem));
@@ -2334,10 +2403,10 @@ pp_status check_cross(const pp_pack_desc* desc, const pp_enc_desc* enc, pp_dtype
     if (bt->rows[b].T * G > INT32_MAX - kCrossRows)
       return fail(PP_ERR_UNSUPPORTED, "row %d: %d tokens of %lld heads a kv-head exceed 2^31 rows", b, bt->rows[b].T, (long long)G);
     if ((*rows)[b].cap > INT32_MAX - kCrossKeys) return fail(PP_ERR_UNSUPPORTED, "row %d has too many encoder states", b);
-    groups += ceil_div(bt->rows[b].T * G, kCrossRows) + ceil_div((*rows)[b].cap, kCrossKeys);
+    groups += ceil_div(bt->rows[b].T * G, kCrossFewRows) + ceil_div((*rows)[b].cap, kCrossKeys);
   }
-  // a launch holds fewer than 2^32 threads, 512 a workgroup; splitting adds at most 4 * kCrossGroups workgroups
-  if (groups * hkv > 0xffffffffll / 512 - 4 * kCrossGroups)
+  // a launch holds fewer than 2^32 threads, 512 a workgroup (a batch that is split has a few thousand)
+  if (groups * hkv > 0xffffffffll / 512)
     return fail(PP_ERR_UNSUPPORTED, "the batch has too many tiles for one launch");
   return PP_OK;
 }
@@ -2355,6 +2424,30 @@ pp_status check_ranges(const int32_t* key_begin, const int32_t* key_end) {
   if (!aligned4(key_begin) || !aligned4(key_end))
     return fail(PP_ERR_INVALID_ARGUMENT, "key_begin and key_end must be 4-byte aligned");
   return PP_OK;
+}
+
+// Copies a call's records to the workspace.  A few ride in launch arguments, and so do
+// all of a call that is being captured: a graph's replays cannot read a staging buffer,
+// which later calls refill.
+pp_status stage_records(void* ws, const MetaImage& img, hipStream_t s, const StageLaunch& zeros = StageLaunch()) {
+  const size_t n = img.buf.size();
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  if (n > kInlineBytes && hipStreamIsCapturing(s, &cap) != hipSuccess) {
+    (void)hipGetLastError();
+    cap = hipStreamCaptureStatusNone;
+  }
+  if (n > kInlineBytes && cap == hipStreamCaptureStatusNone)
+    return stage_with(ws, img.buf.data(), n, s, [&](const void* dev_src) -> pp_status {
+      StageLaunch a = zeros;
+      a.src = dev_src;
+      a.dst = ws;
+      a.bytes = dev_src ? n : 0;
+      const hipError_t e = launch_stage(a, s);
+      return e == hipSuccess ? PP_OK : hip_fail(e, "stage_kernel");
+    });
+  hipError_t e = launch_inline_copy(ws, img.buf.data(), n, s);
+  if (e == hipSuccess) e = launch_stage(zeros, s);
+  return e == hipSuccess ? PP_OK : hip_fail(e, "record copy launch");
 }
 
 inline float scale_or_default(float scale, int head_dim) {
@@ -2387,7 +2480,7 @@ pp_status pp_cross_workspace_size(const pp_pack_desc* desc, const pp_enc_desc* e
     if (st != PP_OK) return st;
     if (fwd) {
       CrossPlan p;
-      plan_cross_fwd(bt, er, hq, hkv, head_dim, &p);
+      plan_cross_fwd(bt, er, dtype, hq, hkv, head_dim, &p);
       *fwd = p.lay.total;
     }
     if (bwd) {
@@ -2414,7 +2507,7 @@ pp_status pp_cross_attn_fwd(const pp_pack_desc* desc, const pp_enc_desc* enc, pp
       return fail(PP_ERR_INVALID_ARGUMENT, "q, k, v and o must be 16-byte aligned, lse 4-byte aligned");
     if ((st = check_ranges(key_begin, key_end)) != PP_OK) return st;
     CrossPlan p;
-    plan_cross_fwd(bt, er, hq, hkv, head_dim, &p);
+    plan_cross_fwd(bt, er, dtype, hq, hkv, head_dim, &p);
     if ((st = check_cross_ws(p.lay, ws, ws_bytes)) != PP_OK) return st;
     if (bt.sumT == 0) return PP_OK;
     hipStream_t s = (hipStream_t)hip_stream;
@@ -2430,6 +2523,7 @@ pp_status pp_cross_attn_fwd(const pp_pack_desc* desc, const pp_enc_desc* enc, pp
     a.host_splits = p.splits.data();
     a.n_items = (int)p.items.size();
     a.n_splits = (int)p.splits.size();
+    a.tile_rows = p.tile_rows;
     a.part = (float*)at(ws, p.lay, p.r_part);
     a.part_ml = (float*)at(ws, p.lay, p.r_ml);
     a.hq = hq;
@@ -2442,7 +2536,7 @@ pp_status pp_cross_attn_fwd(const pp_pack_desc* desc, const pp_enc_desc* enc, pp
       MetaImage img;
       img.put(p.lay.regions[p.r_items], p.items.data(), p.items.size() * sizeof(CrossItem));
       img.put(p.lay.regions[p.r_splits], p.splits.data(), p.splits.size() * sizeof(CrossSplit));
-      if ((st = stage_copy(ws, img.buf.data(), img.buf.size(), s)) != PP_OK) return st;
+      if ((st = stage_records(ws, img, s)) != PP_OK) return st;
       a.items = (const CrossItem*)at(ws, p.lay, p.r_items);
       a.splits = (const CrossSplit*)at(ws, p.lay, p.r_splits);
     }
@@ -2478,7 +2572,7 @@ pp_status pp_cross_attn_bwd(const pp_pack_desc* desc, const pp_enc_desc* enc, pp
     img.put(p.lay.regions[p.r_splits], p.splits.data(), p.splits.size() * sizeof(CrossSplit));
     img.put(p.lay.regions[p.r_kv_items], p.kv_items.data(), p.kv_items.size() * sizeof(CrossKvItem));
     img.put(p.lay.regions[p.r_kv_splits], p.kv_splits.data(), p.kv_splits.size() * sizeof(CrossKvSplit));
-    if ((st = stage_copy(ws, img.buf.data(), img.buf.size(), s)) != PP_OK) return st;
+    if ((st = stage_records(ws, img, s)) != PP_OK) return st;
     CrossLaunch a{};
     a.q = q;
     a.k = k;
@@ -2567,7 +2661,7 @@ pp_status tok_logprob_bwd_impl(const pp_pack_desc* desc, pp_dtype dtype, int voc
   hipStream_t s = (hipStream_t)hip_stream;
   MetaImage img;
   tok_image(bt, p, !gathered, &img);
-  if ((st = stage_copy(ws, img.buf.data(), img.buf.size(), s)) != PP_OK) return st;
+  if ((st = stage_records(ws, img, s)) != PP_OK) return st;
   LogprobBwdLaunch a{};
   a.logits = logits;
   a.tokens = tokens;
@@ -2617,16 +2711,13 @@ pp_status pp_tok_logprob(const pp_pack_desc* desc, pp_dtype logits_dtype, int vo
     a.n_rows = (int)p.n.rows;
     a.vocab = vocab;
     a.dtype = logits_dtype == PP_FP32 ? kFP32 : kBF16;
-    return stage_with(ws, img.buf.data(), img.buf.size(), s, [&](const void* dev_src) -> pp_status {
-      StageLaunch pre = stage_of(ws, dev_src, img.buf.size());
-      pre.zero = tok_logp;  // 0 off the responses
-      pre.zero2 = tok_entropy;
-      pre.n_zero = bt.sumT;
-      hipError_t e = launch_stage(pre, s);
-      if (e != hipSuccess) return hip_fail(e, "stage_kernel");
-      e = launch_logprob(a, s);
-      return e == hipSuccess ? PP_OK : hip_fail(e, "log-prob launch");
-    });
+    StageLaunch zeros;
+    zeros.zero = tok_logp;  // 0 off the responses
+    zeros.zero2 = tok_entropy;
+    zeros.n_zero = bt.sumT;
+    if ((st = stage_records(ws, img, s, zeros)) != PP_OK) return st;
+    const hipError_t e = launch_logprob(a, s);
+    return e == hipSuccess ? PP_OK : hip_fail(e, "log-prob launch");
   });
 }
 
@@ -2763,7 +2854,9 @@ pp_status pp_policy_loss(const pp_pack_desc* desc, const pp_policy_config* cfg, 
     a.slot_counts = (int32_t*)at(ws, p.lay, p.r_counts);
     a.part = (PolicyPartial*)at(ws, p.lay, p.r_part);
     if (!p.inline_slots) {
-      if ((st = stage_copy(ws, p.slots.data(), p.slots.size() * sizeof(PolicySlot), s)) != PP_OK) return st;
+      MetaImage img;
+      img.put(p.lay.regions[p.r_slots], p.slots.data(), p.slots.size() * sizeof(PolicySlot));
+      if ((st = stage_records(ws, img, s)) != PP_OK) return st;
       a.slots = (const PolicySlot*)at(ws, p.lay, p.r_slots);
     }
     const hipError_t e = launch_policy(a, s);

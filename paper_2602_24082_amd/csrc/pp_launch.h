@@ -55,6 +55,11 @@ struct StageLaunch {
 };
 hipError_t launch_stage(const StageLaunch& a, hipStream_t s);
 
+// Copies host bytes into device memory by way of launch arguments, kInlineBytes a launch:
+// nothing of it is left to be read when the call returns, so a captured graph replays it.
+constexpr size_t kInlineBytes = 3584;
+hipError_t launch_inline_copy(void* dst, const void* src, size_t bytes, hipStream_t s);
+
 // Blocks of kStageThreads threads of that launch: the copy's first, then each
 // conversion's, then the zeros'.  A launch holds fewer than 2^32 threads in all, and the
 // conversions of a large fp32 batch may be more vectors than that together, so each
@@ -175,7 +180,8 @@ struct CrossLaunch {
   const CrossKvItem* kv_items = nullptr;
   const CrossKvSplit* kv_splits = nullptr;
   int n_kv_items = 0, n_kv_splits = 0;
-  float* part;               // partial rows of split items, [slot][hkv][kCrossRows][head_dim]
+  int tile_rows = kCrossRows;  // rows of an item (forward: or kCrossFewRows)
+  float* part;               // partial rows of split items, [slot][hkv][tile_rows][head_dim]
   float* part_ml;            // forward: their maximum and sum
   float* kv_part = nullptr;  // [slot][hkv][2][kCrossKeys * head_dim]
   float* ndelta = nullptr;   // [hkv][sumT G]

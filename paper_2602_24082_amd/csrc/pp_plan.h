@@ -176,6 +176,7 @@ struct RespItem {
 // kv-head's group are one list of rows, row r = token r / G, head r % G
 
 constexpr int kCrossRows = 128;    // rows per forward and dQ workgroup
+constexpr int kCrossFewRows = 32;  // rows per workgroup of the forward for few rows
 constexpr int kCrossKeys = 128;    // keys per dK/dV workgroup
 constexpr int kCrossKeyUnit = 64;  // parts of a row's keys are multiples of this
 constexpr int kCrossInline = 64;   // forward items that fit into the launch's arguments

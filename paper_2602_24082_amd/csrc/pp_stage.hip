@@ -10,6 +10,7 @@
 // enqueued seven conversions and two copies of 2 us each, and now two launches.
 
 #include <hip/hip_runtime.h>
+#include <string.h>
 
 #include "pp_device.h"
 #include "pp_launch.h"
@@ -60,7 +61,30 @@ __global__ __launch_bounds__(kThreads) void stage_kernel(StageLaunch a, StageBlo
   }
 }
 
+struct InlineBytes {
+  Chunk16 v[kInlineBytes / 16];
+};
+
+__global__ __launch_bounds__(kInlineBytes / 16) void inline_copy_kernel(Chunk16* dst, int n, InlineBytes b) {
+  if ((int)threadIdx.x < n) dst[threadIdx.x] = b.v[threadIdx.x];
+}
+
 }  // namespace
+
+// dst is 16-byte aligned, with room for whole 16-byte vectors.
+hipError_t launch_inline_copy(void* dst, const void* src, size_t bytes, hipStream_t s) {
+  TimingScope t("pp_stage", s);
+  for (size_t off = 0; off < bytes; off += kInlineBytes) {
+    InlineBytes b;
+    const size_t n = bytes - off < kInlineBytes ? bytes - off : kInlineBytes;
+    memcpy(b.v, static_cast<const uint8_t*>(src) + off, n);
+    hipLaunchKernelGGL(inline_copy_kernel, dim3(1), dim3(kInlineBytes / 16), 0, s,
+                       reinterpret_cast<Chunk16*>(static_cast<uint8_t*>(dst) + off), (int)((n + 15) / 16), b);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 
 hipError_t launch_stage(const StageLaunch& a, hipStream_t s) {
   const StageBlocks nb = stage_blocks(a);

@@ -113,31 +113,52 @@ def test_step_on_another_stream():
         assert torch.equal(want[n], got[n]), n
 
 
-def test_captured_calls_replay():
-    """Each operator captured with its own workspace and replayed on new inputs between eager calls.
-    Batches whose records ride in the launches' arguments need no copy from the host."""
-    pack, enc, x, begin, end = _inputs(740)
-    q, k, v = (x[n].clone() for n in ("q", "k", "v"))
-    f, b = pp.pp_cross_workspace_size(pack, enc, HQ, HKV, D, pp.PP_FP32)
-    lp, adv, mask = x["drift"].clone(), x["adv"].clone(), x["mask"].clone()
-    ws = torch.empty(max(f, 1), dtype=torch.uint8, device=DEV)
-    wp = torch.empty(pp.pp_policy_workspace_size(pack), dtype=torch.uint8, device=DEV)
-    old = x["ref"].clone()
+@pytest.mark.parametrize("rows", [1, 40])
+def test_captured_calls_replay(rows):
+    """Every operator captured with its own workspace and replayed on new inputs between eager calls, which
+    refill the staging buffers: with records that ride in launch arguments, and with many of them."""
+    pack = wl.make_pack([20, 7] * rows, [[9, 30, 1], [0, 12]] * rows, pad=[2, 0] * rows)
+    enc = wl.make_enc([70, 33] * rows, pad=[0, 3] * rows)
+    T, vocab = pack.total_tokens, 200
+    other = wl.make_pack([11] * 2 * rows, [[5, 6, 7]] * 2 * rows), wl.make_enc([15] * 2 * rows)
+    x = {"q": (T, HQ, D), "k": (enc.total_states, HKV, D), "v": (enc.total_states, HKV, D), "do": (T, HQ, D), "lp": (T,),
+         "old": (T,), "adv": (2 * rows, 3), "logits": (T, vocab), "dtok": (T,), "dent": (T,)}
+    x = {n: torch.randn(shape, device=DEV) for n, shape in x.items()}
+    tokens = wl.randint((T,), vocab, 5, DEV)
+    mask = (torch.rand(T, device=DEV) > 0.2).to(torch.uint8)
 
-    def calls(ws, wp):
-        o, lse = pp.pp_cross_attn_fwd(pack, enc, q, k, v, key_begin=begin, key_end=end, ws=ws)
-        loss, stats, counts, dlp, _ = pp.pp_policy_loss(pack, lp, adv, logp_old=old, mask=mask, reduction="seq", ws=wp)
-        return o, lse, loss, stats, counts, dlp
+    def workspaces(pack, enc):
+        f, b = pp.pp_cross_workspace_size(pack, enc, HQ, HKV, D, pp.PP_FP32)
+        n = [f, b, pp.pp_policy_workspace_size(pack)] + [pp.pp_workspace_size(pack, vocab=vocab, fwd=False, bwd=False,
+                                                                             logprob=True, loss=False)[2]] * 3
+        return [torch.empty(max(i, 1), dtype=torch.uint8, device=DEV) for i in n]
 
-    calls(ws, wp)
+    def calls(pack, enc, x, tokens, mask, ws):
+        o, lse = pp.pp_cross_attn_fwd(pack, enc, x["q"], x["k"], x["v"], ws=ws[0])
+        grads = pp.pp_cross_attn_bwd(pack, enc, x["q"], x["k"], x["v"], o, lse, x["do"], ws=ws[1])
+        loss, stats, counts, dlp, _ = pp.pp_policy_loss(pack, x["lp"], x["adv"], logp_old=x["old"], mask=mask, reduction="seq",
+                                                        ws=ws[2])
+        tok, ent = pp.pp_tok_logprob(pack, x["logits"], tokens, want_entropy=True, ws=ws[3])
+        dl = pp.pp_tok_logprob_bwd(pack, x["logits"], tokens, x["dtok"], x["dent"], ws=ws[4])
+        dr, idx = pp.pp_tok_logprob_bwd_rows(pack, x["logits"], tokens, x["dtok"], x["dent"], ws=ws[5])
+        return (o, lse, *grads, loss, stats, counts, dlp, tok, ent, dl, dr, idx)
+
+    ws, ws2 = workspaces(pack, enc), workspaces(*other)
+    n2 = other[0].total_tokens
+    y = {n: torch.randn((n2, *t.shape[1:]) if len(t) == T else (2 * rows, 3) if n == "adv" else
+                        (other[1].total_states, HKV, D), device=DEV) for n, t in x.items()}
+    calls(pack, enc, x, tokens, mask, ws)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
-        out = calls(ws, wp)
+        out = calls(pack, enc, x, tokens, mask, ws)
     for i in range(3):
-        for t in (q, k, v, lp, adv):
+        for _ in range(20):
+            calls(*other, y, tokens[:n2] if n2 <= T else torch.zeros(n2, dtype=torch.int32, device=DEV),
+                  torch.ones(n2, dtype=torch.uint8, device=DEV), ws2)
+        for n, t in x.items():
             t.copy_(torch.randn(t.shape, generator=torch.Generator(DEV).manual_seed(i), device=DEV))
         graph.replay()
         torch.cuda.synchronize()
-        for a, c in zip(out, calls(None, None)):
+        for a, c in zip(out, calls(pack, enc, x, tokens, mask, [None] * 6)):
             assert torch.equal(a, c), i
