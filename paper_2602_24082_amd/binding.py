@@ -635,6 +635,23 @@ def _check_tensor(name: str, t: torch.Tensor, shape, dtype, device):
     raise ValueError(f"{name} must be contiguous")
 
 
+def _addr(t: Optional[torch.Tensor]):
+    """Address of a tensor that has been checked (None: NULL)."""
+    return None if t is None else t.data_ptr()
+
+
+def _raw_stream(dev: torch.device) -> int:
+    # without the Stream object that torch.cuda.current_stream builds (2 us)
+    return torch._C._cuda_getCurrentRawStream(dev.index)
+
+
+def _ws_bytes(ws: torch.Tensor, dev: torch.device) -> int:
+    """Bytes of a workspace, the caller's own checked."""
+    if ws.device != dev or not ws.is_contiguous():
+        raise ValueError(f"ws must be contiguous, on {dev}")
+    return ws.numel() * ws.element_size()
+
+
 _SAME_DEVICE = contextlib.nullcontext()
 
 
@@ -686,12 +703,12 @@ def pp_cross_attn_fwd(pack: Pack, enc: Enc, q: torch.Tensor, k: torch.Tensor, v:
            else _check_tensor("lse", lse, (hq, T), torch.float32, dev))
     if ws is None:
         n = ctypes.c_size_t(0)
-        _check(lib().pp_cross_workspace_size(h.ref, e.ref, dt, hq, hkv, d, ctypes.byref(n), None))
+        _check(lib().pp_cross_workspace_size(h.ref, e.ref, dt, hq, hkv, d, n, None))
         ws = _workspace(n.value, dev)
     with _device_of(dev):
-        _check(lib().pp_cross_attn_fwd(h.ref, e.ref, dt, hq, hkv, d, float(scale), _ptr(q), _ptr(k), _ptr(v),
-                                       _ptr(key_begin), _ptr(key_end), _ptr(out), _ptr(lse), _ptr(ws), ws.numel(),
-                                       _stream(dev)))
+        _check(lib().pp_cross_attn_fwd(h.ref, e.ref, dt, hq, hkv, d, float(scale), _addr(q), _addr(k), _addr(v),
+                                       _addr(key_begin), _addr(key_end), _addr(out), _addr(lse), _addr(ws), _ws_bytes(ws, dev),
+                                       _raw_stream(dev)))
     return out, lse
 
 
@@ -711,9 +728,9 @@ def pp_cross_attn_bwd(pack: Pack, enc: Enc, q, k, v, o, lse, dout, scale: float 
         _check(lib().pp_cross_workspace_size(h.ref, e.ref, dt, hq, hkv, d, None, ctypes.byref(n)))
         ws = _workspace(n.value, dev)
     with _device_of(dev):
-        _check(lib().pp_cross_attn_bwd(h.ref, e.ref, dt, hq, hkv, d, float(scale), _ptr(q), _ptr(k), _ptr(v),
-                                       _ptr(key_begin), _ptr(key_end), _ptr(o), _ptr(lse), _ptr(dout), _ptr(dq), _ptr(dk),
-                                       _ptr(dv), _ptr(ws), ws.numel(), _stream(dev)))
+        _check(lib().pp_cross_attn_bwd(h.ref, e.ref, dt, hq, hkv, d, float(scale), _addr(q), _addr(k), _addr(v),
+                                       _addr(key_begin), _addr(key_end), _addr(o), _addr(lse), _addr(dout), _addr(dq), _addr(dk),
+                                       _addr(dv), _addr(ws), _ws_bytes(ws, dev), _raw_stream(dev)))
     return dq, dk, dv
 
 
@@ -747,8 +764,8 @@ def pp_tok_logprob(pack: Pack, logits: torch.Tensor, tokens: torch.Tensor, want_
     if ws is None:
         ws = _workspace(_workspace_sizes(h, vocab=V, logprob=True)[2], dev)
     with _device_of(dev):
-        _check(lib().pp_tok_logprob(h.ref, dt, V, _ptr(logits), _ptr(tokens), _ptr(tok), _ptr(entropy), _ptr(ws), ws.numel(),
-                                    _stream(dev)))
+        _check(lib().pp_tok_logprob(h.ref, dt, V, _addr(logits), _addr(tokens), _addr(tok), _addr(entropy), _addr(ws), _ws_bytes(ws, dev),
+                                    _raw_stream(dev)))
     return tok, entropy
 
 
@@ -762,8 +779,8 @@ def pp_tok_logprob_bwd(pack: Pack, logits, tokens, dtok: torch.Tensor, dentropy:
     if ws is None:
         ws = _workspace(_workspace_sizes(h, vocab=V, logprob=True)[2], dev)
     with _device_of(dev):
-        _check(lib().pp_tok_logprob_bwd(h.ref, dt, V, _ptr(logits), _ptr(tokens), _ptr(dtok), _ptr(dentropy), _ptr(dlogits),
-                                        _ptr(ws), ws.numel(), _stream(dev)))
+        _check(lib().pp_tok_logprob_bwd(h.ref, dt, V, _addr(logits), _addr(tokens), _addr(dtok), _addr(dentropy), _addr(dlogits),
+                                        _addr(ws), _ws_bytes(ws, dev), _raw_stream(dev)))
     return dlogits
 
 
@@ -779,8 +796,8 @@ def pp_tok_logprob_bwd_rows(pack: Pack, logits, tokens, dtok: torch.Tensor, dent
     if ws is None:
         ws = _workspace(_workspace_sizes(h, vocab=V, logprob=True)[2], dev)
     with _device_of(dev):
-        _check(lib().pp_tok_logprob_bwd_rows(h.ref, dt, V, _ptr(logits), _ptr(tokens), _ptr(dtok), _ptr(dentropy),
-                                             _ptr(dlogits_rows), _ptr(row_index), _ptr(ws), ws.numel(), _stream(dev)))
+        _check(lib().pp_tok_logprob_bwd_rows(h.ref, dt, V, _addr(logits), _addr(tokens), _addr(dtok), _addr(dentropy),
+                                             _addr(dlogits_rows), _addr(row_index), _addr(ws), _ws_bytes(ws, dev), _raw_stream(dev)))
     return dlogits_rows, row_index
 
 
@@ -825,9 +842,9 @@ def pp_policy_loss(pack: Pack, logp: torch.Tensor, adv: torch.Tensor, logp_old: 
         _check(lib().pp_policy_workspace_size(h.ref, ctypes.byref(n)))
         ws = _workspace(n.value, dev)
     with _device_of(dev):
-        _check(lib().pp_policy_loss(h.ref, ctypes.byref(cfg), _ptr(logp), _ptr(logp_old), _ptr(logp_ref), _ptr(entropy),
-                                    _ptr(adv), int(per_token), _ptr(mask), _ptr(loss), _ptr(stats), _ptr(counts), _ptr(dlogp),
-                                    _ptr(dent), _ptr(ws), ws.numel(), _stream(dev)))
+        _check(lib().pp_policy_loss(h.ref, ctypes.byref(cfg), _addr(logp), _addr(logp_old), _addr(logp_ref), _addr(entropy),
+                                    _addr(adv), int(per_token), _addr(mask), _addr(loss), _addr(stats), _addr(counts), _addr(dlogp),
+                                    _addr(dent), _addr(ws), _ws_bytes(ws, dev), _raw_stream(dev)))
     return loss, stats, counts, dlogp, dent
 
 

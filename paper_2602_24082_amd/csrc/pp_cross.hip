@@ -269,6 +269,10 @@ template <typename T>
 constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
 constexpr int kStages = 2;
 constexpr int kWaves = 4;
+template <int D, typename T>
+constexpr int kFwdPerCu = sizeof(T) == 4 ? 1 : D == 64 ? 4 : 2;  // workgroups a compute unit
+template <int D, typename T>
+constexpr int kDqPerCu = sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2;
 static_assert(32 * kWaves == kCrossRows, "rows a workgroup");
 
 // The keys [t0, t1) that a workgroup of kWaves waves walks, from tile-aligned t0.
@@ -297,7 +301,7 @@ __device__ __forceinline__ void block_keys(const CrossItem& it, const WaveKeys& 
 }
 
 template <int D, typename T, bool RANGES>
-__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void cross_fwd_kernel(CrossParams<T> p, InlineItems inl) {
+__global__ __launch_bounds__(kWaves * 64, (kFwdPerCu<D, T>)) void cross_fwd_kernel(CrossParams<T> p, InlineItems inl) {
   using O = Ops<T>;
   using Frag = typename O::Frag;
   constexpr int BN = kKeys<T>, KB = BN / 32, RPW = BN / kWaves;
@@ -421,8 +425,7 @@ __global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void cross_fwd
 // barrier a tile makes a stream of keys wait for the slowest.  Here all waves hold the
 // same 32 rows and walk 32-key blocks of their own, w, w + NW, ..., each through a ring in
 // its own part of LDS that nobody else touches: no barrier until the waves' softmaxes are
-// joined.  Bound by reading keys and values once: 64 KB of them a compute unit are in
-// flight while as much is worked on.
+// joined.  Bound by reading keys and values once.
 template <int D, typename T>
 constexpr int kFewWaves = D * sizeof(T) > 256 ? 2 : 4;  // 128 KB of LDS at most
 
@@ -456,12 +459,21 @@ __global__ __launch_bounds__((kFewWaves<D, T> * 64), 1) void cross_few_kernel(Cr
   const T* vbase = p.v + ((int64_t)it.e0 * p.hkv + g) * D;
   Dma dma;
   dma.init(0, kv_stride * (sizeof(T) / 2), lane);
-  auto issue = [&](int b, int stage) {
-    const int k0 = key0 + b * 32, rows = min(32, it.elen - k0);
-    dma_rows(dma, sm.kv[wave][stage][0], kbase + k0 * kv_stride, rows);
-    dma_rows(dma, sm.kv[wave][stage][1], vbase + k0 * kv_stride, rows);
+  // Block i of this wave: its K and V in stage i & 1, each refilled with block i + 2's as
+  // soon as it has been read, so three quarters of the ring are in flight.
+  auto key_of = [&](int i) { return key0 + (wave + i * NW) * 32; };
+  auto issue = [&](int i, int kv, const T* base) {
+    const int k0 = key_of(i);
+    dma_rows(dma, sm.kv[wave][i & 1][kv], base + k0 * kv_stride, min(32, it.elen - k0));
   };
-  if (wave < nb) issue(wave, 0);
+  const int n = wave < nb ? (nb - wave + NW - 1) / NW : 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (i < n) {
+      issue(i, 0, kbase);
+      issue(i, 1, vbase);
+    }
+  }
   const int64_t qrow = ((int64_t)w.tok * p.hq + w.head) * D;
   Frag qf[NC];
 #pragma unroll
@@ -469,31 +481,35 @@ __global__ __launch_bounds__((kFewWaves<D, T> * 64), 1) void cross_few_kernel(Cr
     qf[c] = w.live ? *reinterpret_cast<const Frag*>(p.q + qrow + 16 * c + 8 * hf) : Frag{};
   RowState<D> st;
   st.init();
-  int stage = 0;
-  for (int b = wave; b < nb; b += NW, stage ^= 1) {
-    // the stage of the block before is free: its reads have returned
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    if (b + NW < nb) {
-      issue(b + NW, stage ^ 1);
-      wait_vmem<2 * Dma::N>();
-    } else {
-      wait_vmem<0>();
-    }
+  for (int i = 0; i < n; ++i) {
+    // in flight behind K(i): V(i), and K and V of block i + 1 if there is one (at the
+    // first block Q's loads too, which then are waited for as well)
+    if (i == 0) wait_vmem<0>();
+    else if (i + 1 < n) wait_vmem<3 * Dma::N>();
+    else wait_vmem<Dma::N>();
     asm volatile("" ::: "memory");
-    const int k0 = key0 + b * 32;
-    const T* sK = sm.kv[wave][stage][0];
-    const T* sV = sm.kv[wave][stage][1];
+    const int k0 = key_of(i);
+    const T* sK = sm.kv[wave][i & 1][0];
+    const T* sV = sm.kv[wave][i & 1][1];
     f32x16 s[1] = {f32x16{}};
 #pragma unroll
     for (int c = 0; c < NC; ++c) s[0] = O::mma(O::template row8<D>(sK, ln, 2 * c + hf), qf[c], s[0]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K's reads have returned
+    if (i + 2 < n) issue(i + 2, 0, kbase);
     if (!wk.every(k0, k0 + 32)) mask_keys<1>(s, k0, hf, w.lo, w.hi);
     st.probabilities(s, p.scale_log2);
+    if (i + 2 < n) wait_vmem<3 * Dma::N>();  // behind V(i): K and V of i + 1, K of i + 2
+    else if (i + 1 < n) wait_vmem<2 * Dma::N>();
+    else wait_vmem<0>();
+    asm volatile("" ::: "memory");
 #pragma unroll
     for (int ch = 0; ch < 2; ++ch) {
       const Frag pb = O::from_acc(s[0], ch);
 #pragma unroll
       for (int m = 0; m < D / 32; ++m) st.o[m] = O::mma(O::template tr8<D>(sV, 16 * ch, 32 * m, lane), pb, st.o[m]);
     }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V's too
+    if (i + 2 < n) issue(i + 2, 1, vbase);
   }
   // the waves' shares, in wave order; wave w finishes D / 8 / NW groups of four columns
   const float l_own = half_swap_sum(st.l);
@@ -592,7 +608,7 @@ __global__ __launch_bounds__(256) void cross_combine_kernel(CrossParams<T> p, co
 // ---------------------------------------------------------------------------
 
 template <int D, typename T, bool RANGES>
-__global__ __launch_bounds__(kWaves * 64, sizeof(T) == 2 ? 2 : 1) void cross_dq_kernel(CrossParams<T> p) {
+__global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel(CrossParams<T> p) {
   using O = Ops<T>;
   using Frag = typename O::Frag;
   constexpr int BN = kKeys<T>, KB = BN / 32, RPW = BN / kWaves;
@@ -781,15 +797,18 @@ __global__ __launch_bounds__(256) void cross_dq_sum_kernel(CrossParams<T> p, con
 // dK, dV: key-major
 // ---------------------------------------------------------------------------
 
-// bf16: eight waves; waves w and w + 4 own keys 32 (w % 4) .. +31 and take the two
-// 32-row halves of every 64-row step; K and V of the tile stay in LDS (head size 128) or
-// in registers (64).  fp32: four waves, 32-row steps, K and V in registers.
+// Head size 128, bf16: eight waves; waves w and w + 4 own keys 32 (w % 4) .. +31 and take
+// the two 32-row halves of every 64-row step; K and V of the tile stay in LDS.
+// Head size 64 or fp32: four waves and 32-row steps, K and V in registers; with bf16 two
+// workgroups share a compute unit, and one's barriers pass under the other's products.
 template <int D, typename T>
 struct KvShape {
-  static constexpr int QB = sizeof(T) == 2 ? 2 : 1;   // row blocks a step
-  static constexpr int STEP = 32 * QB;
+  static constexpr bool HOLD = D * sizeof(T) != 256 || D == 64;
+  static constexpr int QB = HOLD ? 1 : 2;  // row blocks a step
+  static constexpr int STEP = kCrossStep(D, sizeof(T) == 4);
   static constexpr int WAVES = 4 * QB;
-  static constexpr bool HOLD = sizeof(T) == 4 || D == 64;
+  static constexpr int PER_CU = HOLD && sizeof(T) == 2 ? 2 : 1;
+  static_assert(STEP == 32 * QB, "rows a step");
 };
 
 template <int D, typename T>
@@ -817,7 +836,7 @@ struct KvSmem : KvTiles<D, T, KvShape<D, T>::HOLD> {
 };
 
 template <int D, typename T, bool RANGES>
-__global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), 1) void cross_dkdv_kernel(CrossParams<T> p) {
+__global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), (KvShape<D, T>::PER_CU)) void cross_dkdv_kernel(CrossParams<T> p) {
   using O = Ops<T>;
   using Frag = typename O::Frag;
   using S = KvShape<D, T>;
@@ -861,19 +880,28 @@ __global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), 1) void cross_dkdv_ker
     }
   }
 
-  // RANGES: the next step from n on in which some row sees a key of the tile
+  // RANGES: the next step from n on in which some row sees a key of the tile.  A lane
+  // looks at a step, 64 of them at a time.
   const CrossRange* ranges = RANGES ? p.ranges + it.blk0 : nullptr;
+  uint64_t hits = 0;
+  int hits0 = 0, hits_end = 0;  // the steps that `hits` stands for
   auto next_step = [&](int n) {
     if constexpr (RANGES) {
-      for (; n < it.n_end; ++n) {
-        bool hit = false;
+      while (n < it.n_end) {
+        if (n >= hits_end) {
+          hits0 = n;
+          hits_end = n + 64;
+          bool hit = false;
 #pragma unroll
-        for (int b = 0; b < S::QB; ++b) {
-          const int blk = n * S::QB + b;
-          if (blk * 32 >= it.live) break;
-          hit |= scalar_load(&ranges[blk].any_lo) < k1 && scalar_load(&ranges[blk].any_hi) > it.k0;
+          for (int b = 0; b < S::QB; ++b) {
+            const int blk = (n + lane) * S::QB + b;
+            if (n + lane < it.n_end && blk * 32 < it.live) hit |= ranges[blk].any_lo < k1 && ranges[blk].any_hi > it.k0;
+          }
+          hits = __ballot(hit);
         }
-        if (hit) break;
+        const uint64_t rest = hits >> (n - hits0);
+        if (rest) return n + __builtin_ctzll(rest);
+        n = hits_end;
       }
     }
     return n;
@@ -1064,37 +1092,57 @@ __global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), 1) void cross_dkdv_ker
   }
 }
 
-// Adds the parts of key tiles whose rows were split, in part order: a workgroup is four
-// consecutive accumulator registers of the tile's four key blocks, of one gradient.
+// Adds the parts of key tiles whose rows were split, in part order.  A workgroup is one
+// gradient of 32 keys: it reads the parts as they lie in the accumulators and turns the
+// sums through LDS, so that a gradient's row is written by one workgroup and whole lines
+// at a time (written 8 bytes a lane from 16 workgroups, 27 MB of parts took 17 us).
 template <int D, typename T>
 __global__ __launch_bounds__(256) void cross_kv_sum_kernel(CrossParams<T> p, const CrossKvSplit* splits) {
+  constexpr int NQ = D / 8 / 4;  // groups of four registers a wave takes
+  __shared__ T s_row[32][D + 16 / sizeof(T)];
   int b = blockIdx.x;
-  const int ch = b % (D / 8);  // 4 m + r4
-  b /= D / 8;
+  const int kb = b & 3;
+  b >>= 2;
   const int g = b % p.hkv;
   b /= p.hkv;
   const int pass = b & 1;
   const CrossKvSplit sp = load_uniform(splits + (b >> 1));
-  const int kb = threadIdx.x >> 6, lane = threadIdx.x & 63, hf = lane >> 5;
-  const int j = sp.k0 + kb * 32 + (lane & 31);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, hf = lane >> 5;
+  const int j0 = sp.k0 + kb * 32;
+  if (j0 >= sp.ecap) return;
   const int64_t stride = (int64_t)p.hkv * 2 * 4 * (32 * D);
-  const float* part = p.part + ((((int64_t)sp.slot0 * p.hkv + g) * 2 + pass) * 4 + kb) * (32 * D) + (ch * 64 + lane) * 4;
-  f32x4 acc = f32x4{};
-  constexpr int NP = 4;
+  const float* part =
+      p.part + ((((int64_t)sp.slot0 * p.hkv + g) * 2 + pass) * 4 + kb) * (32 * D) + (wave * NQ * 64 + lane) * 4;
+  f32x4 acc[NQ];
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) acc[q] = f32x4{};
+  constexpr int NP = 2;  // parts in flight
   for (int i = 0; i < sp.parts; i += NP, part += NP * stride) {
-    f32x4 x[NP];
+    f32x4 x[NP][NQ];
 #pragma unroll
     for (int n = 0; n < NP; ++n)
-      if (i + n < sp.parts) x[n] = *reinterpret_cast<const f32x4*>(part + n * stride);
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+        if (i + n < sp.parts) x[n][q] = *reinterpret_cast<const f32x4*>(part + n * stride + q * 256);
 #pragma unroll
     for (int n = 0; n < NP; ++n)
-      if (i + n < sp.parts) acc += x[n];
+#pragma unroll
+      for (int q = 0; q < NQ; ++q)
+        if (i + n < sp.parts) acc[q] += x[n][q];
   }
-  if (j >= sp.ecap) return;
-  acc *= pass == 0 ? p.scale : 1.f;
-  if (j >= sp.elen) acc = f32x4{};
-  T* dst = (pass == 0 ? p.dk : p.dv) + ((int64_t)(sp.e0 + j) * p.hkv + g) * D;
-  store4<T>(dst + 32 * (ch >> 2) + 8 * (ch & 3) + 4 * hf, acc);
+  const float sc = pass == 0 ? p.scale : 1.f;
+  const bool real = j0 + (lane & 31) < sp.elen;
+#pragma unroll
+  for (int q = 0; q < NQ; ++q) store4<T>(&s_row[lane & 31][8 * (wave * NQ + q) + 4 * hf], real ? acc[q] * sc : f32x4{});
+  __syncthreads();
+  constexpr int CPR = D * (int)sizeof(T) / 16, V = 16 / (int)sizeof(T);
+  T* dst = (pass == 0 ? p.dk : p.dv) + ((int64_t)(sp.e0 + j0) * p.hkv + g) * D;
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  for (int i = threadIdx.x; i < 32 * CPR; i += 256) {
+    const int r = i / CPR, c = (i % CPR) * V;
+    if (j0 + r < sp.ecap)
+      *reinterpret_cast<u32x4*>(dst + (int64_t)r * p.hkv * D + c) = *reinterpret_cast<const u32x4*>(&s_row[r][c]);
+  }
 }
 
 template <typename T>
@@ -1194,7 +1242,7 @@ hipError_t launch_bwd_t(const CrossLaunch& a, hipStream_t s) {
   }
   if (a.n_kv_splits > 0) {
     TimingScope t("pp_cross_attn_kv_sum", s);
-    const dim3 grid((unsigned)((int64_t)a.n_kv_splits * 2 * a.hkv * (D / 8)));
+    const dim3 grid((unsigned)((int64_t)a.n_kv_splits * 2 * a.hkv * 4));
     hipLaunchKernelGGL((cross_kv_sum_kernel<D, T>), grid, dim3(256), 0, s, p, a.kv_splits);
     e = hipGetLastError();
   }

@@ -2200,9 +2200,10 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 struct CrossCost {
   int64_t slots;      // workgroups that run at once
   double full, half;  // us a unit takes with all slots taken, and with half of them
-  double join;        // us that joining split walks takes, and
-  double join_part;   // us more for every part
+  double start;       // us before a workgroup's first unit
+  double join_part;   // us a part's sums take to be written and read
 };
+constexpr double kCrossJoin = 4.0;  // us of the launch that joins split walks
 
 // One packed row's walks: `tiles` workgroups a kv-head, of `units` each.
 struct CrossWalk {
@@ -2210,8 +2211,8 @@ struct CrossWalk {
 };
 
 // The longest walk, in units, that the pass's workgroups are cut to: none when uncut
-// walks keep the card busy, else a length that fills 1/2, 1, 2 or 3 rounds of its slots,
-// whichever is estimated fastest.
+// walks keep the card busy, else a length that fills half a round to six rounds of its
+// slots, whichever is estimated fastest.
 int64_t cross_part(const std::vector<CrossWalk>& walks, int hkv, const CrossCost& c) {
   int64_t longest = 0, tiles = 0, total = 0;
   for (const CrossWalk& w : walks) {
@@ -2221,13 +2222,11 @@ int64_t cross_part(const std::vector<CrossWalk>& walks, int hkv, const CrossCost
     total += w.tiles * w.units * hkv;
   }
   if (tiles >= 4 * c.slots || longest <= 1) return INT32_MAX;
-  // full rounds, and what is left over, by itself or sharing units
+  // one round: its longest walk; more: an even share and half of the longest at the end
   auto time = [&](int64_t n, int64_t most) {
-    const double mean = (double)total / n, worst = (double)std::min(longest, most);
-    const int64_t rest = n % c.slots;
-    const double last = rest == 0 ? 0 : rest <= c.slots / 2 ? c.half : c.full;
-    const double one = n <= c.slots / 2 ? c.half : c.full;
-    return std::max((n / c.slots) * mean * c.full + mean * last, worst * one);
+    const double worst = (double)std::min(longest, most);
+    if (n <= c.slots) return c.start + worst * (n <= c.slots / 2 ? c.half : c.full);
+    return ceil_div(n, c.slots) * c.start + std::max(worst, (double)total / c.slots + 0.5 * worst) * c.full;
   };
   auto groups = [&](int64_t most) {
     int64_t n = 0;
@@ -2236,7 +2235,7 @@ int64_t cross_part(const std::vector<CrossWalk>& walks, int hkv, const CrossCost
   };
   int64_t best = INT32_MAX;
   double best_t = time(tiles, longest);
-  for (int half_rounds : {1, 2, 4, 6}) {
+  for (int half_rounds : {1, 2, 4, 6, 8, 12}) {
     const int64_t want = half_rounds * c.slots / 2;
     if (want <= tiles) continue;
     int64_t lo = 1, hi = longest;  // the shortest part that stays within `want` workgroups
@@ -2247,7 +2246,7 @@ int64_t cross_part(const std::vector<CrossWalk>& walks, int hkv, const CrossCost
     }
     if (lo >= longest) continue;
     const int64_t n = groups(lo);
-    const double t = time(n, lo) + c.join + c.join_part * n;
+    const double t = time(n, lo) + kCrossJoin + c.join_part * n;
     if (t < best_t) {
       best_t = t;
       best = lo;
@@ -2336,13 +2335,23 @@ void build_cross_kv(const Batch& bt, const std::vector<EncRow>& enc, int G, int 
   });
 }
 
-// Rates measured on the passes (pp_cross.hip) at full and half load; fp32 products take
-// eight times as long and their kernels run one workgroup a compute unit.
+// Units measured on grids of just that many workgroups (pp_cross.hip's passes on 32/8
+// heads, 2048 keys; us): 128 rows x 64 keys of the forward and of dQ, a step of dK/dV
+// against 128 keys.
 constexpr int64_t kUnits = kComputeUnits;
-CrossCost fwd_cost(pp_dtype dtype, int d, int hkv) {
-  const double part = 2e-5 * kCrossRows * d / 128;  // us: a part is written and read once
-  if (dtype == PP_FP32) return CrossCost{kUnits, d == 128 ? 10.0 : 5.0, d == 128 ? 10.0 : 5.0, 4.0, part};
-  return d == 128 ? CrossCost{2 * kUnits, 2.2, 1.4, 4.0, part} : CrossCost{2 * kUnits, 1.5, 1.0, 4.0, part};
+inline double join_us(double floats) { return floats * 8 / 5e6; }  // written and read at 5 TB/s
+struct CrossCosts {
+  CrossCost fwd, dq, dkdv;
+};
+CrossCosts cross_costs(pp_dtype dtype, int d) {
+  const double rows = join_us((double)kCrossRows * d), keys = join_us((double)kCrossKeys * d);  // two gradients, half of it under the walks
+  if (dtype == PP_FP32) {
+    const double h = d / 128.0;
+    return {{kUnits, 9.7 * h, 9.3 * h, 3.0, rows}, {kUnits, 14.1 * h, 13.5 * h, 3.0, rows}, {kUnits, 9.0 * h, 9.0 * h, 3.0, keys}};
+  }
+  if (d == 128)
+    return {{2 * kUnits, 2.3, 1.35, 3.0, rows}, {2 * kUnits, 3.1, 1.75, 3.0, rows}, {kUnits, 1.9, 1.65, 3.0, keys}};
+  return {{4 * kUnits, 2.6, 1.45, 3.0, rows}, {2 * kUnits, 1.75, 1.05, 3.0, rows}, {2 * kUnits, 1.5, 1.0, 3.0, keys}};
 }
 
 void plan_cross_fwd(const Batch& bt, const std::vector<EncRow>& enc, pp_dtype dtype, int hq, int hkv, int d, CrossPlan* p) {
@@ -2351,11 +2360,13 @@ void plan_cross_fwd(const Batch& bt, const std::vector<EncRow>& enc, pp_dtype dt
   for (const Row& r : bt.rows) most = std::max(most, (int64_t)r.valid * G);
   if (most <= kCrossFewRows) {
     p->tile_rows = kCrossFewRows;
-    // a unit's keys and values come at 6 TB/s over all compute units, at 60 GB/s to one
-    const double bytes = (double)kCrossKeyUnit * d * (dtype == PP_FP32 ? 8 : 4);
-    build_cross_items(bt, enc, G, hkv, CrossCost{kUnits, bytes / 23e3, bytes / 46e3, 4.0, 2e-5 * 32 * d / 128}, p);
+    // a unit's 32 KB (bf16, head size 128) come in 1.42 us with all compute units reading
+    // (5.9 TB/s) and in about 1 with half of them
+    const double size = (dtype == PP_FP32 ? 2.0 : 1.0) * d / 128;
+    build_cross_items(bt, enc, G, hkv,
+                      CrossCost{kUnits, 1.42 * size, std::max(0.5, 1.0 * size), 2.0, join_us((double)kCrossFewRows * d)}, p);
   } else {
-    build_cross_items(bt, enc, G, hkv, fwd_cost(dtype, d, hkv), p);
+    build_cross_items(bt, enc, G, hkv, cross_costs(dtype, d).fwd, p);
   }
   p->inline_items = p->items.size() <= (size_t)kCrossInline;  // and at most half as many splits
   if (!p->inline_items) {
@@ -2369,12 +2380,9 @@ void plan_cross_fwd(const Batch& bt, const std::vector<EncRow>& enc, pp_dtype dt
 
 void plan_cross_bwd(const Batch& bt, const std::vector<EncRow>& enc, pp_dtype dtype, int hq, int hkv, int d, CrossPlan* p) {
   const int G = hq / hkv;
-  CrossCost dq = fwd_cost(dtype, d, hkv);
-  dq.full *= 1.3;
-  dq.half *= 1.3;
-  build_cross_items(bt, enc, G, hkv, dq, p);
-  const double step = dtype == PP_FP32 ? (d == 128 ? 10.0 : 5.0) : d == 128 ? 2.1 : 1.4;
-  build_cross_kv(bt, enc, G, hkv, dtype == PP_FP32 ? 32 : 64, CrossCost{kUnits, step, step, 4.0, 4e-5 * kCrossKeys * d / 128}, p);
+  const CrossCosts c = cross_costs(dtype, d);
+  build_cross_items(bt, enc, G, hkv, c.dq, p);
+  build_cross_kv(bt, enc, G, hkv, kCrossStep(d, dtype == PP_FP32), c.dkdv, p);
   p->r_items = p->lay.add(p->items.size() * sizeof(CrossItem));
   p->r_splits = p->lay.add(p->splits.size() * sizeof(CrossSplit));
   p->r_kv_items = p->lay.add(p->kv_items.size() * sizeof(CrossKvItem));

@@ -178,6 +178,8 @@ struct RespItem {
 constexpr int kCrossRows = 128;    // rows per forward and dQ workgroup
 constexpr int kCrossFewRows = 32;  // rows per workgroup of the forward for few rows
 constexpr int kCrossKeys = 128;    // keys per dK/dV workgroup
+// rows a dK/dV step
+constexpr int kCrossStep(int head_dim, bool fp32) { return head_dim == 128 && !fp32 ? 64 : 32; }
 constexpr int kCrossKeyUnit = 64;  // parts of a row's keys are multiples of this
 constexpr int kCrossInline = 64;   // forward items that fit into the launch's arguments
 
