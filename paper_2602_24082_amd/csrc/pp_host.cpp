@@ -2434,17 +2434,19 @@ pp_status check_ranges(const int32_t* key_begin, const int32_t* key_end) {
   return PP_OK;
 }
 
+bool capturing(hipStream_t s) {
+  hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &st) == hipSuccess) return st != hipStreamCaptureStatusNone;
+  (void)hipGetLastError();
+  return false;
+}
+
 // Copies a call's records to the workspace.  A few ride in launch arguments, and so do
 // all of a call that is being captured: a graph's replays cannot read a staging buffer,
 // which later calls refill.
 pp_status stage_records(void* ws, const MetaImage& img, hipStream_t s, const StageLaunch& zeros = StageLaunch()) {
   const size_t n = img.buf.size();
-  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-  if (n > kInlineBytes && hipStreamIsCapturing(s, &cap) != hipSuccess) {
-    (void)hipGetLastError();
-    cap = hipStreamCaptureStatusNone;
-  }
-  if (n > kInlineBytes && cap == hipStreamCaptureStatusNone)
+  if (n > kInlineBytes && !capturing(s))
     return stage_with(ws, img.buf.data(), n, s, [&](const void* dev_src) -> pp_status {
       StageLaunch a = zeros;
       a.src = dev_src;
@@ -2757,27 +2759,30 @@ namespace pp {
 namespace {
 
 struct PolicyPlan {
-  std::vector<PolicySlot> slots;  // responses with tokens, in token order
-  int64_t tokens = 0;
-  bool inline_slots = false;
+  int64_t n_slots = 0, tokens = 0;  // responses with tokens, and those
   Layout lay;
-  size_t r_slots = 0, r_counts = 0, r_part = 0;
+  size_t r_slots = 0, r_counts = 0, r_first = 0, r_part = 0;
 };
 
 void plan_policy(const Batch& bt, PolicyPlan* p) {
-  for (int b = 0; b < bt.B; ++b) {
-    const Row& r = bt.rows[b];
+  for (const Row& r : bt.rows)
     for (int k = 0; k < r.K; ++k) {
-      if (r.len[k] == 0) continue;
-      p->slots.push_back(PolicySlot{r.tok0 + r.off[k], r.len[k], b * bt.Kmax + k});
+      p->n_slots += r.len[k] > 0;
       p->tokens += r.len[k];
     }
-  }
-  p->inline_slots = p->slots.size() <= (size_t)kPolicyInline;
-  if (!p->inline_slots) p->r_slots = p->lay.add(p->slots.size() * sizeof(PolicySlot));
-  p->lay.meta_bytes = p->lay.total;
-  p->r_counts = p->lay.add(p->slots.size() * 4);
+  if (policy_small(bt.sumT, p->n_slots)) return;
+  p->r_slots = p->lay.add(p->n_slots * sizeof(PolicySlot));
+  p->r_counts = p->lay.add(p->n_slots * 4);
+  p->r_first = p->lay.add((size_t)policy_blocks(bt.sumT) * 4);
   p->r_part = p->lay.add((size_t)policy_blocks(bt.sumT) * sizeof(PolicyPartial));
+}
+
+void fill_policy_slots(const Batch& bt, PolicySlot* out) {
+  for (int b = 0; b < bt.B; ++b) {
+    const Row& r = bt.rows[b];
+    for (int k = 0; k < r.K; ++k)
+      if (r.len[k] > 0) *out++ = PolicySlot{r.tok0 + r.off[k], r.len[k], b * bt.Kmax + k};
+  }
 }
 
 }  // namespace
@@ -2857,18 +2862,25 @@ pp_status pp_policy_loss(const pp_pack_desc* desc, const pp_policy_config* cfg, 
     a.reduction = cfg->reduction;
     a.sumT = bt.sumT;
     a.tokens = p.tokens;
-    a.n_slots = (int)p.slots.size();
-    a.host_slots = p.slots.data();
-    a.slot_counts = (int32_t*)at(ws, p.lay, p.r_counts);
-    a.part = (PolicyPartial*)at(ws, p.lay, p.r_part);
-    if (!p.inline_slots) {
-      MetaImage img;
-      img.put(p.lay.regions[p.r_slots], p.slots.data(), p.slots.size() * sizeof(PolicySlot));
-      if ((st = stage_records(ws, img, s)) != PP_OK) return st;
-      a.slots = (const PolicySlot*)at(ws, p.lay, p.r_slots);
+    a.n_slots = (int)p.n_slots;
+    std::vector<PolicySlot> slots(p.n_slots);
+    fill_policy_slots(bt, slots.data());
+    a.host_slots = slots.data();
+    if (p.lay.total) {
+      a.slots = (PolicySlot*)at(ws, p.lay, p.r_slots);
+      a.slot_counts = (int32_t*)at(ws, p.lay, p.r_counts);
+      a.first = (int32_t*)at(ws, p.lay, p.r_first);
+      a.part = (PolicyPartial*)at(ws, p.lay, p.r_part);
     }
-    const hipError_t e = launch_policy(a, s);
-    return e == hipSuccess ? PP_OK : hip_fail(e, "policy loss launch");
+    auto launch = [&](const void* dev_src) -> pp_status {
+      a.from = (const PolicySlot*)dev_src;
+      const hipError_t e = launch_policy(a, s);
+      return e == hipSuccess ? PP_OK : hip_fail(e, "policy loss launch");
+    };
+    if (policy_inline(p.n_slots)) return launch(nullptr);
+    if (!capturing(s)) return stage_with(a.slots, slots.data(), slots.size() * sizeof(PolicySlot), s, launch);
+    const hipError_t e = launch_inline_copy(a.slots, slots.data(), slots.size() * sizeof(PolicySlot), s);
+    return e == hipSuccess ? launch(nullptr) : hip_fail(e, "record copy launch");
   });
 }
 

@@ -294,7 +294,10 @@ hipError_t launch_loss(const LossLaunch& a, hipStream_t s);
 
 // Clipped policy loss (pp_policy.hip).
 constexpr int kPolicyThreads = 256;
-constexpr int kPolicyInline = 256;  // responses that ride in the launches' arguments
+constexpr int kPolicyInline = 256;     // responses that ride in a launch's arguments
+constexpr int64_t kPolicySmall = 4096;   // tokens that one workgroup takes
+inline bool policy_inline(int64_t n_slots) { return n_slots <= kPolicyInline; }
+inline bool policy_small(int64_t sumT, int64_t n_slots) { return sumT <= kPolicySmall && policy_inline(n_slots); }
 struct PolicySlot {
   int32_t begin;  // flat position of the response's first token
   int32_t len;    // >= 1
@@ -318,17 +321,20 @@ struct PolicyParams {
   int32_t* counts;        // [2] or null
   float* dlogp;           // [sumT] or null
   float* dentropy;        // [sumT] or null
-  const PolicySlot* slots;  // in token order; null: in the launch's arguments
-  int32_t* slot_counts;   // scratch
-  PolicyPartial* part;    // scratch
+  PolicySlot* slots;      // workspace: the responses with tokens, in token order
+  int32_t* slot_counts;   // workspace: their counted tokens
+  int32_t* first;         // workspace: the first response that each of policy_tokens' workgroups meets
+  PolicyPartial* part;    // workspace: sums of policy_tokens' workgroups
   double clip_low, clip_high, dual_clip, kl_coef, ent_coef, norm;
   int64_t sumT, tokens;
   int n_slots;
   int kl, reduction;
   bool adv_per_token;
+  bool in_place;          // `slots` holds the records already
 };
 struct PolicyLaunch : PolicyParams {
-  const PolicySlot* host_slots;
+  const PolicySlot* host_slots;       // host records
+  const PolicySlot* from = nullptr;   // their copy in mapped host memory; null: in launch arguments or in `slots`
 };
 hipError_t launch_policy(const PolicyLaunch& a, hipStream_t s);
 

@@ -10,15 +10,17 @@
 //   gradient   w_t (-A r, 0 where the clip holds, + kl_coef dKL/dlogp), -ent_coef w_t
 //
 // with w_t = 1 / (counted tokens), 1 / (responses x the response's counted tokens), or
-// 1 / norm.  Kernels:
+// 1 / norm.  Bytes are few (33 per token at most), so launches and latency set the time:
 //
-//   policy_count    counted tokens of every response, where a mask decides
+//   policy_small    one workgroup does it all: up to kPolicySmall tokens
+//   policy_records  the responses' records to the workspace, and their counted tokens
 //   policy_tokens   the terms, token by token, and a workgroup's sums
-//   policy_reduce   the sums in workgroup order (no atomics)
+//   policy_reduce   the sums in workgroup order (no atomics on results)
 //
-// Bytes are few (33 per token at most), so launches and latency set the time.  A token's terms are formed
-// in 64 bits: whether a clip holds is then decided by the ratio and not by its rounding to
-// fp32, and e^x - 1 - x keeps its digits for small x; sums too.
+// A token's terms are fp32, to a few roundings: differences of log-probs are exact to one,
+// e^x - 1 - x of a small x comes from its series, and a ratio that fp32 cannot tell from a
+// clip's end is formed in 64 bits, so that what counts as clipped is what the exact ratio
+// says.  Sums are 64 bits.  (All in 64 bits took 14.5 us for 1.3M tokens instead of 9.)
 
 #include <hip/hip_runtime.h>
 #include <math.h>
@@ -36,9 +38,7 @@ struct InlineSlots {
   PolicySlot slot[kPolicyInline];
 };
 
-__device__ __forceinline__ PolicySlot slot_of(const PolicyParams& p, const InlineSlots& inl, int i) {
-  return p.slots ? p.slots[i] : inl.slot[i];
-}
+struct NoSlots {};
 
 __device__ __forceinline__ double wave_sum_d(double x) {
   for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
@@ -49,15 +49,42 @@ __device__ __forceinline__ int wave_sum_i(int x) {
   return x;
 }
 
-// A wave a response.
-__global__ __launch_bounds__(kThreads) void policy_count_kernel(PolicyParams p, InlineSlots inl) {
+// Counted tokens of a response, by a wave.
+__device__ __forceinline__ int count_tokens(const PolicyParams& p, const PolicySlot& sl) {
+  if (!p.mask) return sl.len;
+  const uint8_t* m = p.mask + sl.begin;
+  constexpr int U = 16;  // bytes in flight a lane: most responses in one go
+  int n = 0;
+  for (int j = threadIdx.x & 63; j < sl.len; j += 64 * U) {
+    uint8_t v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = j + 64 * u < sl.len ? m[j + 64 * u] : (uint8_t)0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) n += v[u] != 0;
+  }
+  return wave_sum_i(n);
+}
+
+// A wave a response; `from`: records in mapped host memory, or null (inl, or in place).
+// It also notes, for the workgroups of policy_tokens (chunk tokens each) that start
+// between the end of the response ahead and its own, that it is the first they meet.
+__global__ __launch_bounds__(kThreads) void policy_records_kernel(PolicyParams p, const PolicySlot* from, int in_args, int chunk,
+                                                                  InlineSlots inl) {
   const int i = (int)((blockIdx.x * kThreads + threadIdx.x) >> 6), lane = threadIdx.x & 63;
   if (i >= p.n_slots) return;
-  const PolicySlot sl = slot_of(p, inl, i);
-  int n = 0;
-  for (int j = lane; j < sl.len; j += 64) n += p.mask[(int64_t)sl.begin + j] != 0;
-  n = wave_sum_i(n);
-  if (lane == 0) p.slot_counts[i] = n;
+  auto at = [&](int k) { return from ? from[k] : in_args ? inl.slot[k] : p.slots[k]; };
+  const PolicySlot sl = at(i);
+  const int64_t from_t = i > 0 ? (int64_t)at(i - 1).begin + at(i - 1).len : 0, to_t = (int64_t)sl.begin + sl.len;
+  const int chunks = (int)((p.sumT + chunk - 1) / chunk);
+  const int c_first = (int)((from_t + chunk - 1) / chunk), c_end = min(chunks, (int)((to_t + chunk - 1) / chunk));
+  for (int c = c_first + lane; c < c_end; c += 64) p.first[c] = i;
+  if (i == p.n_slots - 1)
+    for (int c = c_end + lane; c < chunks; c += 64) p.first[c] = p.n_slots;
+  const int n = count_tokens(p, sl);
+  if (lane == 0) {
+    if (!p.in_place) p.slots[i] = sl;
+    p.slot_counts[i] = n;
+  }
 }
 
 __device__ __forceinline__ void write_results(const PolicyParams& p, const PolicyPartial& t) {
@@ -74,8 +101,9 @@ __device__ __forceinline__ void write_results(const PolicyParams& p, const Polic
 }
 
 // The workgroup's sums in a fixed order, valid in thread 0.
+template <int THREADS>
 __device__ __forceinline__ PolicyPartial block_sum(PolicyPartial t) {
-  __shared__ PolicyPartial part[kThreads / 64];
+  __shared__ PolicyPartial part[THREADS / 64];
 #pragma unroll
   for (int i = 0; i < 4; ++i) t.sum[i] = wave_sum_d(t.sum[i]);
   t.counted = wave_sum_i(t.counted);
@@ -83,7 +111,7 @@ __device__ __forceinline__ PolicyPartial block_sum(PolicyPartial t) {
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = t;
   __syncthreads();
   if (threadIdx.x == 0) {
-    for (int w = 1; w < kThreads / 64; ++w) {
+    for (int w = 1; w < THREADS / 64; ++w) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) t.sum[i] += part[w].sum[i];
       t.counted += part[w].counted;
@@ -93,15 +121,104 @@ __device__ __forceinline__ PolicyPartial block_sum(PolicyPartial t) {
   return t;
 }
 
+// What a counted token adds, before its weight.
+struct PolicyTerms {
+  float grad;        // of the unweighted loss, but for the entropy
+  float surr, kl, ratio;
+  bool clipped;
+};
+
+__device__ __forceinline__ PolicyTerms policy_terms(const PolicyParams& p, float lp, float old, float ref, float A) {
+  PolicyTerms t;
+  t.ratio = p.old ? expf(lp - old) : 1.f;
+  float used = t.ratio;
+  t.clipped = false;
+  // fp32's ratio is off by (2 + |ln ratio|) 2^-24 of it, less than 2^-17; next to an end
+  // 64 bits decide
+  auto above = [&](double end) {
+    const float e = (float)end;
+    if (fabsf(t.ratio - e) > e * 0x1p-16f) return t.ratio > e;
+    return exp((double)lp - (double)old) > end;
+  };
+  if (A > 0.f && p.old && above(1.0 + p.clip_high)) {
+    t.clipped = true;
+    used = (float)(1.0 + p.clip_high);
+  } else if (A < 0.f && p.old) {
+    // below the low end: not above it and not on it
+    const double low = 1.0 - p.clip_low;
+    const float e = (float)low;
+    const bool below = fabsf(t.ratio - e) > e * 0x1p-16f ? t.ratio < e : exp((double)lp - (double)old) < low;
+    if (below) {
+      t.clipped = true;
+      used = e;
+    } else if (p.dual_clip > 0 && above(p.dual_clip)) {
+      t.clipped = true;
+      used = (float)p.dual_clip;
+    }
+  }
+  t.surr = used * A;
+  t.grad = t.clipped ? 0.f : -A * t.ratio;
+  t.kl = 0.f;
+  if (p.ref) {
+    const float x = ref - lp;
+    float d;
+    if (p.kl == PP_KL_K1) {
+      t.kl = -x;
+      d = 1.f;
+    } else if (p.kl == PP_KL_K2) {
+      t.kl = 0.5f * x * x;
+      d = -x;
+    } else if (fabsf(x) <= 0.5f) {
+      // the series from x^2 / 2 on: its x^11 / 11! is 2^-33 of it at most
+      float s = 1.f / 3628800;
+      s = fmaf(s, x, 1.f / 362880);
+      s = fmaf(s, x, 1.f / 40320);
+      s = fmaf(s, x, 1.f / 5040);
+      s = fmaf(s, x, 1.f / 720);
+      s = fmaf(s, x, 1.f / 120);
+      s = fmaf(s, x, 1.f / 24);
+      s = fmaf(s, x, 1.f / 6);
+      s = fmaf(s, x, 0.5f);
+      t.kl = s * x * x;
+      d = -fmaf(s * x, x, x);
+    } else {
+      const float em = expm1f(x);
+      t.kl = em - x;
+      d = -em;
+    }
+    if (p.kl_coef != 0) t.grad = fmaf((float)p.kl_coef, d, t.grad);
+  }
+  return t;
+}
+
+// A token's share of the sums.
+__device__ __forceinline__ void add_token(PolicyPartial& sum, const PolicyTerms& t, double w, float ent, bool with_ent) {
+  sum.sum[0] -= w * t.surr;
+  sum.sum[1] += w * t.kl;
+  if (with_ent) sum.sum[2] += w * ent;
+  sum.sum[3] += w * t.ratio;
+  sum.counted += 1;
+  sum.clipped += t.clipped;
+}
+
+// The weight of a response's tokens: `some` responses have a counted one, `total` tokens
+// are counted, n of this response.
+__device__ __forceinline__ double slot_weight(const PolicyParams& p, int64_t total, int some, int n) {
+  if (p.reduction == PP_REDUCE_SUM) return 1.0 / p.norm;
+  if (p.reduction == PP_REDUCE_TOKEN) return 1.0 / (double)(total > 0 ? total : 1);
+  return n > 0 ? 1.0 / ((double)some * n) : 0.0;
+}
+
 // The first response that ends behind position c: 64 probes a round.
-__device__ __forceinline__ int first_slot(const PolicyParams& p, const InlineSlots& inl, int64_t c) {
+template <typename At>
+__device__ __forceinline__ int first_slot(int n_slots, int64_t c, At&& at) {
   const int lane = threadIdx.x & 63;
-  int lo = 0, hi = p.n_slots;
+  int lo = 0, hi = n_slots;
   while (lo < hi) {
     const int step = (hi - lo + 63) / 64, i = lo + lane * step;
     bool before = false;
     if (i < hi) {
-      const PolicySlot s = slot_of(p, inl, i);
+      const PolicySlot s = at(i);
       before = (int64_t)s.begin + s.len <= c;
     }
     const int n = __popcll(__ballot(before));
@@ -112,30 +229,85 @@ __device__ __forceinline__ int first_slot(const PolicyParams& p, const InlineSlo
   return lo;
 }
 
-// TPT consecutive tokens a thread.
-template <int TPT>
-__global__ __launch_bounds__(kThreads) void policy_tokens_kernel(PolicyParams p, InlineSlots inl) {
+// TPT consecutive tokens a thread; their values are on the way while the responses that
+// they belong to are found.  IN_ARGS: the records come with the launch and nothing is
+// masked, so there are no counts to read.
+template <int TPT, bool IN_ARGS, typename Inline>
+__global__ __launch_bounds__(kThreads) void policy_tokens_kernel(PolicyParams p, Inline inl) {
   constexpr int CH = kThreads * TPT;
-  __shared__ int s_begin[CH + 1], s_end[CH + 1], s_out[CH + 1];
-  __shared__ double s_w[CH + 1];
+  __shared__ int s_begin[CH], s_end[CH], s_out[CH], s_count[CH];
+  __shared__ double s_w[CH];
   __shared__ int s_first, s_n, s_total, s_some;
   const int tid = threadIdx.x;
+  const bool masked = !IN_ARGS && p.mask != nullptr;
   const int64_t c0 = (int64_t)blockIdx.x * CH, c1 = c0 + CH < p.sumT ? c0 + CH : p.sumT;
-  if (tid == 0) s_n = s_total = s_some = 0;
-  if (tid < 64) {
-    const int f = first_slot(p, inl, c0);
-    if (tid == 0) s_first = f;
-  }
-  __syncthreads();
-  const int first = s_first;
-  const bool masked = p.mask != nullptr;
-  if (masked && p.reduction != PP_REDUCE_SUM) {  // what the mask counts of all the batch
-    int total = 0, some = 0;
-    for (int i = tid; i < p.n_slots; i += kThreads) {
-      const int n = p.slot_counts[i];
-      total += n;
-      some += n > 0;
+  auto slot_at = [&](int i) {
+    if constexpr (IN_ARGS) return inl.slot[i];
+    else return p.slots[i];
+  };
+  const int64_t t0 = c0 + (int64_t)tid * TPT;
+  typedef float fvec __attribute__((ext_vector_type(TPT)));
+  const bool whole = t0 + TPT <= p.sumT;
+  float lp[TPT], old[TPT], ref[TPT], ent[TPT], adv[TPT];
+  uint8_t keep[TPT];
+  auto load = [&](const float* src, float* dst) {
+#pragma unroll
+    for (int e = 0; e < TPT; ++e) dst[e] = 0.f;
+    if (!src) return;
+    if (TPT > 1 && whole) {
+      const fvec v = *reinterpret_cast<const fvec*>(src + t0);
+#pragma unroll
+      for (int e = 0; e < TPT; ++e) dst[e] = v[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < TPT; ++e)
+        if (t0 + e < p.sumT) dst[e] = src[t0 + e];
     }
+  };
+  load(p.logp, lp);
+  load(p.old, old);
+  load(p.ref, ref);
+  load(p.entropy, ent);
+  load(p.adv_per_token ? p.adv : nullptr, adv);
+  if (masked) {
+    if (TPT == 4 && whole) {  // 4-byte aligned here
+      const uint32_t v = *reinterpret_cast<const uint32_t*>(p.mask + t0);
+#pragma unroll
+      for (int e = 0; e < TPT; ++e) keep[e] = (uint8_t)(v >> (8 * e));
+    } else {
+#pragma unroll
+      for (int e = 0; e < TPT; ++e) keep[e] = t0 + e < p.sumT ? p.mask[t0 + e] : (uint8_t)0;
+    }
+  }
+  if (tid == 0) s_n = s_total = s_some = 0;
+  // what the mask counts of all the batch, eight responses in flight a thread
+  int total = 0, some = 0;
+  if (masked && p.reduction != PP_REDUCE_SUM) {
+    constexpr int U = 8;
+    for (int i = tid; i < p.n_slots; i += kThreads * U) {
+      int v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = i + kThreads * u < p.n_slots ? p.slot_counts[i + kThreads * u] : 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        total += v[u];
+        some += v[u] > 0;
+      }
+    }
+  }
+  int first;
+  if constexpr (IN_ARGS) {
+    if (tid < 64) {
+      const int f = first_slot(p.n_slots, c0, slot_at);
+      if (tid == 0) s_first = f;
+    }
+    __syncthreads();
+    first = s_first;
+  } else {
+    first = p.n_slots > 0 ? p.first[blockIdx.x] : 0;
+    __syncthreads();
+  }
+  if (masked && p.reduction != PP_REDUCE_SUM) {
     total = wave_sum_i(total);
     some = wave_sum_i(some);
     if ((tid & 63) == 0) {
@@ -145,56 +317,23 @@ __global__ __launch_bounds__(kThreads) void policy_tokens_kernel(PolicyParams p,
   }
   // the responses that reach into [c0, c1): CH at most, none being empty
   for (int i = tid; i < CH && first + i < p.n_slots; i += kThreads) {
-    const PolicySlot sl = slot_of(p, inl, first + i);
+    const PolicySlot sl = slot_at(first + i);
     if (sl.begin >= c1) break;
     s_begin[i] = sl.begin;
     s_end[i] = sl.begin + sl.len;
     s_out[i] = sl.out;
+    s_count[i] = masked ? p.slot_counts[first + i] : sl.len;
     atomicMax(&s_n, i + 1);
   }
   __syncthreads();
   const int n = s_n;
-  {
-    const double total = masked ? (double)s_total : (double)p.tokens;
-    const double some = masked ? (double)s_some : (double)p.n_slots;
-    for (int i = tid; i < n; i += kThreads) {
-      double w = 1.0 / p.norm;
-      if (p.reduction == PP_REDUCE_TOKEN) w = 1.0 / fmax(total, 1.0);
-      else if (p.reduction == PP_REDUCE_SEQ)
-        w = 1.0 / (some * (double)max(1, masked ? p.slot_counts[first + i] : s_end[i] - s_begin[i]));
-      s_w[i] = w;
-    }
-  }
+  for (int i = tid; i < n; i += kThreads)
+    s_w[i] = slot_weight(p, masked ? (int64_t)s_total : p.tokens, masked ? s_some : p.n_slots, s_count[i]);
   __syncthreads();
 
-  const int64_t t0 = c0 + (int64_t)tid * TPT;
   PolicyPartial sum{};
   if (t0 < c1) {
-    typedef float fvec __attribute__((ext_vector_type(TPT)));
     float out_lp[TPT], out_ent[TPT];
-    float lp[TPT], old[TPT], ref[TPT], ent[TPT], adv[TPT];
-    uint8_t keep[TPT];
-    const bool whole = t0 + TPT <= p.sumT;
-    auto load = [&](const float* src, float* dst) {
-      if (!src) return;
-      if (TPT > 1 && whole) {
-        const fvec v = *reinterpret_cast<const fvec*>(src + t0);
-#pragma unroll
-        for (int e = 0; e < TPT; ++e) dst[e] = v[e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < TPT; ++e) dst[e] = t0 + e < p.sumT ? src[t0 + e] : 0.f;
-      }
-    };
-    load(p.logp, lp);
-    load(p.old, old);
-    load(p.ref, ref);
-    load(p.entropy, ent);
-    if (p.adv_per_token) load(p.adv, adv);
-    if (masked) {
-#pragma unroll
-      for (int e = 0; e < TPT; ++e) keep[e] = t0 + e < p.sumT ? p.mask[t0 + e] : (uint8_t)0;
-    }
     // the last response that begins at or ahead of t0
     int lo = 0, hi = n;
     while (lo < hi) {
@@ -210,46 +349,10 @@ __global__ __launch_bounds__(kThreads) void policy_tokens_kernel(PolicyParams p,
       out_lp[e] = out_ent[e] = 0.f;
       if (i < 0 || t >= s_end[i] || t >= c1 || (masked && !keep[e])) continue;
       const double w = s_w[i];
-      const double A = p.adv_per_token ? adv[e] : p.adv[s_out[i]];
-      const double ratio = p.old ? exp((double)lp[e] - (double)old[e]) : 1.0;
-      double used = ratio;
-      bool off = false;
-      if (A > 0 && ratio > 1.0 + p.clip_high) {
-        off = true;
-        used = 1.0 + p.clip_high;
-      } else if (A < 0 && ratio < 1.0 - p.clip_low) {
-        off = true;
-        used = 1.0 - p.clip_low;
-      } else if (A < 0 && p.dual_clip > 0 && ratio > p.dual_clip) {
-        off = true;
-        used = p.dual_clip;
-      }
-      double g = off ? 0.0 : -A * ratio;
-      double kl = 0.0;
-      if (p.ref) {
-        const double x = (double)ref[e] - (double)lp[e];
-        double dkl;
-        if (p.kl == PP_KL_K1) {
-          kl = -x;
-          dkl = 1.0;
-        } else if (p.kl == PP_KL_K2) {
-          kl = 0.5 * x * x;
-          dkl = -x;
-        } else {
-          const double em = expm1(x);
-          kl = em - x;
-          dkl = -em;
-        }
-        if (p.kl_coef != 0) g += p.kl_coef * dkl;
-      }
-      out_lp[e] = (float)(w * g);
+      const PolicyTerms x = policy_terms(p, lp[e], old[e], ref[e], p.adv_per_token ? adv[e] : p.adv[s_out[i]]);
+      out_lp[e] = (float)w * x.grad;
       out_ent[e] = (float)(-p.ent_coef * w);
-      sum.sum[0] -= w * (used * A);
-      sum.sum[1] += w * kl;
-      if (p.entropy) sum.sum[2] += w * (double)ent[e];
-      sum.sum[3] += w * ratio;
-      sum.counted += 1;
-      sum.clipped += off;
+      add_token(sum, x, w, ent[e], p.entropy != nullptr);
     }
     auto store = [&](float* dst, const float* src) {
       if (!dst) return;
@@ -267,11 +370,77 @@ __global__ __launch_bounds__(kThreads) void policy_tokens_kernel(PolicyParams p,
     store(p.dlogp, out_lp);
     store(p.dentropy, out_ent);
   }
-  sum = block_sum(sum);
-  if (tid == 0) {
-    if (gridDim.x == 1) write_results(p, sum);
-    else p.part[blockIdx.x] = sum;
+  sum = block_sum<kThreads>(sum);
+  if (tid == 0) p.part[blockIdx.x] = sum;
+}
+
+// Few tokens of few responses: a call of one launch.  16 waves count the responses'
+// tokens, then every thread takes each 1024th token, its response found by stepping on.
+constexpr int kSmallThreads = 1024;
+__global__ __launch_bounds__(kSmallThreads) void policy_small_kernel(PolicyParams p, InlineSlots inl) {
+  __shared__ int s_begin[kPolicyInline], s_end[kPolicyInline], s_out[kPolicyInline], s_n[kPolicyInline];
+  __shared__ double s_w[kPolicyInline];
+  __shared__ int s_total, s_some;
+  const int tid = threadIdx.x, wave = tid >> 6;
+  if (tid == 0) s_total = s_some = 0;
+  for (int i = wave; i < p.n_slots; i += kSmallThreads / 64) {
+    const PolicySlot sl = inl.slot[i];
+    const int n = count_tokens(p, sl);
+    if ((tid & 63) == 0) {
+      s_begin[i] = sl.begin;
+      s_end[i] = sl.begin + sl.len;
+      s_out[i] = sl.out;
+      s_n[i] = n;
+    }
   }
+  __syncthreads();
+  if (tid < p.n_slots && s_n[tid] > 0) {
+    atomicAdd(&s_total, s_n[tid]);
+    atomicAdd(&s_some, 1);
+  }
+  __syncthreads();
+  if (tid < p.n_slots) s_w[tid] = slot_weight(p, s_total, s_some, s_n[tid]);
+  __syncthreads();
+  PolicyPartial sum{};
+  constexpr int U = 4;  // tokens in flight a thread
+  int i = 0;
+  for (int t0 = tid; t0 < (int)p.sumT; t0 += kSmallThreads * U) {
+    float lp[U], old[U], ref[U], ent[U], adv[U];
+    int slot[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * kSmallThreads;
+      while (i < p.n_slots && s_end[i] <= t) ++i;
+      slot[u] = t < (int)p.sumT && i < p.n_slots && t >= s_begin[i] ? i : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = slot[u] < 0 ? 0 : t0 + u * kSmallThreads;
+      if (p.mask && !p.mask[t]) slot[u] = -1;
+      lp[u] = p.logp[t];
+      old[u] = p.old ? p.old[t] : 0.f;
+      ref[u] = p.ref ? p.ref[t] : 0.f;
+      ent[u] = p.entropy ? p.entropy[t] : 0.f;
+      adv[u] = slot[u] < 0 ? 0.f : p.adv[p.adv_per_token ? t : s_out[slot[u]]];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * kSmallThreads;
+      if (t >= (int)p.sumT) break;
+      float out_lp = 0.f, out_ent = 0.f;
+      if (slot[u] >= 0) {
+        const double w = s_w[slot[u]];
+        const PolicyTerms x = policy_terms(p, lp[u], old[u], ref[u], adv[u]);
+        out_lp = (float)w * x.grad;
+        out_ent = (float)(-p.ent_coef * w);
+        add_token(sum, x, w, ent[u], p.entropy != nullptr);
+      }
+      if (p.dlogp) p.dlogp[t] = out_lp;
+      if (p.dentropy) p.dentropy[t] = out_ent;
+    }
+  }
+  sum = block_sum<kSmallThreads>(sum);
+  if (tid == 0) write_results(p, sum);
 }
 
 __global__ __launch_bounds__(kThreads) void policy_reduce_kernel(PolicyParams p, int n) {
@@ -283,43 +452,55 @@ __global__ __launch_bounds__(kThreads) void policy_reduce_kernel(PolicyParams p,
     t.counted += x.counted;
     t.clipped += x.clipped;
   }
-  t = block_sum(t);
+  t = block_sum<kThreads>(t);
   if (threadIdx.x == 0) write_results(p, t);
 }
 
 }  // namespace
 
 hipError_t launch_policy(const PolicyLaunch& a, hipStream_t s) {
-  const PolicyParams p = a;
-  InlineSlots inl{};
-  if (!a.slots)
-    for (int i = 0; i < a.n_slots; ++i) inl.slot[i] = a.host_slots[i];
+  PolicyParams p = a;
   hipError_t e = hipSuccess;
-  if (a.mask && a.n_slots > 0 && a.reduction != PP_REDUCE_SUM) {
-    TimingScope t("pp_policy_count", s);
-    const int per = kThreads / 64;
-    hipLaunchKernelGGL(policy_count_kernel, dim3((a.n_slots + per - 1) / per), dim3(kThreads), 0, s, p, inl);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+  InlineSlots inl;
+  const bool in_args = policy_inline(a.n_slots);
+  if (in_args)
+    for (int i = 0; i < a.n_slots; ++i) inl.slot[i] = a.host_slots[i];
+  if (policy_small(a.sumT, a.n_slots)) {
+    TimingScope t("pp_policy_tokens", s);
+    hipLaunchKernelGGL(policy_small_kernel, dim3(1), dim3(kSmallThreads), 0, s, p, inl);
+    return hipGetLastError();
   }
   uintptr_t any = 0;
   for (const void* x : {(const void*)a.logp, (const void*)a.old, (const void*)a.ref, (const void*)a.entropy,
                         a.adv_per_token ? (const void*)a.adv : nullptr, (const void*)a.dlogp, (const void*)a.dentropy})
     any |= reinterpret_cast<uintptr_t>(x);
-  const bool vec = (any & 15) == 0 && a.sumT >= 1 << 18;
+  const bool vec = (any & 15) == 0 && (reinterpret_cast<uintptr_t>(a.mask) & 3) == 0 && a.sumT >= 1 << 18;
   const int64_t ch = kThreads * (vec ? 4 : 1);
-  const int blocks = a.sumT > 0 ? (int)((a.sumT + ch - 1) / ch) : 1;
-  {
-    TimingScope t("pp_policy_tokens", s);
-    if (vec) hipLaunchKernelGGL(policy_tokens_kernel<4>, dim3(blocks), dim3(kThreads), 0, s, p, inl);
-    else hipLaunchKernelGGL(policy_tokens_kernel<1>, dim3(blocks), dim3(kThreads), 0, s, p, inl);
+  const int blocks = (int)((a.sumT + ch - 1) / ch);
+  const bool plain = in_args && !a.mask;  // no records to stage, nothing to count
+  if (a.n_slots > 0 && !plain) {
+    TimingScope t("pp_policy_records", s);
+    p.in_place = !a.from && !in_args;
+    const int per = kThreads / 64;
+    hipLaunchKernelGGL(policy_records_kernel, dim3((a.n_slots + per - 1) / per), dim3(kThreads), 0, s, p, a.from, (int)in_args,
+                       (int)ch, inl);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (blocks > 1) {
-    TimingScope t("pp_policy_reduce", s);
-    hipLaunchKernelGGL(policy_reduce_kernel, dim3(1), dim3(kThreads), 0, s, p, blocks);
-    e = hipGetLastError();
+  {
+    TimingScope t("pp_policy_tokens", s);
+    auto launch = [&](auto kernel, auto& records) {
+      hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, s, p, records);
+    };
+    const NoSlots none;
+    if (plain && vec) launch(policy_tokens_kernel<4, true, InlineSlots>, inl);
+    else if (plain) launch(policy_tokens_kernel<1, true, InlineSlots>, inl);
+    else if (vec) launch(policy_tokens_kernel<4, false, NoSlots>, none);
+    else launch(policy_tokens_kernel<1, false, NoSlots>, none);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  return e;
+  TimingScope t("pp_policy_reduce", s);
+  hipLaunchKernelGGL(policy_reduce_kernel, dim3(1), dim3(kThreads), 0, s, p, blocks);
+  return hipGetLastError();
 }
 
 }  // namespace pp

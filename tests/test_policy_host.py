@@ -91,10 +91,14 @@ def test_policy_refusals():
                 {"clip_high": float("inf")}, {"dual_clip": 1.0}, {"dual_clip": float("nan")}, {"kl_coef": float("inf")},
                 {"ent_coef": float("nan")}, {"kl": 3}, {"kl": -1}, {"reduction": 3}, {"reduction": 2, "norm": 0.0},
                 {"reduction": 2, "norm": float("nan")}, {"kl_coef": 0.1}, {"ent_coef": 0.1}, {"dent": OK}, {"loss": None},
-                {"logp": None}, {"adv": None}, {"logp": ODD}, {"old": ODD}, {"dlogp": ODD}, {"ws": None}, {"ws": OK.value + 16}):
+                {"logp": None}, {"adv": None}, {"logp": ODD}, {"old": ODD}, {"dlogp": ODD}, {"ws": OK.value + 16}):
         assert _policy(**bad) == 1, bad
         assert pp.lib().pp_last_error()
-    assert _policy(n=1) == 4
+    # a few tokens of few responses need no workspace; others do
+    assert pp.pp_policy_workspace_size(PACK) == 0
+    for big in (wl.make_pack([20000], [[5]]), wl.make_pack([1], [[1] * 300])):
+        assert pp.pp_policy_workspace_size(big) > 0
+        assert _policy(_desc(big), n=1) == 4 and _policy(_desc(big), ws=None) == 1
     assert pp.lib().pp_policy_workspace_size(_desc().ref, None) == 1
 
 
