@@ -967,8 +967,18 @@ __global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), (KvShape<D, T>::PER_CU
       if (rg.any_hi <= wk0 || rg.any_lo >= wk1) continue;
       masked = !(rg.all_lo <= wk0 && rg.all_hi >= wk1);
     }
-    // S = Q K^T and dP = dO V^T: lane = key, registers = rows
+    // S = Q K^T and dP = dO V^T: lane = key, registers = rows.  At head size 64 dP's
+    // accumulator starts from -delta, which spares the subtractions.
+    constexpr bool kAccDelta = D == 64 && sizeof(T) == 2;
     f32x16 s = f32x16{}, dp = f32x16{};
+    if constexpr (kAccDelta) {
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 d4 = *reinterpret_cast<const f32x4*>(&sg.ndelta[qb * 32 + 8 * r4 + 4 * hf]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) dp[4 * r4 + e] = d4[e];
+      }
+    }
     {
       constexpr int NC = D / 16;
       Frag fq[2], fk[2], fo[2], fv[2];
@@ -992,7 +1002,7 @@ __global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), (KvShape<D, T>::PER_CU
       }
       if constexpr (sizeof(T) == 2) {
         constexpr int R = S::HOLD ? 1 : 2;  // reads ahead of each MFMA
-        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 2 * R, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedDsRead, (kAccDelta ? 4 : 0) + 2 * R, 0);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           if (c + 1 < NC) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, R, 0);
@@ -1024,13 +1034,14 @@ __global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), (KvShape<D, T>::PER_CU
     for (int r4 = 0; r4 < 4; ++r4) {
       const int il = qb * 32 + 8 * r4 + 4 * hf;
       const f32x4 l4 = *reinterpret_cast<const f32x4*>(&sg.nlse2[il]);
-      const f32x4 d4 = *reinterpret_cast<const f32x4*>(&sg.ndelta[il]);
+      f32x4 d4 = f32x4{};
+      if constexpr (!kAccDelta) d4 = *reinterpret_cast<const f32x4*>(&sg.ndelta[il]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int x = 4 * r4 + e;
         const float pr = fast_exp2(fmaf(s[x], p.scale_log2, l4[e]));
         s[x] = pr;
-        dp[x] = pr * (dp[x] + d4[e]);
+        dp[x] = pr * (kAccDelta ? dp[x] : dp[x] + d4[e]);
       }
     }
     // dV^T += dO^T P and dK^T += Q^T dS over two 16-row chunks

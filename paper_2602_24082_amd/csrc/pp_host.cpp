@@ -2222,11 +2222,11 @@ int64_t cross_part(const std::vector<CrossWalk>& walks, int hkv, const CrossCost
     total += w.tiles * w.units * hkv;
   }
   if (tiles >= 4 * c.slots || longest <= 1) return INT32_MAX;
-  // one round: its longest walk; more: an even share and half of the longest at the end
+  // one round: its longest walk; more: an even share and a quarter of the longest at the end
   auto time = [&](int64_t n, int64_t most) {
     const double worst = (double)std::min(longest, most);
     if (n <= c.slots) return c.start + worst * (n <= c.slots / 2 ? c.half : c.full);
-    return ceil_div(n, c.slots) * c.start + std::max(worst, (double)total / c.slots + 0.5 * worst) * c.full;
+    return ceil_div(n, c.slots) * c.start + std::max(worst, (double)total / c.slots + 0.25 * worst) * c.full;
   };
   auto groups = [&](int64_t most) {
     int64_t n = 0;
