@@ -17,9 +17,8 @@
 //   cross_few      one workgroup = 32 rows, its waves walking different keys
 //   cross_combine  joins forwards whose keys were split over workgroups
 //   cross_dq       delta and -lse log2(e), then dQ, shaped as cross_fwd
-//   cross_dq_sum   adds dQ of split keys
 //   cross_dkdv     key-major: one workgroup = 128 keys, walking the rows
-//   cross_kv_sum   adds dK, dV of split rows
+//   cross_sum      adds dQ of split keys, dK and dV of split rows
 //
 // No atomics: the sums' order depends on the batch's shape alone.  All matrix products
 // run on the 32 x 32 MFMAs with fp32 accumulation: bf16 inputs on v_mfma_f32_32x32x16_bf16
@@ -765,15 +764,17 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
     }
 }
 
-// Adds the parts of dQ rows whose keys were split, in part order.
+// Adds the parts of dQ rows whose keys were split, in part order; block b of the splits'.
 template <int D, typename T>
-__global__ __launch_bounds__(256) void cross_dq_sum_kernel(CrossParams<T> p, const CrossSplit* splits) {
-  constexpr int LPR = D / 4, RPB = 256 / LPR;
-  const int si = blockIdx.x / p.hkv, g = blockIdx.x - si * p.hkv;
+__device__ __forceinline__ void dq_sum_block(const CrossParams<T>& p, const CrossSplit* splits, int b) {
+  constexpr int LPR = D / 4, RPB = 256 / LPR, YB = kCrossRows / RPB;
+  const int y = b % YB;
+  b /= YB;
+  const int si = b / p.hkv, g = b - si * p.hkv;
   const CrossSplit sp = load_uniform(splits + si);
-  const int lr = blockIdx.y * RPB + threadIdx.x / LPR, c = (threadIdx.x % LPR) * 4;
+  const int lr = y * RPB + threadIdx.x / LPR, c = (threadIdx.x % LPR) * 4;
   const int r = sp.r0 + lr;
-  if (lr >= kCrossRows || r >= sp.rows) return;
+  if (r >= sp.rows) return;
   const int i = (int)((unsigned)r / (unsigned)p.G);
   f32x4 acc = f32x4{};
   if (r < sp.live) {
@@ -1106,12 +1107,11 @@ __global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), (KvShape<D, T>::PER_CU
 // Adds the parts of key tiles whose rows were split, in part order.  A workgroup is one
 // gradient of 32 keys: it reads the parts as they lie in the accumulators and turns the
 // sums through LDS, so that a gradient's row is written by one workgroup and whole lines
-// at a time (written 8 bytes a lane from 16 workgroups, 27 MB of parts took 17 us).
+// at a time (written 8 bytes a lane from 16 workgroups, 27 MB of parts took 17 us, now 5).
 template <int D, typename T>
-__global__ __launch_bounds__(256) void cross_kv_sum_kernel(CrossParams<T> p, const CrossKvSplit* splits) {
+__device__ __forceinline__ void kv_sum_block(const CrossParams<T>& p, const float* kv_part, const CrossKvSplit* splits, int b) {
   constexpr int NQ = D / 8 / 4;  // groups of four registers a wave takes
   __shared__ T s_row[32][D + 16 / sizeof(T)];
-  int b = blockIdx.x;
   const int kb = b & 3;
   b >>= 2;
   const int g = b % p.hkv;
@@ -1123,7 +1123,7 @@ __global__ __launch_bounds__(256) void cross_kv_sum_kernel(CrossParams<T> p, con
   if (j0 >= sp.ecap) return;
   const int64_t stride = (int64_t)p.hkv * 2 * 4 * (32 * D);
   const float* part =
-      p.part + ((((int64_t)sp.slot0 * p.hkv + g) * 2 + pass) * 4 + kb) * (32 * D) + (wave * NQ * 64 + lane) * 4;
+      kv_part + ((((int64_t)sp.slot0 * p.hkv + g) * 2 + pass) * 4 + kb) * (32 * D) + (wave * NQ * 64 + lane) * 4;
   f32x4 acc[NQ];
 #pragma unroll
   for (int q = 0; q < NQ; ++q) acc[q] = f32x4{};
@@ -1154,6 +1154,15 @@ __global__ __launch_bounds__(256) void cross_kv_sum_kernel(CrossParams<T> p, con
     if (j0 + r < sp.ecap)
       *reinterpret_cast<u32x4*>(dst + (int64_t)r * p.hkv * D + c) = *reinterpret_cast<const u32x4*>(&s_row[r][c]);
   }
+}
+
+// Both joins of a backward pass, in one launch: dQ's workgroups first.
+template <int D, typename T>
+__global__ __launch_bounds__(256) void cross_sum_kernel(CrossParams<T> p, const float* kv_part, const CrossSplit* splits,
+                                                        const CrossKvSplit* kv_splits, int dq_blocks) {
+  const int b = blockIdx.x;
+  if (b < dq_blocks) dq_sum_block<D, T>(p, splits, b);
+  else kv_sum_block<D, T>(p, kv_part, kv_splits, b - dq_blocks);
 }
 
 template <typename T>
@@ -1227,7 +1236,7 @@ hipError_t launch_fwd_t(const CrossLaunch& a, hipStream_t s) {
 
 template <int D, typename T>
 hipError_t launch_bwd_t(const CrossLaunch& a, hipStream_t s) {
-  CrossParams<T> p = params_of<T>(a);
+  const CrossParams<T> p = params_of<T>(a);
   hipError_t e = hipSuccess;
   if (a.n_items > 0) {
     TimingScope t("pp_cross_attn_dq", s);
@@ -1236,25 +1245,21 @@ hipError_t launch_bwd_t(const CrossLaunch& a, hipStream_t s) {
     else hipLaunchKernelGGL((cross_dq_kernel<D, T, false>), grid, dim3(kWaves * 64), 0, s, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (a.n_splits > 0) {
-    TimingScope t("pp_cross_attn_dq_sum", s);
-    constexpr int RPB = 256 / (D / 4);
-    const dim3 grid((unsigned)((int64_t)a.n_splits * a.hkv), (unsigned)((kCrossRows + RPB - 1) / RPB));
-    hipLaunchKernelGGL((cross_dq_sum_kernel<D, T>), grid, dim3(256), 0, s, p, a.splits);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
   if (a.n_kv_items > 0) {
     TimingScope t("pp_cross_attn_dkdv", s);
-    p.part = a.kv_part;
+    CrossParams<T> pk = p;
+    pk.part = a.kv_part;
     const dim3 grid((unsigned)((int64_t)a.n_kv_items * a.hkv)), block(KvShape<D, T>::WAVES * 64);
-    if (a.key_begin) hipLaunchKernelGGL((cross_dkdv_kernel<D, T, true>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((cross_dkdv_kernel<D, T, false>), grid, block, 0, s, p);
+    if (a.key_begin) hipLaunchKernelGGL((cross_dkdv_kernel<D, T, true>), grid, block, 0, s, pk);
+    else hipLaunchKernelGGL((cross_dkdv_kernel<D, T, false>), grid, block, 0, s, pk);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (a.n_kv_splits > 0) {
-    TimingScope t("pp_cross_attn_kv_sum", s);
-    const dim3 grid((unsigned)((int64_t)a.n_kv_splits * 2 * a.hkv * 4));
-    hipLaunchKernelGGL((cross_kv_sum_kernel<D, T>), grid, dim3(256), 0, s, p, a.kv_splits);
+  const int64_t dq_blocks = (int64_t)a.n_splits * a.hkv * (kCrossRows * (D / 4) / 256);
+  const int64_t kv_blocks = (int64_t)a.n_kv_splits * 2 * a.hkv * 4;
+  if (dq_blocks + kv_blocks > 0) {
+    TimingScope t("pp_cross_attn_sum", s);
+    hipLaunchKernelGGL((cross_sum_kernel<D, T>), dim3((unsigned)(dq_blocks + kv_blocks)), dim3(256), 0, s, p, a.kv_part, a.splits,
+                       a.kv_splits, (int)dq_blocks);
     e = hipGetLastError();
   }
   return e;

@@ -2264,7 +2264,7 @@ struct CrossPlan {
   int tile_rows = kCrossRows;
   bool inline_items = false;
   Layout lay;
-  size_t r_items = 0, r_splits = 0, r_kv_items = 0, r_kv_splits = 0, r_part = 0, r_ml = 0, r_ndelta = 0, r_nlse2 = 0,
+  size_t r_items = 0, r_splits = 0, r_kv_items = 0, r_kv_splits = 0, r_part = 0, r_kv_part = 0, r_ml = 0, r_ndelta = 0, r_nlse2 = 0,
          r_ranges = 0;
 };
 
@@ -2391,8 +2391,8 @@ void plan_cross_bwd(const Batch& bt, const std::vector<EncRow>& enc, pp_dtype dt
   p->r_ndelta = p->lay.add((size_t)bt.sumT * hq * 4);
   p->r_nlse2 = p->lay.add((size_t)bt.sumT * hq * 4);
   p->r_ranges = p->lay.add((size_t)p->blocks * sizeof(CrossRange));
-  // one pass's partial sums are joined before the next pass runs
-  p->r_part = p->lay.add(std::max((size_t)p->slots * hkv * kCrossRows * d * 4, (size_t)p->kv_slots * hkv * kCrossKeys * d * 8));
+  p->r_part = p->lay.add((size_t)p->slots * hkv * kCrossRows * d * 4);
+  p->r_kv_part = p->lay.add((size_t)p->kv_slots * hkv * kCrossKeys * d * 8);
 }
 
 // What both directions check, and the row's limits: a packed row's rows are counted in
@@ -2603,7 +2603,8 @@ pp_status pp_cross_attn_bwd(const pp_pack_desc* desc, const pp_enc_desc* enc, pp
     a.n_splits = (int)p.splits.size();
     a.n_kv_items = (int)p.kv_items.size();
     a.n_kv_splits = (int)p.kv_splits.size();
-    a.part = a.kv_part = (float*)at(ws, p.lay, p.r_part);
+    a.part = (float*)at(ws, p.lay, p.r_part);
+    a.kv_part = (float*)at(ws, p.lay, p.r_kv_part);
     a.ndelta = (float*)at(ws, p.lay, p.r_ndelta);
     a.nlse2 = (float*)at(ws, p.lay, p.r_nlse2);
     a.ranges = (CrossRange*)at(ws, p.lay, p.r_ranges);
