@@ -395,28 +395,38 @@ struct RowEnt {
   __device__ __forceinline__ float entropy() const { return (log2f(s) - t / s) * kLn2; }
 };
 
-template <int THREADS, bool FAR, typename Work>
-__device__ __forceinline__ RowEnt block_ent(MaxSumEnt acc, Work&& work) {
-  for (int off = 32; off > 0; off >>= 1) {
+// SAME: a wave's threads have one maximum, so their sums just add up.  The waves' are
+// joined by every thread for itself, a lane a wave, in one order (thread 0 alone, one
+// after the other, and a barrier to hand the result on took 5% of a long row's time).
+template <int THREADS, bool FAR, bool SAME>
+__device__ __forceinline__ RowEnt block_ent(MaxSumEnt acc) {
+  if constexpr (SAME) {
+    acc.s = wave_sum(acc.s);
+    acc.t = wave_sum(acc.t);
+  } else {
+    for (int off = 32; off > 0; off >>= 1) {
+      MaxSumEnt o;
+      o.m = __shfl_xor(acc.m, off, 64);
+      o.s = __shfl_xor(acc.s, off, 64);
+      o.t = __shfl_xor(acc.t, off, 64);
+      acc = combine_ent<FAR>(acc, o);
+    }
+  }
+  constexpr int W = THREADS / 64;
+  static_assert((W & (W - 1)) == 0 && W <= 64, "a lane a wave");
+  __shared__ MaxSumEnt part[W];
+  const int tid = threadIdx.x;
+  if ((tid & 63) == 0) part[tid >> 6] = acc;
+  __syncthreads();
+  acc = part[tid & (W - 1)];
+  for (int off = W / 2; off > 0; off >>= 1) {
     MaxSumEnt o;
     o.m = __shfl_xor(acc.m, off, 64);
     o.s = __shfl_xor(acc.s, off, 64);
     o.t = __shfl_xor(acc.t, off, 64);
     acc = combine_ent<FAR>(acc, o);
   }
-  __shared__ MaxSumEnt part[THREADS / 64];
-  __shared__ MaxSumEnt s_row;
-  const int tid = threadIdx.x;
-  if ((tid & 63) == 0) part[tid >> 6] = acc;
-  __syncthreads();
-  if (tid == 0) {
-    MaxSumEnt t = part[0];
-    for (int w = 1; w < THREADS / 64; ++w) t = combine_ent<FAR>(t, part[w]);
-    s_row = t;
-    work();
-  }
-  __syncthreads();
-  return {s_row.m, s_row.s, s_row.t, FAR};
+  return {acc.m, acc.s, acc.t, FAR};
 }
 
 // The log-prob pass with entropies: a label token gets the entropy of the distribution
@@ -433,12 +443,11 @@ __global__ __launch_bounds__(THREADS) void logprob_ent_kernel(
   const u32x4* xv = reinterpret_cast<const u32x4*>(x + rs.head);
   MaxSumEnt acc = stream_ent<T, THREADS>(xv, 0, rs.nvec);
   if (tid < rs.n_extra) acc = combine_ent<false>(acc, one_ent(xe));
-  RowEnt r = block_ent<THREADS, false>(acc, [] {});
+  RowEnt r = block_ent<THREADS, false, false>(acc);
   if (r.redo()) {
     acc = any_ent<T, THREADS>(xv, rs.nvec);
     if (tid < rs.n_extra) acc = combine_ent<true>(acc, MaxSumEnt{xe, 1.f, 0.f});
-    __syncthreads();
-    r = block_ent<THREADS, true>(acc, [] {});
+    r = block_ent<THREADS, true, false>(acc);
   }
   for (int j = tid; j < it.label_cnt; j += THREADS) {
     const int32_t pos = labels[it.label_off + j];
@@ -567,7 +576,6 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
   __shared__ float s_g[kMaxRowLabels];
   __shared__ float s_c;
   __shared__ float s_e[ENT ? kMaxRowLabels : 1];
-  __shared__ float s_h;
   __shared__ int s_bad;
   const int cnt = it.label_cnt;
   if (tid == 0) s_bad = 0;
@@ -579,16 +587,6 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
     if constexpr (ENT) s_e[j] = a.dent[a.label_out[it.label_off + j]];
     if (y < 0 || y >= vocab) s_bad = 1;
   }
-  auto sum_labels = [&] {
-    float c = 0.f;
-    for (int j = 0; j < cnt; ++j) c += s_g[j];
-    s_c = c;
-    if constexpr (ENT) {
-      float h = 0.f;
-      for (int j = 0; j < cnt; ++j) h += s_e[j];
-      s_h = h;
-    }
-  };
   MaxSum over = {kNegInf, 0.f};  // of the vectors past the registers
   MaxSumEnt over_ent = {kNegInf, 0.f, 0.f};
   if constexpr (OVER) {
@@ -597,13 +595,32 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
   }
   // logsumexp of the row from the registers
   float m = kNegInf;
-#pragma unroll
-  for (int j = 0; j < R; ++j) {
-    if (j * THREADS + tid < nvec) {
+  // ENT: instead of its values' maximum a thread takes that of its wave's first vectors.
+  // What exceeds it by more than fp32's exponents go makes the sum infinite, and the row
+  // is summed again.  A wave whose first vectors are masked looks at all.
+  bool look = true;
+  if constexpr (ENT) {
+    if (tid < nvec) {
       float f[N];
-      Vec16<T>::unpack(u[j], f);
+      Vec16<T>::unpack(u[0], f);
 #pragma unroll
       for (int e = 0; e < N; ++e) m = max_or_nan(m, f[e]);
+    }
+    for (int off = 32; off > 0; off >>= 1) m = max_or_nan(m, __shfl_xor(m, off, 64));
+    look = __builtin_amdgcn_readfirstlane(m <= -1e30f) != 0;
+  }
+  if (look) {
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      if (j * THREADS + tid < nvec) {
+        float f[N];
+        Vec16<T>::unpack(u[j], f);
+#pragma unroll
+        for (int e = 0; e < N; ++e) m = max_or_nan(m, f[e]);
+      }
+    }
+    if constexpr (ENT) {
+      for (int off = 32; off > 0; off >>= 1) m = max_or_nan(m, __shfl_xor(m, off, 64));
     }
   }
   // the packed vectors count as rewritten here, so each pass below unpacks
@@ -631,24 +648,36 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
   float lse2;
   if constexpr (ENT) {
     MaxSumEnt acc = {m, s, t};
-    if constexpr (OVER) acc = combine_ent<false>(acc, over_ent);
     if (EDGE && tid < n_extra) acc = combine_ent<false>(acc, one_ent(xe));
-    row = block_ent<THREADS, false>(acc, sum_labels);
+    if constexpr (OVER) acc = combine_ent<false>(acc, over_ent);
+    row = block_ent<THREADS, false, !EDGE && !OVER>(acc);
     lse2 = base2(row.m) + log2f(row.s);
   } else {
     MaxSum acc = {m, s};
     if constexpr (OVER) acc = combine(acc, over);
     if (EDGE && tid < n_extra) acc = combine(acc, MaxSum{xe, 1.f});
-    lse = block_lse<THREADS>(acc, sum_labels);
+    lse = block_lse<THREADS>(acc, [&] {
+      float c = 0.f;
+      for (int j = 0; j < cnt; ++j) c += s_g[j];
+      s_c = c;
+    });
     lse2 = lse.lse * kLog2e;
   }
-  const float c = s_c;
+  float c = 0.f, h = 0.f;
+  if constexpr (ENT) {
+    for (int j = 0; j < cnt; ++j) {
+      c += s_g[j];
+      h += s_e[j];
+    }
+  } else {
+    c = s_c;
+  }
   const bool bad = s_bad != 0;
   // -(c + h (ln p + H)) = ent_a + ent_b log2 p
   float ent_a = 0.f, ent_b = 0.f;
   if constexpr (ENT) {
-    ent_a = -fmaf(s_h, row.entropy(), c);
-    ent_b = -s_h * kLn2;
+    ent_a = -fmaf(h, row.entropy(), c);
+    ent_b = -h * kLn2;
   }
   // an element's gradient, its label's terms aside, from the exponent of its softmax
   auto slope = [&](float y) {
@@ -680,8 +709,8 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
     if constexpr (ENT) {
       MaxSumEnt acc = any_ent<T, THREADS>(xv, nvec);
       if (EDGE && tid < n_extra) acc = combine_ent<true>(acc, MaxSumEnt{xe, 1.f, 0.f});
-      row = block_ent<THREADS, true>(acc, [] {});
-      ent_a = -fmaf(s_h, row.entropy(), c);
+      row = block_ent<THREADS, true, false>(acc);
+      ent_a = -fmaf(h, row.entropy(), c);
       far_m = row.m;
       far_ln = logf(row.s);
     } else {
