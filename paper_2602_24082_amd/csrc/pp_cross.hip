@@ -1058,7 +1058,7 @@ __global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), (KvShape<D, T>::PER_CU
   }
 
   wait_vmem<0>();  // K and V of a tile that no row looks at are still on their way
-  const int64_t krow = ((int64_t)(it.e0 + j) * p.hkv + g) * D;
+  const int64_t krow = (((int64_t)it.e0 + j) * p.hkv + g) * D;
 #pragma unroll
   for (int pass = 0; pass < 2; ++pass) {
     f32x16(&row)[D / 32] = pass == 0 ? acc_dk : acc_dv;
