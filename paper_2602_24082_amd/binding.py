@@ -606,6 +606,10 @@ class _EncHolder:
         self.arrays = [np.ascontiguousarray(a, dtype=np.int32) for a in (enc.enc_start, enc.enc_len)]
         self.desc = _EncDesc(*[a.ctypes.data for a in self.arrays])
         self.ref = ctypes.byref(self.desc)
+        self.rows, self.states = len(enc.enc_len), max(0, enc.total_states)
+        if len(enc.enc_start) != self.rows + 1:
+            raise ValueError(f"enc_start must have {self.rows + 1} entries, got {len(enc.enc_start)}")
+        self.sizes = {}  # workspace bytes by pack and heads
 
 
 def _enc_of(enc: Enc) -> _EncHolder:
@@ -645,8 +649,10 @@ def _raw_stream(dev: torch.device) -> int:
     return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
-def _ws_bytes(ws: torch.Tensor, dev: torch.device) -> int:
+def _ws_bytes(ws: Optional[torch.Tensor], dev: torch.device) -> int:
     """Bytes of a workspace, the caller's own checked."""
+    if ws is None:
+        return 0
     if ws.device != dev or not ws.is_contiguous():
         raise ValueError(f"ws must be contiguous, on {dev}")
     return ws.numel() * ws.element_size()
@@ -667,28 +673,46 @@ def _on_gpu(t: torch.Tensor):
 
 def _cross_args(pack: Pack, enc: Enc, q, k, v, key_begin, key_end):
     """Checks the inputs of cross attention; (pack holder, enc holder, hq, hkv, d, dtype code)."""
-    if len(enc.enc_len) != pack.num_rows or len(enc.enc_start) != pack.num_rows + 1:
-        raise ValueError(f"enc describes {len(enc.enc_len)} rows, pack {pack.num_rows}")
+    h, e = _desc_of(pack), _enc_of(enc)
+    if e.rows != pack.num_rows:
+        raise ValueError(f"enc describes {e.rows} rows, pack {pack.num_rows}")
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q and k must be [tokens, heads, head_dim]")
-    T, E = max(0, pack.total_tokens), max(0, enc.total_states)
-    hq, d, hkv = q.shape[1], q.shape[2], k.shape[1]
-    _check_tensor("q", q, (T, hq, d), q.dtype, q.device)
-    _check_tensor("k", k, (E, hkv, d), q.dtype, q.device)
-    _check_tensor("v", v, (E, hkv, d), q.dtype, q.device)
-    for name, t in (("key_begin", key_begin), ("key_end", key_end)):
-        if t is not None:
-            _check_tensor(name, t, (T,), torch.int32, q.device)
+    T = max(0, pack.total_tokens)
+    _, hq, d = q.shape
+    hkv, dt, dev = k.shape[1], q.dtype, q.device
+    _check_tensor("q", q, (T, hq, d), dt, dev)
+    _check_tensor("k", k, (e.states, hkv, d), dt, dev)
+    _check_tensor("v", v, (e.states, hkv, d), dt, dev)
+    if key_begin is not None:
+        _check_tensor("key_begin", key_begin, (T,), torch.int32, dev)
+    if key_end is not None:
+        _check_tensor("key_end", key_end, (T,), torch.int32, dev)
+    code = _dtype_code(q)
     _on_gpu(q)
-    return _desc_of(pack), _enc_of(enc), hq, hkv, d, _dtype_code(q)
+    return h, e, hq, hkv, d, code
+
+
+def _cross_sizes(h: _DescHolder, e: _EncHolder, hq: int, hkv: int, d: int, dtype: int):
+    """(fwd, bwd) workspace bytes, kept with the enc (they follow from the descriptors' contents)."""
+    key = (h.key, hq, hkv, d, dtype)
+    out = e.sizes.get(key)
+    if out is None:
+        f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
+        _check(lib().pp_cross_workspace_size(h.ref, e.ref, dtype, hq, hkv, d, f, b))
+        if len(e.sizes) >= 16:
+            e.sizes.clear()
+        out = e.sizes[key] = (f.value, b.value)
+    return out
+
+
+def _maybe_workspace(nbytes: int, dev: torch.device) -> Optional[torch.Tensor]:
+    return torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
 
 
 def pp_cross_workspace_size(pack: Pack, enc: Enc, hq: int, hkv: int, head_dim: int, dtype: int = PP_BF16):
     """(fwd, bwd) workspace bytes of cross attention."""
-    f, b = ctypes.c_size_t(0), ctypes.c_size_t(0)
-    _check(lib().pp_cross_workspace_size(_desc_of(pack).ref, _enc_of(enc).ref, dtype, hq, hkv, head_dim,
-                                         ctypes.byref(f), ctypes.byref(b)))
-    return int(f.value), int(b.value)
+    return _cross_sizes(_desc_of(pack), _enc_of(enc), hq, hkv, head_dim, dtype)
 
 
 def pp_cross_attn_fwd(pack: Pack, enc: Enc, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float = 0.0,
@@ -702,9 +726,7 @@ def pp_cross_attn_fwd(pack: Pack, enc: Enc, q: torch.Tensor, k: torch.Tensor, v:
     lse = (torch.empty(hq, T, dtype=torch.float32, device=dev) if lse is None
            else _check_tensor("lse", lse, (hq, T), torch.float32, dev))
     if ws is None:
-        n = ctypes.c_size_t(0)
-        _check(lib().pp_cross_workspace_size(h.ref, e.ref, dt, hq, hkv, d, n, None))
-        ws = _workspace(n.value, dev)
+        ws = _maybe_workspace(_cross_sizes(h, e, hq, hkv, d, dt)[0], dev)
     with _device_of(dev):
         _check(lib().pp_cross_attn_fwd(h.ref, e.ref, dt, hq, hkv, d, float(scale), _addr(q), _addr(k), _addr(v),
                                        _addr(key_begin), _addr(key_end), _addr(out), _addr(lse), _addr(ws), _ws_bytes(ws, dev),
@@ -724,9 +746,7 @@ def pp_cross_attn_bwd(pack: Pack, enc: Enc, q, k, v, o, lse, dout, scale: float 
     dk = torch.empty_like(k) if dk is None else _check_tensor("dk", dk, k.shape, q.dtype, dev)
     dv = torch.empty_like(v) if dv is None else _check_tensor("dv", dv, v.shape, q.dtype, dev)
     if ws is None:
-        n = ctypes.c_size_t(0)
-        _check(lib().pp_cross_workspace_size(h.ref, e.ref, dt, hq, hkv, d, None, ctypes.byref(n)))
-        ws = _workspace(n.value, dev)
+        ws = _maybe_workspace(_cross_sizes(h, e, hq, hkv, d, dt)[1], dev)
     with _device_of(dev):
         _check(lib().pp_cross_attn_bwd(h.ref, e.ref, dt, hq, hkv, d, float(scale), _addr(q), _addr(k), _addr(v),
                                        _addr(key_begin), _addr(key_end), _addr(o), _addr(lse), _addr(dout), _addr(dq), _addr(dk),
@@ -839,8 +859,8 @@ def pp_policy_loss(pack: Pack, logp: torch.Tensor, adv: torch.Tensor, logp_old: 
     dent = new(T) if want_grad and entropy is not None else None
     if ws is None:
         n = ctypes.c_size_t(0)
-        _check(lib().pp_policy_workspace_size(h.ref, ctypes.byref(n)))
-        ws = _workspace(n.value, dev)
+        _check(lib().pp_policy_workspace_size(h.ref, n))
+        ws = _maybe_workspace(n.value, dev)
     with _device_of(dev):
         _check(lib().pp_policy_loss(h.ref, ctypes.byref(cfg), _addr(logp), _addr(logp_old), _addr(logp_ref), _addr(entropy),
                                     _addr(adv), int(per_token), _addr(mask), _addr(loss), _addr(stats), _addr(counts), _addr(dlogp),
