@@ -134,12 +134,13 @@ struct CrossParams {
 
 // Few items ride in the launch's arguments, so that a small call needs no copy ahead of
 // its kernels.
+template <int N>
 struct InlineItems {
-  CrossItem item[kCrossInline];
+  CrossItem item[N];
 };
 
-template <typename P>
-__device__ __forceinline__ CrossItem cross_item(const P& p, const InlineItems& inl, int idx) {
+template <typename P, int N>
+__device__ __forceinline__ CrossItem cross_item(const P& p, const InlineItems<N>& inl, int idx) {
   if (p.items) return load_uniform(p.items + idx);
   return inl.item[idx];
 }
@@ -299,8 +300,8 @@ __device__ __forceinline__ void block_keys(const CrossItem& it, const WaveKeys& 
   }
 }
 
-template <int D, typename T, bool RANGES>
-__global__ __launch_bounds__(kWaves * 64, (kFwdPerCu<D, T>)) void cross_fwd_kernel(CrossParams<T> p, InlineItems inl) {
+template <int D, typename T, bool RANGES, int N>
+__global__ __launch_bounds__(kWaves * 64, (kFwdPerCu<D, T>)) void cross_fwd_kernel(CrossParams<T> p, InlineItems<N> inl) {
   using O = Ops<T>;
   using Frag = typename O::Frag;
   constexpr int BN = kKeys<T>, KB = BN / 32, RPW = BN / kWaves;
@@ -428,8 +429,8 @@ __global__ __launch_bounds__(kWaves * 64, (kFwdPerCu<D, T>)) void cross_fwd_kern
 template <int D, typename T>
 constexpr int kFewWaves = D * sizeof(T) > 256 ? 2 : 4;  // 128 KB of LDS at most
 
-template <int D, typename T, bool RANGES>
-__global__ __launch_bounds__((kFewWaves<D, T> * 64), 1) void cross_few_kernel(CrossParams<T> p, InlineItems inl) {
+template <int D, typename T, bool RANGES, int N>
+__global__ __launch_bounds__((kFewWaves<D, T> * 64), 1) void cross_few_kernel(CrossParams<T> p, InlineItems<N> inl) {
   using O = Ops<T>;
   using Frag = typename O::Frag;
   constexpr int NW = kFewWaves<D, T>, NC = D / 16;
@@ -557,8 +558,8 @@ __global__ __launch_bounds__((kFewWaves<D, T> * 64), 1) void cross_few_kernel(Cr
 
 // Joins the parts of rows whose keys were split, in part order: a row is D / 4 lanes,
 // four parts' loads in flight.
-template <int D, typename T>
-__global__ __launch_bounds__(256) void cross_combine_kernel(CrossParams<T> p, const CrossSplit* splits, CrossSplitList inl,
+template <int D, typename T, int N>
+__global__ __launch_bounds__(256) void cross_combine_kernel(CrossParams<T> p, const CrossSplit* splits, CrossSplitList<N> inl,
                                                             int bm) {
   constexpr int LPR = D / 4, RPB = 256 / LPR;
   const int si = blockIdx.x / p.hkv, g = blockIdx.x - si * p.hkv;
@@ -1197,41 +1198,48 @@ CrossParams<T> params_of(const CrossLaunch& a) {
   return p;
 }
 
-void fill_inline(const CrossLaunch& a, InlineItems* inl, CrossSplitList* sl) {
-  if (!a.items)
-    for (int i = 0; i < a.n_items; ++i) inl->item[i] = a.host_items[i];
-  if (!a.splits)
-    for (int i = 0; i < a.n_splits; ++i) sl->split[i] = a.host_splits[i];
+// A launch with 3 KB of arguments takes the host 4.3 us, one with 500 bytes 3.5: few
+// items, few splits or none of them have launches of their own.
+template <int D, typename T, int N>
+hipError_t launch_fwd_items(const CrossLaunch& a, const CrossParams<T>& p, hipStream_t s) {
+  InlineItems<N> inl;
+  for (int i = 0; i < N; ++i) inl.item[i] = !a.items && i < a.n_items ? a.host_items[i] : CrossItem{};
+  const dim3 grid((unsigned)((int64_t)a.n_items * a.hkv));
+  auto launch = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, s, p, inl); };
+  if (a.tile_rows == kCrossFewRows) {
+    if (a.key_begin) launch(cross_few_kernel<D, T, true, N>, kFewWaves<D, T>);
+    else launch(cross_few_kernel<D, T, false, N>, kFewWaves<D, T>);
+  } else {
+    if (a.key_begin) launch(cross_fwd_kernel<D, T, true, N>, kWaves);
+    else launch(cross_fwd_kernel<D, T, false, N>, kWaves);
+  }
+  return hipGetLastError();
+}
+
+template <int D, typename T, int N>
+hipError_t launch_combine(const CrossLaunch& a, const CrossParams<T>& p, hipStream_t s) {
+  CrossSplitList<N> sl;
+  for (int i = 0; i < N; ++i) sl.split[i] = !a.splits && i < a.n_splits ? a.host_splits[i] : CrossSplit{};
+  constexpr int RPB = 256 / (D / 4);
+  const dim3 grid((unsigned)((int64_t)a.n_splits * a.hkv), (unsigned)((a.tile_rows + RPB - 1) / RPB));
+  hipLaunchKernelGGL((cross_combine_kernel<D, T, N>), grid, dim3(256), 0, s, p, a.splits, sl, a.tile_rows);
+  return hipGetLastError();
 }
 
 template <int D, typename T>
 hipError_t launch_fwd_t(const CrossLaunch& a, hipStream_t s) {
   const CrossParams<T> p = params_of<T>(a);
-  InlineItems inl{};
-  CrossSplitList sl{};
-  fill_inline(a, &inl, &sl);
   if (a.n_items > 0) {
     TimingScope t("pp_cross_attn_fwd", s);
-    const dim3 grid((unsigned)((int64_t)a.n_items * a.hkv));
-    auto launch = [&](auto kernel, int waves) { hipLaunchKernelGGL(kernel, grid, dim3(waves * 64), 0, s, p, inl); };
-    if (a.tile_rows == kCrossFewRows) {
-      if (a.key_begin) launch(cross_few_kernel<D, T, true>, kFewWaves<D, T>);
-      else launch(cross_few_kernel<D, T, false>, kFewWaves<D, T>);
-    } else {
-      if (a.key_begin) launch(cross_fwd_kernel<D, T, true>, kWaves);
-      else launch(cross_fwd_kernel<D, T, false>, kWaves);
-    }
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = a.items ? launch_fwd_items<D, T, 1>(a, p, s)
+                                 : a.n_items <= 16 ? launch_fwd_items<D, T, 16>(a, p, s)
+                                                   : launch_fwd_items<D, T, kCrossInline>(a, p, s);
     if (e != hipSuccess) return e;
   }
-  if (a.n_splits > 0) {
-    TimingScope t("pp_cross_attn_combine", s);
-    constexpr int RPB = 256 / (D / 4);
-    const dim3 grid((unsigned)((int64_t)a.n_splits * a.hkv), (unsigned)((a.tile_rows + RPB - 1) / RPB));
-    hipLaunchKernelGGL((cross_combine_kernel<D, T>), grid, dim3(256), 0, s, p, a.splits, sl, a.tile_rows);
-    return hipGetLastError();
-  }
-  return hipSuccess;
+  if (a.n_splits == 0) return hipSuccess;
+  TimingScope t("pp_cross_attn_combine", s);
+  if (a.splits || a.n_splits <= 8) return launch_combine<D, T, 8>(a, p, s);
+  return launch_combine<D, T, kCrossInline / 2>(a, p, s);
 }
 
 template <int D, typename T>

@@ -202,8 +202,9 @@ struct CrossSplit {
   int32_t tok0, r0, rows, live;
   int32_t slot0, parts;
 };
+template <int N>
 struct CrossSplitList {
-  CrossSplit split[kCrossInline / 2];
+  CrossSplit split[N];
 };
 
 // Keys [k0, k0 + kCrossKeys) of a packed row's states against the row steps [n_begin, n_end).

@@ -33,12 +33,18 @@ namespace {
 
 constexpr int kThreads = kPolicyThreads;
 
-// Responses ride in the launch's arguments when they are few.
+// Responses ride in the launch's arguments when they are few.  A launch with 3 KB of
+// arguments takes the host 4.3 us, one with 500 bytes 3.5 and one with 64 bytes 2.5, so
+// there are two sizes, and none.
+template <int N>
 struct InlineSlots {
-  PolicySlot slot[kPolicyInline];
+  static constexpr int kSlots = N;
+  PolicySlot slot[N];
 };
 
-struct NoSlots {};
+struct NoSlots {
+  static constexpr int kSlots = 0;
+};
 
 __device__ __forceinline__ double wave_sum_d(double x) {
   for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
@@ -68,11 +74,14 @@ __device__ __forceinline__ int count_tokens(const PolicyParams& p, const PolicyS
 // A wave a response; `from`: records in mapped host memory, or null (inl, or in place).
 // It also notes, for the workgroups of policy_tokens (chunk tokens each) that start
 // between the end of the response ahead and its own, that it is the first they meet.
-__global__ __launch_bounds__(kThreads) void policy_records_kernel(PolicyParams p, const PolicySlot* from, int in_args, int chunk,
-                                                                  InlineSlots inl) {
+template <typename Inline>
+__global__ __launch_bounds__(kThreads) void policy_records_kernel(PolicyParams p, const PolicySlot* from, int chunk, Inline inl) {
   const int i = (int)((blockIdx.x * kThreads + threadIdx.x) >> 6), lane = threadIdx.x & 63;
   if (i >= p.n_slots) return;
-  auto at = [&](int k) { return from ? from[k] : in_args ? inl.slot[k] : p.slots[k]; };
+  auto at = [&](int k) {
+    if constexpr (Inline::kSlots > 0) return inl.slot[k];
+    else return from ? from[k] : p.slots[k];
+  };
   const PolicySlot sl = at(i);
   const int64_t from_t = i > 0 ? (int64_t)at(i - 1).begin + at(i - 1).len : 0, to_t = (int64_t)sl.begin + sl.len;
   const int chunks = (int)((p.sumT + chunk - 1) / chunk);
@@ -230,10 +239,11 @@ __device__ __forceinline__ int first_slot(int n_slots, int64_t c, At&& at) {
 }
 
 // TPT consecutive tokens a thread; their values are on the way while the responses that
-// they belong to are found.  IN_ARGS: the records come with the launch and nothing is
-// masked, so there are no counts to read.
-template <int TPT, bool IN_ARGS, typename Inline>
+// they belong to are found.  Records that come with the launch are those of an unmasked
+// batch: there are no counts to read.
+template <int TPT, typename Inline>
 __global__ __launch_bounds__(kThreads) void policy_tokens_kernel(PolicyParams p, Inline inl) {
+  constexpr bool IN_ARGS = Inline::kSlots > 0;
   constexpr int CH = kThreads * TPT;
   __shared__ int s_begin[CH], s_end[CH], s_out[CH], s_count[CH];
   __shared__ double s_w[CH];
@@ -377,9 +387,11 @@ __global__ __launch_bounds__(kThreads) void policy_tokens_kernel(PolicyParams p,
 // Few tokens of few responses: a call of one launch.  16 waves count the responses'
 // tokens, then every thread takes each 1024th token, its response found by stepping on.
 constexpr int kSmallThreads = 1024;
-__global__ __launch_bounds__(kSmallThreads) void policy_small_kernel(PolicyParams p, InlineSlots inl) {
-  __shared__ int s_begin[kPolicyInline], s_end[kPolicyInline], s_out[kPolicyInline], s_n[kPolicyInline];
-  __shared__ double s_w[kPolicyInline];
+template <typename Inline>
+__global__ __launch_bounds__(kSmallThreads) void policy_small_kernel(PolicyParams p, Inline inl) {
+  constexpr int S = Inline::kSlots;
+  __shared__ int s_begin[S], s_end[S], s_out[S], s_n[S];
+  __shared__ double s_w[S];
   __shared__ int s_total, s_some;
   const int tid = threadIdx.x, wave = tid >> 6;
   if (tid == 0) s_total = s_some = 0;
@@ -456,19 +468,17 @@ __global__ __launch_bounds__(kThreads) void policy_reduce_kernel(PolicyParams p,
   if (threadIdx.x == 0) write_results(p, t);
 }
 
-}  // namespace
-
-hipError_t launch_policy(const PolicyLaunch& a, hipStream_t s) {
+template <typename Inline>
+hipError_t launch_policy_t(const PolicyLaunch& a, const Inline& inl, hipStream_t s) {
   PolicyParams p = a;
   hipError_t e = hipSuccess;
-  InlineSlots inl;
-  const bool in_args = policy_inline(a.n_slots);
-  if (in_args)
-    for (int i = 0; i < a.n_slots; ++i) inl.slot[i] = a.host_slots[i];
-  if (policy_small(a.sumT, a.n_slots)) {
-    TimingScope t("pp_policy_tokens", s);
-    hipLaunchKernelGGL(policy_small_kernel, dim3(1), dim3(kSmallThreads), 0, s, p, inl);
-    return hipGetLastError();
+  constexpr bool in_args = Inline::kSlots > 0;
+  if constexpr (in_args) {
+    if (policy_small(a.sumT, a.n_slots)) {
+      TimingScope t("pp_policy_tokens", s);
+      hipLaunchKernelGGL(policy_small_kernel<Inline>, dim3(1), dim3(kSmallThreads), 0, s, p, inl);
+      return hipGetLastError();
+    }
   }
   uintptr_t any = 0;
   for (const void* x : {(const void*)a.logp, (const void*)a.old, (const void*)a.ref, (const void*)a.entropy,
@@ -482,8 +492,8 @@ hipError_t launch_policy(const PolicyLaunch& a, hipStream_t s) {
     TimingScope t("pp_policy_records", s);
     p.in_place = !a.from && !in_args;
     const int per = kThreads / 64;
-    hipLaunchKernelGGL(policy_records_kernel, dim3((a.n_slots + per - 1) / per), dim3(kThreads), 0, s, p, a.from, (int)in_args,
-                       (int)ch, inl);
+    hipLaunchKernelGGL(policy_records_kernel<Inline>, dim3((a.n_slots + per - 1) / per), dim3(kThreads), 0, s, p, a.from, (int)ch,
+                       inl);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   {
@@ -492,15 +502,30 @@ hipError_t launch_policy(const PolicyLaunch& a, hipStream_t s) {
       hipLaunchKernelGGL(kernel, dim3(blocks), dim3(kThreads), 0, s, p, records);
     };
     const NoSlots none;
-    if (plain && vec) launch(policy_tokens_kernel<4, true, InlineSlots>, inl);
-    else if (plain) launch(policy_tokens_kernel<1, true, InlineSlots>, inl);
-    else if (vec) launch(policy_tokens_kernel<4, false, NoSlots>, none);
-    else launch(policy_tokens_kernel<1, false, NoSlots>, none);
+    if (plain && vec) launch(policy_tokens_kernel<4, Inline>, inl);
+    else if (plain) launch(policy_tokens_kernel<1, Inline>, inl);
+    else if (vec) launch(policy_tokens_kernel<4, NoSlots>, none);
+    else launch(policy_tokens_kernel<1, NoSlots>, none);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   TimingScope t("pp_policy_reduce", s);
   hipLaunchKernelGGL(policy_reduce_kernel, dim3(1), dim3(kThreads), 0, s, p, blocks);
   return hipGetLastError();
+}
+
+template <int N>
+hipError_t launch_policy_inline(const PolicyLaunch& a, hipStream_t s) {
+  InlineSlots<N> inl;
+  for (int i = 0; i < N; ++i) inl.slot[i] = i < a.n_slots ? a.host_slots[i] : PolicySlot{};
+  return launch_policy_t(a, inl, s);
+}
+
+}  // namespace
+
+hipError_t launch_policy(const PolicyLaunch& a, hipStream_t s) {
+  if (a.n_slots <= 40) return launch_policy_inline<40>(a, s);
+  if (policy_inline(a.n_slots)) return launch_policy_inline<kPolicyInline>(a, s);
+  return launch_policy_t(a, NoSlots{}, s);
 }
 
 }  // namespace pp
