@@ -46,6 +46,9 @@ struct Ops<__bf16> {
   using Frag = bf16x8;
   template <int D>
   static constexpr int kRowD = D;  // the row as 2-byte elements, for the DMA and its swizzle
+  static __device__ __forceinline__ Frag load(const __bf16* p) { return *reinterpret_cast<const Frag*>(p); }
+  using Held = Frag;  // a fragment that stays in registers
+  static __device__ __forceinline__ const Frag& use(const Held& x) { return x; }
   static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, const f32x16& c) { return mfma32(a, b, c); }
   static __device__ __forceinline__ Frag from_acc(const f32x16& acc, int s) { return acc_half_to_bf16(acc, s); }
   template <int D>
@@ -58,42 +61,63 @@ struct Ops<__bf16> {
   }
 };
 
-// fp32: the MFMA takes one element of the contraction axis from either half of the wave,
-// so a fragment's element e pairs contraction indices e and 8 + e, alike in both operands.
+// fp32 on the bf16 matrix units: x = h + m + l, three bf16 numbers that hold all 24 bits
+// of it (each the rest rounded to nearest: |m| <= 2^-9 |x|, |l| <= 2^-18 |x|).  Of the
+// nine products of two such sums the six above 2^-26 of the whole are taken, smallest
+// first, so a product is as good as an fp32 one: 6 x 32 cycles for 16 steps of the
+// contraction, against 8 x 64 on v_mfma_f32_32x32x2_f32.
+struct Split3 {
+  bf16x8 h, m, l;
+};
+__device__ __forceinline__ Split3 split3(const f32x8& x) {
+  Split3 s;
+  s.h = __builtin_convertvector(x, bf16x8);
+  const f32x8 r = x - __builtin_convertvector(s.h, f32x8);
+  s.m = __builtin_convertvector(r, bf16x8);
+  s.l = __builtin_convertvector(r - __builtin_convertvector(s.m, f32x8), bf16x8);
+  return s;
+}
+
 template <>
 struct Ops<float> {
-  using Frag = f32x8;
+  using Frag = Split3;
   template <int D>
   static constexpr int kRowD = 2 * D;
+  static __device__ __forceinline__ Frag load(const float* p) { return split3(*reinterpret_cast<const f32x8*>(p)); }
+  using Held = f32x8;  // whole: 64 registers of K and V at head size 128 instead of 96, split at each use
+  static __device__ __forceinline__ Frag use(const Held& x) { return split3(x); }
   static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, f32x16 c) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
-    return c;
+    c = mfma32(a.l, b.h, c);
+    c = mfma32(a.h, b.l, c);
+    c = mfma32(a.m, b.m, c);
+    c = mfma32(a.m, b.h, c);
+    c = mfma32(a.h, b.m, c);
+    return mfma32(a.h, b.h, c);
   }
   static __device__ __forceinline__ Frag from_acc(const f32x16& acc, int s) {
-    Frag f;
+    f32x8 f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = acc[8 * s + e];
-    return f;
+    return split3(f);
   }
   template <int D>
   static __device__ __forceinline__ Frag row8(const float* tile, int r, int lc) {
     const int sw = swz<2 * D>(r);
     const f32x4 a = *reinterpret_cast<const f32x4*>(tile + r * D + (((2 * lc) ^ sw) << 2));
     const f32x4 b = *reinterpret_cast<const f32x4*>(tile + r * D + (((2 * lc + 1) ^ sw) << 2));
-    return Frag{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    return split3(f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
   }
   // column col0 + l % 32 of the rows that from_acc's elements stand for
   template <int D>
   static __device__ __forceinline__ Frag tr8(const float* tile, int row16, int col0, int lane) {
     const int c = col0 + (lane & 31), h = lane >> 5;
-    Frag f;
+    f32x8 f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       const int r = row16 + 8 * (e >> 2) + 4 * h + (e & 3);
       f[e] = tile[r * D + (((c >> 2) ^ swz<2 * D>(r)) << 2) + (c & 3)];
     }
-    return f;
+    return split3(f);
   }
 };
 
@@ -319,7 +343,7 @@ __global__ __launch_bounds__(kWaves * 64, (kFwdPerCu<D, T>)) void cross_fwd_kern
   Frag qf[D / 16];
 #pragma unroll
   for (int c = 0; c < D / 16; ++c)
-    qf[c] = w.live ? *reinterpret_cast<const Frag*>(p.q + qrow + 16 * c + 8 * hf) : Frag{};
+    qf[c] = w.live ? O::load(p.q + qrow + 16 * c + 8 * hf) : Frag{};
 
   int key0, key1;
   block_keys<RANGES, BN>(it, wk, wave, key0, key1);
@@ -478,7 +502,7 @@ __global__ __launch_bounds__((kFewWaves<D, T> * 64), 1) void cross_few_kernel(Cr
   Frag qf[NC];
 #pragma unroll
   for (int c = 0; c < NC; ++c)
-    qf[c] = w.live ? *reinterpret_cast<const Frag*>(p.q + qrow + 16 * c + 8 * hf) : Frag{};
+    qf[c] = w.live ? O::load(p.q + qrow + 16 * c + 8 * hf) : Frag{};
   RowState<D> st;
   st.init();
   for (int i = 0; i < n; ++i) {
@@ -627,8 +651,8 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
   Frag qf[D / 16], df[D / 16];
 #pragma unroll
   for (int c = 0; c < D / 16; ++c) {
-    qf[c] = w.live ? *reinterpret_cast<const Frag*>(p.q + qrow + 16 * c + 8 * hf) : Frag{};
-    df[c] = w.live ? *reinterpret_cast<const Frag*>(p.dout + qrow + 16 * c + 8 * hf) : Frag{};
+    qf[c] = w.live ? O::load(p.q + qrow + 16 * c + 8 * hf) : Frag{};
+    df[c] = w.live ? O::load(p.dout + qrow + 16 * c + 8 * hf) : Frag{};
   }
   // delta = dO . O and -lse log2(e) of the lane's row, kept for the dK/dV pass
   float nlse2 = 0.f, dlt = 0.f;
@@ -637,9 +661,11 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
     if (w.live) {
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
-        const Frag b = *reinterpret_cast<const Frag*>(p.o_in + qrow + 16 * c + 8 * hf);
+        typedef T vec8 __attribute__((ext_vector_type(8)));
+        const vec8 a = *reinterpret_cast<const vec8*>(p.dout + qrow + 16 * c + 8 * hf);
+        const vec8 b = *reinterpret_cast<const vec8*>(p.o_in + qrow + 16 * c + 8 * hf);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc += (float)df[c][e] * (float)b[e];
+        for (int e = 0; e < 8; ++e) acc += (float)a[e] * (float)b[e];
       }
       nlse2 = -p.lse_in[(int64_t)w.head * p.sumT + w.tok] * kLog2e;
     }
@@ -861,15 +887,16 @@ __global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), (KvShape<D, T>::PER_CU
   const int64_t kv_stride = (int64_t)p.hkv * D;
 
   // rows past the states repeat the last one
-  Frag kf[S::HOLD ? D / 16 : 1], vf[S::HOLD ? D / 16 : 1];
+  using Held = typename O::Held;
+  Held kf[S::HOLD ? D / 16 : 1], vf[S::HOLD ? D / 16 : 1];
   const bool any = it.n_begin < it.n_end;
   if constexpr (S::HOLD) {
     if (any) {
       const int64_t row = ((int64_t)(it.e0 + min(j, it.elen - 1)) * p.hkv + g) * D;
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
-        kf[c] = *reinterpret_cast<const Frag*>(p.k + row + 16 * c + 8 * hf);
-        vf[c] = *reinterpret_cast<const Frag*>(p.v + row + 16 * c + 8 * hf);
+        kf[c] = *reinterpret_cast<const Held*>(p.k + row + 16 * c + 8 * hf);
+        vf[c] = *reinterpret_cast<const Held*>(p.v + row + 16 * c + 8 * hf);
       }
     }
   } else {
@@ -995,8 +1022,10 @@ __global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), (KvShape<D, T>::PER_CU
       for (int c = 0; c < NC; ++c) {
         if (c + 1 < NC) load(c + 1, (c + 1) & 1);
         if constexpr (S::HOLD) {
-          s = O::mma(fq[c & 1], kf[c], s);
-          dp = O::mma(fo[c & 1], vf[c], dp);
+          // counts as rewritten, or the split parts of all of K and V would be kept across steps
+          if constexpr (sizeof(T) == 4 && D == 128) asm volatile("" : "+v"(kf[c]), "+v"(vf[c]));
+          s = O::mma(fq[c & 1], O::use(kf[c]), s);
+          dp = O::mma(fo[c & 1], O::use(vf[c]), dp);
         } else {
           s = O::mma(fq[c & 1], fk[c & 1], s);
           dp = O::mma(fo[c & 1], fv[c & 1], dp);
