@@ -422,11 +422,13 @@ typedef struct pp_enc_desc {
  *   q, o, dout, dq [sumT, hq, head_dim], k, v, dk, dv [sumE, hkv, head_dim],
  *   lse float [hq, sumT]; head_dim 64 or 128, hq at most 4096.
  * PP_BF16: the probabilities (and dS) are rounded to bf16 for the second product,
- * sums are fp32.  PP_FP32: nothing is rounded below fp32 (unlike pp_attn_fwd).
+ * sums are fp32.  PP_FP32: products and sums are as exact as fp32's (unlike
+ * pp_attn_fwd, which rounds its inputs).
  * The backward takes the forward's o and lse, and writes all of dq, dk and dv
  * (0 in the states' padding).  Results do not depend on scheduling (no atomics).
  * Scores and values of every state of [0, enc_len[b]) enter tile-wise products:
- * a state that is not finite may reach tokens whose range leaves it out.
+ * a state that is not finite may reach tokens whose range leaves it out, and
+ * infinities come out as NaN (for PP_FP32 so do elements above bf16's 3.39e38).
  * ws_bytes >= pp_cross_workspace_size's fwd or bwd (either output may be NULL);
  * a batch of a few short rows needs none in the forward.
  * Errors as pp_attn_fwd; PP_ERR_BAD_LAYOUT also for a broken enc. */

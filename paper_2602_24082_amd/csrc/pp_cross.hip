@@ -23,8 +23,8 @@
 // No atomics: the sums' order depends on the batch's shape alone.  All matrix products
 // run on the 32 x 32 MFMAs with fp32 accumulation: bf16 inputs on v_mfma_f32_32x32x16_bf16
 // with P and dS rounded to bf16 (nearest even; half a step of 2^-8 relative each, as small
-// as the rounding of the results), fp32 inputs on v_mfma_f32_32x32x2_f32 with nothing
-// rounded below fp32.
+// as the rounding of the results), fp32 numbers as sums of three of bf16 on the same
+// instruction, which loses nothing that an fp32 product would keep (see Split3).
 
 #include <hip/hip_runtime.h>
 

@@ -2346,8 +2346,9 @@ struct CrossCosts {
 CrossCosts cross_costs(pp_dtype dtype, int d) {
   const double rows = join_us((double)kCrossRows * d), keys = join_us((double)kCrossKeys * d);  // two gradients, half of it under the walks
   if (dtype == PP_FP32) {
-    const double h = d / 128.0;
-    return {{kUnits, 9.7 * h, 9.3 * h, 3.0, rows}, {kUnits, 14.1 * h, 13.5 * h, 3.0, rows}, {kUnits, 9.0 * h, 9.0 * h, 3.0, keys}};
+    if (d == 128)
+      return {{kUnits, 8.2, 8.2, 3.0, rows}, {kUnits, 11.1, 11.1, 3.0, rows}, {kUnits, 8.9, 8.9, 3.0, keys}};
+    return {{kUnits, 4.6, 4.6, 3.0, rows}, {kUnits, 6.0, 6.0, 3.0, rows}, {kUnits, 4.0, 4.0, 3.0, keys}};
   }
   if (d == 128)
     return {{2 * kUnits, 2.3, 1.35, 3.0, rows}, {2 * kUnits, 3.1, 1.75, 3.0, rows}, {kUnits, 1.9, 1.65, 3.0, keys}};
