@@ -165,8 +165,10 @@ __device__ __forceinline__ PolicyTerms policy_terms(const PolicyParams& p, float
       used = (float)p.dual_clip;
     }
   }
+  const float d_lp = p.old ? lp - old : 0.f;
+  if (A == 0.f && d_lp > 88.f && d_lp < __builtin_inff()) used = 0.f;  // no advantage of a ratio past fp32
   t.surr = used * A;
-  t.grad = t.clipped ? 0.f : -A * t.ratio;
+  t.grad = t.clipped ? 0.f : -A * used;
   t.kl = 0.f;
   if (p.ref) {
     const float x = ref - lp;

@@ -307,3 +307,16 @@ def test_policy_small_divergence_keeps_its_digits():
     got = _check_policy(pack, lp, np.zeros((1, 1), np.float32), {"ref": ref}, kl_coef=1.0)
     want = orc.policy_loss(*pack.oracle_args(), lp, np.zeros((1, 1)), ref=ref, kl_coef=1.0)[1][1]
     assert float(got[1][1]) == pytest.approx(want, rel=12 * E + E)
+
+
+@pytest.mark.parametrize("lens", [[3, 2], [3000, 2]])
+def test_policy_ratio_past_fp32_without_advantage(lens):
+    pack = wl.make_pack([4], [lens])
+    T = pack.total_tokens
+    lp, old = torch.full((T,), -1.0, device=DEV), torch.full((T,), -1.0, device=DEV)
+    old[5] = -101.0  # e^100 is past fp32, its product with an advantage of 0 is 0
+    loss, stats, counts, dlogp, _ = pp.pp_policy_loss(pack, lp, torch.tensor([[0.0, 1.0]], device=DEV), logp_old=old, reduction="sum")
+    assert loss.item() == -2.0 and stats[0].item() == -2.0 and counts.tolist() == [sum(lens), 0]
+    want = torch.zeros(T, device=DEV)
+    want[4 + lens[0]:] = -1.0
+    assert torch.equal(dlogp, want)
