@@ -672,7 +672,7 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
   } else {
     c = s_c;
   }
-  const bool bad = s_bad != 0;
+  if (s_bad != 0) c = -__builtin_nanf("");  // a label outside the vocabulary: all of the row is NaN
   // -(c + h (ln p + H)) = ent_a + ent_b log2 p
   float ent_a = 0.f, ent_b = 0.f;
   if constexpr (ENT) {
@@ -685,28 +685,24 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
     if constexpr (ENT) return fast_exp2(y) * fmaf(ent_b, fmaxf(y, kLeastExp), ent_a);
     else return fast_exp2(y);
   };
-  auto finish = [&](int vi, float* f) {  // f: the slopes of vector vi
+  auto finish = [&](int vi, float* f, bool labels) {  // f: the slopes of vector vi; labels: it may hold one
     if constexpr (!ENT) {
 #pragma unroll
       for (int e = 0; e < N; ++e) f[e] *= -c;
     }
-    for (int l = 0; l < cnt; ++l) {
-      const int d = s_y[l] - (head + vi * N);
-      if ((unsigned)d < (unsigned)N) {
+    if (labels) {
+      for (int l = 0; l < cnt; ++l) {
+        const int d = s_y[l] - (head + vi * N);
 #pragma unroll
         for (int e = 0; e < N; ++e) f[e] += (e == d) ? s_g[l] : 0.f;
       }
-    }
-    if (bad) {
-#pragma unroll
-      for (int e = 0; e < N; ++e) f[e] = __builtin_nanf("");
     }
     store(vi, Pack16<T>::pack(f));
   };
   auto finish_extra = [&](float f) {
     if constexpr (!ENT) f *= -c;
     for (int l = 0; l < cnt; ++l) f += s_y[l] == xi ? s_g[l] : 0.f;
-    out[xi] = (T)(bad ? __builtin_nanf("") : f);
+    out[xi] = (T)f;
   };
   const bool redo = ENT ? row.redo() : lse.redo();
   if (__builtin_expect(__builtin_amdgcn_readfirstlane(redo ? 1 : 0), 0)) {
@@ -733,17 +729,17 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
       Vec16<T>::unpack(xv[vi], f);
 #pragma unroll
       for (int e = 0; e < N; ++e) f[e] = far(f[e]);
-      finish(vi, f);
+      finish(vi, f, true);
     }
     if (EDGE && tid < n_extra) finish_extra(far(xe));
     return;
   }
-  auto gradient = [&](int vi, const u32x4& x16) {
+  auto gradient = [&](int vi, const u32x4& x16, bool labels) {
     float f[N];
     Vec16<T>::unpack(x16, f);
 #pragma unroll
     for (int e = 0; e < N; ++e) f[e] = slope(fmaf(f[e], kLog2e, -lse2));
-    finish(vi, f);
+    finish(vi, f, labels);
   };
   if constexpr (OVER) {
     for (int base = R * THREADS + tid; base < nvec; base += THREADS * kLpUnroll) {
@@ -755,14 +751,20 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
       }
 #pragma unroll
       for (int j = 0; j < kLpUnroll; ++j)
-        if (base + j * THREADS < nvec) gradient(base + j * THREADS, w[j]);
+        if (base + j * THREADS < nvec) gradient(base + j * THREADS, w[j], true);
     }
   }
   opaque(u);
+  // which of the thread's vectors hold a label: one look at the labels instead of one a vector
+  uint32_t hits = 0;
+  for (int l = 0; l < cnt; ++l) {
+    const int vi = (s_y[l] - head) / N;
+    if (s_y[l] >= head && vi % THREADS == tid) hits |= 1u << (vi / THREADS & 31);
+  }
 #pragma unroll
   for (int j = 0; j < R; ++j) {
     const int vi = j * THREADS + tid;
-    if (vi < nvec) gradient(vi, u[j]);
+    if (vi < nvec) gradient(vi, u[j], (hits >> j & 1) != 0);
   }
   if (EDGE && tid < n_extra) finish_extra(slope(fmaf(xe, kLog2e, -lse2)));
 }
