@@ -827,15 +827,17 @@ __device__ __forceinline__ void dq_sum_block(const CrossParams<T>& p, const Cros
 
 // Head size 128, bf16: eight waves; waves w and w + 4 own keys 32 (w % 4) .. +31 and take
 // the two 32-row halves of every 64-row step; K and V of the tile stay in LDS.
-// Head size 64 or fp32: four waves and 32-row steps, K and V in registers; with bf16 two
-// workgroups share a compute unit, and one's barriers pass under the other's products.
+// Head size 64 or fp32: four waves and 32-row steps, K and V in registers; with bf16 three
+// workgroups share a compute unit, and one's barriers pass under the others' products (three
+// for two: 162 -> 148 us on 24 rows of 14/2 heads, 280 -> 263 on long rows; a third stage of
+// the ring instead was slower).
 template <int D, typename T>
 struct KvShape {
   static constexpr bool HOLD = D * sizeof(T) != 256 || D == 64;
   static constexpr int QB = HOLD ? 1 : 2;  // row blocks a step
   static constexpr int STEP = kCrossStep(D, sizeof(T) == 4);
   static constexpr int WAVES = 4 * QB;
-  static constexpr int PER_CU = HOLD && sizeof(T) == 2 ? 2 : 1;
+  static constexpr int PER_CU = HOLD && sizeof(T) == 2 ? 3 : 1;
   static_assert(STEP == 32 * QB, "rows a step");
 };
 
