@@ -129,6 +129,36 @@ __device__ __forceinline__ void dma_rows(const TileDma<RD, NR>& d, T* lds_tile, 
   d.template issue<ONCE>(reinterpret_cast<__bf16*>(lds_tile), reinterpret_cast<const __bf16*>(src), rows_valid);
 }
 
+// A lane's 16 columns 8 r4 + 4 hf + 0..3 of a row's block of 32, times sc, or zeros.  As bf16
+// the wave's halves exchange groups of four first, so that a lane writes 16 bytes and the
+// two lanes of a row 32: half the requests of 8-byte stores (17 rows of 12/12 heads with one
+// to five states, the forward 52 -> 43 us, dQ 116 -> 107; dK and dV, few beside what their
+// walks read, gain nothing from it).
+template <typename T>
+__device__ __forceinline__ void store_block(T* dst, int hf, const f32x16& x, float sc, bool some) {
+  f32x4 v[4];
+#pragma unroll
+  for (int r4 = 0; r4 < 4; ++r4) {
+    v[r4] = f32x4{};
+    if (some) v[r4] = f32x4{x[4 * r4] * sc, x[4 * r4 + 1] * sc, x[4 * r4 + 2] * sc, x[4 * r4 + 3] * sc};
+  }
+  if constexpr (sizeof(T) == 2) {
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int r4 = 0; r4 < 4; r4 += 2) {
+      const u32x2 a = __builtin_bit_cast(u32x2, __builtin_convertvector(v[r4], bf16x4));
+      const u32x2 b = __builtin_bit_cast(u32x2, __builtin_convertvector(v[r4 + 1], bf16x4));
+      const auto x0 = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false);
+      const auto x1 = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
+      *reinterpret_cast<u32x4*>(dst + 8 * r4 + 8 * hf) = u32x4{x0[0], x1[0], x0[1], x1[1]};
+    }
+  } else {
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) store4<T>(dst + 8 * r4 + 4 * hf, v[r4]);
+  }
+}
+
 template <typename T>
 struct CrossParams {
   const T* q;
@@ -430,14 +460,7 @@ __global__ __launch_bounds__(kWaves * 64, (kFwdPerCu<D, T>)) void cross_fwd_kern
   const bool seen = w.hi > w.lo;
   const float inv = seen ? 1.f / l_tot : 0.f;
 #pragma unroll
-  for (int m = 0; m < D / 32; ++m)
-#pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      f32x4 v4 = f32x4{};
-      if (seen) v4 = f32x4{st.o[m][4 * r4] * inv, st.o[m][4 * r4 + 1] * inv, st.o[m][4 * r4 + 2] * inv,
-                           st.o[m][4 * r4 + 3] * inv};
-      store4<T>(p.o + qrow + 32 * m + 8 * r4 + 4 * hf, v4);
-    }
+  for (int m = 0; m < D / 32; ++m) store_block<T>(p.o + qrow + 32 * m, hf, st.o[m], inv, seen);
   if (hf == 0) p.lse[(int64_t)w.head * p.sumT + w.tok] = seen ? (st.m_ref + __log2f(l_tot)) * (1.0f / kLog2e) : 0.f;
 }
 
@@ -649,11 +672,32 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
   const WaveKeys wk = wave_keys<RANGES>(it, w, it.r0 + wave * 32);
   const int64_t qrow = ((int64_t)w.tok * p.hq + w.head) * D;
   Frag qf[D / 16], df[D / 16];
+  // Q, then dO, then O: eight loads pass over a row's two cache lines, which the first level
+  // keeps that long for one tensor, but not for two; the first keys are on their way behind
+  // them, ahead of delta (12 rows with 129 to 349 states 256 -> 240 us, 24 ragged rows of head
+  // size 64 87 -> 79)
 #pragma unroll
-  for (int c = 0; c < D / 16; ++c) {
-    qf[c] = w.live ? O::load(p.q + qrow + 16 * c + 8 * hf) : Frag{};
-    df[c] = w.live ? O::load(p.dout + qrow + 16 * c + 8 * hf) : Frag{};
-  }
+  for (int c = 0; c < D / 16; ++c) qf[c] = w.live ? O::load(p.q + qrow + 16 * c + 8 * hf) : Frag{};
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) df[c] = w.live ? O::load(p.dout + qrow + 16 * c + 8 * hf) : Frag{};
+  int key0, key1;
+  block_keys<RANGES, BN>(it, wk, wave, key0, key1);
+  const int n_tiles = (key1 - key0 + BN - 1) / BN;
+  const int64_t kv_stride = (int64_t)p.hkv * D;
+  const T* kbase = p.k + ((int64_t)it.e0 * p.hkv + g) * D;
+  const T* vbase = p.v + ((int64_t)it.e0 * p.hkv + g) * D;
+  Dma dma;
+  dma.init(wave * RPW, kv_stride * (sizeof(T) / 2), lane);
+  auto issue = [&](int t) {
+    const int k0 = key0 + t * BN;
+    const int rows = min(BN, it.elen - k0);
+    dma_rows(dma, sKV[t % kStages][0], kbase + k0 * kv_stride, rows);
+    dma_rows(dma, sKV[t % kStages][1], vbase + k0 * kv_stride, rows);
+  };
+#pragma unroll
+  for (int t = 0; t < kStages - 1; ++t)
+    if (t < n_tiles) issue(t);
+
   // delta = dO . O and -lse log2(e) of the lane's row, kept for the dK/dV pass
   float nlse2 = 0.f, dlt = 0.f;
   {
@@ -662,7 +706,9 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
         typedef T vec8 __attribute__((ext_vector_type(8)));
-        const vec8 a = *reinterpret_cast<const vec8*>(p.dout + qrow + 16 * c + 8 * hf);
+        vec8 a;
+        if constexpr (sizeof(T) == 2) a = df[c];
+        else a = *reinterpret_cast<const vec8*>(p.dout + qrow + 16 * c + 8 * hf);
         const vec8 b = *reinterpret_cast<const vec8*>(p.o_in + qrow + 16 * c + 8 * hf);
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc += (float)a[e] * (float)b[e];
@@ -691,24 +737,6 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
       if (lane == 0 && it.r0 + wave * 32 < it.live) p.ranges[it.blk0 + ((it.r0 + wave * 32) >> 5)] = rg;
     }
   }
-
-  int key0, key1;
-  block_keys<RANGES, BN>(it, wk, wave, key0, key1);
-  const int n_tiles = (key1 - key0 + BN - 1) / BN;
-  const int64_t kv_stride = (int64_t)p.hkv * D;
-  const T* kbase = p.k + ((int64_t)it.e0 * p.hkv + g) * D;
-  const T* vbase = p.v + ((int64_t)it.e0 * p.hkv + g) * D;
-  Dma dma;
-  dma.init(wave * RPW, kv_stride * (sizeof(T) / 2), lane);
-  auto issue = [&](int t) {
-    const int k0 = key0 + t * BN;
-    const int rows = min(BN, it.elen - k0);
-    dma_rows(dma, sKV[t % kStages][0], kbase + k0 * kv_stride, rows);
-    dma_rows(dma, sKV[t % kStages][1], vbase + k0 * kv_stride, rows);
-  };
-#pragma unroll
-  for (int t = 0; t < kStages - 1; ++t)
-    if (t < n_tiles) issue(t);
 
   f32x16 acc[D / 32];
 #pragma unroll
@@ -781,14 +809,7 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
   }
   const bool seen = w.hi > w.lo;
 #pragma unroll
-  for (int m = 0; m < D / 32; ++m)
-#pragma unroll
-    for (int r4 = 0; r4 < 4; ++r4) {
-      f32x4 v4 = f32x4{};
-      if (seen) v4 = f32x4{acc[m][4 * r4] * p.scale, acc[m][4 * r4 + 1] * p.scale, acc[m][4 * r4 + 2] * p.scale,
-                           acc[m][4 * r4 + 3] * p.scale};
-      store4<T>(p.o + qrow + 32 * m + 8 * r4 + 4 * hf, v4);
-    }
+  for (int m = 0; m < D / 32; ++m) store_block<T>(p.o + qrow + 32 * m, hf, acc[m], p.scale, seen);
 }
 
 // Adds the parts of dQ rows whose keys were split, in part order; block b of the splits'.
