@@ -693,8 +693,10 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
     if (labels) {
       for (int l = 0; l < cnt; ++l) {
         const int d = s_y[l] - (head + vi * N);
+        if ((unsigned)d < (unsigned)N) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) f[e] += (e == d) ? s_g[l] : 0.f;
+          for (int e = 0; e < N; ++e) f[e] += (e == d) ? s_g[l] : 0.f;
+        }
       }
     }
     store(vi, Pack16<T>::pack(f));
