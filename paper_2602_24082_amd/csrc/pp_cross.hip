@@ -52,7 +52,7 @@ struct Ops<__bf16> {
   static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, const f32x16& c) { return mfma32(a, b, c); }
   static __device__ __forceinline__ Frag from_acc(const f32x16& acc, int s) { return acc_half_to_bf16(acc, s); }
   template <int D>
-  static __device__ __forceinline__ Frag row8(const __bf16* tile, int r, int lc) {
+  static __device__ __forceinline__ Held row8(const __bf16* tile, int r, int lc) {
     return lds_row8<D>(tile, r, lc);
   }
   template <int D>
@@ -86,6 +86,7 @@ struct Ops<float> {
   static __device__ __forceinline__ Frag load(const float* p) { return split3(*reinterpret_cast<const f32x8*>(p)); }
   using Held = f32x8;  // whole: 64 registers of K and V at head size 128 instead of 96, split at each use
   static __device__ __forceinline__ Frag use(const Held& x) { return split3(x); }
+  static __device__ __forceinline__ const Frag& use(const Frag& x) { return x; }
   static __device__ __forceinline__ f32x16 mma(const Frag& a, const Frag& b, f32x16 c) {
     c = mfma32(a.l, b.h, c);
     c = mfma32(a.h, b.l, c);
@@ -101,11 +102,11 @@ struct Ops<float> {
     return split3(f);
   }
   template <int D>
-  static __device__ __forceinline__ Frag row8(const float* tile, int r, int lc) {
+  static __device__ __forceinline__ Held row8(const float* tile, int r, int lc) {
     const int sw = swz<2 * D>(r);
     const f32x4 a = *reinterpret_cast<const f32x4*>(tile + r * D + (((2 * lc) ^ sw) << 2));
     const f32x4 b = *reinterpret_cast<const f32x4*>(tile + r * D + (((2 * lc + 1) ^ sw) << 2));
-    return split3(f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]});
+    return f32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
   }
   // column col0 + l % 32 of the rows that from_acc's elements stand for
   template <int D>
@@ -120,6 +121,15 @@ struct Ops<float> {
     return split3(f);
   }
 };
+
+// A fragment read ahead of its products.  fp32 at head size 64 keeps it whole, which leaves two
+// workgroups of the forward and of dQ room on a compute unit (dQ 632 -> 505 us on 6 rows of
+// 16/4 heads); at head size 128, with one a unit, it is split at once (dQ 2355 us, whole 2452).
+template <int D, typename T>
+__device__ __forceinline__ auto ahead(const typename Ops<T>::Held& x) {
+  if constexpr (sizeof(T) == 4 && D == 128) return Ops<T>::use(x);
+  else return x;
+}
 
 // Wave-cooperative DMA of NR rows of D elements of T (see TileDma).
 template <typename T, int D, int NR>
@@ -324,9 +334,9 @@ constexpr int kKeys = sizeof(T) == 2 ? 64 : 32;
 constexpr int kStages = 2;
 constexpr int kWaves = 4;
 template <int D, typename T>
-constexpr int kFwdPerCu = sizeof(T) == 4 ? 1 : D == 64 ? 4 : 2;  // workgroups a compute unit
+constexpr int kFwdPerCu = sizeof(T) == 4 ? (D == 64 ? 2 : 1) : D == 64 ? 4 : 2;  // workgroups a compute unit
 template <int D, typename T>
-constexpr int kDqPerCu = sizeof(T) == 4 ? 1 : D == 64 ? 3 : 2;
+constexpr int kDqPerCu = sizeof(T) == 4 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : 2;
 static_assert(32 * kWaves == kCrossRows, "rows a workgroup");
 
 // The keys [t0, t1) that a workgroup of kWaves waves walks, from tile-aligned t0.
@@ -358,6 +368,7 @@ template <int D, typename T, bool RANGES, int N>
 __global__ __launch_bounds__(kWaves * 64, (kFwdPerCu<D, T>)) void cross_fwd_kernel(CrossParams<T> p, InlineItems<N> inl) {
   using O = Ops<T>;
   using Frag = typename O::Frag;
+  using Ahead = decltype(ahead<D, T>(typename O::Held{}));
   constexpr int BN = kKeys<T>, KB = BN / 32, RPW = BN / kWaves;
   using Dma = RowDma<T, D, RPW>;
   __shared__ __attribute__((aligned(1024))) T sKV[kStages][2][BN * D];
@@ -407,17 +418,18 @@ __global__ __launch_bounds__(kWaves * 64, (kFwdPerCu<D, T>)) void cross_fwd_kern
     // S^T = K Q^T: lane = row, registers = keys; K fragments read PD steps ahead
     f32x16 s[KB];
     {
-      constexpr int NC = D / 16, NI = KB * NC, PD = 3;
-      Frag a[PD + 1];
+      constexpr int NC = D / 16, NI = KB * NC, PD = sizeof(T) == 4 && D == 64 ? 1 : 3;
+      Ahead a[PD + 1];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) s[kb] = f32x16{};
 #pragma unroll
-      for (int n = 0; n < PD; ++n) a[n] = O::template row8<D>(sK, (n / NC) * 32 + ln, 2 * (n % NC) + hf);
+      for (int n = 0; n < PD; ++n) a[n] = ahead<D, T>(O::template row8<D>(sK, (n / NC) * 32 + ln, 2 * (n % NC) + hf));
 #pragma unroll
       for (int n = 0; n < NI; ++n) {
         if (n + PD < NI)
-          a[(n + PD) % (PD + 1)] = O::template row8<D>(sK, ((n + PD) / NC) * 32 + ln, 2 * ((n + PD) % NC) + hf);
-        s[n / NC] = O::mma(a[n % (PD + 1)], qf[n % NC], s[n / NC]);
+          a[(n + PD) % (PD + 1)] =
+              ahead<D, T>(O::template row8<D>(sK, ((n + PD) / NC) * 32 + ln, 2 * ((n + PD) % NC) + hf));
+        s[n / NC] = O::mma(O::use(a[n % (PD + 1)]), qf[n % NC], s[n / NC]);
       }
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -540,7 +552,7 @@ __global__ __launch_bounds__((kFewWaves<D, T> * 64), 1) void cross_few_kernel(Cr
     const T* sV = sm.kv[wave][i & 1][1];
     f32x16 s[1] = {f32x16{}};
 #pragma unroll
-    for (int c = 0; c < NC; ++c) s[0] = O::mma(O::template row8<D>(sK, ln, 2 * c + hf), qf[c], s[0]);
+    for (int c = 0; c < NC; ++c) s[0] = O::mma(O::use(O::template row8<D>(sK, ln, 2 * c + hf)), qf[c], s[0]);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K's reads have returned
     if (i + 2 < n) issue(i + 2, 0, kbase);
     if (!wk.every(k0, k0 + 32)) mask_keys<1>(s, k0, hf, w.lo, w.hi);
@@ -658,6 +670,7 @@ template <int D, typename T, bool RANGES>
 __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel(CrossParams<T> p) {
   using O = Ops<T>;
   using Frag = typename O::Frag;
+  using Ahead = decltype(ahead<D, T>(typename O::Held{}));
   constexpr int BN = kKeys<T>, KB = BN / 32, RPW = BN / kWaves;
   using Dma = RowDma<T, D, RPW>;
   __shared__ __attribute__((aligned(1024))) T sKV[kStages][2][BN * D];
@@ -754,9 +767,9 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
     {
       constexpr int NC = D / 16, NI = 2 * KB * NC, PD = 3;
       auto frag = [&](int n) {
-        return O::template row8<D>(((n / NC) & 1) ? sV : sK, (n / (2 * NC)) * 32 + ln, 2 * (n % NC) + hf);
+        return ahead<D, T>(O::template row8<D>(((n / NC) & 1) ? sV : sK, (n / (2 * NC)) * 32 + ln, 2 * (n % NC) + hf));
       };
-      Frag a[PD + 1];
+      Ahead a[PD + 1];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) {
         s[kb] = f32x16{};
@@ -768,8 +781,8 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
       for (int n = 0; n < NI; ++n) {
         if (n + PD < NI) a[(n + PD) % (PD + 1)] = frag(n + PD);
         const int kb = n / (2 * NC), c = n % NC;
-        if ((n / NC) & 1) dp[kb] = O::mma(a[n % (PD + 1)], df[c], dp[kb]);
-        else s[kb] = O::mma(a[n % (PD + 1)], qf[c], s[kb]);
+        if ((n / NC) & 1) dp[kb] = O::mma(O::use(a[n % (PD + 1)]), df[c], dp[kb]);
+        else s[kb] = O::mma(O::use(a[n % (PD + 1)]), qf[c], s[kb]);
       }
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -849,7 +862,7 @@ __device__ __forceinline__ void dq_sum_block(const CrossParams<T>& p, const Cros
 // Head size 128, bf16: eight waves; waves w and w + 4 own keys 32 (w % 4) .. +31 and take
 // the two 32-row halves of every 64-row step; K and V of the tile stay in LDS.
 // Head size 64 or fp32: four waves and 32-row steps, K and V in registers; with bf16 three
-// workgroups share a compute unit, and one's barriers pass under the others' products (three
+// (fp32 of head size 64 two) workgroups share a compute unit, and one's barriers pass under the others' products (three
 // for two: 162 -> 148 us on 24 rows of 14/2 heads, 280 -> 263 on long rows; a third stage of
 // the ring instead was slower).
 template <int D, typename T>
@@ -858,7 +871,7 @@ struct KvShape {
   static constexpr int QB = HOLD ? 1 : 2;  // row blocks a step
   static constexpr int STEP = kCrossStep(D, sizeof(T) == 4);
   static constexpr int WAVES = 4 * QB;
-  static constexpr int PER_CU = HOLD && sizeof(T) == 2 ? 3 : 1;
+  static constexpr int PER_CU = HOLD && sizeof(T) == 2 ? 3 : D == 64 ? 2 : 1;
   static_assert(STEP == 32 * QB, "rows a step");
 };
 
@@ -1033,7 +1046,7 @@ __global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), (KvShape<D, T>::PER_CU
     }
     {
       constexpr int NC = D / 16;
-      Frag fq[2], fk[2], fo[2], fv[2];
+      Held fq[2], fk[2], fo[2], fv[2];
       auto load = [&](int c, int b) {
         fq[b] = O::template row8<D>(sg.q, qb * 32 + ln, 2 * c + hf);
         if constexpr (!S::HOLD) fk[b] = O::template row8<D>(sm.k, kb * 32 + ln, 2 * c + hf);
@@ -1047,11 +1060,11 @@ __global__ __launch_bounds__((KvShape<D, T>::WAVES * 64), (KvShape<D, T>::PER_CU
         if constexpr (S::HOLD) {
           // counts as rewritten, or the split parts of all of K and V would be kept across steps
           if constexpr (sizeof(T) == 4 && D == 128) asm volatile("" : "+v"(kf[c]), "+v"(vf[c]));
-          s = O::mma(fq[c & 1], O::use(kf[c]), s);
-          dp = O::mma(fo[c & 1], O::use(vf[c]), dp);
+          s = O::mma(O::use(fq[c & 1]), O::use(kf[c]), s);
+          dp = O::mma(O::use(fo[c & 1]), O::use(vf[c]), dp);
         } else {
-          s = O::mma(fq[c & 1], fk[c & 1], s);
-          dp = O::mma(fo[c & 1], fv[c & 1], dp);
+          s = O::mma(O::use(fq[c & 1]), O::use(fk[c & 1]), s);
+          dp = O::mma(O::use(fo[c & 1]), O::use(fv[c & 1]), dp);
         }
       }
       if constexpr (sizeof(T) == 2) {

@@ -2347,8 +2347,8 @@ CrossCosts cross_costs(pp_dtype dtype, int d) {
   const double rows = join_us((double)kCrossRows * d), keys = join_us((double)kCrossKeys * d);  // two gradients, half of it under the walks
   if (dtype == PP_FP32) {
     if (d == 128)
-      return {{kUnits, 8.2, 8.2, 3.0, rows}, {kUnits, 11.1, 11.1, 3.0, rows}, {kUnits, 8.9, 8.9, 3.0, keys}};
-    return {{kUnits, 4.6, 4.6, 3.0, rows}, {kUnits, 6.0, 6.0, 3.0, rows}, {kUnits, 4.0, 4.0, 3.0, keys}};
+      return {{kUnits, 8.2, 8.2, 3.0, rows}, {kUnits, 11.1, 11.1, 3.0, rows}, {kUnits, 8.3, 8.3, 3.0, keys}};
+    return {{2 * kUnits, 8.9, 4.8, 3.0, rows}, {2 * kUnits, 9.6, 5.4, 3.0, rows}, {2 * kUnits, 7.4, 4.1, 3.0, keys}};
   }
   if (d == 128)
     return {{2 * kUnits, 2.3, 1.35, 3.0, rows}, {2 * kUnits, 3.1, 1.75, 3.0, rows}, {kUnits, 1.9, 1.65, 3.0, keys}};
