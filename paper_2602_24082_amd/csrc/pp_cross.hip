@@ -711,8 +711,21 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
   for (int t = 0; t < kStages - 1; ++t)
     if (t < n_tiles) issue(t);
 
-  // delta = dO . O and -lse log2(e) of the lane's row, kept for the dK/dV pass
+  // delta = dO . O and -lse log2(e) of the lane's row, kept for the dK/dV pass.  O as stored is
+  // rounded to bf16, and where a row sees two or three keys dP - delta is small beside delta:
+  // a row whose keys lie in one tile (a bit of `single`) gets delta = sum P dP there, which costs
+  // short walks 2% and halves the error of dQ and dK (0.0037 to 0.002 relative at about two keys).
   float nlse2 = 0.f, dlt = 0.f;
+  uint64_t single = 0;
+  auto stat = [&] { return (int64_t)g * p.sumT * p.G + (int64_t)it.tok0 * p.G + (it.r0 + wave * 32 + (threadIdx.x & 31)); };
+  if constexpr (sizeof(T) == 2) {
+    int lo = 0, hi = it.elen;
+    if (RANGES && w.live) {
+      lo = max(0, p.kbeg[w.tok]);
+      hi = min(hi, p.kend[w.tok]);
+    }
+    single = __ballot(w.live && hi > lo && lo / BN == (hi - 1) / BN);
+  }
   {
     float acc = 0.f;
     if (w.live) {
@@ -731,9 +744,8 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
     dlt = half_swap_sum(acc);
     if (it.k_begin == 0) {  // the first part, if the keys are split
       if (w.live && hf == 0) {
-        const int64_t at = (int64_t)g * p.sumT * p.G + (int64_t)it.tok0 * p.G + r;
-        p.ndelta[at] = -dlt;
-        p.nlse2[at] = nlse2;
+        if (!(single >> lane & 1)) p.ndelta[stat()] = -dlt;
+        p.nlse2[stat()] = nlse2;
       }
     }
   }
@@ -798,7 +810,26 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) dp[kb][e] = fast_exp2(fmaf(s[kb][e], p.scale_log2, nlse2)) * (dp[kb][e] - dlt);
+      for (int e = 0; e < 16; ++e) s[kb][e] = fast_exp2(fmaf(s[kb][e], p.scale_log2, nlse2));
+    if constexpr (sizeof(T) == 2) {
+      const bool here = (single >> lane & 1) && w.hi > w.lo && (unsigned)(w.lo - k0) < (unsigned)BN;
+      if (single && wave_any(here)) {
+        float sum = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) sum = fmaf(s[kb][e], dp[kb][e], sum);
+        sum = half_swap_sum(sum);
+        if (here) {
+          dlt = sum;
+          if (hf == 0) p.ndelta[stat()] = -sum;
+        }
+      }
+    }
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) dp[kb][e] = s[kb][e] * (dp[kb][e] - dlt);
     // dQ^T += K^T dS^T over 16-key chunks
 #pragma unroll
     for (int ch = 0; ch < 2 * KB; ++ch) {
