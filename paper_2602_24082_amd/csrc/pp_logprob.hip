@@ -594,41 +594,16 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
     else over = stream_max_sum<T, THREADS>(xv, R * THREADS, nvec, n_extra > 0);
   }
   // logsumexp of the row from the registers
-  float m = kNegInf;
-  // ENT: instead of its values' maximum a thread takes that of its wave's first vectors.
-  // What exceeds it by more than fp32's exponents go makes the sum infinite, and the row
-  // is summed again.  A wave whose first vectors are masked looks at all.
-  bool look = true;
-  if constexpr (ENT) {
-    if (tid < nvec) {
+  float m = kNegInf, s = 0.f, t = 0.f;
+  auto vec_max = [&](int j) {
+    if (j * THREADS + tid < nvec) {
       float f[N];
-      Vec16<T>::unpack(u[0], f);
+      Vec16<T>::unpack(u[j], f);
 #pragma unroll
       for (int e = 0; e < N; ++e) m = max_or_nan(m, f[e]);
     }
-    for (int off = 32; off > 0; off >>= 1) m = max_or_nan(m, __shfl_xor(m, off, 64));
-    look = __builtin_amdgcn_readfirstlane(m <= -1e30f) != 0;
-  }
-  if (look) {
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-      if (j * THREADS + tid < nvec) {
-        float f[N];
-        Vec16<T>::unpack(u[j], f);
-#pragma unroll
-        for (int e = 0; e < N; ++e) m = max_or_nan(m, f[e]);
-      }
-    }
-    if constexpr (ENT) {
-      for (int off = 32; off > 0; off >>= 1) m = max_or_nan(m, __shfl_xor(m, off, 64));
-    }
-  }
-  // the packed vectors count as rewritten here, so each pass below unpacks
-  // them again instead of keeping the whole row live as floats
-  opaque(u);
-  float s = 0.f, t = 0.f;
-  if (m != kNegInf) {
-    const float ml = ENT ? base2(m) : m * kLog2e;
+  };
+  auto sums = [&](float ml) {
 #pragma unroll
     for (int j = 0; j < R; ++j) {
       if (j * THREADS + tid < nvec) {
@@ -641,7 +616,38 @@ __global__ __launch_bounds__(THREADS, R <= 8 ? 8 : 4) void logprob_bwd_kernel(Lo
         }
       }
     }
-    if constexpr (EDGE && !ENT) s = exact_base(s, m, ml, n_extra > 0);
+  };
+  if constexpr (ENT) {
+    // A wave first sums relative to the maximum of its threads' first vectors.  That is as good
+    // as its values' maximum while no value lies far above it: a lane whose sum passes
+    // kMostFirst (11 nats; the rounding of t and of ln s grows with the exponents, and from 84
+    // nats on t overflows), or first vectors that are all -inf, and the wave sums again from the
+    // maximum of all its values.  Looking at all of them at once takes 152064-entry rows 7% more;
+    // summing again costs them 3% for one peak a row (336 us instead of 324) and 15% where
+    // finite masks cover every wave's first vectors (410 us).
+    constexpr float kMostFirst = 65536.f;
+    vec_max(0);
+#pragma unroll 1
+    for (bool all = false;; all = true) {
+      for (int off = 32; off > 0; off >>= 1) m = max_or_nan(m, __shfl_xor(m, off, 64));
+      // the packed vectors count as rewritten here, so each pass unpacks them again
+      // instead of keeping the whole row live as floats
+      opaque(u);
+      s = t = 0.f;
+      if (m != kNegInf) sums(base2(m));
+      if (all || !wave_any(m == kNegInf || !(s <= kMostFirst))) break;
+#pragma unroll
+      for (int j = 0; j < R; ++j) vec_max(j);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < R; ++j) vec_max(j);
+    opaque(u);  // as above
+    if (m != kNegInf) {
+      const float ml = m * kLog2e;
+      sums(ml);
+      if constexpr (EDGE) s = exact_base(s, m, ml, n_extra > 0);
+    }
   }
   RowLse lse;
   RowEnt row;
