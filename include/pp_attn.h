@@ -511,8 +511,8 @@ typedef struct pp_policy_config {
  *   counts dev int32 [2] or NULL: counted tokens, and those that a clip holds
  *   dlogp, dentropy  dev float [sumT] or NULL: the loss's gradients, all of them
  *     written (0 off the counted tokens); a clipped token's gradient is its KL's.
- * Terms are formed in fp32, which side of a clip a ratio lies on and all sums in
- * 64 bits.  Without a counted token the loss is 0.
+ * Terms and sums are formed in 64 bits, the results rounded once.  Without a
+ * counted token the loss is 0.
  * ws_bytes >= pp_policy_workspace_size's bytes.  Float and int32 arrays must be
  * 4-byte aligned. */
 pp_status pp_policy_workspace_size(const pp_pack_desc* desc, size_t* bytes);
