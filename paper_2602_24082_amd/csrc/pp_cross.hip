@@ -214,6 +214,7 @@ struct RowOf {
   bool in_tile, live;
   int tok, head;  // flat token, query head
   int lo, hi;     // visible keys of the item's part
+  int all_lo, all_hi;  // and of all the states, if any
 };
 
 template <bool RANGES, typename P>
@@ -226,9 +227,14 @@ __device__ __forceinline__ RowOf row_of(const P& p, const CrossItem& it, int g, 
   w.head = g * p.G + (r - i * p.G);
   w.lo = it.k_begin;
   w.hi = w.live ? it.k_end : it.k_begin;
+  w.all_lo = 0;
+  w.all_hi = w.live ? it.elen : 0;
   if (RANGES && w.live) {
-    w.lo = max(w.lo, p.kbeg[w.tok]);
-    w.hi = min(w.hi, p.kend[w.tok]);
+    const int lo = p.kbeg[w.tok], hi = p.kend[w.tok];
+    w.lo = max(w.lo, lo);
+    w.hi = min(w.hi, hi);
+    w.all_lo = max(0, lo);
+    w.all_hi = min(it.elen, hi);
   }
   if (w.hi <= w.lo) w.lo = w.hi = it.k_begin;
   return w;
@@ -339,29 +345,47 @@ template <int D, typename T>
 constexpr int kDqPerCu = sizeof(T) == 4 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : 2;
 static_assert(32 * kWaves == kCrossRows, "rows a workgroup");
 
-// The keys [t0, t1) that a workgroup of kWaves waves walks, from tile-aligned t0.
-template <bool RANGES, int BN>
-__device__ __forceinline__ void block_keys(const CrossItem& it, const WaveKeys& wk, int wave, int& t0, int& t1) {
-  t0 = it.k_begin;
-  t1 = it.k_end;
-  if constexpr (RANGES) {
-    __shared__ int s_lo[kWaves], s_hi[kWaves];
-    if ((threadIdx.x & 63) == 0) {
-      s_lo[wave] = wk.any_lo;
-      s_hi[wave] = wk.any_hi;
+// A range of keys, from tile-aligned t0 on; none: t1 = t0 = 0.
+struct TileKeys {
+  int t0, t1;
+};
+
+// What the kWaves waves of a workgroup need together of N ranges that each has: lo[i] <
+// hi[i], or no key of it.
+template <int N, int BN>
+__device__ __forceinline__ void block_join(const int (&lo)[N], const int (&hi)[N], int wave, TileKeys (&out)[N]) {
+  __shared__ int s_lo[N][kWaves], s_hi[N][kWaves];
+  if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      s_lo[i][wave] = lo[i];
+      s_hi[i][wave] = hi[i];
     }
-    __syncthreads();
-    int lo = s_lo[0], hi = s_hi[0];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    int l = s_lo[i][0], h = s_hi[i][0];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) {
-      lo = min(lo, s_lo[w]);
-      hi = max(hi, s_hi[w]);
+      l = min(l, s_lo[i][w]);
+      h = max(h, s_hi[i][w]);
     }
-    lo = __builtin_amdgcn_readfirstlane(lo);
-    hi = __builtin_amdgcn_readfirstlane(hi);
-    t0 = hi > lo ? lo / BN * BN : 0;
-    t1 = hi > lo ? hi : 0;
+    l = __builtin_amdgcn_readfirstlane(l);
+    h = __builtin_amdgcn_readfirstlane(h);
+    out[i] = h > l ? TileKeys{l / BN * BN, h} : TileKeys{0, 0};
   }
+}
+
+// The keys that a workgroup walks.
+template <bool RANGES, int BN>
+__device__ __forceinline__ TileKeys block_keys(const CrossItem& it, const WaveKeys& wk, int wave) {
+  TileKeys t[1] = {{it.k_begin, it.k_end}};
+  if constexpr (RANGES) {
+    const int lo[1] = {wk.any_lo}, hi[1] = {wk.any_hi};
+    block_join<1, BN>(lo, hi, wave, t);
+  }
+  return t[0];
 }
 
 template <int D, typename T, bool RANGES, int N>
@@ -386,9 +410,8 @@ __global__ __launch_bounds__(kWaves * 64, (kFwdPerCu<D, T>)) void cross_fwd_kern
   for (int c = 0; c < D / 16; ++c)
     qf[c] = w.live ? O::load(p.q + qrow + 16 * c + 8 * hf) : Frag{};
 
-  int key0, key1;
-  block_keys<RANGES, BN>(it, wk, wave, key0, key1);
-  const int n_tiles = (key1 - key0 + BN - 1) / BN;
+  const TileKeys tk = block_keys<RANGES, BN>(it, wk, wave);
+  const int key0 = tk.t0, n_tiles = (tk.t1 - tk.t0 + BN - 1) / BN;
   const int64_t kv_stride = (int64_t)p.hkv * D;
   const T* kbase = p.k + ((int64_t)it.e0 * p.hkv + g) * D;
   const T* vbase = p.v + ((int64_t)it.e0 * p.hkv + g) * D;
@@ -693,39 +716,114 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
   for (int c = 0; c < D / 16; ++c) qf[c] = w.live ? O::load(p.q + qrow + 16 * c + 8 * hf) : Frag{};
 #pragma unroll
   for (int c = 0; c < D / 16; ++c) df[c] = w.live ? O::load(p.dout + qrow + 16 * c + 8 * hf) : Frag{};
-  int key0, key1;
-  block_keys<RANGES, BN>(it, wk, wave, key0, key1);
-  const int n_tiles = (key1 - key0 + BN - 1) / BN;
+  // delta = dO . O and -lse log2(e) of the lane's row, kept for the dK/dV pass.  O as stored is
+  // rounded to bf16, and where a row sees few keys dP - delta is small beside delta: a row of at
+  // most BN keys gets delta = sum P dP.  Where they lie in one tile (a bit of `single`) that is
+  // formed in the tile's step; where they lie across a border (`two`) the workgroup goes over
+  // those tiles once before its walk.  dQ and dK at about two keys are off by 0.0024 of them
+  // instead of 0.0037.  It costs short walks 2%, the backward of texts whose images of 64 states
+  // start off the borders 7% (221 us for 206 on 8 rows of 32/8 heads of 128), others nothing.
+  float dlt = 0.f;
+  uint64_t single = 0, two = 0;
+  auto stat = [&] { return (int64_t)g * p.sumT * p.G + (int64_t)it.tok0 * p.G + (it.r0 + wave * 32 + (threadIdx.x & 31)); };
+  if constexpr (sizeof(T) == 2) {
+    const bool few = w.all_hi > w.all_lo && w.all_hi - w.all_lo <= BN;
+    single = __ballot(few && w.all_lo / BN == (w.all_hi - 1) / BN);
+    two = RANGES ? __ballot(few) & ~single : 0;
+  }
   const int64_t kv_stride = (int64_t)p.hkv * D;
   const T* kbase = p.k + ((int64_t)it.e0 * p.hkv + g) * D;
   const T* vbase = p.v + ((int64_t)it.e0 * p.hkv + g) * D;
   Dma dma;
   dma.init(wave * RPW, kv_stride * (sizeof(T) / 2), lane);
-  auto issue = [&](int t) {
-    const int k0 = key0 + t * BN;
+  auto issue = [&](int k0, int t) {
     const int rows = min(BN, it.elen - k0);
     dma_rows(dma, sKV[t % kStages][0], kbase + k0 * kv_stride, rows);
     dma_rows(dma, sKV[t % kStages][1], vbase + k0 * kv_stride, rows);
   };
+  // S^T = K Q^T and dP^T = V dO^T of a tile, fragments read PD ahead
+  auto products = [&](const T* sK, const T* sV, f32x16 (&s)[KB], f32x16 (&dp)[KB]) {
+    constexpr int NC = D / 16, NI = 2 * KB * NC, PD = 3;
+    auto frag = [&](int n) {
+      return ahead<D, T>(O::template row8<D>(((n / NC) & 1) ? sV : sK, (n / (2 * NC)) * 32 + ln, 2 * (n % NC) + hf));
+    };
+    Ahead a[PD + 1];
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      s[kb] = f32x16{};
+      dp[kb] = f32x16{};
+    }
+#pragma unroll
+    for (int n = 0; n < PD; ++n) a[n] = frag(n);
+#pragma unroll
+    for (int n = 0; n < NI; ++n) {
+      if (n + PD < NI) a[(n + PD) % (PD + 1)] = frag(n + PD);
+      const int kb = n / (2 * NC), c = n % NC;
+      if ((n / NC) & 1) dp[kb] = O::mma(O::use(a[n % (PD + 1)]), df[c], dp[kb]);
+      else s[kb] = O::mma(O::use(a[n % (PD + 1)]), qf[c], s[kb]);
+    }
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (int n = 0; n < PD; ++n) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+#pragma unroll
+      for (int n = 0; n < NI; ++n) {
+        if (n + PD < NI) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+      }
+    }
+  };
+  auto sum_products = [&](const f32x16 (&s)[KB], const f32x16 (&dp)[KB]) {
+    float sum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sum = fmaf(s[kb][e], dp[kb][e], sum);
+    return sum;
+  };
+
+  TileKeys tk;
+  if constexpr (RANGES && sizeof(T) == 2) {
+    // rows of `two` with keys in this part; their tiles may lie in the next or the last one,
+    // and every part that has a row's keys sums the same numbers in the same order
+    const bool mine = (two >> lane & 1) && w.hi > w.lo;
+    const int lo[2] = {wk.any_lo, wave_min_i(mine ? w.all_lo : 0x7fffffff)}, hi[2] = {wk.any_hi, wave_max_i(mine ? w.all_hi : 0)};
+    TileKeys t[2];
+    block_join<2, BN>(lo, hi, wave, t);
+    tk = t[0];
+    const int n_ahead = (t[1].t1 - t[1].t0 + BN - 1) / BN;
+    if (n_ahead > 0) {
+      const float nl = mine ? -p.lse_in[(int64_t)w.head * p.sumT + w.tok] * kLog2e : 0.f;
+      float sum = 0.f;
+      issue(t[1].t0, 0);
+#pragma unroll 1
+      for (int i = 0; i < n_ahead; ++i) {
+        const int k0 = t[1].t0 + i * BN;
+        wait_vmem<0>();
+        __syncthreads();
+        if (i + 1 < n_ahead) issue(k0 + BN, i + 1);
+        if (k0 + BN <= lo[1] || k0 >= hi[1]) continue;
+        f32x16 s[KB], dp[KB];
+        products(sKV[i % kStages][0], sKV[i % kStages][1], s, dp);
+        mask_keys<KB>(s, k0, hf, mine ? w.all_lo : 0, mine ? w.all_hi : 0);
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) s[kb][e] = fast_exp2(fmaf(s[kb][e], p.scale_log2, nl));
+        sum += sum_products(s, dp);
+      }
+      dlt = half_swap_sum(sum);
+      if (mine && hf == 0 && w.all_lo == w.lo) p.ndelta[stat()] = -dlt;  // the part of its first key writes
+      __syncthreads();  // the stages are free
+    }
+  } else {
+    tk = block_keys<RANGES, BN>(it, wk, wave);
+  }
+  const int key0 = tk.t0, n_tiles = (tk.t1 - tk.t0 + BN - 1) / BN;
 #pragma unroll
   for (int t = 0; t < kStages - 1; ++t)
-    if (t < n_tiles) issue(t);
+    if (t < n_tiles) issue(key0 + t * BN, t);
 
-  // delta = dO . O and -lse log2(e) of the lane's row, kept for the dK/dV pass.  O as stored is
-  // rounded to bf16, and where a row sees two or three keys dP - delta is small beside delta:
-  // a row whose keys lie in one tile (a bit of `single`) gets delta = sum P dP there.  It costs
-  // short walks 2%, and dQ and dK at about two keys are off by 0.0024 of them instead of 0.0037.
-  float nlse2 = 0.f, dlt = 0.f;
-  uint64_t single = 0;
-  auto stat = [&] { return (int64_t)g * p.sumT * p.G + (int64_t)it.tok0 * p.G + (it.r0 + wave * 32 + (threadIdx.x & 31)); };
-  if constexpr (sizeof(T) == 2) {
-    int lo = 0, hi = it.elen;
-    if (RANGES && w.live) {
-      lo = max(0, p.kbeg[w.tok]);
-      hi = min(hi, p.kend[w.tok]);
-    }
-    single = __ballot(w.live && hi > lo && lo / BN == (hi - 1) / BN);
-  }
+  float nlse2 = 0.f;
   {
     float acc = 0.f;
     if (w.live) {
@@ -741,22 +839,18 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
       }
       nlse2 = -p.lse_in[(int64_t)w.head * p.sumT + w.tok] * kLog2e;
     }
-    dlt = half_swap_sum(acc);
+    acc = half_swap_sum(acc);
+    if (!(two >> lane & 1)) dlt = acc;
     if (it.k_begin == 0) {  // the first part, if the keys are split
       if (w.live && hf == 0) {
-        if (!(single >> lane & 1)) p.ndelta[stat()] = -dlt;
+        if (!((single | two) >> lane & 1)) p.ndelta[stat()] = -dlt;
         p.nlse2[stat()] = nlse2;
       }
     }
   }
   if constexpr (RANGES) {
     if (it.k_begin == 0 && g == 0) {
-      int lo = 0, hi = 0;
-      if (w.live) {
-        lo = max(0, p.kbeg[w.tok]);
-        hi = min(it.elen, p.kend[w.tok]);
-        if (hi <= lo) lo = hi = 0;
-      }
+      const int lo = w.all_hi > w.all_lo ? w.all_lo : 0, hi = w.all_hi > w.all_lo ? w.all_hi : 0;
       const CrossRange rg = {wave_min_i(hi > lo ? lo : 0x7fffffff), wave_max_i(hi > lo ? hi : 0), wave_max_i(w.live ? lo : 0),
                              wave_min_i(w.live ? hi : 0x7fffffff)};
       if (lane == 0 && it.r0 + wave * 32 < it.live) p.ranges[it.blk0 + ((it.r0 + wave * 32) >> 5)] = rg;
@@ -770,42 +864,12 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
     const int k0 = key0 + t * BN;
     wait_tile<kStages, 2 * Dma::N>(t, n_tiles);
     __syncthreads();
-    if (t + kStages - 1 < n_tiles) issue(t + kStages - 1);
+    if (t + kStages - 1 < n_tiles) issue(k0 + (kStages - 1) * BN, t + kStages - 1);
     if (wk.none(k0, k0 + BN)) continue;
     const T* sK = sKV[t % kStages][0];
     const T* sV = sKV[t % kStages][1];
-    // S^T = K Q^T and dP^T = V dO^T, fragments read PD ahead
     f32x16 s[KB], dp[KB];
-    {
-      constexpr int NC = D / 16, NI = 2 * KB * NC, PD = 3;
-      auto frag = [&](int n) {
-        return ahead<D, T>(O::template row8<D>(((n / NC) & 1) ? sV : sK, (n / (2 * NC)) * 32 + ln, 2 * (n % NC) + hf));
-      };
-      Ahead a[PD + 1];
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        s[kb] = f32x16{};
-        dp[kb] = f32x16{};
-      }
-#pragma unroll
-      for (int n = 0; n < PD; ++n) a[n] = frag(n);
-#pragma unroll
-      for (int n = 0; n < NI; ++n) {
-        if (n + PD < NI) a[(n + PD) % (PD + 1)] = frag(n + PD);
-        const int kb = n / (2 * NC), c = n % NC;
-        if ((n / NC) & 1) dp[kb] = O::mma(O::use(a[n % (PD + 1)]), df[c], dp[kb]);
-        else s[kb] = O::mma(O::use(a[n % (PD + 1)]), qf[c], s[kb]);
-      }
-      if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int n = 0; n < PD; ++n) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
-#pragma unroll
-        for (int n = 0; n < NI; ++n) {
-          if (n + PD < NI) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
-        }
-      }
-    }
+    products(sK, sV, s, dp);
     if (!wk.every(k0, k0 + BN)) mask_keys<KB>(s, k0, hf, w.lo, w.hi);
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
@@ -814,12 +878,7 @@ __global__ __launch_bounds__(kWaves * 64, (kDqPerCu<D, T>)) void cross_dq_kernel
     if constexpr (sizeof(T) == 2) {
       const bool here = (single >> lane & 1) && w.hi > w.lo && (unsigned)(w.lo - k0) < (unsigned)BN;
       if (single && wave_any(here)) {
-        float sum = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) sum = fmaf(s[kb][e], dp[kb][e], sum);
-        sum = half_swap_sum(sum);
+        const float sum = half_swap_sum(sum_products(s, dp));
         if (here) {
           dlt = sum;
           if (hf == 0) p.ndelta[stat()] = -sum;
