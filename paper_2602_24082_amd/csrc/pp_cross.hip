@@ -954,7 +954,8 @@ __device__ __forceinline__ void dq_sum_block(const CrossParams<T>& p, const Cros
 // Head size 64 or fp32: four waves and 32-row steps, K and V in registers; with bf16 three
 // (fp32 of head size 64 two) workgroups share a compute unit, and one's barriers pass under the others' products (three
 // for two: 162 -> 148 us on 24 rows of 14/2 heads, 280 -> 263 on long rows; a third stage of
-// the ring instead was slower).
+// the ring instead was slower).  Two workgroups of fp32 at head size 64 leave 30 registers to
+// memory, which the steps reload, and are faster all the same (810 -> 745 us on 6 rows of 16/4 heads).
 template <int D, typename T>
 struct KvShape {
   static constexpr bool HOLD = D * sizeof(T) != 256 || D == 64;
