@@ -24,6 +24,10 @@
  *                   and an entropy term, and its gradient
  *   pp_cross_attn_fwd, pp_cross_attn_bwd
  *                   attention of packed rows to an encoder's states
+ *   pp_cache_*      paged cache of keys and values, whose prompt pages the K responses
+ *                   of a group share while they are sampled
+ *   pp_tree_attn_fwd  attention of new tokens (one a sequence, or a drafted tree) over it
+ *   pp_verify_draft verification of drafted tokens, or plain sampling, from given numbers
  *   pp_plan_create, pp_attn_fwd_planned, pp_attn_bwd_planned
  *                   the same attention on a plan built once per packed batch
  *                   and reused (e.g. by every layer of a model)
@@ -520,6 +524,143 @@ pp_status pp_policy_loss(const pp_pack_desc* desc, const pp_policy_config* cfg, 
                          const float* logp_ref, const float* entropy, const float* adv, int adv_per_token, const uint8_t* mask,
                          float* loss, float* stats, int32_t* counts, float* dlogp, float* dentropy, void* ws, size_t ws_bytes,
                          void* hip_stream);
+
+/* Paged cache: the keys and values of sequences that are being sampled, such as the K
+ * responses to a prompt that a packed row will hold.  All of it is the caller's
+ * device memory, and every call works on it in stream order, so that a sampling
+ * loop needs no copy to the host and can be captured.
+ *
+ * A slot is a sequence: it lists held[s] pages in its row of page_table and has
+ * seq_len[s] tokens; token t lies in page page_table[s][t / page_size], row
+ * t % page_size.  refs[p] counts how often page p is listed; a page with refs 0 is
+ * free.  An empty cache is all zeros.  Pages are taken lowest number first, in the
+ * order of a call's entries and of their pages.
+ * Keys and values lie in pools k_pages, v_pages [layers, num_pages, hkv, page_size,
+ * head_dim] (bf16 or fp32); the attention and pp_cache_append take one layer's.
+ * page_size is 16, 32, 64, 128 or 256.
+ * Entries of slots below 0 are left out.  A slot named twice in a call counts once,
+ * by its first entry, in reserve, fork (as dst), free and accept; in append it may
+ * stand once.  What the arrays on the device say is checked on the device: an entry
+ * that names no slot, or whose lengths and pages do not belong together, is
+ * refused, which leaves its sequence as it was.  Workspace: pp_cache_workspace_size. */
+typedef struct pp_cache {
+  int32_t num_slots, max_pages;  /* rows and columns of page_table */
+  int32_t num_pages, page_size;
+  int32_t* page_table;           /* dev [num_slots, max_pages] */
+  int32_t* seq_len;              /* dev [num_slots] */
+  int32_t* held;                 /* dev [num_slots] */
+  int32_t* refs;                 /* dev [num_pages] */
+} pp_cache;
+
+/* Bytes for the calls below that take ws, with n entries or fewer. */
+pp_status pp_cache_workspace_size(const pp_cache* cache, int n, size_t* bytes);
+
+/* Room for add[i] (dev) more tokens in slots[i] (dev, [n]): pages up to
+ * ceil((seq_len + add) / page_size).  status (dev int32 [2]): pages that are missing
+ * (then nothing has changed, else 0), and entries refused (also those that would
+ * need more than max_pages). */
+pp_status pp_cache_reserve(const pp_cache* cache, int n, const int32_t* slots, const int32_t* add, int32_t* status, void* ws,
+                           size_t ws_bytes, void* hip_stream);
+
+/* Makes dst[i] (dev, an empty slot) a copy of src[i] (dev): it lists the same whole
+ * pages; a last page that is not full is copied, its rows in use in every layer.
+ * One source may be forked many times in a call; the state ahead of the call
+ * counts.  status as for reserve. */
+pp_status pp_cache_fork(const pp_cache* cache, int n, const int32_t* src, const int32_t* dst, pp_dtype dtype, int layers, int hkv,
+                        int head_dim, void* k_pages, void* v_pages, int32_t* status, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Empties slots: their pages lose a reference each. */
+pp_status pp_cache_free(const pp_cache* cache, int n, const int32_t* slots, void* hip_stream);
+
+/* Moves pages so that the live ones are the first *live (dev) of the pool, for a pool
+ * that shrinks or lends its end: with L live pages the i-th live page at L or above goes
+ * to the i-th free one below L, all rows of it, and tables follow. */
+pp_status pp_cache_compact(const pp_cache* cache, pp_dtype dtype, int layers, int hkv, int head_dim, void* k_pages, void* v_pages,
+                           int32_t* live, void* ws, size_t ws_bytes, void* hip_stream);
+
+/* shared[g] (dev): leading pages that all sequences slots[g * group ..] (dev) list
+ * alike and have filled, for pp_tree_attn_fwd; 0 for a group of one. */
+pp_status pp_cache_shared(const pp_cache* cache, int n, const int32_t* slots, int group, int32_t* shared, void* hip_stream);
+
+/* Writes one layer's keys and values of new tokens behind the sequences' cached ones:
+ * token j < count[i] (dev; NULL: max_new) of slots[i] at place seq_len + j, which has to
+ * have been reserved (a token without a page is not written); seq_len stays.
+ * Its row in k, v (dev [rows, hkv, head_dim]) and q is start[i] + j (dev; a packed
+ * batch's row_start, say), or i * max_new + j without start.
+ * With rope_base > 0 keys, and queries if given, are rotated as by pp_rope, at
+ * position seq_len + (nodes between the token and the tree's root): parents (dev
+ * [n, max_new], max_new <= 64) gives every node's parent, an earlier node or -1 for
+ * the root; NULL: token j follows j - 1.  q_rot (dev [rows, hq, head_dim]) may be q;
+ * without start its rows that hold no token are written as 0. */
+pp_status pp_cache_append(const pp_cache* cache, int n, const int32_t* slots, int max_new, const int32_t* count, const int32_t* start,
+                          int64_t rows, const int32_t* parents, pp_dtype dtype, int hq, int hkv, int head_dim, float rope_base,
+                          const void* q, const void* k, const void* v, void* q_rot, void* k_pages, void* v_pages, void* hip_stream);
+
+/* Keeps count[i] (dev) of the tokens that were appended to slots[i]: those at path[i][j]
+ * (dev [n, max_new], ascending; pp_verify_draft's), which move to the places
+ * seq_len + j in every layer, or the first count[i] where path is NULL; seq_len grows by
+ * count[i].  Pages stay reserved.  status (dev int32 [2]): 0, and entries refused (a
+ * path that does not ascend, or leaves max_new or the reserved pages). */
+pp_status pp_cache_accept(const pp_cache* cache, int n, const int32_t* slots, int max_new, const int32_t* count, const int32_t* path,
+                          pp_dtype dtype, int layers, int hkv, int head_dim, void* k_pages, void* v_pages, int32_t* status, void* ws,
+                          size_t ws_bytes, void* hip_stream);
+
+/* Attention of new tokens over the cache: max_new (<= 64) nodes of each of n (<= 2048)
+ * sequences, count[i] (dev; NULL: all) of them in use, appended with pp_cache_append.
+ * Node i of a sequence sees the sequence's seq_len cached tokens and the nodes on its
+ * path to the root, itself included; parents as there (a single token: max_new 1, a
+ * draft without branches: NULL).  With P the softmax of scale q k over them, o = P v and
+ * lse is the natural log of the softmax denominator; nodes not in use get 0.
+ *   q, o dev [n, max_new, hq, head_dim], lse dev float [hq, n * max_new]; head_dim 64
+ *   or 128; q-head h reads kv-head h / (hq / hkv); scale <= 0 means 1/sqrt(head_dim).
+ * group, shared: sequences g * group .. + group - 1 list the same first shared[g] (dev
+ * [n / group]; pp_cache_shared's) pages, whose keys are then read once for all of
+ * them; NULL: nothing is shared.  More than whole pages of the shortest count as those.
+ * PP_BF16: probabilities are rounded to bf16 for the second product, sums are fp32;
+ * PP_FP32: as exact as fp32 products (as pp_cross_attn_fwd, also where infinities and
+ * NaN are concerned: a node that is not finite may reach the other nodes of its
+ * sequence).  A sequence that names no slot, or whose nodes have not all been reserved,
+ * and a node with a parent that is no earlier one, come out as NaN.
+ * planned != 0: ws holds the plan of an earlier call with the same cache state and
+ * arguments but q, the pools and the results, as for every layer after a step's first.
+ * ws_bytes >= pp_tree_workspace_size's bytes. */
+pp_status pp_tree_workspace_size(const pp_cache* cache, int n, int group, int max_new, pp_dtype dtype, int hq, int hkv, int head_dim,
+                                 size_t* bytes);
+pp_status pp_tree_attn_fwd(const pp_cache* cache, int n, const int32_t* slots, int group, const int32_t* shared, int max_new,
+                           const int32_t* count, const int32_t* parents, pp_dtype dtype, int hq, int hkv, int head_dim, float scale,
+                           const void* q, const void* k_pages, const void* v_pages, void* o, float* lse, int planned, void* ws,
+                           size_t ws_bytes, void* hip_stream);
+
+/* Verifies drafted tokens against the model's distributions, from given numbers, and
+ * samples the token that follows; with max_new 1 it is plain sampling.
+ * Of a sequence's count[i] (dev; NULL: max_new; 0: left out) nodes node 0 is its last token
+ * and the others, tokens (dev int32 [n, max_new]), were drafted as a tree (parents as for
+ * the attention; a node without a parent is never reached).  target (dev [n, max_new,
+ * vocab], dtype) are the model's logits at the nodes, p = softmax(target / T), draft (dev,
+ * same shape) the drafter's from which the children of a node were drawn, q; T =
+ * temperature[i] (dev; NULL: 1).
+ * From node 0 on, a node's children y are tried in order, at most max_children of them:
+ *   w = p, Z = 1, a = 0 at first;  y follows if u[i][y's node] q(y) Z < w(y), else
+ *   a += Z, w = max(p - a q, 0), Z = sum w
+ * so that what comes out is distributed as p.  draft NULL: the drafts are given, y
+ * follows if u Z < w(y), else w(y) = 0 and Z = sum w.  From the node that none of its
+ * children follow, the next token is the first x with w(0) + .. + w(x) > u[i][0] Z.
+ * T not above 0: y follows if it is the first largest logit, which is also the next token.
+ * u dev float [n, max_new] in [0, 1).  Entries of -inf or of the type's lowest value are
+ * masked ones, p = 0.  A row that holds a NaN or +inf or nothing else than masks gives no
+ * token (-1, log-prob NaN), and a draft row like that is not used: its node has no child
+ * that follows.
+ *   out_count  dev int32 [n]: nodes kept, node 0 included (0 for sequences left out)
+ *   out_path   dev int32 [n, max_new]: those nodes (pp_cache_accept's path), then -1
+ *   out_tokens dev int32 [n, max_new]: out_count new tokens, the last of them sampled, then -1
+ *   out_logp   dev float [n, max_new]: their ln p (at T = 1 where T is not above 0),
+ *              pp_policy_loss's logp_old; then 0
+ * Probabilities and sums are 64 bits.  max_new <= 64, n * max_new <= 65535. */
+pp_status pp_verify_workspace_size(int n, int max_new, int vocab, pp_dtype dtype, size_t* bytes);
+pp_status pp_verify_draft(int n, int max_new, int vocab, pp_dtype dtype, int max_children, const int32_t* count,
+                          const int32_t* parents, const int32_t* tokens, const void* target, const void* draft,
+                          const float* temperature, const float* u, int32_t* out_count, int32_t* out_tokens, int32_t* out_path,
+                          float* out_logp, void* ws, size_t ws_bytes, void* hip_stream);
 
 /* Host-only export of the planner's integer view of a batch (no GPU needed):
  *   position_ids[sumT]  prompt token t -> t, response token j -> P_b + j,

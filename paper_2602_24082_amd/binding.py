@@ -39,6 +39,9 @@ EXPORTED = [
     "pp_bwd_stored_ds_workspace_size",
     "pp_cross_workspace_size", "pp_cross_attn_fwd", "pp_cross_attn_bwd",
     "pp_tok_logprob", "pp_tok_logprob_bwd", "pp_tok_logprob_bwd_rows", "pp_policy_workspace_size", "pp_policy_loss",
+    "pp_cache_workspace_size", "pp_cache_reserve", "pp_cache_fork", "pp_cache_free", "pp_cache_compact", "pp_cache_shared",
+    "pp_cache_append", "pp_cache_accept", "pp_tree_workspace_size", "pp_tree_attn_fwd", "pp_verify_workspace_size",
+    "pp_verify_draft",
 ]
 
 NOALLOC_SCRATCH_BYTES = 4 << 20  # PP_NOALLOC_SCRATCH_BYTES
@@ -78,6 +81,11 @@ class _EncDesc(ctypes.Structure):
 class _PolicyConfig(ctypes.Structure):
     _fields_ = [(n, ctypes.c_double) for n in ("clip_low", "clip_high", "dual_clip", "kl_coef", "ent_coef", "norm")] + [
         ("kl", ctypes.c_int), ("reduction", ctypes.c_int)]
+
+
+class _CacheDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_slots", "max_pages", "num_pages", "page_size")] + [
+        (n, ctypes.c_void_p) for n in ("page_table", "seq_len", "held", "refs")]
 
 
 _lib = None
@@ -137,6 +145,19 @@ def lib() -> ctypes.CDLL:
     L.pp_tok_logprob_bwd_rows.argtypes = [D, i, i, P, P, P, P, P, P, P, sz, P]
     L.pp_policy_workspace_size.argtypes = [D, ctypes.POINTER(sz)]
     L.pp_policy_loss.argtypes = [D, ctypes.POINTER(_PolicyConfig), P, P, P, P, P, i, P, P, P, P, P, P, P, sz, P]
+    C, S, i64 = ctypes.POINTER(_CacheDesc), ctypes.POINTER(sz), ctypes.c_int64
+    L.pp_cache_workspace_size.argtypes = [C, i, S]
+    L.pp_cache_reserve.argtypes = [C, i, P, P, P, P, sz, P]
+    L.pp_cache_fork.argtypes = [C, i, P, P, i, i, i, i, P, P, P, P, sz, P]
+    L.pp_cache_free.argtypes = [C, i, P, P]
+    L.pp_cache_compact.argtypes = [C, i, i, i, i, P, P, P, P, sz, P]
+    L.pp_cache_shared.argtypes = [C, i, P, i, P, P]
+    L.pp_cache_append.argtypes = [C, i, P, i, P, P, i64, P, i, i, i, i, f32, P, P, P, P, P, P, P]
+    L.pp_cache_accept.argtypes = [C, i, P, i, P, P, i, i, i, i, P, P, P, P, sz, P]
+    L.pp_tree_workspace_size.argtypes = [C, i, i, i, i, i, i, i, S]
+    L.pp_tree_attn_fwd.argtypes = [C, i, P, i, P, i, P, P, i, i, i, i, f32, P, P, P, P, P, i, P, sz, P]
+    L.pp_verify_workspace_size.argtypes = [i, i, i, i, S]
+    L.pp_verify_draft.argtypes = [i, i, i, i, i, P, P, P, P, P, P, P, P, P, P, P, P, sz, P]
     L.pp_pack_export.argtypes = [D, i, i, P, P, P, sz]
     L.pp_tile_class_len.argtypes = [D, i, i, ctypes.POINTER(sz)]
     L.pp_timing_enable.argtypes = [i]
@@ -866,6 +887,300 @@ def pp_policy_loss(pack: Pack, logp: torch.Tensor, adv: torch.Tensor, logp_old: 
                                     _addr(adv), int(per_token), _addr(mask), _addr(loss), _addr(stats), _addr(counts), _addr(dlogp),
                                     _addr(dent), _addr(ws), _ws_bytes(ws, dev), _raw_stream(dev)))
     return loss, stats, counts, dlogp, dent
+
+
+# ---------------------------------------------------------------- sampling
+
+
+class Cache:
+    """A paged cache's bookkeeping (struct pp_cache): page_table [slots, max_pages], seq_len and held [slots], refs [pages],
+    int32 on the GPU, all zeros when empty.  The tensors stay the caller's to read; keys and values lie in pools
+    [layers, pages, hkv, page_size, head_dim] that go to each call."""
+
+    def __init__(self, page_table: torch.Tensor, seq_len: torch.Tensor, held: torch.Tensor, refs: torch.Tensor, page_size: int):
+        if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or not isinstance(refs, torch.Tensor) or refs.dim() != 1:
+            raise ValueError("page_table must be [slots, max_pages], refs [pages]")
+        dev, slots = page_table.device, page_table.shape[0]
+        _check_tensor("page_table", page_table, page_table.shape, torch.int32, dev)
+        _check_tensor("seq_len", seq_len, (slots,), torch.int32, dev)
+        _check_tensor("held", held, (slots,), torch.int32, dev)
+        _check_tensor("refs", refs, refs.shape, torch.int32, dev)
+        _on_gpu(page_table)
+        self.page_table, self.seq_len, self.held, self.refs = page_table, seq_len, held, refs
+        self.num_pages, self.page_size, self.device = refs.shape[0], int(page_size), dev
+        self._desc = _CacheDesc(slots, page_table.shape[1], refs.shape[0], self.page_size, page_table.data_ptr(),
+                                seq_len.data_ptr(), held.data_ptr(), refs.data_ptr())
+        self.ref = ctypes.byref(self._desc)
+        self._sizes = {}
+
+    def _ws_size(self, name: str, *args) -> int:
+        """Workspace bytes, kept (they follow from the sizes)."""
+        key = (name, *args)
+        out = self._sizes.get(key)
+        if out is None:
+            n = ctypes.c_size_t(0)
+            _check(getattr(lib(), name)(self.ref, *args, ctypes.byref(n)))
+            if len(self._sizes) >= 64:
+                self._sizes.clear()
+            out = self._sizes[key] = n.value
+        return out
+
+
+def make_cache(num_slots: int, max_pages: int, num_pages: int, page_size: int, device) -> Cache:
+    """An empty cache."""
+    z = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=device)
+    return Cache(z(num_slots, max_pages), z(num_slots), z(num_slots), z(num_pages), page_size)
+
+
+def _ints_of(name: str, t: torch.Tensor, n: int, dev: torch.device):
+    return _check_tensor(name, t, (n,), torch.int32, dev)
+
+
+def _slots_of(name: str, t: torch.Tensor, dev: torch.device) -> int:
+    if not isinstance(t, torch.Tensor) or t.dim() != 1:
+        raise ValueError(f"{name} must be a tensor [n]")
+    _check_tensor(name, t, t.shape, torch.int32, dev)
+    return t.shape[0]
+
+
+def _pools(cache: Cache, k_pages: torch.Tensor, v_pages: torch.Tensor, layered: bool):
+    """(dtype code, layers, hkv, head_dim) of the pools of keys and values, checked."""
+    want = 5 if layered else 4
+    if k_pages.dim() != want:
+        raise ValueError("k_pages must be [%spages, hkv, page_size, head_dim]" % ("layers, " if layered else ""))
+    hkv, d = k_pages.shape[-3], k_pages.shape[-1]
+    layers = k_pages.shape[0] if layered else 1
+    shape = ((layers,) if layered else ()) + (cache.num_pages, hkv, cache.page_size, d)
+    _check_tensor("k_pages", k_pages, shape, k_pages.dtype, cache.device)
+    _check_tensor("v_pages", v_pages, shape, k_pages.dtype, cache.device)
+    return _dtype_code(k_pages), layers, hkv, d
+
+
+def _cache_ws(cache: Cache, n: int, ws):
+    return _maybe_workspace(cache._ws_size("pp_cache_workspace_size", n), cache.device) if ws is None else ws
+
+
+def _new_ints(n, dev, out=None, name="status"):
+    return torch.empty(n, dtype=torch.int32, device=dev) if out is None else _ints_of(name, out, n, dev)
+
+
+def pp_cache_workspace_size(cache: Cache, n: int) -> int:
+    return cache._ws_size("pp_cache_workspace_size", n)
+
+
+def pp_cache_reserve(cache: Cache, slots: torch.Tensor, add: torch.Tensor, status=None, ws=None) -> torch.Tensor:
+    """Room for add[i] more tokens in slots[i]; returns status [2]: pages missing (then nothing changed), entries refused."""
+    dev = cache.device
+    n = _slots_of("slots", slots, dev)
+    _ints_of("add", add, n, dev)
+    status, ws = _new_ints(2, dev, status), _cache_ws(cache, n, ws)
+    with _device_of(dev):
+        _check(lib().pp_cache_reserve(cache.ref, n, _addr(slots), _addr(add), _addr(status), _addr(ws), _ws_bytes(ws, dev),
+                                      _raw_stream(dev)))
+    return status
+
+
+def pp_cache_fork(cache: Cache, src: torch.Tensor, dst: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, status=None,
+                  ws=None) -> torch.Tensor:
+    """Makes the empty slots dst[i] copies of src[i]: whole pages shared, a partial last page copied in every layer of the
+    pools [layers, pages, hkv, page_size, head_dim]; returns status [2] as pp_cache_reserve."""
+    dev = cache.device
+    n = _slots_of("src", src, dev)
+    _ints_of("dst", dst, n, dev)
+    dt, layers, hkv, d = _pools(cache, k_pages, v_pages, True)
+    status, ws = _new_ints(2, dev, status), _cache_ws(cache, n, ws)
+    with _device_of(dev):
+        _check(lib().pp_cache_fork(cache.ref, n, _addr(src), _addr(dst), dt, layers, hkv, d, _addr(k_pages), _addr(v_pages),
+                                   _addr(status), _addr(ws), _ws_bytes(ws, dev), _raw_stream(dev)))
+    return status
+
+
+def pp_cache_free(cache: Cache, slots: torch.Tensor):
+    """Empties slots."""
+    dev = cache.device
+    n = _slots_of("slots", slots, dev)
+    with _device_of(dev):
+        _check(lib().pp_cache_free(cache.ref, n, _addr(slots), _raw_stream(dev)))
+
+
+def pp_cache_compact(cache: Cache, k_pages: torch.Tensor, v_pages: torch.Tensor, live=None, ws=None) -> torch.Tensor:
+    """Moves the live pages to the pool's front; returns their number [1]."""
+    dev = cache.device
+    dt, layers, hkv, d = _pools(cache, k_pages, v_pages, True)
+    live, ws = _new_ints(1, dev, live, "live"), _cache_ws(cache, 0, ws)
+    with _device_of(dev):
+        _check(lib().pp_cache_compact(cache.ref, dt, layers, hkv, d, _addr(k_pages), _addr(v_pages), _addr(live), _addr(ws),
+                                      _ws_bytes(ws, dev), _raw_stream(dev)))
+    return live
+
+
+def pp_cache_shared(cache: Cache, slots: torch.Tensor, group: int, shared=None) -> torch.Tensor:
+    """Leading whole pages that the sequences of each group have in common: [n / group]."""
+    dev = cache.device
+    n = _slots_of("slots", slots, dev)
+    if group < 1 or n % group:
+        raise ValueError(f"{n} slots do not make groups of {group}")
+    shared = _new_ints(n // group, dev, shared, "shared")
+    with _device_of(dev):
+        _check(lib().pp_cache_shared(cache.ref, n, _addr(slots), group, _addr(shared), _raw_stream(dev)))
+    return shared
+
+
+def pp_cache_append(cache: Cache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor,
+                    v_pages: torch.Tensor, count: Optional[torch.Tensor] = None, start: Optional[torch.Tensor] = None,
+                    max_new: Optional[int] = None, parents: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                    rope_base: float = 0.0, q_rot=None) -> Optional[torch.Tensor]:
+    """Writes keys and values of new tokens into one layer's pages behind the cached ones, keys (and q) rotated if rope_base
+    is not 0.  k, v [n, max_new, hkv, d], or [rows, hkv, d] with max_new (and start [n], the sequences' first rows); q
+    alike.  Returns the rotated q (None without q)."""
+    dev = cache.device
+    n = _slots_of("slots", slots, dev)
+    dt, _, hkv, d = _pools(cache, k_pages, v_pages, False)
+    if k.dim() not in (3, 4) or (k.dim() == 3 and max_new is None):
+        raise ValueError("k must be [n, max_new, hkv, head_dim], or [rows, hkv, head_dim] with max_new")
+    if k.dim() == 4:
+        if max_new is not None and max_new != k.shape[1]:
+            raise ValueError(f"max_new is {max_new}, k has {k.shape[1]} rows a sequence")
+        max_new = k.shape[1]
+        if k.shape[0] != n:
+            raise ValueError(f"k has {k.shape[0]} sequences, slots {n}")
+    lead = k.shape[:-2]
+    rows = k.shape[0] if k.dim() == 3 else n * max_new
+    _check_tensor("k", k, (*lead, hkv, d), k_pages.dtype, dev)
+    _check_tensor("v", v, (*lead, hkv, d), k_pages.dtype, dev)
+    hq = 0
+    if q is not None:
+        if q.dim() != k.dim():
+            raise ValueError("q must be shaped as k but for its heads")
+        hq = q.shape[-2]
+        _check_tensor("q", q, (*lead, hq, d), k_pages.dtype, dev)
+        q_rot = torch.empty_like(q) if q_rot is None else _check_tensor("q_rot", q_rot, q.shape, q.dtype, dev)
+    elif q_rot is not None:
+        raise ValueError("q_rot without q")
+    for name, t in (("count", count), ("start", start)):
+        if t is not None:
+            _ints_of(name, t, n, dev)
+    if parents is not None:
+        _check_tensor("parents", parents, (n, max_new), torch.int32, dev)
+    with _device_of(dev):
+        _check(lib().pp_cache_append(cache.ref, n, _addr(slots), max_new, _addr(count), _addr(start), rows, _addr(parents), dt, hq,
+                                     hkv, d, float(rope_base), _addr(q), _addr(k), _addr(v), _addr(q_rot), _addr(k_pages),
+                                     _addr(v_pages), _raw_stream(dev)))
+    return q_rot
+
+
+def pp_cache_accept(cache: Cache, slots: torch.Tensor, count: torch.Tensor, path: Optional[torch.Tensor] = None,
+                    k_pages: Optional[torch.Tensor] = None, v_pages: Optional[torch.Tensor] = None, max_new: Optional[int] = None,
+                    status=None, ws=None) -> torch.Tensor:
+    """Keeps count[i] of the tokens appended to slots[i]: the nodes path[i] ([n, max_new]) of a drafted tree, whose rows move
+    together in every layer of the pools, or without path the first ones.  Returns status [2]: 0, entries refused."""
+    dev = cache.device
+    n = _slots_of("slots", slots, dev)
+    _ints_of("count", count, n, dev)
+    dt, layers, hkv, d = PP_BF16, 0, 1, 64
+    if path is not None:
+        if path.dim() != 2 or k_pages is None or v_pages is None:
+            raise ValueError("path must be [n, max_new], and comes with k_pages and v_pages")
+        _check_tensor("path", path, (n, path.shape[1]), torch.int32, dev)
+        max_new = path.shape[1]
+        dt, layers, hkv, d = _pools(cache, k_pages, v_pages, True)
+    elif max_new is None:
+        max_new = 2**31 - 1
+    status, ws = _new_ints(2, dev, status), _cache_ws(cache, n, ws)
+    with _device_of(dev):
+        _check(lib().pp_cache_accept(cache.ref, n, _addr(slots), max_new, _addr(count), _addr(path), dt, layers, hkv, d,
+                                     _addr(k_pages), _addr(v_pages), _addr(status), _addr(ws), _ws_bytes(ws, dev),
+                                     _raw_stream(dev)))
+    return status
+
+
+def pp_tree_workspace_size(cache: Cache, n: int, group: int, max_new: int, hq: int, hkv: int, head_dim: int,
+                           dtype: int = PP_BF16) -> int:
+    return cache._ws_size("pp_tree_workspace_size", n, group, max_new, dtype, hq, hkv, head_dim)
+
+
+def pp_tree_attn_fwd(cache: Cache, slots: torch.Tensor, q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                     parents: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None, group: int = 1,
+                     shared: Optional[torch.Tensor] = None, scale: float = 0.0, out=None, lse=None, planned: bool = False, ws=None):
+    """Attention of new tokens q [n, max_new, hq, d] over the cache, each to its sequence's cached tokens and its path to the
+    tree's root; returns (o like q, lse [hq, n * max_new] fp32).  planned: ws holds the plan of an earlier call of the same
+    step (another layer's)."""
+    dev = cache.device
+    n = _slots_of("slots", slots, dev)
+    dt, _, hkv, d = _pools(cache, k_pages, v_pages, False)
+    if q.dim() != 4:
+        raise ValueError("q must be [n, max_new, hq, head_dim]")
+    N, hq = q.shape[1], q.shape[2]
+    _check_tensor("q", q, (n, N, hq, d), k_pages.dtype, dev)
+    if parents is not None:
+        _check_tensor("parents", parents, (n, N), torch.int32, dev)
+    if count is not None:
+        _ints_of("count", count, n, dev)
+    if group < 1 or n % group:
+        raise ValueError(f"{n} sequences do not make groups of {group}")
+    if shared is not None:
+        _ints_of("shared", shared, n // group, dev)
+    out = torch.empty_like(q) if out is None else _check_tensor("out", out, q.shape, q.dtype, dev)
+    lse = (torch.empty(hq, n * N, dtype=torch.float32, device=dev) if lse is None
+           else _check_tensor("lse", lse, (hq, n * N), torch.float32, dev))
+    if ws is None:
+        if planned:
+            raise ValueError("planned comes with the ws that holds the plan")
+        ws = _maybe_workspace(cache._ws_size("pp_tree_workspace_size", n, group, N, dt, hq, hkv, d), dev)
+    with _device_of(dev):
+        _check(lib().pp_tree_attn_fwd(cache.ref, n, _addr(slots), group, _addr(shared), N, _addr(count), _addr(parents), dt, hq, hkv,
+                                      d, float(scale), _addr(q), _addr(k_pages), _addr(v_pages), _addr(out), _addr(lse),
+                                      int(planned), _addr(ws), _ws_bytes(ws, dev), _raw_stream(dev)))
+    return out, lse
+
+
+_verify_sizes = {}
+
+
+def pp_verify_workspace_size(n: int, max_new: int, vocab: int, dtype: int = PP_BF16) -> int:
+    key = (n, max_new, vocab, dtype)
+    out = _verify_sizes.get(key)
+    if out is None:
+        b = ctypes.c_size_t(0)
+        _check(lib().pp_verify_workspace_size(*key, ctypes.byref(b)))
+        if len(_verify_sizes) >= 64:
+            _verify_sizes.clear()
+        out = _verify_sizes[key] = b.value
+    return out
+
+
+def pp_verify_draft(target: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor, draft: Optional[torch.Tensor] = None,
+                    parents: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                    temperature: Optional[torch.Tensor] = None, max_children: int = 1, ws=None):
+    """Verifies drafted tokens [n, max_new] (node 0 the last token) against the model's logits target [n, max_new, vocab]
+    with the numbers u [n, max_new], draft [n, max_new, vocab] the drafter's logits (None: given drafts), and samples the
+    token that follows.  Returns (count [n], new tokens [n, max_new], path [n, max_new], their log-probs [n, max_new])."""
+    if target.dim() != 3:
+        raise ValueError("target must be [n, max_new, vocab]")
+    (n, N, V), dev = target.shape, target.device
+    _check_tensor("target", target, target.shape, target.dtype, dev)
+    _check_tensor("tokens", tokens, (n, N), torch.int32, dev)
+    _check_tensor("u", u, (n, N), torch.float32, dev)
+    if draft is not None:
+        _check_tensor("draft", draft, target.shape, target.dtype, dev)
+    if parents is not None:
+        _check_tensor("parents", parents, (n, N), torch.int32, dev)
+    if count is not None:
+        _ints_of("count", count, n, dev)
+    if temperature is not None:
+        _check_tensor("temperature", temperature, (n,), torch.float32, dev)
+    dt = _dtype_code(target)
+    _on_gpu(target)
+    out = torch.empty(2 * n * N + n, dtype=torch.int32, device=dev)
+    out_tokens, path, out_count = out[:n * N].view(n, N), out[n * N:2 * n * N].view(n, N), out[2 * n * N:]
+    logp = torch.empty(n, N, dtype=torch.float32, device=dev)
+    if ws is None:
+        ws = _maybe_workspace(pp_verify_workspace_size(n, N, V, dt), dev)
+    with _device_of(dev):
+        _check(lib().pp_verify_draft(n, N, V, dt, max_children, _addr(count), _addr(parents), _addr(tokens), _addr(target),
+                                     _addr(draft), _addr(temperature), _addr(u), _addr(out_count), _addr(out_tokens), _addr(path),
+                                     _addr(logp), _addr(ws), _ws_bytes(ws, dev), _raw_stream(dev)))
+    return out_count, out_tokens, path, logp
 
 
 # ---------------------------------------------------------------- timing

@@ -25,7 +25,7 @@ BUILD_DIR = os.path.join(PKG, "_build")
 ARCH = "gfx950"
 
 SOURCES = ["pp_host.cpp", "pp_attn_fwd.hip", "pp_attn_bwd.hip", "pp_cross.hip", "pp_logprob.hip", "pp_rm.hip", "pp_rope.hip", "pp_stage.hip",
-           "pp_noalloc.hip", "pp_policy.hip"]
+           "pp_noalloc.hip", "pp_policy.hip", "pp_sample_host.cpp", "pp_cache.hip", "pp_tree.hip", "pp_draft.hip"]
 
 COMMON = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
@@ -119,7 +119,9 @@ def build_host_sanitized(lib_path: str, verbose: bool = False) -> str:
         obj = os.path.join(build_dir, os.path.splitext(src)[0] + ".o")
         cmd = [hipcc(), *COMMON, "-g"]
         if src == "pp_host.cpp":
-            cmd += san + [f'-DPP_BUILD_ID="{source_digest()}"']
+            cmd.append(f'-DPP_BUILD_ID="{source_digest()}"')
+        if src.endswith(".cpp"):
+            cmd += san
         else:
             cmd += ["-x", "hip"]
         cmd += ["-c", os.path.join(CSRC, src), "-o", obj]

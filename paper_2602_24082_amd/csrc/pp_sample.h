@@ -1,0 +1,191 @@
+// Internal interface of the sampling operators: the paged cache, attention of drafted trees
+// over it, draft verification.  Host entry points in pp_sample_host.cpp.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "pp_launch.h"
+
+namespace pp {
+
+// pp_cache as the kernels see it.
+struct CacheView {
+  int32_t* table;    // [num_slots, max_pages]
+  int32_t* seq_len;  // [num_slots]
+  int32_t* held;     // [num_slots]
+  int32_t* refs;     // [num_pages]
+  int num_slots, max_pages, num_pages, page_size, page_log2;
+  __host__ __device__ bool has_slot(int s) const { return (unsigned)s < (unsigned)num_slots; }
+  __host__ __device__ bool has_page(int p) const { return (unsigned)p < (unsigned)num_pages; }
+  __host__ __device__ int32_t* row(int s) const { return table + (int64_t)s * max_pages; }
+  // a sequence's length and pages belong together
+  __host__ __device__ bool sound(int64_t len, int64_t n) const {
+    return n >= 0 && n <= max_pages && len >= 0 && len <= n << page_log2;
+  }
+};
+
+// Pools [layers, num_pages, hkv, page_size, head_dim] of keys and values, in bytes.
+struct CachePools {
+  char* k;
+  char* v;
+  int64_t layer_bytes, page_bytes;
+  int head_bytes;  // a page's rows of one head
+  int row_bytes;
+  int layers, hkv;
+};
+
+struct ForkEntry {
+  int32_t src, dst;  // dst < 0: none
+  int32_t whole;     // pages that both list
+  int32_t rest;      // rows of the partial page
+  int32_t old_page, new_page;
+};
+struct AcceptEntry {
+  int32_t slot;  // < 0: none
+  int32_t len;   // ahead of the call
+  int32_t count;
+  int32_t moved;  // any node lies elsewhere
+};
+constexpr int kAcceptNodes = 64;  // nodes of a drafted tree
+
+struct CacheScratch {
+  int32_t* mark;   // [num_slots]
+  int32_t* first;  // [n]
+  int32_t* list;   // [num_pages]
+  int32_t* list2;  // [num_pages]
+  int32_t* renum;  // [num_pages]
+  int32_t* moves;  // [2]
+  void* entries;   // [n] ForkEntry or AcceptEntry
+};
+
+struct AppendParams {
+  const int32_t* slots;    // [n]
+  const int32_t* count;    // [n] or null: max_new
+  const int32_t* start;    // [n] or null: i * max_new
+  const int32_t* parents;  // [n, max_new] or null: a chain
+  const void* q;           // null: none
+  const void* k;
+  const void* v;
+  void* q_rot;
+  void* k_pages;
+  void* v_pages;
+  int64_t rows;  // tokens that k, v and q have
+  int max_new, hq, hkv;
+  bool turns;           // rotate
+  double inv_freq[64];  // base^(-2j / head_dim)
+};
+
+hipError_t launch_cache_reserve(const CacheView& c, int n, const int32_t* slots, const int32_t* add, int32_t* status,
+                                const CacheScratch& w, hipStream_t s);
+hipError_t launch_cache_fork(const CacheView& c, const CachePools& p, int n, const int32_t* src, const int32_t* dst,
+                             int32_t* status, const CacheScratch& w, hipStream_t s);
+hipError_t launch_cache_free(const CacheView& c, int n, const int32_t* slots, hipStream_t s);
+hipError_t launch_cache_compact(const CacheView& c, const CachePools& p, int32_t* live, const CacheScratch& w, hipStream_t s);
+hipError_t launch_cache_accept(const CacheView& c, const CachePools& p, int n, const int32_t* slots, int max_new,
+                               const int32_t* count, const int32_t* path, int32_t* status, const CacheScratch& w, hipStream_t s);
+hipError_t launch_cache_shared(const CacheView& c, int groups, const int32_t* slots, int group, int32_t* shared, hipStream_t s);
+hipError_t launch_cache_append(const CacheView& c, const AppendParams& a, int n, int head_dim, int dtype, hipStream_t s);
+
+// Attention of drafted trees over the cache (pp_tree.hip).
+constexpr int kTreeSeqs = 2048;  // sequences a call
+constexpr int kTreeNodes = 64;   // nodes a sequence
+constexpr int kTreeKeys = 32;    // keys a block
+constexpr int kCus = 256;
+// Rows a tile: blocks of 32 that a wave holds in registers.
+template <typename T>
+constexpr int kTreeTiles = sizeof(T) == 2 ? 2 : 1;
+// Waves a compute unit: each has a ring of two blocks of keys and values in LDS.
+template <int D, typename T>
+constexpr int kTreePerCu = D * sizeof(T) > 256 ? 2 : D * sizeof(T) > 128 ? 4 : 8;
+
+struct TreeItem {
+  int32_t blocks;  // of keys, for every tile of rows and head
+  int32_t slot;    // whose pages
+  int32_t k0, k1;  // keys [k0, k1)
+  int32_t seen;    // all rows see the keys below
+  int32_t seq;     // the (first) sequence of its rows
+  int32_t bad;     // nodes asked for of a sequence that is not sound
+  int32_t pad;
+};
+struct TreeShape {
+  int n, nodes, group, groups;  // sequences, nodes of each, sequences a group
+  int hq, hkv, G;
+  int rows_shared, rows_own;    // of an item, for one kv-head
+  int tile_rows;                // 32 if the rows fit, else 32 kTreeTiles
+  int tiles_shared, tiles_own;  // of tile_rows rows; tiles_shared 0: nothing is shared
+  int waves;
+  int part_rows;                // rows of a partial result
+};
+struct TreePlan {
+  TreeItem* items;     // [n + groups]
+  int64_t* first;      // [n + groups]: units ahead of an item
+  int64_t* head;       // units in all, units a wave
+  int32_t* live;       // [n]: nodes of a sequence
+  int32_t* wave_item;  // [waves]: where a wave starts
+};
+struct TreeLaunch {
+  TreeShape shape;
+  TreePlan plan;
+  bool planned;  // the plan stands already
+  const int32_t* slots;
+  const int32_t* count;    // or null: all nodes
+  const int32_t* shared;   // [groups] or null
+  const int32_t* parents;  // [n, nodes] or null: chains
+  const void* q;
+  const void* k;
+  const void* v;
+  void* o;
+  float* lse;
+  float* part;
+  float* part_ml;
+  float scale;
+  int head_dim, dtype;
+};
+hipError_t launch_tree_attn(const CacheView& c, const TreeLaunch& a, hipStream_t s);
+
+// Draft verification (pp_draft.hip).
+constexpr int kDraftChunk = 8192;  // entries of a row that a workgroup takes
+struct DraftShape {
+  int n, nodes, vocab, chunks, max_children;
+};
+// What a row's entries in one chunk hold: their maximum (NaN: a NaN or +inf among them), the
+// sum of e^((x - max) / T), and the first entry at the maximum.
+struct DraftPart {
+  double sum;
+  float max;
+  int32_t arg;
+};
+// Where a sequence's walk ends.
+struct DraftEnd {
+  double sum, a;   // of the node's row; the draft's factor in what is left of it (0: nothing taken off that way)
+  float max;
+  int32_t node;    // < 0: no such sequence
+  int32_t len;     // nodes kept
+  int32_t tried;   // children that were rejected
+  int32_t last;    // the last of them
+  int32_t arg;     // < 0: nothing to sample from
+  int32_t greedy;
+  int32_t pad;
+};
+struct DraftParams {
+  DraftShape shape;
+  const void* target;
+  const void* draft;         // or null: given drafts
+  const int32_t* tokens;
+  const int32_t* parents;    // or null: chains
+  const int32_t* count;      // or null
+  const float* temperature;  // or null: 1
+  const float* u;
+  int32_t* out_count;
+  int32_t* out_tokens;
+  int32_t* out_path;
+  float* out_logp;
+  DraftPart* part;  // [2, n, nodes, chunks]: of the target's rows, of the draft's
+  double* left;     // [n, nodes, chunks]: Z after a node is rejected
+  double* ends;     // [n, chunks]: Z where the walk ends
+  DraftEnd* end;    // [n]
+};
+hipError_t launch_verify_draft(const DraftParams& p, int dtype, hipStream_t s);
+
+}  // namespace pp
