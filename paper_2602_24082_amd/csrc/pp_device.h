@@ -122,6 +122,14 @@ __device__ __forceinline__ void lds_dma16_once(const void* src, const void* lds_
   asm volatile("global_load_lds_dwordx4 %0, off nt" ::"v"(src), "{m0}"(base) : "memory");
 }
 
+// Either to a byte address in LDS (wave-uniform).
+template <bool ONCE>
+__device__ __forceinline__ void lds_dma16_at(const void* src, unsigned lds_byte) {
+  const unsigned base = __builtin_amdgcn_readfirstlane(lds_byte);
+  if constexpr (ONCE) asm volatile("global_load_lds_dwordx4 %0, off nt" ::"v"(src), "{m0}"(base) : "memory");
+  else asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(base) : "memory");
+}
+
 // One 4-byte element per lane into LDS (lane l -> lds + 4*l): the per-query
 // scalars of a 64-query tile.  Issued like lds_dma16.
 __device__ __forceinline__ void dma_dword(void* lds, const void* src) {

@@ -90,15 +90,19 @@ hipError_t launch_cache_append(const CacheView& c, const AppendParams& a, int n,
 // Attention of drafted trees over the cache (pp_tree.hip).
 constexpr int kTreeSeqs = 2048;  // sequences a call
 constexpr int kTreeNodes = 64;   // nodes a sequence
-constexpr int kTreeKeys = 32;    // keys a block
 constexpr int kCus = 256;
-// Rows a tile: blocks of 32 that a wave holds in registers.
-template <typename T>
-constexpr int kTreeTiles = sizeof(T) == 2 ? 2 : 1;
-// Waves a compute unit: each has a ring of two blocks of keys and values in LDS.
+// Workgroups a compute unit: of one wave, each with a ring of two blocks of 32 keys and values
+// in LDS, and of a team of four waves, with two blocks of 64 (fp32: 32) between them.
 template <int D, typename T>
-constexpr int kTreePerCu = D * sizeof(T) > 256 ? 2 : D * sizeof(T) > 128 ? 4 : 8;
+constexpr int kTreeSolo = D * sizeof(T) > 256 ? 2 : D * sizeof(T) > 128 ? 4 : 8;
+template <int D, typename T>
+constexpr int kTreeTeam = sizeof(T) == 4 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : 2;
+template <typename T>
+constexpr int kTeamKeys = sizeof(T) == 2 ? 64 : 32;
+constexpr int kSoloKeys = 32, kSoloRows = 32, kTeamWaves = 4, kTeamRows = 128;
 
+// An item: rows against a range of keys; its units: a block of keys, for a tile of rows of one
+// kv-head.
 struct TreeItem {
   int32_t blocks;  // of keys, for every tile of rows and head
   int32_t slot;    // whose pages
@@ -108,21 +112,27 @@ struct TreeItem {
   int32_t bad;     // nodes asked for of a sequence that is not sound
   int32_t pad;
 };
+// The two kinds of items: a group's shared keys, a sequence's own.
+struct TreeKind {
+  int rows;       // of an item, for one kv-head
+  int team;       // more than 32: taken by teams
+  int keys;       // of a block
+  int tiles;      // of rows; 0: no such items
+  int part_rows;  // of a partial result
+  int64_t part0;  // row of the first one
+};
 struct TreeShape {
   int n, nodes, group, groups;  // sequences, nodes of each, sequences a group
   int hq, hkv, G;
-  int rows_shared, rows_own;    // of an item, for one kv-head
-  int tile_rows;                // 32 if the rows fit, else 32 kTreeTiles
-  int tiles_shared, tiles_own;  // of tile_rows rows; tiles_shared 0: nothing is shared
-  int waves;
-  int part_rows;                // rows of a partial result
+  TreeKind kind[2];  // shared, own
+  int workers[2];    // solo waves, teams
 };
 struct TreePlan {
-  TreeItem* items;     // [n + groups]
-  int64_t* first;      // [n + groups]: units ahead of an item
-  int64_t* head;       // units in all, units a wave
-  int32_t* live;       // [n]: nodes of a sequence
-  int32_t* wave_item;  // [waves]: where a wave starts
+  TreeItem* items;         // [n + groups]
+  int32_t* live;           // [n]: nodes of a sequence
+  int64_t* first[2];       // [n + groups]: units ahead of an item, of those that solo waves / teams take
+  int64_t* head;           // [2][2]: units in all, units a worker
+  int32_t* start_item[2];  // [workers]: where a worker starts
 };
 struct TreeLaunch {
   TreeShape shape;

@@ -146,7 +146,7 @@ pp_status check_call(const pp_cache* cache, int n, const void* ws, size_t ws_byt
   return check_ws(ws, ws_bytes, carve_cache(*c, n, const_cast<void*>(ws), w), what);
 }
 
-bool shape_tree(const CacheView& c, int n, int group, int nodes, int hq, int hkv, pp_dtype dtype, int d, bool shared, TreeShape* t) {
+bool shape_tree(int n, int group, int nodes, int hq, int hkv, pp_dtype dtype, int d, bool shared, TreeShape* t) {
   t->n = n;
   t->nodes = nodes;
   t->group = group;
@@ -154,31 +154,43 @@ bool shape_tree(const CacheView& c, int n, int group, int nodes, int hq, int hkv
   t->hq = hq;
   t->hkv = hkv;
   t->G = hq / hkv;
-  const int64_t own = (int64_t)nodes * t->G, all = own * group;
-  if (all > INT32_MAX / 2) return false;
-  t->rows_own = (int)own;
-  t->rows_shared = shared && group > 1 ? (int)all : 0;
-  const int most = t->rows_shared > t->rows_own ? t->rows_shared : t->rows_own;
-  t->tile_rows = dtype == PP_BF16 && most > 32 ? 32 * kTreeTiles<uint16_t> : 32;
-  t->tiles_own = (t->rows_own + t->tile_rows - 1) / t->tile_rows;
-  t->tiles_shared = (t->rows_shared + t->tile_rows - 1) / t->tile_rows;
-  t->part_rows = most < t->tile_rows ? most : t->tile_rows;
-  const int per_cu = dtype == PP_BF16 ? (d == 128 ? kTreePerCu<128, uint16_t> : kTreePerCu<64, uint16_t>)
-                                      : (d == 128 ? kTreePerCu<128, float> : kTreePerCu<64, float>);
-  t->waves = kCus * per_cu;
-  // tiles and partial results are counted in 32 bits
-  return ((int64_t)t->groups * t->tiles_shared + (int64_t)n * t->tiles_own) * hkv + t->waves <= INT32_MAX / t->part_rows;
+  const bool bf16 = dtype == PP_BF16;
+  t->workers[0] = kCus * (bf16 ? (d == 128 ? kTreeSolo<128, uint16_t> : kTreeSolo<64, uint16_t>)
+                               : (d == 128 ? kTreeSolo<128, float> : kTreeSolo<64, float>));
+  t->workers[1] = kCus * (bf16 ? (d == 128 ? kTreeTeam<128, uint16_t> : kTreeTeam<64, uint16_t>)
+                               : (d == 128 ? kTreeTeam<128, float> : kTreeTeam<64, float>));
+  int64_t parts = 0;
+  for (int k = 0; k < 2; ++k) {
+    const int64_t rows = (int64_t)nodes * t->G * (k == 0 ? group : 1);
+    if (rows > INT32_MAX / 2) return false;
+    TreeKind& x = t->kind[k];
+    x = TreeKind{};
+    x.rows = k == 0 && (group == 1 || !shared) ? 0 : (int)rows;
+    x.team = x.rows > kSoloRows;
+    x.keys = x.team ? (bf16 ? kTeamKeys<uint16_t> : kTeamKeys<float>) : kSoloKeys;
+    const int tile = x.team ? kTeamRows : kSoloRows;
+    x.tiles = (x.rows + tile - 1) / tile;
+    x.part_rows = x.rows < tile ? x.rows : tile;
+    x.part0 = parts;
+    const int64_t results = (int64_t)(k == 0 ? t->groups : n) * x.tiles * hkv + t->workers[x.team];
+    if (results > INT32_MAX) return false;  // tiles and partial results are counted in 32 bits
+    parts += results * x.part_rows;
+  }
+  return true;
 }
 
 size_t carve_tree(const TreeShape& t, int d, void* ws, TreeLaunch* a) {
   Carve at(ws);
   const int items = t.n + t.groups;
   a->plan.items = at.take<TreeItem>(items);
-  a->plan.first = at.take<int64_t>(items);
-  a->plan.head = at.take<int64_t>(2);
   a->plan.live = at.take<int32_t>(t.n);
-  a->plan.wave_item = at.take<int32_t>(t.waves);
-  const int64_t parts = (((int64_t)t.groups * t.tiles_shared + (int64_t)t.n * t.tiles_own) * t.hkv + t.waves) * t.part_rows;
+  a->plan.head = at.take<int64_t>(4);
+  for (int c = 0; c < 2; ++c) {
+    a->plan.first[c] = at.take<int64_t>(items);
+    a->plan.start_item[c] = at.take<int32_t>(t.workers[c]);
+  }
+  const TreeKind& last = t.kind[1];
+  const int64_t parts = last.part0 + ((int64_t)t.n * last.tiles * t.hkv + t.workers[last.team]) * last.part_rows;
   a->part_ml = at.take<float>(2 * parts);
   a->part = at.take<float>(parts * d);
   return at.used;
@@ -373,7 +385,7 @@ pp_status pp_tree_workspace_size(const pp_cache* cache, int n, int group, int ma
   if ((st = check_tree(n, group, max_new, dtype, hq, hkv, head_dim)) != PP_OK) return st;
   if (!bytes) return report_error(PP_ERR_INVALID_ARGUMENT, "bytes is NULL");
   TreeLaunch a{};
-  if (!shape_tree(c, n, group, max_new, hq, hkv, dtype, head_dim, true, &a.shape))
+  if (!shape_tree(n, group, max_new, hq, hkv, dtype, head_dim, true, &a.shape))
     return report_error(PP_ERR_UNSUPPORTED, "the call has too many rows");
   *bytes = carve_tree(a.shape, head_dim, nullptr, &a);
   return PP_OK;
@@ -388,10 +400,10 @@ pp_status pp_tree_attn_fwd(const pp_cache* cache, int n, const int32_t* slots, i
   if (st != PP_OK) return st;
   if ((st = check_tree(n, group, max_new, dtype, hq, hkv, head_dim)) != PP_OK) return st;
   TreeLaunch a{};
-  if (!shape_tree(c, n, group, max_new, hq, hkv, dtype, head_dim, true, &a.shape))
+  if (!shape_tree(n, group, max_new, hq, hkv, dtype, head_dim, true, &a.shape))
     return report_error(PP_ERR_UNSUPPORTED, "the call has too many rows");
   if ((st = check_ws(ws, ws_bytes, carve_tree(a.shape, head_dim, ws, &a), "tree attention")) != PP_OK) return st;
-  if (!shared) shape_tree(c, n, group, max_new, hq, hkv, dtype, head_dim, false, &a.shape);
+  if (!shared) shape_tree(n, group, max_new, hq, hkv, dtype, head_dim, false, &a.shape);
   if (n == 0) return PP_OK;
   if (!q || !k_pages || !v_pages || !o || !lse)
     return report_error(PP_ERR_INVALID_ARGUMENT, "q, k_pages, v_pages, o and lse must be non-NULL");

@@ -10,16 +10,17 @@
 // once for all of them.  The whole pages that a group's K sequences share are one more list
 // of keys, seen by the rows of all K: they are read once a group, not once a response.  So
 // there is an item for each group's shared keys and one for each sequence's own, and a unit
-// is a block of 32 keys of an item, for one head and one tile of up to 64 rows (32 of fp32).
+// is a block of keys of an item, for one head and one tile of its rows.
 //
-//   tree_plan     one workgroup: items, and their units dealt out evenly over all waves
-//   tree_attn     a wave walks its run of units, through a ring of its own in LDS: no barrier
-//                 anywhere.  Where an item ends or the run does, it leaves a partial result
-//   tree_combine  joins a row's partial results, in order
+//   tree_plan     one workgroup: items, and their units dealt out evenly over all workers
+//   tree_solo     up to 32 rows: a worker is a wave, which walks its run of units through a
+//                 ring of its own in LDS, without a barrier anywhere
+//   tree_team     more rows: a worker is four waves of 32 rows, which share a ring
+//   tree_combine  joins a row's partial results, in order: a worker leaves one wherever an item
+//                 ends or its run does
 //
-// Bound by reading keys and values once.  A wave of RT x 32 rows reads each key fragment from
-// LDS once and multiplies it RT times, so that only rows beyond a tile's read keys again.  No
-// atomics on results: sums depend on lengths alone.  Products as in cross attention (pp_rows.h).
+// Bound by reading keys and values once, and for teams by the matrix units as well.  No
+// atomics: sums depend on lengths alone.  Products as in cross attention (pp_rows.h).
 
 #include <hip/hip_runtime.h>
 
@@ -57,6 +58,7 @@ __device__ __forceinline__ int64_t plan_scan64(int64_t x, int64_t* total) {
 __global__ __launch_bounds__(kPlan) void tree_plan_kernel(CacheView c, TreeShape t, const int32_t* slots, const int32_t* count,
                                                           const int32_t* shared, TreePlan out) {
   __shared__ int s_shared[kTreeSeqs], s_lead[kTreeSeqs], s_members[kTreeSeqs];
+  __shared__ int s_blocks[2 * kTreeSeqs];
   __shared__ int64_t s_first[2 * kTreeSeqs];
   const int tid = threadIdx.x, items = t.n + t.groups;
   for (int g = tid; g < t.groups; g += kPlan) {
@@ -80,7 +82,7 @@ __global__ __launch_bounds__(kPlan) void tree_plan_kernel(CacheView c, TreeShape
     int len, live;
     look(i, len, live);
     out.live[i] = live;
-    if (!live || !shared) continue;
+    if (!live || !t.kind[0].tiles) continue;
     const int g = i / t.group;
     atomicMin(&s_shared[g], len);
     atomicMin(&s_lead[g], i);
@@ -89,16 +91,16 @@ __global__ __launch_bounds__(kPlan) void tree_plan_kernel(CacheView c, TreeShape
   __syncthreads();
   for (int g = tid; g < t.groups; g += kPlan) {
     TreeItem it{};
-    if (shared && s_members[g] > 1) {
+    if (t.kind[0].tiles && s_members[g] > 1) {
       const int pages = max(0, min(shared[g], s_shared[g] >> c.page_log2));
       it.k1 = it.seen = pages << c.page_log2;
-      it.blocks = (it.k1 + kTreeKeys - 1) / kTreeKeys;
+      it.blocks = (it.k1 + t.kind[0].keys - 1) / t.kind[0].keys;
       it.slot = slots[s_lead[g]];
     }
     it.seq = g * t.group;
     s_shared[g] = it.k1;
     out.items[g * (t.group + 1)] = it;
-    s_first[g * (t.group + 1)] = (int64_t)it.blocks * t.tiles_shared * t.hkv;
+    s_blocks[g * (t.group + 1)] = it.blocks;
   }
   __syncthreads();
   for (int i = tid; i < t.n; i += kPlan) {
@@ -112,48 +114,46 @@ __global__ __launch_bounds__(kPlan) void tree_plan_kernel(CacheView c, TreeShape
       it.k0 = s_shared[g];
       it.k1 = len + live;
       it.seen = len;
-      it.blocks = (it.k1 - it.k0 + kTreeKeys - 1) / kTreeKeys;
+      it.blocks = (it.k1 - it.k0 + t.kind[1].keys - 1) / t.kind[1].keys;
     }
     out.items[at] = it;
-    s_first[at] = (int64_t)it.blocks * t.tiles_own * t.hkv;
+    s_blocks[at] = it.blocks;
   }
-  __syncthreads();
-  constexpr int PER = 2 * kTreeSeqs / kPlan;
-  int64_t w[PER], sum = 0, total;
+  for (int cls = 0; cls < 2; ++cls) {
+    const bool takes[2] = {t.kind[0].tiles > 0 && t.kind[0].team == cls, t.kind[1].team == cls};
+    if (!takes[0] && !takes[1]) continue;
+    __syncthreads();
+    constexpr int PER = 2 * kTreeSeqs / kPlan;
+    int64_t w[PER], sum = 0, total;
 #pragma unroll
-  for (int u = 0; u < PER; ++u) {
-    const int at = tid * PER + u;
-    w[u] = at < items ? s_first[at] : 0;
-    sum += w[u];
-  }
-  int64_t before = plan_scan64(sum, &total);
-#pragma unroll
-  for (int u = 0; u < PER; ++u) {
-    const int at = tid * PER + u;
-    if (at < items) s_first[at] = out.first[at] = before;
-    before += w[u];
-  }
-  __syncthreads();
-  const int64_t run = max((int64_t)1, (total + t.waves - 1) / t.waves);
-  if (tid == 0) {
-    out.head[0] = total;
-    out.head[1] = run;
-  }
-  for (int i = tid; i < t.waves; i += kPlan) {
-    int lo = 0, hi = items - 1;  // the last item that starts at or before the wave's run (one with units)
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_first[mid] <= i * run) lo = mid;
-      else hi = mid - 1;
+    for (int u = 0; u < PER; ++u) {
+      const int at = tid * PER + u, own = at % (t.group + 1) != 0;
+      w[u] = at < items && takes[own] ? (int64_t)s_blocks[at] * t.kind[own].tiles * t.hkv : 0;
+      sum += w[u];
     }
-    out.wave_item[i] = lo;
+    int64_t before = plan_scan64(sum, &total);
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int at = tid * PER + u;
+      if (at < items) s_first[at] = out.first[cls][at] = before;
+      before += w[u];
+    }
+    __syncthreads();
+    const int64_t run = max((int64_t)1, (total + t.workers[cls] - 1) / t.workers[cls]);
+    if (tid == 0) {
+      out.head[2 * cls] = total;
+      out.head[2 * cls + 1] = run;
+    }
+    for (int i = tid; i < t.workers[cls]; i += kPlan) {
+      int lo = 0, hi = items - 1;  // the last item that starts at or before the worker's run (one with units)
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (s_first[mid] <= i * run) lo = mid;
+        else hi = mid - 1;
+      }
+      out.start_item[cls][i] = lo;
+    }
   }
-}
-
-// The number of tiles (of one head) ahead of an item's.
-__device__ __forceinline__ int tiles_before(const TreeShape& t, int g, int member) {
-  const int per = (t.tiles_shared + t.group * t.tiles_own) * t.hkv;
-  return g * per + (member < 0 ? 0 : (t.tiles_shared + member * t.tiles_own) * t.hkv);
 }
 
 template <typename T>
@@ -196,225 +196,340 @@ __device__ __forceinline__ uint64_t tree_paths(const int32_t* parents, int nodes
   return m;
 }
 
-// One head's keys of a run of blocks.
+// A worker's run of units of one item, tile and head.
 struct TreeRun {
-  int slot;    // whose table row
-  int key, k1; // from key (16-key aligned) up to k1
-  int blocks;
-  int seen;    // all rows see the keys below
+  TreeItem it;
+  int own;         // which kind of item
+  int g, tile;     // kv-head, tile of rows
+  int key, blocks; // from key on (a multiple of 16)
+  int64_t prow;    // row of its partial result
 };
 
+// The unit at `pos`, and the run from there to the item's end or `end`; `item` moves on to the
+// one that has it.
+__device__ __forceinline__ TreeRun tree_run(const TreeShape& sh, const TreePlan& plan, int cls, int worker, int64_t pos, int64_t end,
+                                            int& item) {
+  TreeRun r;
+  for (;; ++item) {
+    const int grp = item / (sh.group + 1), member = item - grp * (sh.group + 1) - 1;
+    r.own = member >= 0;
+    const TreeKind& kind = sh.kind[r.own];
+    if (kind.tiles == 0 || kind.team != cls) continue;
+    r.it = load_uniform(plan.items + item);
+    const int64_t rel = pos - plan.first[cls][item];
+    if (rel >= (int64_t)r.it.blocks * kind.tiles * sh.hkv) continue;  // none, or this one's end
+    const int j = (int)(rel / r.it.blocks), b0 = (int)(rel - (int64_t)j * r.it.blocks);
+    r.g = j / kind.tiles;
+    r.tile = j - r.g * kind.tiles;
+    r.key = r.it.k0 + kind.keys * b0;
+    r.blocks = (int)min((int64_t)(r.it.blocks - b0), end - pos);
+    const int64_t tile = (int64_t)(r.own ? r.it.seq : grp) * kind.tiles * sh.hkv + j;
+    r.prow = kind.part0 + (tile + worker) * kind.part_rows;
+    return r;
+  }
+}
+
+// A lane's row of a tile: where its query lies (-1: no such row), and the nodes that it sees.
+struct TreeRow {
+  int64_t q;
+  uint64_t tree;
+  bool fine;
+};
 template <int D, typename T>
-struct TreeRing {
-  T kv[2][2][kTreeKeys * D];  // [stage][K / V]
-};
+__device__ __forceinline__ TreeRow tree_row(const TreeShape& sh, const TreeParams<T>& p, const TreeRun& r, int row, uint64_t path,
+                                            bool path_fine) {
+  const int node_at = row / sh.G, head = r.g * sh.G + (row - node_at * sh.G);
+  const int m = r.own ? 0 : node_at / sh.nodes, node = node_at - m * sh.nodes, seq = r.it.seq + m;
+  const bool live = row < sh.kind[r.own].rows && node < p.plan.live[min(seq, sh.n - 1)];
+  TreeRow x;
+  x.q = live ? (((int64_t)seq * sh.nodes + node) * sh.hq + head) * D : -1;
+  const uint64_t tree = __shfl(path, min(node_at, 63), 64);
+  const int fine = __shfl((int)path_fine, min(node_at, 63), 64);
+  x.tree = r.own ? tree : 0;
+  x.fine = !r.own || fine;
+  return x;
+}
 
-// Walks a run with RT x 32 rows, row 32 t + ln of the tile in lanes ln and ln + 32, and leaves
-// a partial result in rows `prow` and on.
-template <int D, typename T, int RT>
-__device__ __forceinline__ void tree_walk(const CacheView& c, const TreeShape& sh, const TreeParams<T>& p,
-                                          __attribute__((address_space(3))) TreeRing<D, T>* ring,
-                                          const TreeRun& run, int g, const int64_t* qrow, const uint64_t* tree, const bool* fine,
-                                          int64_t prow) {
-  using O = Ops<T>;
-  using Frag = typename O::Frag;
-  using Dma = RowDma<T, D, 16>;
-  constexpr int NC = D / 16, HN = Dma::N, KN = 2 * HN;
-  const int lane = threadIdx.x & 63, ln = lane & 31, hf = lane >> 5;
-  const int lg = c.page_log2;
-  Dma dma;
-  dma.init(0, (int64_t)D * (sizeof(T) / 2), lane);
+// Numbers of the pages that a wave reads, 64 at a time, a lane each.
+struct TreePages {
+  const int32_t* table;
+  int last, page0, pages, lg, mask;
+  int64_t page_rows, head_row;  // rows of a page (all heads), first of the head
+  bool bad;
 
-  // numbers of 64 pages at a time, a lane each
-  const int last_page = (run.k1 - 1) >> lg;
-  const int32_t* table = c.row(run.slot);
-  bool bad = false;
-  int pages = 0, page0 = run.key >> lg;
-  auto refill = [&]() {
-    const int at = page0 + lane;
-    pages = at <= last_page ? table[at] : 0;
+  __device__ __forceinline__ void init(const CacheView& c, const TreeShape& sh, const TreeRun& r) {
+    table = c.row(r.it.slot);
+    lg = c.page_log2;
+    mask = c.page_size - 1;
+    last = (r.it.k1 - 1) >> lg;
+    page_rows = (int64_t)sh.hkv << lg;
+    head_row = (int64_t)r.g << lg;
+    bad = false;
+    page0 = r.key >> lg;
+    refill(c);
+  }
+  __device__ __forceinline__ void refill(const CacheView& c) {
+    const int at = page0 + (threadIdx.x & 63);
+    pages = at <= last ? table[at] : 0;
     if (!c.has_page(pages)) {
       bad = true;
       pages = 0;
     }
-  };
-  refill();
-  auto page_of = [&](int key) {
+  }
+  // the pool's row of a key (at most k1 - 1, and never behind an earlier one's page)
+  __device__ __forceinline__ int64_t row(const CacheView& c, int key) {
     int at = (key >> lg) - page0;
     if (at >= 64) {
       page0 += at;
       at = 0;
-      refill();
+      refill(c);
     }
-    return __builtin_amdgcn_readlane(pages, at);
-  };
-  const int64_t page_rows = (int64_t)sh.hkv << lg;  // of a page, all heads
-  struct Place {
-    int64_t a, b;  // first row of the block's two halves of 16 keys
-    int na, nb;    // keys of them
-  };
-  auto place = [&](int i) {
-    const int key = run.key + kTreeKeys * i;
-    Place x;
-    x.a = page_of(key) * page_rows + ((int64_t)g << lg) + (key & (c.page_size - 1));
-    x.na = min(16, run.k1 - key);
-    x.nb = min(16, run.k1 - key - 16);
-    x.b = x.a + 16;
-    if (x.nb <= 0) {  // nothing there: what is read instead is not seen
-      x.b = x.a;
-      x.nb = x.na;
-    } else if (c.page_size == 16) {
-      x.b = page_of(key + 16) * page_rows + ((int64_t)g << lg);
-    }
-    return x;
-  };
-  auto issue = [&](int i, int kv, const T* pool, const Place& x) {
-    T* tile = (T*)ring->kv[i & 1][kv];
-    dma_rows<true>(dma, tile, pool + x.a * D, x.na);
-    dma_rows<true>(dma, tile + 16 * D, pool + x.b * D, x.nb);
-  };
-  const int n = run.blocks;
-  Place next = place(0);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if (i < n) {
-      if (i == 1) next = place(1);
-      issue(i, 0, p.k, next);
-      issue(i, 1, p.v, next);
-    }
+    return __builtin_amdgcn_readlane(pages, at) * page_rows + head_row + (key & mask);
   }
-  Frag qf[RT][NC];
-  RowState<D> st[RT];
+};
+
+// Scores of a block of 32 keys from k0 on: those that the row does not see become -inf.
+__device__ __forceinline__ void tree_mask(f32x16& s, int k0, int seen, uint64_t tree, int hf) {
+  const int d = seen - k0;  // keys of the block that all rows see
+  uint32_t word = bits_below32(d);
+  if (d > -64 && d < 32) word |= d >= 0 ? (uint32_t)tree << d : (uint32_t)(tree >> -d);
+  word >>= 4 * hf;
 #pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    st[t].init();
+  for (int r = 0; r < 16; ++r) s[r] = keep_or_neginf(s[r], word, 8 * (r >> 2) + (r & 3));
+}
+
+template <int D, typename T>
+__device__ __forceinline__ void leave_partial(const TreeParams<T>& p, const RowState<D>& st, const TreeRow& row, int64_t at, bool bad,
+                                              int hf) {
+  const float l = half_swap_sum(st.l);
+  if (row.q < 0) return;
+  float* o = p.part + at * D + 4 * hf;
 #pragma unroll
-    for (int cc = 0; cc < NC; ++cc) qf[t][cc] = qrow[t] >= 0 ? O::load(p.q + qrow[t] + 16 * cc + 8 * hf) : Frag{};
-  }
-  for (int i = 0; i < n; ++i) {
-    // in flight behind K(i): V(i), and K and V of block i + 1 if there is one
-    if (i == 0) wait_vmem<0>();
-    else if (i + 1 < n) wait_vmem<3 * KN>();
-    else wait_vmem<KN>();
-    asm volatile("" ::: "memory");
-    const int k0 = run.key + kTreeKeys * i;
-    const T* sK = (const T*)ring->kv[i & 1][0];
-    const T* sV = (const T*)ring->kv[i & 1][1];
-    f32x16 s[RT][1];
+  for (int m = 0; m < D / 32; ++m)
 #pragma unroll
-    for (int t = 0; t < RT; ++t) s[t][0] = f32x16{};
-#pragma unroll
-    for (int cc = 0; cc < NC; ++cc) {
-      const Frag kf = O::use(O::template row8<D>(sK, ln, 2 * cc + hf));
-#pragma unroll
-      for (int t = 0; t < RT; ++t) s[t][0] = O::mma(kf, qf[t][cc], s[t][0]);
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K's reads have returned
-    if (i + 2 < n) {
-      next = place(i + 2);
-      issue(i + 2, 0, p.k, next);
-    }
-    if (k0 + kTreeKeys > run.seen) {
-      const int d = run.seen - k0;  // keys of the block that all rows see
-#pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        uint32_t word = bits_below32(d);
-        if (d > -64) word |= d >= 0 ? (d < 32 ? (uint32_t)tree[t] << d : 0u) : (uint32_t)(tree[t] >> -d);
-        word >>= 4 * hf;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[t][0][r] = keep_or_neginf(s[t][0][r], word, 8 * (r >> 2) + (r & 3));
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < RT; ++t) st[t].probabilities(s[t], p.scale_log2);
-    if (i + 2 < n) wait_vmem<3 * KN>();  // behind V(i): K and V of i + 1, K of i + 2
-    else if (i + 1 < n) wait_vmem<2 * KN>();
-    else wait_vmem<0>();
-    asm volatile("" ::: "memory");
-#pragma unroll
-    for (int ch = 0; ch < 2; ++ch) {
-      Frag pb[RT];
-#pragma unroll
-      for (int t = 0; t < RT; ++t) pb[t] = O::from_acc(s[t][0], ch);
-#pragma unroll
-      for (int m = 0; m < D / 32; ++m) {
-        const Frag vf = O::template tr8<D>(sV, 16 * ch, 32 * m, lane);
-#pragma unroll
-        for (int t = 0; t < RT; ++t) st[t].o[m] = O::mma(vf, pb[t], st[t].o[m]);
-      }
-    }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V's too
-    if (i + 2 < n) issue(i + 2, 1, p.v, next);
-  }
-  bad = wave_any(bad);
-#pragma unroll
-  for (int t = 0; t < RT; ++t) {
-    const float l = half_swap_sum(st[t].l);
-    if (qrow[t] < 0) continue;
-    const int64_t row = prow + 32 * t + ln;
-    float* o = p.part + row * D + 4 * hf;
-#pragma unroll
-    for (int m = 0; m < D / 32; ++m)
-#pragma unroll
-      for (int r4 = 0; r4 < 4; ++r4)
-        *reinterpret_cast<f32x4*>(o + 32 * m + 8 * r4) =
-            f32x4{st[t].o[m][4 * r4], st[t].o[m][4 * r4 + 1], st[t].o[m][4 * r4 + 2], st[t].o[m][4 * r4 + 3]};
-    if (hf == 0) {
-      p.part_ml[2 * row] = st[t].m_ref;
-      p.part_ml[2 * row + 1] = bad || !fine[t] ? __builtin_nanf("") : l;
-    }
+    for (int r4 = 0; r4 < 4; ++r4)
+      *reinterpret_cast<f32x4*>(o + 32 * m + 8 * r4) =
+          f32x4{st.o[m][4 * r4], st.o[m][4 * r4 + 1], st.o[m][4 * r4 + 2], st.o[m][4 * r4 + 3]};
+  if (hf == 0) {
+    p.part_ml[2 * at] = st.m_ref;
+    p.part_ml[2 * at + 1] = bad || !row.fine ? __builtin_nanf("") : l;
   }
 }
 
-template <int D, typename T, int RT>
-__global__ __launch_bounds__(64, 2) void tree_attn_kernel(CacheView c, TreeShape sh, TreeParams<T> p) {
-  __shared__ __attribute__((aligned(1024))) TreeRing<D, T> ring;
-  const int w = blockIdx.x, lane = threadIdx.x & 63, ln = lane & 31;
+// Two stages of keys and values.  The DMA goes by byte addresses in LDS: a generic pointer,
+// carried round the kernels' outer loops, is checked for null where it is turned back, in a
+// form that the compiler cannot encode.
+template <typename T, int N>
+struct TreeRing {
+  T kv[2][2][N];  // [stage][K / V]
+};
+template <typename X>
+__device__ __forceinline__ __attribute__((address_space(3))) X* in_lds(X* x) {
+  return (__attribute__((address_space(3))) X*)x;
+}
+// Rows of a tile at LDS byte `to` (the DMA's first row included), as dma_rows; ONCE: nobody reads
+// them again.
+template <bool ONCE, int RD, int NR, typename T>
+__device__ __forceinline__ void dma_rows_at(const TileDma<RD, NR>& d, unsigned to, const T* src, int rows_valid) {
+  using Dma = TileDma<RD, NR>;
+  const char* base = reinterpret_cast<const char*>(src);
+#pragma unroll
+  for (int i = 0; i < Dma::N; ++i) {
+    const uint32_t rs = (uint32_t)min(d.row_of(i), rows_valid - 1);
+    lds_dma16_at<ONCE>(base + (rs * d.stride_b + d.chunk_b(i)), to + i * 1024);
+  }
+}
+
+// Up to 32 rows, row ln in lanes ln and ln + 32.
+template <int D, typename T>
+__global__ __launch_bounds__(64, 2) void tree_solo_kernel(CacheView c, TreeShape sh, TreeParams<T> p) {
+  using O = Ops<T>;
+  using Frag = typename O::Frag;
+  using Dma = RowDma<T, D, 16>;
+  constexpr int NC = D / 16, KN = 2 * Dma::N;
+  __shared__ __attribute__((aligned(1024))) TreeRing<T, kSoloKeys * D> smem;
+  auto* ring = in_lds(&smem);
+  const int worker = blockIdx.x, lane = threadIdx.x & 63, ln = lane & 31, hf = lane >> 5;
   const int64_t total = p.plan.head[0], run_len = p.plan.head[1];
-  int64_t pos = w * run_len;
+  int64_t pos = worker * run_len;
   const int64_t end = min(pos + run_len, total);
   if (pos >= end) return;
-  int item = scalar_load(p.plan.wave_item + w);
+  int item = scalar_load(p.plan.start_item[0] + worker);
+  Dma dma;
+  dma.init(0, (int64_t)D * (sizeof(T) / 2), lane);
   while (pos < end) {
-    const TreeItem it = load_uniform(p.plan.items + item);
-    const int64_t rel = pos - p.plan.first[item];
-    const int grp = item / (sh.group + 1), member = item - grp * (sh.group + 1) - 1;
-    const int tiles = member < 0 ? sh.tiles_shared : sh.tiles_own, rows = member < 0 ? sh.rows_shared : sh.rows_own;
-    if (rel >= (int64_t)it.blocks * tiles * sh.hkv) {  // the next item (one without units, or this one's end)
-      ++item;
-      continue;
+    const TreeRun r = tree_run(sh, p.plan, 0, worker, pos, end, item);
+    TreePages pages;
+    pages.init(c, sh, r);
+    struct Place {
+      int64_t a, b;  // first row of the block's two halves of 16 keys
+      int na, nb;    // keys of them
+    };
+    auto place = [&](int i) {
+      const int key = r.key + kSoloKeys * i;
+      Place x;
+      x.a = pages.row(c, key);
+      x.na = min(16, r.it.k1 - key);
+      x.nb = min(16, r.it.k1 - key - 16);
+      x.b = x.a + 16;
+      if (x.nb <= 0) {  // nothing there: what is read instead is not seen
+        x.b = x.a;
+        x.nb = x.na;
+      } else if (c.page_size == 16) {
+        x.b = pages.row(c, key + 16);
+      }
+      return x;
+    };
+    auto issue = [&](int i, int kv, const T* pool, const Place& x) {
+      const unsigned tile = (unsigned)(uintptr_t)&ring->kv[i & 1][kv][0];
+      dma_rows_at<true>(dma, tile, pool + x.a * D, x.na);
+      dma_rows_at<true>(dma, tile + 16 * D * sizeof(T), pool + x.b * D, x.nb);
+    };
+    const int n = r.blocks;
+    Place next = place(0);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (i < n) {
+        if (i == 1) next = place(1);
+        issue(i, 0, p.k, next);
+        issue(i, 1, p.v, next);
+      }
     }
-    const int j = (int)(rel / it.blocks), b0 = (int)(rel - (int64_t)j * it.blocks);
-    const int g = j / tiles, tile = j - g * tiles;
-    TreeRun run;
-    run.slot = it.slot;
-    run.key = it.k0 + kTreeKeys * b0;
-    run.k1 = it.k1;
-    run.blocks = (int)min((int64_t)(it.blocks - b0), end - pos);
-    run.seen = it.seen;
     bool path_fine = true;
     uint64_t path = 0;
-    if (member >= 0) path = tree_paths(p.parents ? p.parents + (int64_t)it.seq * sh.nodes : nullptr, sh.nodes, lane, path_fine);
-    int64_t qrow[RT];
-    uint64_t tree[RT];
-    bool fine[RT];
-    const int in_tile = min(rows - tile * 32 * RT, 32 * RT);
+    if (r.own) path = tree_paths(p.parents ? p.parents + (int64_t)r.it.seq * sh.nodes : nullptr, sh.nodes, lane, path_fine);
+    const TreeRow row = tree_row<D>(sh, p, r, ln, path, path_fine);
+    Frag qf[NC];
+    RowState<D> st;
+    st.init();
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-      const int r = 32 * t + ln, row = tile * 32 * RT + r;
-      const int node_at = row / sh.G, head = g * sh.G + (row - node_at * sh.G);
-      const int m = member < 0 ? node_at / sh.nodes : 0, node = node_at - m * sh.nodes;
-      const int seq = it.seq + m;
-      const bool live = r < in_tile && node < p.plan.live[min(seq, sh.n - 1)];
-      qrow[t] = live ? (((int64_t)seq * sh.nodes + node) * sh.hq + head) * D : -1;
-      const int from = member < 0 ? 0 : min(node_at, 63);
-      tree[t] = __shfl(path, from, 64);
-      fine[t] = member < 0 || __shfl((int)path_fine, from, 64);
-      if (member < 0) tree[t] = 0;
+    for (int cc = 0; cc < NC; ++cc) qf[cc] = row.q >= 0 ? O::load(p.q + row.q + 16 * cc + 8 * hf) : Frag{};
+    for (int i = 0; i < n; ++i) {
+      // in flight behind K(i): V(i), and K and V of block i + 1 if there is one
+      if (i == 0) wait_vmem<0>();
+      else if (i + 1 < n) wait_vmem<3 * KN>();
+      else wait_vmem<KN>();
+      asm volatile("" ::: "memory");
+      const int k0 = r.key + kSoloKeys * i;
+      const T* sK = (const T*)ring->kv[i & 1][0];
+      const T* sV = (const T*)ring->kv[i & 1][1];
+      f32x16 s[1] = {f32x16{}};
+#pragma unroll
+      for (int cc = 0; cc < NC; ++cc) s[0] = O::mma(O::use(O::template row8<D>(sK, ln, 2 * cc + hf)), qf[cc], s[0]);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // K's reads have returned
+      if (i + 2 < n) {
+        next = place(i + 2);
+        issue(i + 2, 0, p.k, next);
+      }
+      if (k0 + kSoloKeys > r.it.seen) tree_mask(s[0], k0, r.it.seen, row.tree, hf);
+      st.probabilities(s, p.scale_log2);
+      if (i + 2 < n) wait_vmem<3 * KN>();  // behind V(i): K and V of i + 1, K of i + 2
+      else if (i + 1 < n) wait_vmem<2 * KN>();
+      else wait_vmem<0>();
+      asm volatile("" ::: "memory");
+#pragma unroll
+      for (int ch = 0; ch < 2; ++ch) {
+        const Frag pb = O::from_acc(s[0], ch);
+#pragma unroll
+        for (int m = 0; m < D / 32; ++m) st.o[m] = O::mma(O::template tr8<D>(sV, 16 * ch, 32 * m, lane), pb, st.o[m]);
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // V's too
+      if (i + 2 < n) issue(i + 2, 1, p.v, next);
     }
-    const int64_t prow = (int64_t)(tiles_before(sh, grp, member) + j + w) * sh.part_rows;
-    tree_walk<D, T, RT>(c, sh, p, (__attribute__((address_space(3))) TreeRing<D, T>*)&ring, run, g, qrow, tree, fine, prow);
-    pos += run.blocks;
+    leave_partial<D>(p, st, row, r.prow + ln, wave_any(pages.bad), hf);
+    pos += r.blocks;
+  }
+}
+
+// Tiles of 128 rows: four waves of 32, which fetch a quarter of every block each.
+template <int D, typename T>
+__global__ __launch_bounds__(kTeamWaves * 64, (kTreeTeam<D, T>)) void tree_team_kernel(CacheView c, TreeShape sh, TreeParams<T> p) {
+  using O = Ops<T>;
+  using Frag = typename O::Frag;
+  constexpr int BN = kTeamKeys<T>, KB = BN / 32, RPW = BN / kTeamWaves, NC = D / 16, NI = KB * NC, PD = 3;
+  using Dma = RowDma<T, D, RPW>;
+  __shared__ __attribute__((aligned(1024))) TreeRing<T, BN * D> smem;
+  auto* ring = in_lds(&smem);
+  const int worker = blockIdx.x, tid = threadIdx.x, lane = tid & 63, ln = lane & 31, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int64_t total = p.plan.head[2], run_len = p.plan.head[3];
+  int64_t pos = worker * run_len;
+  const int64_t end = min(pos + run_len, total);
+  if (pos >= end) return;
+  int item = scalar_load(p.plan.start_item[1] + worker);
+  Dma dma;
+  dma.init(wave * RPW, (int64_t)D * (sizeof(T) / 2), lane);
+  for (bool first = true; pos < end; first = false) {
+    const TreeRun r = tree_run(sh, p.plan, 1, worker, pos, end, item);
+    TreePages pages;
+    pages.init(c, sh, r);
+    auto issue = [&](int t) {
+      // this wave's rows of the block lie in one page; past the last key it fetches the block's first ones again
+      const int key = r.key + BN * t, mine = key + wave * RPW;
+      const int64_t at = pages.row(c, mine < r.it.k1 ? mine : key);
+      const int rows = mine < r.it.k1 ? min(RPW, r.it.k1 - mine) : min(RPW, r.it.k1 - key);
+      const int64_t base = (at - wave * RPW) * D;  // (the DMA adds the wave's first row)
+      const unsigned tile = (unsigned)(uintptr_t)&ring->kv[t & 1][0][wave * RPW * D];
+      dma_rows_at<false>(dma, tile, p.k + base, wave * RPW + rows);
+      dma_rows_at<false>(dma, tile + BN * D * sizeof(T), p.v + base, wave * RPW + rows);
+    };
+    if (!first) __syncthreads();  // the ring is free
+    issue(0);
+    bool path_fine = true;
+    uint64_t path = 0;
+    if (r.own) path = tree_paths(p.parents ? p.parents + (int64_t)r.it.seq * sh.nodes : nullptr, sh.nodes, lane, path_fine);
+    const TreeRow row = tree_row<D>(sh, p, r, r.tile * kTeamRows + wave * 32 + ln, path, path_fine);
+    const bool some = wave_any(row.q >= 0);
+    Frag qf[NC];
+    RowState<D> st;
+    st.init();
+#pragma unroll
+    for (int cc = 0; cc < NC; ++cc) qf[cc] = row.q >= 0 ? O::load(p.q + row.q + 16 * cc + 8 * hf) : Frag{};
+    const int n = r.blocks;
+    for (int t = 0; t < n; ++t) {
+      wait_vmem<0>();
+      __syncthreads();  // block t has landed for every wave; the stage of block t - 1 is free
+      if (t + 1 < n) issue(t + 1);
+      if (!some) continue;
+      const int k0 = r.key + BN * t;
+      const T* sK = (const T*)ring->kv[t & 1][0];
+      const T* sV = (const T*)ring->kv[t & 1][1];
+      f32x16 s[KB];
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) s[kb] = f32x16{};
+      Frag a[PD + 1];  // K's fragments, read ahead
+#pragma unroll
+      for (int x = 0; x < PD; ++x) a[x] = O::use(O::template row8<D>(sK, (x / NC) * 32 + ln, 2 * (x % NC) + hf));
+#pragma unroll
+      for (int x = 0; x < NI; ++x) {
+        if (x + PD < NI) a[(x + PD) % (PD + 1)] = O::use(O::template row8<D>(sK, ((x + PD) / NC) * 32 + ln, 2 * ((x + PD) % NC) + hf));
+        s[x / NC] = O::mma(a[x % (PD + 1)], qf[x % NC], s[x / NC]);
+      }
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int x = 0; x < PD; ++x) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+#pragma unroll
+        for (int x = 0; x < NI; ++x) {
+          if (x + PD < NI) __builtin_amdgcn_sched_group_barrier(kSchedDsRead, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
+        }
+      }
+      if (k0 + BN > r.it.seen) {
+#pragma unroll
+        for (int kb = 0; kb < KB; ++kb) tree_mask(s[kb], k0 + 32 * kb, r.it.seen, row.tree, hf);
+      }
+      st.probabilities(s, p.scale_log2);
+#pragma unroll
+      for (int ch = 0; ch < 2 * KB; ++ch) {
+        const Frag pb = O::from_acc(s[ch >> 1], ch & 1);
+#pragma unroll
+        for (int m = 0; m < D / 32; ++m) st.o[m] = O::mma(O::template tr8<D>(sV, 16 * ch, 32 * m, lane), pb, st.o[m]);
+      }
+    }
+    // a page that is none may be another wave's
+    const bool bad = __syncthreads_or(pages.bad);
+    leave_partial<D>(p, st, row, r.prow + wave * 32 + ln, bad, hf);
+    pos += r.blocks;
   }
 }
 
@@ -431,25 +546,25 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeShape sh, TreePar
   const int seq = (int)(tok / sh.nodes), node = (int)(tok - (int64_t)seq * sh.nodes);
   const int grp = seq / sh.group, member = seq - grp * sh.group;
   const int g = head / sh.G, h = head - g * sh.G;
-  const int64_t run = p.plan.head[1];
   const int own = seq + grp + 1;
   f32x4 acc = f32x4{};
   float m = kNegInf, l = 0.f;
   if (node < p.plan.live[seq]) {
-    auto join = [&](int item, int who, int tiles, int row) {
+    auto join = [&](int item, const TreeKind& kind, int64_t tile0, int row) {
       const int blocks = p.plan.items[item].blocks;
       if (blocks == 0) return;
-      const int j = g * tiles + row / sh.tile_rows;
-      const int64_t from = p.plan.first[item] + (int64_t)j * blocks;
+      const int per = kind.team ? kTeamRows : kSoloRows;
+      const int j = g * kind.tiles + row / per;
+      const int64_t run = p.plan.head[2 * kind.team + 1], from = p.plan.first[kind.team][item] + (int64_t)j * blocks;
       const int64_t w0 = from / run, parts = (from + blocks - 1) / run - w0 + 1;
-      int64_t prow = (tiles_before(sh, grp, who) + j + w0) * sh.part_rows + row % sh.tile_rows;
-      for (int64_t n0 = 0; n0 < parts; n0 += NP, prow += (int64_t)NP * sh.part_rows) {
+      int64_t prow = kind.part0 + (tile0 + j + w0) * kind.part_rows + row % per;
+      for (int64_t n0 = 0; n0 < parts; n0 += NP, prow += (int64_t)NP * kind.part_rows) {
         f32x4 x[NP];
         float pm[NP], pl[NP];
 #pragma unroll
         for (int n = 0; n < NP; ++n) {
           const bool on = n0 + n < parts;
-          const int64_t r = prow + (on ? n : 0) * sh.part_rows;
+          const int64_t r = prow + (on ? n : 0) * (int64_t)kind.part_rows;
           x[n] = *reinterpret_cast<const f32x4*>(p.part + r * D + col);
           pm[n] = p.part_ml[2 * r];
           pl[n] = on ? p.part_ml[2 * r + 1] : 0.f;
@@ -465,8 +580,9 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeShape sh, TreePar
         }
       }
     };
-    if (sh.tiles_shared) join(own - member - 1, -1, sh.tiles_shared, (member * sh.nodes + node) * sh.G + h);
-    join(own, member, sh.tiles_own, node * sh.G + h);
+    const TreeKind &ks = sh.kind[0], &ko = sh.kind[1];
+    if (ks.tiles) join(own - member - 1, ks, (int64_t)grp * ks.tiles * sh.hkv, (member * sh.nodes + node) * sh.G + h);
+    join(own, ko, (int64_t)seq * ko.tiles * sh.hkv, node * sh.G + h);
   } else if (node < p.plan.items[own].bad) {
     l = __builtin_nanf("");
   }
@@ -490,15 +606,18 @@ hipError_t launch_tree_t(const CacheView& c, const TreeLaunch& a, hipStream_t s)
   p.part = a.part;
   p.part_ml = a.part_ml;
   p.scale_log2 = a.scale * kLog2e;
-  {
-    TimingScope t("pp_tree_attn_fwd", s);
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(sh.waves), dim3(64), 0, s, c, sh, p); };
-    if constexpr (kTreeTiles<T> > 1) {
-      if (sh.tile_rows > 32) launch(tree_attn_kernel<D, T, kTreeTiles<T>>);
-      else launch(tree_attn_kernel<D, T, 1>);
-    } else {
-      launch(tree_attn_kernel<D, T, 1>);
-    }
+  bool takes[2] = {false, false};
+  for (const TreeKind& k : sh.kind)
+    if (k.tiles) takes[k.team] = true;
+  if (takes[1]) {
+    TimingScope t("pp_tree_attn_team", s);
+    hipLaunchKernelGGL((tree_team_kernel<D, T>), dim3(sh.workers[1]), dim3(kTeamWaves * 64), 0, s, c, sh, p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (takes[0]) {
+    TimingScope t("pp_tree_attn_solo", s);
+    hipLaunchKernelGGL((tree_solo_kernel<D, T>), dim3(sh.workers[0]), dim3(64), 0, s, c, sh, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
