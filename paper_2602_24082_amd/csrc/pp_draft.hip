@@ -51,35 +51,37 @@ template <>
 __device__ __forceinline__ float lowest<float>() {
   return -3.4028234663852886e38f;
 }
+template <typename T>
+constexpr uint32_t kInfBits = sizeof(T) == 2 ? 0x7f80u : 0x7f800000u;
 
-// e^y for y <= 0 in 64 bits: e^y = 2^n e^r, |r| <= ln 2 / 2, by the series of e^r through r^13
-// (the rest is below 2^-57 of it).
-__device__ __forceinline__ double exp_neg(double y) {
-  const double n = rint(fmax(y, -1000.0) * 1.4426950408889634);
-  double r = fma(n, -0.6931471805599453, fmax(y, -1000.0));
-  r = fma(n, -2.3190468138462996e-17, r);  // ln 2 less its 64-bit value
-  double s = 1.0 / 6227020800.0;
-  s = fma(s, r, 1.0 / 479001600.0);
-  s = fma(s, r, 1.0 / 39916800.0);
-  s = fma(s, r, 1.0 / 3628800.0);
-  s = fma(s, r, 1.0 / 362880.0);
-  s = fma(s, r, 1.0 / 40320.0);
-  s = fma(s, r, 1.0 / 5040.0);
-  s = fma(s, r, 1.0 / 720.0);
-  s = fma(s, r, 1.0 / 120.0);
-  s = fma(s, r, 1.0 / 24.0);
-  s = fma(s, r, 1.0 / 6.0);
-  s = fma(s, r, 0.5);
-  s = fma(s, r, 1.0);
-  s = fma(s, r, 1.0);
-  return ldexp(s, (int)n);
+// 2^t for t <= 0 in 64 bits: 2^n by the exponent's bits, 2^f, |f| <= 1/2, by the polynomial of
+// degree 9 through Chebyshev's points, good to 2e-14 of it (degree 14 of the series takes five
+// more multiplications).  n comes out of the low bits of t + 1.5 2^52.  Below 2^-1000, and for
+// -inf and NaN, 2^-1000.
+constexpr double kTiny = -1000.0;
+__device__ __forceinline__ double exp2_neg(double t) {
+  t = fmax(t, kTiny);
+  const double u = t + 6755399441055744.0;
+  const double f = t - (u - 6755399441055744.0);
+  double s = 1.0205757125041537e-07;
+  s = fma(s, f, 1.325968083523609e-06);
+  s = fma(s, f, 1.5252674538194317e-05);
+  s = fma(s, f, 0.00015403433618713555);
+  s = fma(s, f, 0.001333355819593412);
+  s = fma(s, f, 0.009618129194074796);
+  s = fma(s, f, 0.05550410866470368);
+  s = fma(s, f, 0.2402265069563986);
+  s = fma(s, f, 0.6931471805599446);
+  s = fma(s, f, 1.0000000000000135);
+  return __hiloint2double(__double2hiint(s) + (__double2loint(u) << 20), __double2loint(s));
 }
 
 // A thread's entries of one chunk of a row: load u holds entries at(u) .. + kVec - 1, -inf
-// where masked or outside the row.  Loads lie on the row's 16-byte boundaries; those that
-// reach over an end of the row are taken entry by entry.
+// outside the row.  Loads lie on the row's 16-byte boundaries; those that reach over an end of
+// the row are taken entry by entry.
 template <typename T>
 struct ChunkOf {
+  typedef T Raw __attribute__((ext_vector_type(kVec<T>)));
   const T* row;
   int64_t first;  // entry of the thread's first load
   int vocab;
@@ -91,20 +93,39 @@ struct ChunkOf {
     first = (int64_t)chunk * kDraftChunk + thread * kVec<T> - ahead;
   }
   __device__ __forceinline__ int64_t at(int u) const { return first + (int64_t)u * kThreads * kVec<T>; }
-  __device__ __forceinline__ void load(int u, float (&x)[kVec<T>]) const {
+  __device__ __forceinline__ Raw load(int u) const {
     const int64_t e = at(u);
-    if (e >= 0 && e + kVec<T> <= vocab) {
-      typedef T Raw __attribute__((ext_vector_type(kVec<T>)));
-      const Raw v = *reinterpret_cast<const Raw*>(row + e);
+    if (e >= 0 && e + kVec<T> <= vocab) return *reinterpret_cast<const Raw*>(row + e);
+    Raw x;
+    const T none = sizeof(T) == 2 ? (T)0xff80 : (T)kNegInf;
 #pragma unroll
-      for (int i = 0; i < kVec<T>; ++i) x[i] = to_float(v[i]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kVec<T>; ++i) x[i] = e + i >= 0 && e + i < vocab ? to_float(row[e + i]) : kNegInf;
-    }
-#pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) x[i] = x[i] == lowest<T>() ? kNegInf : x[i];
+    for (int i = 0; i < kVec<T>; ++i) x[i] = e + i >= 0 && e + i < vocab ? row[e + i] : none;
+    return x;
   }
+};
+
+// The largest of the entries' bits without their signs: NaN and infinities lie at the top.
+__device__ __forceinline__ void track_bits(ChunkOf<uint16_t>::Raw& most, const ChunkOf<uint16_t>::Raw& x) {
+  most = __builtin_elementwise_max(most, x & (uint16_t)0x7fff);
+}
+__device__ __forceinline__ void track_bits(uint32_t& most, const ChunkOf<float>::Raw& x) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+}
+__device__ __forceinline__ uint32_t most_bits(const ChunkOf<uint16_t>::Raw& m) {
+  uint32_t r = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r = max(r, (uint32_t)m[i]);
+  return r;
+}
+__device__ __forceinline__ uint32_t most_bits(uint32_t m) { return m; }
+template <typename T>
+struct BitsOf {
+  using Type = uint32_t;
+};
+template <>
+struct BitsOf<uint16_t> {
+  using Type = ChunkOf<uint16_t>::Raw;
 };
 
 __device__ __forceinline__ double wave_sum_d(double x) {
@@ -141,72 +162,81 @@ __device__ __forceinline__ TreeOf tree_of(const DraftShape& d, const int32_t* pa
   return t;
 }
 
+// log2(e) / T.  T is taken as at most 10^6, where masked entries still come out as 0.
 __device__ __forceinline__ double inv_temp(const float* temperature, int s) {
   const double t = temperature ? (double)temperature[s] : 1.0;
-  return t > 0 ? 1.0 / t : 1.0;
+  return 1.4426950408889634 / (t > 0 ? fmin(t, 1e6) : 1.0);
 }
 __device__ __forceinline__ bool greedy(const float* temperature, int s) { return temperature && !(temperature[s] > 0); }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
   __shared__ float s_m[kWavesD];
-  __shared__ int s_arg[kWavesD];
+  __shared__ int s_arg[kWavesD], s_bad[kWavesD];
   __shared__ double s_sum[kWavesD];
-  __shared__ int s_bad;
   const DraftShape& d = p.shape;
   const int row = blockIdx.y, chunk = blockIdx.x, s = row / d.nodes, node = row - s * d.nodes;
-  const bool is_draft = blockIdx.z != 0;
+  const bool is_draft = blockIdx.z != 0, argmax = greedy(p.temperature, s);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = max(0, min(p.count ? p.count[s] : d.nodes, d.nodes));
   if (node >= n) return;
   if (is_draft) {
-    if (greedy(p.temperature, s)) return;
+    if (argmax) return;
     bool kid = false;  // only nodes with children have drafts
     for (int j = node + 1 + lane; j < n; j += 64)
       kid = kid || (p.parents ? p.parents[(int64_t)s * d.nodes + j] == node : j == node + 1);
     if (!__any(kid)) return;
   }
-  if (tid == 0) s_bad = 0;
   ChunkOf<T> c;
   c.init((const T*)(is_draft ? p.draft : p.target) + (int64_t)row * d.vocab, d.vocab, chunk, tid);
-  float x[kLoads<T>][kVec<T>];
+  typename ChunkOf<T>::Raw x[kLoads<T>];
 #pragma unroll
-  for (int u = 0; u < kLoads<T>; ++u) c.load(u, x[u]);
+  for (int u = 0; u < kLoads<T>; ++u) x[u] = c.load(u);
   float m = kNegInf;
-  int arg = 0x7fffffff;
-  bool bad = false;
+  typename BitsOf<T>::Type bits{};
 #pragma unroll
-  for (int u = 0; u < kLoads<T>; ++u)
+  for (int u = 0; u < kLoads<T>; ++u) {
+    track_bits(bits, x[u]);
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) {
-      bad = bad || !(x[u][i] < -kNegInf);  // NaN and +inf
-      if (x[u][i] > m) {
-        m = x[u][i];
-        arg = (int)(c.at(u) + i);
-      }
-    }
-  const float wm = wave_max(m);
-  int wa = m == wm ? arg : 0x7fffffff;
-  for (int off = 32; off > 0; off >>= 1) wa = min(wa, __shfl_xor(wa, off, 64));
+    for (int i = 0; i < kVec<T>; ++i) m = fmaxf(m, to_float(x[u][i]));
+  }
+  m = wave_max(m);
+  const bool nan = __any(most_bits(bits) > kInfBits<T>);
   if (lane == 0) {
-    s_m[wave] = wm;
-    s_arg[wave] = wa;
+    s_m[wave] = m;
+    s_bad[wave] = nan;
   }
   __syncthreads();
-  if (bad) s_bad = 1;
   float top = kNegInf;
+  bool bad = false;
 #pragma unroll
-  for (int w = 0; w < kWavesD; ++w) top = fmaxf(top, s_m[w]);
-  const double it = inv_temp(p.temperature, s);
+  for (int w = 0; w < kWavesD; ++w) {
+    top = fmaxf(top, s_m[w]);
+    bad = bad || s_bad[w];
+  }
+  bad = bad || top == -kNegInf;
+  const double a = inv_temp(p.temperature, s), b = -(double)top * a;
   double sum = 0;
-  if (top > kNegInf) {
+  int arg = 0x7fffffff;
+  if (top > lowest<T>() && !bad) {
 #pragma unroll
     for (int u = 0; u < kLoads<T>; ++u)
 #pragma unroll
-      for (int i = 0; i < kVec<T>; ++i) sum += x[u][i] > kNegInf ? exp_neg(((double)x[u][i] - (double)top) * it) : 0.0;
+      for (int i = 0; i < kVec<T>; ++i) sum += exp2_neg(fma((double)to_float(x[u][i]), a, b));
+    sum = wave_sum_d(sum);
+    if (argmax) {
+#pragma unroll
+      for (int u = 0; u < kLoads<T>; ++u)
+#pragma unroll
+        for (int i = 0; i < kVec<T>; ++i)
+          if (to_float(x[u][i]) == top) arg = min(arg, (int)(c.at(u) + i));
+      for (int off = 32; off > 0; off >>= 1) arg = min(arg, __shfl_xor(arg, off, 64));
+    }
   }
-  sum = wave_sum_d(sum);
-  if (lane == 0) s_sum[wave] = sum;
+  if (lane == 0) {
+    s_sum[wave] = sum;
+    s_arg[wave] = arg;
+  }
   __syncthreads();
   if (tid == 0) {
     DraftPart out;
@@ -214,19 +244,24 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
     out.arg = 0x7fffffff;
     for (int w = 0; w < kWavesD; ++w) {
       out.sum += s_sum[w];
-      if (s_m[w] == top) out.arg = min(out.arg, s_arg[w]);
+      out.arg = min(out.arg, s_arg[w]);
     }
-    out.max = s_bad ? __builtin_nanf("") : top;
+    out.max = bad ? __builtin_nanf("") : top > lowest<T>() ? top : kNegInf;
     p.part[((int64_t)blockIdx.z * d.n * d.nodes + row) * d.chunks + chunk] = out;
   }
 }
 
-// A row's distribution: e^((x - max) / T) / sum.
+// A row's distribution, 2^(a x + b) / sum, a = log2(e) / T.
 struct RowDist {
+  double a, b, sum;
   float max;
-  double sum;
   int arg;
   bool usable;
+  // e^((x - max) / T); 0 where masked (or below 2^-999)
+  __device__ __forceinline__ double raw(float x) const {
+    const double t = fma((double)x, a, b);
+    return t > kTiny + 1 ? exp2_neg(t) : 0.0;
+  }
 };
 // By a wave, from the parts of the row's chunks.
 __device__ __forceinline__ RowDist row_dist(const DraftPart* part, int chunks, double it, int lane) {
@@ -240,12 +275,14 @@ __device__ __forceinline__ RowDist row_dist(const DraftPart* part, int chunks, d
   RowDist r;
   r.max = wave_max(m);
   r.usable = !__any(bad) && r.max > kNegInf;
+  r.a = it;
+  r.b = -(double)r.max * it;
   double s = 0;
   int arg = 0x7fffffff;
   if (r.usable)
     for (int c = lane; c < chunks; c += 64) {
       const float x = part[c].max;
-      if (x > kNegInf) s += part[c].sum * exp_neg(((double)x - (double)r.max) * it);
+      if (x > kNegInf) s += part[c].sum * r.raw(x);
       if (x == r.max) arg = min(arg, part[c].arg);
     }
   r.sum = wave_sum_d(s);
@@ -253,47 +290,68 @@ __device__ __forceinline__ RowDist row_dist(const DraftPart* part, int chunks, d
   r.arg = arg;
   return r;
 }
-__device__ __forceinline__ double prob(float x, const RowDist& r, double it) {
-  return x > kNegInf ? exp_neg(((double)x - (double)r.max) * it) / r.sum : 0.0;
-}
-__device__ __forceinline__ double weight(float x, const RowDist& r, double it, double inv_sum) {
-  return x > kNegInf ? exp_neg(((double)x - (double)r.max) * it) * inv_sum : 0.0;
-}
 
-// Sum over a chunk of max(p - a q, 0), valid in thread 0.
+// What is left of a row's distribution: max(p - a q, 0), or p where there is no q.
 template <typename T>
-__device__ __forceinline__ double residual_sum(const DraftParams& p, int row, int chunk, const RowDist& tp, const RowDist& tq, double a,
-                                               double it, double* s_sum) {
-  const DraftShape& d = p.shape;
-  const int tid = threadIdx.x;
-  ChunkOf<T> c;
-  double sum = 0;
-  const double ip = 1.0 / tp.sum, iq = a / tq.sum;
-  // the two rows may lie differently on 16-byte boundaries: entries are taken where the target's lie
-  c.init((const T*)p.target + (int64_t)row * d.vocab, d.vocab, chunk, tid);
-  const T* q = (const T*)p.draft + (int64_t)row * d.vocab;
-  const bool alike = ((reinterpret_cast<uintptr_t>(q) ^ reinterpret_cast<uintptr_t>(c.row)) & 15) == 0;
-  ChunkOf<T> cq = c;
-  cq.row = q;
-  for (int u = 0; u < kLoads<T>; ++u) {
-    float x[kVec<T>], y[kVec<T>];
-    c.load(u, x);
-    if (alike) {
-      cq.load(u, y);
-    } else {
+struct LeftOf {
+  ChunkOf<T> c;   // the target's row
+  const T* q;     // or null
+  RowDist tp, tq;
+  double ip, iq;  // 1 / sum, a / sum
+  bool alike;     // the rows lie alike on 16-byte boundaries
+
+  __device__ __forceinline__ void init(const DraftParams& p, int64_t row, int chunk, const RowDist& p_, const RowDist& q_, double a) {
+    tp = p_;
+    tq = q_;
+    c.init((const T*)p.target + row * p.shape.vocab, p.shape.vocab, chunk, threadIdx.x);
+    q = a > 0 ? (const T*)p.draft + row * p.shape.vocab : nullptr;
+    ip = 1.0 / tp.sum;
+    iq = a > 0 ? a / tq.sum : 0.0;
+    alike = ((reinterpret_cast<uintptr_t>(q) ^ reinterpret_cast<uintptr_t>(c.row)) & 15) == 0;
+  }
+  __device__ __forceinline__ double of(float x, float y) const {
+    const double w = tp.raw(x) * ip;
+    return q ? fmax(fma(-tq.raw(y), iq, w), 0.0) : w;
+  }
+  // weights of load u's entries
+  __device__ __forceinline__ void load(int u, double (&w)[kVec<T>]) const {
+    const typename ChunkOf<T>::Raw x = c.load(u);
+    typename ChunkOf<T>::Raw y = x;
+    if (q) {
+      if (alike) {
+        ChunkOf<T> cq = c;
+        cq.row = q;
+        y = cq.load(u);
+      } else {
 #pragma unroll
-      for (int i = 0; i < kVec<T>; ++i) {
-        const int64_t e = c.at(u) + i;
-        y[i] = e >= 0 && e < d.vocab ? to_float(q[e]) : kNegInf;
-        y[i] = y[i] == lowest<T>() ? kNegInf : y[i];
+        for (int i = 0; i < kVec<T>; ++i) {
+          const int64_t e = c.at(u) + i;
+          if (e >= 0 && e < c.vocab) y[i] = q[e];
+        }
       }
     }
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) sum += fmax(weight(x[i], tp, it, ip) - weight(y[i], tq, it, iq), 0.0);
+    for (int i = 0; i < kVec<T>; ++i) w[i] = of(to_float(x[i]), to_float(y[i]));
+  }
+};
+
+// Sum over a chunk of max(p - a q, 0), valid in every thread.
+template <typename T>
+__device__ __forceinline__ double residual_sum(const DraftParams& p, int64_t row, int chunk, const RowDist& tp, const RowDist& tq,
+                                               double a, double* s_sum) {
+  LeftOf<T> left;
+  left.init(p, row, chunk, tp, tq, a);
+  double sum = 0;
+#pragma unroll 2
+  for (int u = 0; u < kLoads<T>; ++u) {
+    double w[kVec<T>];
+    left.load(u, w);
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) sum += w[i];
   }
   sum = wave_sum_d(sum);
   __syncthreads();
-  if ((tid & 63) == 0) s_sum[tid >> 6] = sum;
+  if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
   __syncthreads();
   sum = 0;
   for (int w = 0; w < kWavesD; ++w) sum += s_sum[w];
@@ -328,7 +386,7 @@ __global__ __launch_bounds__(kThreads) void draft_residual_kernel(DraftParams p,
     for (int c = lane; c < d.chunks; c += 64) z += p.left[at * d.chunks + c];
     a += wave_sum_d(z);
   }
-  const double sum = residual_sum<T>(p, row, chunk, tp, tq, a, it, s_sum);
+  const double sum = residual_sum<T>(p, row, chunk, tp, tq, a, s_sum);
   if (threadIdx.x == 0) p.left[(int64_t)blockIdx.y * d.chunks + chunk] = sum;
 }
 
@@ -388,12 +446,8 @@ __global__ __launch_bounds__(kThreads) void draft_walk_kernel(DraftParams p) {
     s_py[tid] = s_qy[tid] = 0;
     if (t.up >= 0 && y >= 0 && y < d.vocab) {
       const int64_t at = (row0 + t.up) * d.vocab + y;
-      auto value = [&](const void* x) {
-        const float v = to_float(((const T*)x)[at]);
-        return v == lowest<T>() ? kNegInf : v;
-      };
-      if (s_p[t.up].usable) s_py[tid] = prob(value(p.target), s_p[t.up], it);
-      if (sampled && s_q[t.up].usable) s_qy[tid] = prob(value(p.draft), s_q[t.up], it);
+      if (s_p[t.up].usable) s_py[tid] = s_p[t.up].raw(to_float(((const T*)p.target)[at])) / s_p[t.up].sum;
+      if (sampled && s_q[t.up].usable) s_qy[tid] = s_q[t.up].raw(to_float(((const T*)p.draft)[at])) / s_q[t.up].sum;
     }
   }
   __syncthreads();
@@ -459,23 +513,40 @@ __global__ __launch_bounds__(kThreads) void draft_walk_kernel(DraftParams p) {
   }
   if (!(s_end.a > 0)) return;
   const int at = s_end.node;
-  const double sum = residual_sum<T>(p, (int)row0 + at, chunk, s_p[at], s_q[at], s_end.a, it, s_sum);
+  const double sum = residual_sum<T>(p, row0 + at, chunk, s_p[at], s_q[at], s_end.a, s_sum);
   if (tid == 0) p.ends[(int64_t)s * d.chunks + chunk] = sum;
+}
+
+// The first lane whose running sum passes `want`, or the last that adds anything; `before`: the
+// sum ahead of it.  -1: no lane adds anything.  `upto`: the lane's running sum.
+__device__ __forceinline__ int pass_lane(double mine, double start, double want, int lane, double& before, bool& passed) {
+  double upto = mine;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const double y = __shfl_up(upto, off, 64);
+    if (lane >= off) upto += y;
+  }
+  upto += start;
+  const uint64_t past = __ballot(upto > want && mine > 0), some = __ballot(mine > 0);
+  passed = past != 0;
+  const int who = past ? __ffsll((unsigned long long)past) - 1 : some ? 63 - __clzll((long long)some) : -1;
+  before = who > 0 ? __shfl(upto, who - 1, 64) : start;
+  return who;
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void draft_sample_kernel(DraftParams p) {
-  constexpr int PER = kDraftChunk / kVec<T> / 64;  // loads of the chunk a lane of the last search has
-  __shared__ double s_w[kDraftChunk / kVec<T>];
-  __shared__ double s_target, s_total;
-  __shared__ int s_chunk, s_tok;
+  constexpr int VPC = kDraftChunk / kVec<T>, PER = VPC / 64;  // loads of a chunk, and a lane's
+  __shared__ double s_w[VPC];
+  __shared__ double s_want;
+  __shared__ int s_chunk, s_whole, s_gone[kTreeNodes], s_n_gone;
   const DraftShape& d = p.shape;
   const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
   const DraftEnd e = p.end[s];
   if (e.node < 0) return;
   const int64_t row0 = (int64_t)s * d.nodes, row = row0 + e.node;
-  auto finish = [&](int y, double logp) {
-    p.out_tokens[row0 + e.len - 1] = y;
+  auto finish = [&](int64_t y, double logp) {
+    p.out_tokens[row0 + e.len - 1] = (int32_t)y;
     p.out_logp[row0 + e.len - 1] = (float)logp;
   };
   const double it = inv_temp(p.temperature, s);
@@ -487,129 +558,130 @@ __global__ __launch_bounds__(kThreads) void draft_sample_kernel(DraftParams p) {
     if (tid == 0) finish(e.arg, -log(e.sum));
     return;
   }
-  RowDist tp;
+  RowDist tp{};
   tp.max = e.max;
   tp.sum = e.sum;
-  tp.usable = true;
-  const T* target = (const T*)p.target + row * d.vocab;
-  const T* draft = (const T*)p.draft + (p.draft ? row * d.vocab : 0);
+  tp.a = it;
+  tp.b = -(double)e.max * it;
   bool residual = e.a > 0;
   const DraftPart* part = p.part + row * d.chunks;
-  const DraftPart* qpart = p.part + ((int64_t)d.n * d.nodes + row) * d.chunks;
-  const RowDist tq = residual ? row_dist(qpart, d.chunks, it, lane) : RowDist{};
-  const int n = max(0, min(p.count ? p.count[s] : d.nodes, d.nodes));
-  // given drafts: is y one of the tried children?
-  const bool given = !residual && e.tried > 0;
-  auto tried = [&](int64_t y) {
-    for (int j = e.node + 1; j <= e.last && j < n; ++j)
-      if ((p.parents ? p.parents[row0 + j] : j - 1) == e.node && p.tokens[row0 + j] == y) return true;
-    return false;
-  };
-  auto entry = [&](const T* r, int64_t y) {
-    const float v = to_float(r[y]);
-    return v == lowest<T>() ? kNegInf : v;
-  };
-  if (tid == 0) {
-    auto share = [&](int c) {  // of chunk c in Z
-      if (residual) return p.ends[(int64_t)s * d.chunks + c];
-      const float m = part[c].max;
-      return m > kNegInf ? part[c].sum * exp_neg(((double)m - (double)e.max) * it) / e.sum : 0.0;
-    };
-    auto less = [&](int c) {  // what tried tokens take off it
-      double x = 0;
-      if (!given) return x;
-      const int ahead = (int)((reinterpret_cast<uintptr_t>(target) / sizeof(T)) % kVec<T>);
-      for (int j = e.node + 1; j <= e.last && j < n; ++j) {
-        if ((p.parents ? p.parents[row0 + j] : j - 1) != e.node) continue;
-        const int y = p.tokens[row0 + j];
-        if (y < 0 || y >= d.vocab || (y + ahead) / kDraftChunk != c) continue;
-        bool again = false;
-        for (int i = e.node + 1; i < j; ++i)
-          again = again || ((p.parents ? p.parents[row0 + i] : i - 1) == e.node && p.tokens[row0 + i] == y);
-        if (!again) x += prob(entry(target, y), tp, it);
+  RowDist tq{};
+  if (residual) tq = row_dist(p.part + ((int64_t)d.n * d.nodes + row) * d.chunks, d.chunks, it, lane);
+  const T* target = (const T*)p.target + row * d.vocab;
+  if (tid < 64) {
+    // given drafts: the tokens of the children that were tried are gone, a lane each
+    double gone = 0;
+    int gone_at = -1, y = -1;
+    if (!residual && e.tried > 0) {
+      const TreeOf t = tree_of(d, p.parents, p.count, s, lane);
+      bool is = t.up == e.node && lane <= e.last;
+      y = is ? p.tokens[row0 + lane] : -1;
+      is = is && y >= 0 && y < d.vocab;
+      for (uint64_t m = __ballot(is); m; m &= m - 1) {
+        const int j = __ffsll((unsigned long long)m) - 1;
+        if (lane > j && __builtin_amdgcn_readlane(y, j) == y) is = false;  // the same again
       }
-      return x;
+      if (is) {
+        const int ahead = (int)((reinterpret_cast<uintptr_t>(target) / sizeof(T)) % kVec<T>);
+        gone_at = (y + ahead) / kDraftChunk;
+        gone = tp.raw(to_float(target[y])) / tp.sum;
+      }
+    }
+    uint64_t takes = __ballot(gone_at >= 0);
+    auto share = [&](int c) {  // of chunk c in what is left
+      const bool is = c < d.chunks;
+      if (residual) return is ? p.ends[(int64_t)s * d.chunks + c] : 0.0;
+      double x = is && part[c].max > kNegInf ? part[c].sum * tp.raw(part[c].max) / tp.sum : 0.0;
+      for (uint64_t m = takes; m; m &= m - 1) {  // (all lanes: they read each other's)
+        const int j = __ffsll((unsigned long long)m) - 1;
+        const double off = __shfl(gone, j, 64);
+        if (__shfl(gone_at, j, 64) == c) x -= off;
+      }
+      return fmax(x, 0.0);
     };
     double total = 0;
-    for (int c = 0; c < d.chunks; ++c) total += fmax(share(c) - less(c), 0.0);
+    for (int c0 = 0; c0 < d.chunks; c0 += 64) total += share(c0 + lane);
+    total = wave_sum_d(total);
     if (!(total > 0)) {  // nothing is left: from p itself
       residual = false;
+      takes = 0;
       total = 0;
-      for (int c = 0; c < d.chunks; ++c) total += share(c);
-      s_total = -total;
-    } else {
-      s_total = total;
+      for (int c0 = 0; c0 < d.chunks; c0 += 64) total += share(c0 + lane);
+      total = wave_sum_d(total);
     }
-    const bool whole = s_total < 0;
-    const double target_sum = (double)p.u[row0] * total;
-    double before = 0;
+    const double want = (double)p.u[row0] * total;
+    double start = 0, ahead = 0;
     int pick = -1;
-    double ahead_of = 0;
-    for (int c = 0; c < d.chunks; ++c) {
-      const double x = fmax(share(c) - (whole ? 0.0 : less(c)), 0.0);
-      if (x > 0) {  // (the last one that has any, should none pass)
-        pick = c;
-        ahead_of = before;
+    for (int c0 = 0; c0 < d.chunks; c0 += 64) {
+      const double x = share(c0 + lane);
+      double before;
+      bool passed;
+      const int who = pass_lane(x, start, want, lane, before, passed);
+      if (who >= 0) {  // (the last chunk that has any, should none pass)
+        pick = c0 + who;
+        ahead = before;
       }
-      before += x;
-      if (before > target_sum) break;
+      if (passed) break;
+      start += wave_sum_d(x);
     }
-    s_chunk = pick;
-    s_target = target_sum - ahead_of;
+    const bool here = gone_at == pick && (takes >> lane & 1);
+    const uint64_t in_chunk = __ballot(here);
+    if (here) s_gone[__popcll(in_chunk & ((1ull << lane) - 1))] = y;
+    if (lane == 0) {
+      s_n_gone = __popcll(in_chunk);
+      s_chunk = pick;
+      s_want = want - ahead;
+      s_whole = !residual;
+    }
   }
   __syncthreads();
-  const bool whole = s_total < 0;
-  if (whole) residual = false;
-  const bool drop = given && !whole;
-  ChunkOf<T> c;
-  c.init(target, d.vocab, s_chunk, tid);
-  const double ip = 1.0 / tp.sum, iq = residual ? e.a / tq.sum : 0.0;
-  auto left = [&](int64_t y) {
-    if (y < 0 || y >= d.vocab) return 0.0;
-    const double w = weight(entry(target, y), tp, it, ip);
-    if (residual) return fmax(w - weight(entry(draft, y), tq, it, iq), 0.0);
-    return drop && tried(y) ? 0.0 : w;
+  LeftOf<T> left;
+  left.init(p, row, s_chunk, tp, tq, s_whole ? 0.0 : e.a);
+  const int n_gone = s_n_gone;
+  auto is_gone = [&](int64_t y) {
+    for (int i = 0; i < n_gone; ++i)
+      if (s_gone[i] == y) return true;
+    return false;
   };
   for (int u = 0; u < kLoads<T>; ++u) {
-    double sum = 0;
-    for (int i = 0; i < kVec<T>; ++i) sum += left(c.at(u) + i);
+    double w[kVec<T>], sum = 0;
+    left.load(u, w);
+#pragma unroll
+    for (int i = 0; i < kVec<T>; ++i) sum += n_gone && is_gone(left.c.at(u) + i) ? 0.0 : w[i];
     s_w[u * kThreads + tid] = sum;
   }
   __syncthreads();
   if (tid >= 64) return;
-  // one wave: which load, then which entry
-  double mine = 0;
+  // one wave: a lane's loads, then the load, then the entry
+  double mine = 0, before;
+  bool passed;
   for (int i = 0; i < PER; ++i) mine += s_w[lane * PER + i];
-  double upto = mine;
-  for (int off = 1; off < 64; off <<= 1) {
-    const double y = __shfl_up(upto, off, 64);
-    if (lane >= off) upto += y;
-  }
-  const double want = s_target;
-  const uint64_t past = __ballot(upto > want && mine > 0), some = __ballot(mine > 0);
-  const int who = past ? __ffsll((unsigned long long)past) - 1 : some ? 63 - __clzll((long long)some) : 0;
-  if (lane != who) return;
-  double at = upto - mine;
-  const int64_t first = c.first - (int64_t)tid * kVec<T>;  // the chunk's first entry
-  int64_t best = -1;
-  for (int i = lane * PER; i < lane * PER + PER; ++i) {
-    const bool here = at + s_w[i] > want;
-    if (s_w[i] > 0) {
-      double run = at;
-      for (int v = 0; v < kVec<T>; ++v) {
-        const int64_t y = first + (int64_t)i * kVec<T> + v;
-        const double w = left(y);
-        run += w;
-        if (w > 0) {
-          best = y;
-          if (here && run > want) break;
-        }
+  const double want = s_want;
+  const int who = pass_lane(mine, 0.0, want, lane, before, passed);
+  int load = 0;
+  double ahead = before;
+  if (who >= 0) {
+    double run = before;
+    for (int i = who * PER; i < who * PER + PER; ++i) {
+      const double w = s_w[i];
+      if (w > 0) {  // (the last one that has any, should none pass)
+        load = i;
+        ahead = run;
       }
+      run += w;
+      if (w > 0 && run > want) break;
     }
-    if (here) break;
-    at += s_w[i];
   }
-  finish((int)best, best >= 0 ? ((double)entry(target, best) - (double)tp.max) * it - log(tp.sum) : (double)__builtin_nanf(""));
+  const int64_t y = left.c.first - (int64_t)tid * kVec<T> + (int64_t)load * kVec<T> + lane;  // (first: the thread's)
+  double w = 0;
+  if (who >= 0 && lane < kVec<T> && y >= 0 && y < d.vocab && !(n_gone && is_gone(y)))
+    w = left.of(to_float(left.c.row[y]), left.q ? to_float(left.q[y]) : 0.f);
+  const int last = pass_lane(w, ahead, want, lane, before, passed);
+  if (last < 0) {
+    if (lane == 0) finish(-1, (double)__builtin_nanf(""));
+  } else if (lane == last) {
+    finish(y, fma((double)to_float(left.c.row[y]), tp.a, tp.b) * 0.6931471805599453 - log(tp.sum));
+  }
 }
 
 template <typename T>
