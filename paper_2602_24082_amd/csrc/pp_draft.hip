@@ -12,11 +12,14 @@
 // drafts are given: y stays if u Z < w(y), else w(y) = 0.  From a node that none of its
 // children follow the next token is the first x at which the running sum of w passes u_0 Z.
 //
-//   draft_rows     a workgroup for 8192 entries of a row: maximum, sum, where the maximum is
-//   draft_residual Z after a rejected child that has siblings behind it, one launch a sibling
-//   draft_walk     every workgroup walks the tree on its own (nothing but LDS by then) and sums
-//                  its entries of w at the node where the walk ends
-//   draft_sample   a workgroup a sequence: the entry at which the running sum passes
+//   draft_rows      a workgroup for 8192 entries of a row: maximum, sum, where the maximum is
+//   draft_edges     a workgroup a sequence: rows' sums joined, p and q of every drafted token,
+//                   and which nodes can be reached at all: a first child's fate is known here
+//   draft_residual  Z after a rejected child that has siblings behind it and can be reached; one
+//                   launch for each place among siblings
+//   draft_end       a workgroup for 2048 entries of w at the node where the walk ends, which each
+//                   finds by walking again (a few steps in registers); the last of a sequence's
+//                   searches the entry at which the running sum passes
 //
 // Probabilities are 64 bits throughout: numbers are compared with given ones, and a running
 // sum over 10^5 entries in 32 bits passes a number u elsewhere in one case of some hundred.
@@ -36,8 +39,8 @@ constexpr int kWavesD = kThreads / 64;
 
 template <typename T>
 constexpr int kVec = 16 / sizeof(T);  // entries of a 16-byte load
-template <typename T>
-constexpr int kLoads = kDraftChunk / (kThreads * kVec<T>);  // a thread's
+template <typename T, int CH>
+constexpr int kLoads = CH / (kThreads * kVec<T>);  // a thread's of a chunk
 
 __device__ __forceinline__ float to_float(uint16_t x) { return bf16_bits_to_f32(x); }
 __device__ __forceinline__ float to_float(float x) { return x; }
@@ -76,12 +79,15 @@ __device__ __forceinline__ double exp2_neg(double t) {
   return __hiloint2double(__double2hiint(s) + (__double2loint(u) << 20), __double2loint(s));
 }
 
-// A thread's entries of one chunk of a row: load u holds entries at(u) .. + kVec - 1, -inf
+template <typename T>
+using RawOf = T __attribute__((ext_vector_type(kVec<T>)));
+
+// A thread's entries of one chunk (CH entries) of a row: load u holds entries at(u) .. + kVec - 1, -inf
 // outside the row.  Loads lie on the row's 16-byte boundaries; those that reach over an end of
 // the row are taken entry by entry.
-template <typename T>
+template <typename T, int CH>
 struct ChunkOf {
-  typedef T Raw __attribute__((ext_vector_type(kVec<T>)));
+  using Raw = RawOf<T>;
   const T* row;
   int64_t first;  // entry of the thread's first load
   int vocab;
@@ -90,7 +96,7 @@ struct ChunkOf {
     row = r;
     vocab = v;
     const int ahead = (int)((reinterpret_cast<uintptr_t>(r) / sizeof(T)) % kVec<T>);
-    first = (int64_t)chunk * kDraftChunk + thread * kVec<T> - ahead;
+    first = (int64_t)chunk * CH + thread * kVec<T> - ahead;
   }
   __device__ __forceinline__ int64_t at(int u) const { return first + (int64_t)u * kThreads * kVec<T>; }
   __device__ __forceinline__ Raw load(int u) const {
@@ -105,14 +111,14 @@ struct ChunkOf {
 };
 
 // The largest of the entries' bits without their signs: NaN and infinities lie at the top.
-__device__ __forceinline__ void track_bits(ChunkOf<uint16_t>::Raw& most, const ChunkOf<uint16_t>::Raw& x) {
+__device__ __forceinline__ void track_bits(RawOf<uint16_t>& most, const RawOf<uint16_t>& x) {
   most = __builtin_elementwise_max(most, x & (uint16_t)0x7fff);
 }
-__device__ __forceinline__ void track_bits(uint32_t& most, const ChunkOf<float>::Raw& x) {
+__device__ __forceinline__ void track_bits(uint32_t& most, const RawOf<float>& x) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
 }
-__device__ __forceinline__ uint32_t most_bits(const ChunkOf<uint16_t>::Raw& m) {
+__device__ __forceinline__ uint32_t most_bits(const RawOf<uint16_t>& m) {
   uint32_t r = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r = max(r, (uint32_t)m[i]);
@@ -125,13 +131,36 @@ struct BitsOf {
 };
 template <>
 struct BitsOf<uint16_t> {
-  using Type = ChunkOf<uint16_t>::Raw;
+  using Type = RawOf<uint16_t>;
 };
 
-__device__ __forceinline__ double wave_sum_d(double x) {
-  for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off, 64);
-  return x;
+__device__ __forceinline__ double lane_d(double x, int lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), lane), __builtin_amdgcn_readlane(__double2loint(x), lane));
 }
+__device__ __forceinline__ float lane_f(float x, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(x), lane));
+}
+__device__ __forceinline__ uint64_t lane_u64(uint64_t x, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, lane);
+}
+
+// Running sums over the wave's lanes, in registers (DPP: lanes 1, 2, 4, 8 to the left within rows
+// of 16, then the rows' last lanes), a sixth of the time of exchanges through LDS.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double add_moved(double x) {
+  const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(x), CTRL, ROWS, 0xf, false);
+  const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(x), CTRL, ROWS, 0xf, false);
+  return x + __hiloint2double(hi, lo);
+}
+__device__ __forceinline__ double wave_scan_d(double x) {
+  x = add_moved<0x111, 0xf>(x);
+  x = add_moved<0x112, 0xf>(x);
+  x = add_moved<0x114, 0xf>(x);
+  x = add_moved<0x118, 0xf>(x);
+  x = add_moved<0x142, 0xa>(x);
+  return add_moved<0x143, 0xc>(x);
+}
+__device__ __forceinline__ double wave_sum_d(double x) { return lane_d(wave_scan_d(x), 63); }
 
 // A sequence's tree: lane l of a wave looks at node l.
 struct TreeOf {
@@ -149,8 +178,7 @@ __device__ __forceinline__ TreeOf tree_of(const DraftShape& d, const int32_t* pa
   for (int j = 1; j < t.count; ++j) {
     const int uj = __builtin_amdgcn_readlane(up, j);
     if (uj < 0) continue;
-    const int before = __popcll(__builtin_amdgcn_readlane((int)(t.kids >> 32), uj) & 0xffffffffu) +
-                       __popcll(__builtin_amdgcn_readlane((int)t.kids, uj) & 0xffffffffu);
+    const int before = __popcll(lane_u64(t.kids, uj));
     if (lane == j) t.rank = before;
     if (before >= d.max_children) {
       if (lane == j) up = -1;
@@ -174,11 +202,13 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
   __shared__ float s_m[kWavesD];
   __shared__ int s_arg[kWavesD], s_bad[kWavesD];
   __shared__ double s_sum[kWavesD];
+  constexpr int L = kLoads<T, kDraftChunk>;
   const DraftShape& d = p.shape;
   const int row = blockIdx.y, chunk = blockIdx.x, s = row / d.nodes, node = row - s * d.nodes;
   const bool is_draft = blockIdx.z != 0, argmax = greedy(p.temperature, s);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = max(0, min(p.count ? p.count[s] : d.nodes, d.nodes));
+  if (node == 0 && chunk == 0 && !is_draft && tid == 0) p.arrived[s] = 0;
   if (node >= n) return;
   if (is_draft) {
     if (argmax) return;
@@ -187,15 +217,15 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
       kid = kid || (p.parents ? p.parents[(int64_t)s * d.nodes + j] == node : j == node + 1);
     if (!__any(kid)) return;
   }
-  ChunkOf<T> c;
+  ChunkOf<T, kDraftChunk> c;
   c.init((const T*)(is_draft ? p.draft : p.target) + (int64_t)row * d.vocab, d.vocab, chunk, tid);
-  typename ChunkOf<T>::Raw x[kLoads<T>];
+  RawOf<T> x[L];
 #pragma unroll
-  for (int u = 0; u < kLoads<T>; ++u) x[u] = c.load(u);
+  for (int u = 0; u < L; ++u) x[u] = c.load(u);
   float m = kNegInf;
   typename BitsOf<T>::Type bits{};
 #pragma unroll
-  for (int u = 0; u < kLoads<T>; ++u) {
+  for (int u = 0; u < L; ++u) {
     track_bits(bits, x[u]);
 #pragma unroll
     for (int i = 0; i < kVec<T>; ++i) m = fmaxf(m, to_float(x[u][i]));
@@ -220,13 +250,13 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
   int arg = 0x7fffffff;
   if (top > lowest<T>() && !bad) {
 #pragma unroll
-    for (int u = 0; u < kLoads<T>; ++u)
+    for (int u = 0; u < L; ++u)
 #pragma unroll
       for (int i = 0; i < kVec<T>; ++i) sum += exp2_neg(fma((double)to_float(x[u][i]), a, b));
     sum = wave_sum_d(sum);
     if (argmax) {
 #pragma unroll
-      for (int u = 0; u < kLoads<T>; ++u)
+      for (int u = 0; u < L; ++u)
 #pragma unroll
         for (int i = 0; i < kVec<T>; ++i)
           if (to_float(x[u][i]) == top) arg = min(arg, (int)(c.at(u) + i));
@@ -263,11 +293,26 @@ struct RowDist {
     return t > kTiny + 1 ? exp2_neg(t) : 0.0;
   }
 };
+__device__ __forceinline__ RowDist row_dist(const DraftRow& x, double it) {
+  RowDist r;
+  r.max = x.max;
+  r.sum = x.sum;
+  r.arg = x.arg;
+  r.usable = x.arg >= 0;
+  r.a = it;
+  r.b = -(double)x.max * it;
+  return r;
+}
 // By a wave, from the parts of the row's chunks.
 __device__ __forceinline__ RowDist row_dist(const DraftPart* part, int chunks, double it, int lane) {
-  float m = kNegInf;
-  bool bad = false;
-  for (int c = lane; c < chunks; c += 64) {
+  DraftPart mine;  // of the first 64 chunks
+  mine.sum = 0;
+  mine.max = kNegInf;
+  mine.arg = 0x7fffffff;
+  if (lane < chunks) mine = part[lane];
+  float m = mine.max;
+  bool bad = m != m;
+  for (int c = lane + 64; c < chunks; c += 64) {
     const float x = part[c].max;
     bad = bad || x != x;
     m = fmaxf(m, x);
@@ -277,14 +322,17 @@ __device__ __forceinline__ RowDist row_dist(const DraftPart* part, int chunks, d
   r.usable = !__any(bad) && r.max > kNegInf;
   r.a = it;
   r.b = -(double)r.max * it;
+  r.sum = 0;
+  r.arg = 0x7fffffff;
+  if (!r.usable) return r;
   double s = 0;
   int arg = 0x7fffffff;
-  if (r.usable)
-    for (int c = lane; c < chunks; c += 64) {
-      const float x = part[c].max;
-      if (x > kNegInf) s += part[c].sum * r.raw(x);
-      if (x == r.max) arg = min(arg, part[c].arg);
-    }
+  auto add = [&](const DraftPart& x) {
+    if (x.max > kNegInf) s = fma(x.sum, r.raw(x.max), s);
+    if (x.max == r.max) arg = min(arg, x.arg);
+  };
+  add(mine);
+  for (int c = lane + 64; c < chunks; c += 64) add(part[c]);
   r.sum = wave_sum_d(s);
   for (int off = 32; off > 0; off >>= 1) arg = min(arg, __shfl_xor(arg, off, 64));
   r.arg = arg;
@@ -292,9 +340,10 @@ __device__ __forceinline__ RowDist row_dist(const DraftPart* part, int chunks, d
 }
 
 // What is left of a row's distribution: max(p - a q, 0), or p where there is no q.
-template <typename T>
+template <typename T, int CH>
 struct LeftOf {
-  ChunkOf<T> c;   // the target's row
+  static constexpr int L = kLoads<T, CH>;
+  ChunkOf<T, CH> c;  // the target's row
   const T* q;     // or null
   RowDist tp, tq;
   double ip, iq;  // 1 / sum, a / sum
@@ -313,42 +362,43 @@ struct LeftOf {
     const double w = tp.raw(x) * ip;
     return q ? fmax(fma(-tq.raw(y), iq, w), 0.0) : w;
   }
-  // weights of load u's entries
-  __device__ __forceinline__ void load(int u, double (&w)[kVec<T>]) const {
-    const typename ChunkOf<T>::Raw x = c.load(u);
-    typename ChunkOf<T>::Raw y = x;
-    if (q) {
-      if (alike) {
-        ChunkOf<T> cq = c;
-        cq.row = q;
-        y = cq.load(u);
-      } else {
+  // use(load, entry of it, weight) for the thread's entries; all loads ahead
+  template <typename Use>
+  __device__ __forceinline__ void each(Use&& use) const {
+    RawOf<T> x[L], y[L];
+    ChunkOf<T, CH> cq = c;
+    cq.row = q;
+#pragma unroll
+    for (int u = 0; u < L; ++u) x[u] = c.load(u);
+    if (q && alike) {
+#pragma unroll
+      for (int u = 0; u < L; ++u) y[u] = cq.load(u);
+    } else if (q) {
+#pragma unroll
+      for (int u = 0; u < L; ++u) {
+        y[u] = x[u];
 #pragma unroll
         for (int i = 0; i < kVec<T>; ++i) {
           const int64_t e = c.at(u) + i;
-          if (e >= 0 && e < c.vocab) y[i] = q[e];
+          if (e >= 0 && e < c.vocab) y[u][i] = q[e];
         }
       }
     }
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) w[i] = of(to_float(x[i]), to_float(y[i]));
+    for (int u = 0; u < L; ++u)
+#pragma unroll
+      for (int i = 0; i < kVec<T>; ++i) use(u, i, of(to_float(x[u][i]), q ? to_float(y[u][i]) : 0.f));
   }
 };
 
-// Sum over a chunk of max(p - a q, 0), valid in every thread.
+// Sum over a short chunk of max(p - a q, 0), valid in every thread.
 template <typename T>
 __device__ __forceinline__ double residual_sum(const DraftParams& p, int64_t row, int chunk, const RowDist& tp, const RowDist& tq,
                                                double a, double* s_sum) {
-  LeftOf<T> left;
+  LeftOf<T, kDraftShort> left;
   left.init(p, row, chunk, tp, tq, a);
   double sum = 0;
-#pragma unroll 2
-  for (int u = 0; u < kLoads<T>; ++u) {
-    double w[kVec<T>];
-    left.load(u, w);
-#pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) sum += w[i];
-  }
+  left.each([&](int, int, double w) { sum += w; });
   sum = wave_sum_d(sum);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
@@ -358,306 +408,186 @@ __device__ __forceinline__ double residual_sum(const DraftParams& p, int64_t row
   return sum;
 }
 
-// Z after child j is rejected, the chunk's share: for children of rank `round` that have a
-// sibling behind them.
+// Of a drafted token, a lane each.
+struct EdgeOf {
+  double p, q;
+  float u;
+  int tok;
+  int p_arg, q_arg;  // of the lane's own rows
+};
+__device__ __forceinline__ EdgeOf edge_of(const DraftParams& p, int64_t row0, int lane, int n) {
+  EdgeOf e{};
+  e.tok = -1;
+  if (lane < n) {
+    const DraftEdge x = p.edge[row0 + lane];
+    e.p = x.p;
+    e.q = x.q;
+    e.u = p.u[row0 + lane];
+    e.tok = p.tokens[row0 + lane];
+    e.p_arg = p.row[row0 + lane].arg;
+    e.q_arg = p.row[(int64_t)p.shape.n * p.shape.nodes + row0 + lane].arg;
+  }
+  return e;
+}
+
+// Z after a node is rejected, by a wave.
+__device__ __forceinline__ double left_after(const DraftParams& p, int64_t node, int lane) {
+  double z = 0;
+  for (int c = lane; c < p.shape.shorts; c += 64) z += p.left[node * p.shape.shorts + c];
+  return wave_sum_d(z);
+}
+
+constexpr int kEdgeThreads = 1024;  // a wave a row, as far as they reach
+
+template <typename T>
+__global__ __launch_bounds__(kEdgeThreads) void draft_edges_kernel(DraftParams p) {
+  __shared__ DraftRow s_p[kTreeNodes], s_q[kTreeNodes];
+  const DraftShape& d = p.shape;
+  const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const TreeOf t = tree_of(d, p.parents, p.count, s, lane);
+  const int n = t.count;
+  const int64_t row0 = (int64_t)s * d.nodes, rows = (int64_t)d.n * d.nodes;
+  const bool argmax = greedy(p.temperature, s), sampled = p.draft != nullptr && !argmax;
+  const double it = inv_temp(p.temperature, s);
+  for (int i = wave; i < 2 * n; i += kEdgeThreads / 64) {
+    const int node = i >> 1, is_q = i & 1;
+    if (is_q && !(sampled && lane_u64(t.kids, node))) continue;
+    const RowDist r = row_dist(p.part + (is_q * rows + row0 + node) * d.chunks, d.chunks, it, lane);
+    if (lane == 0) {
+      DraftRow x;
+      x.sum = r.sum;
+      x.max = r.max;
+      x.arg = r.usable ? r.arg : -1;
+      (is_q ? s_q : s_p)[node] = x;
+      p.row[is_q * rows + row0 + node] = x;
+    }
+  }
+  __syncthreads();
+  if (tid >= 64) return;
+  DraftEdge e{};
+  bool tried = false, stays = false;  // as a first child
+  if (lane < n && t.up >= 0) {
+    const int y = p.tokens[row0 + lane];
+    const DraftRow rp = s_p[t.up], rq = sampled ? s_q[t.up] : rp;
+    tried = rp.arg >= 0 && rq.arg >= 0;
+    if (tried && y >= 0 && y < d.vocab) {
+      const int64_t at = (row0 + t.up) * d.vocab + y;
+      e.p = row_dist(rp, it).raw(to_float(((const T*)p.target)[at])) / rp.sum;
+      if (sampled) e.q = row_dist(rq, it).raw(to_float(((const T*)p.draft)[at])) / rq.sum;
+    }
+    const double u = (double)p.u[row0 + lane];
+    stays = tried && (sampled ? u * e.q < e.p : argmax ? y == rp.arg : u < e.p);
+  }
+  // a node can be reached if its edge can be taken, and its parent's, ..: a first child's if it
+  // stays, another's if the first does not
+  const int up = t.up;
+  const uint64_t kids = __shfl(t.kids, max(up, 0), 64);
+  const int first = up >= 0 ? __ffsll((unsigned long long)kids) - 1 : 0;
+  const int first_stays = __shfl((int)stays, max(first, 0), 64);
+  int ok = lane == 0 ? 1 : up >= 0 && tried && (t.rank == 0 ? stays : !first_stays);
+  int to = up;
+  for (int i = 0; i < 6; ++i) {
+    const int from = max(to, 0);
+    const int ok2 = __shfl(ok, from, 64), to2 = __shfl(to, from, 64);
+    if (to >= 0) {
+      ok &= ok2;
+      to = to2;
+    }
+  }
+  ok &= to < 0;
+  const int parent_ok = __shfl(ok, max(up, 0), 64);
+  e.need = up >= 0 && sampled && tried && !stays && t.rank == 0 && parent_ok && (kids >> lane) != 1;
+  if (lane < n) p.edge[row0 + lane] = e;
+}
+
+// Z after a child of rank `round` is rejected that has a sibling behind it, a short chunk's
+// share, for every node where it may be asked for.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void draft_residual_kernel(DraftParams p, int round) {
   __shared__ double s_sum[kWavesD];
   const DraftShape& d = p.shape;
-  const int chunk = blockIdx.x, s = blockIdx.y / d.nodes, j = blockIdx.y - s * d.nodes, lane = threadIdx.x & 63;
-  if (greedy(p.temperature, s)) return;
-  const TreeOf t = tree_of(d, p.parents, p.count, s, lane);
-  if (j >= t.count) return;
-  const int up = __builtin_amdgcn_readlane(t.up, j);
-  if (up < 0 || __builtin_amdgcn_readlane(t.rank, j) != round) return;
-  const uint64_t kids = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(t.kids >> 32), up) << 32 |
-                        (uint32_t)__builtin_amdgcn_readlane((int)t.kids, up);
-  if ((kids >> j) == 1) return;  // the last
-  const double it = inv_temp(p.temperature, s);
-  const int row = s * d.nodes + up;
-  const int64_t rows = (int64_t)d.n * d.nodes;
-  const RowDist tp = row_dist(p.part + (int64_t)row * d.chunks, d.chunks, it, lane);
-  const RowDist tq = row_dist(p.part + (rows + row) * d.chunks, d.chunks, it, lane);
-  if (!tp.usable || !tq.usable) return;
-  double a = 1.0;
-  for (uint64_t m = kids & ((1ull << j) - 1); m; m &= m - 1) {  // the siblings rejected ahead of it
-    const int64_t at = (int64_t)s * d.nodes + __ffsll((unsigned long long)m) - 1;
-    double z = 0;
-    for (int c = lane; c < d.chunks; c += 64) z += p.left[at * d.chunks + c];
-    a += wave_sum_d(z);
-  }
-  const double sum = residual_sum<T>(p, row, chunk, tp, tq, a, s_sum);
-  if (threadIdx.x == 0) p.left[(int64_t)blockIdx.y * d.chunks + chunk] = sum;
-}
-
-template <typename T>
-__global__ __launch_bounds__(kThreads) void draft_walk_kernel(DraftParams p) {
-  __shared__ RowDist s_p[kTreeNodes], s_q[kTreeNodes];
-  __shared__ double s_py[kTreeNodes], s_qy[kTreeNodes], s_left[kTreeNodes], s_sum[kWavesD];
-  __shared__ float s_u[kTreeNodes], s_logp[kTreeNodes];
-  __shared__ int s_tok[kTreeNodes], s_up[kTreeNodes], s_path[kTreeNodes];
-  __shared__ DraftEnd s_end;
-  const DraftShape& d = p.shape;
-  const int s = blockIdx.y, chunk = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const TreeOf t = tree_of(d, p.parents, p.count, s, lane);
-  const int n = t.count;
+  const int chunk = blockIdx.x, s = blockIdx.y, lane = threadIdx.x & 63;
   const int64_t row0 = (int64_t)s * d.nodes, rows = (int64_t)d.n * d.nodes;
-  if (n == 0) {
-    if (chunk == 0 && tid < d.nodes) {
-      p.out_tokens[row0 + tid] = p.out_path[row0 + tid] = -1;
-      p.out_logp[row0 + tid] = 0.f;
-    }
-    if (chunk == 0 && tid == 0) {
-      p.out_count[s] = 0;
-      p.end[s].node = -1;
-    }
-    return;
-  }
-  const bool argmax = greedy(p.temperature, s), sampled = p.draft != nullptr && !argmax;
+  const int n = max(0, min(p.count ? p.count[s] : d.nodes, d.nodes));
+  uint64_t need = __ballot(lane < n && p.edge[row0 + lane].need);
+  if (need == 0) return;
+  const TreeOf t = tree_of(d, p.parents, p.count, s, lane);
+  const EdgeOf e = edge_of(p, row0, lane, n);
   const double it = inv_temp(p.temperature, s);
-  for (int i = wave; i < n; i += kWavesD) {
-    const RowDist r = row_dist(p.part + (row0 + i) * d.chunks, d.chunks, it, lane);
-    const uint64_t kids = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(t.kids >> 32), i) << 32 |
-                          (uint32_t)__builtin_amdgcn_readlane((int)t.kids, i);
-    RowDist q{};
-    if (sampled && kids) q = row_dist(p.part + (rows + row0 + i) * d.chunks, d.chunks, it, lane);
-    const int up = __builtin_amdgcn_readlane(t.up, i);
-    double z = 0;
-    if (sampled && up >= 0) {
-      const uint64_t sib = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(t.kids >> 32), up) << 32 |
-                           (uint32_t)__builtin_amdgcn_readlane((int)t.kids, up);
-      if (sib >> i != 1) {
-        for (int c = lane; c < d.chunks; c += 64) z += p.left[(row0 + i) * d.chunks + c];
-        z = wave_sum_d(z);
-      }
+  for (; need; need &= need - 1) {
+    const int first = __ffsll((unsigned long long)need) - 1, up = __builtin_amdgcn_readlane(t.up, first);
+    const uint64_t kids = lane_u64(t.kids, up);
+    const int j_rank = __popcll(kids) - 1;
+    if (j_rank <= round) continue;  // none, or the last
+    // the siblings up to it, all rejected?
+    double a = 0, Z = 1.0;
+    int j = first, rank = 0;
+    bool stays = false;
+    for (uint64_t m = kids; m; m &= m - 1, ++rank) {
+      j = __ffsll((unsigned long long)m) - 1;
+      const double q = lane_d(e.q, j), w = fmax(fma(-a, q, lane_d(e.p, j)), 0.0);  // (as draft_end)
+      stays = (double)lane_f(e.u, j) * q * Z < w;
+      a += Z;
+      if (stays || rank == round) break;
+      Z = left_after(p, row0 + j, lane);
     }
-    if (lane == 0) {
-      s_p[i] = r;
-      s_q[i] = q;
-      s_left[i] = z;
-    }
+    if (stays) continue;
+    const RowDist tp = row_dist(p.row[row0 + up], it), tq = row_dist(p.row[rows + row0 + up], it);
+    const double sum = residual_sum<T>(p, row0 + up, chunk, tp, tq, a, s_sum);
+    if (threadIdx.x == 0) p.left[(row0 + j) * d.shorts + chunk] = sum;
   }
-  __syncthreads();
-  if (tid < n) {  // (the first wave)
-    const int y = p.tokens[row0 + tid];
-    s_up[tid] = t.up;
-    s_tok[tid] = y;
-    s_u[tid] = p.u[row0 + tid];
-    s_py[tid] = s_qy[tid] = 0;
-    if (t.up >= 0 && y >= 0 && y < d.vocab) {
-      const int64_t at = (row0 + t.up) * d.vocab + y;
-      if (s_p[t.up].usable) s_py[tid] = s_p[t.up].raw(to_float(((const T*)p.target)[at])) / s_p[t.up].sum;
-      if (sampled && s_q[t.up].usable) s_qy[tid] = s_q[t.up].raw(to_float(((const T*)p.draft)[at])) / s_q[t.up].sum;
-    }
-  }
-  __syncthreads();
-  if (tid == 0) {
-    // children of a node come behind it, so one pass over the nodes sees every step of the walk
-    int at = 0, len = 1, tried = 0, last = -1;
-    double Z = 1.0, a = 0.0;
-    s_path[0] = 0;
-    for (int j = 1; j < n; ++j) {
-      if (s_up[j] != at) continue;
-      const int y = s_tok[j];
-      bool stays;
-      double w = s_py[j];
-      if (!s_p[at].usable || (sampled && !s_q[at].usable)) {
-        continue;  // nothing to try it against
-      } else if (argmax) {
-        stays = y == s_p[at].arg;
-      } else if (sampled) {
-        w = fmax(w - a * s_qy[j], 0.0);
-        stays = (double)s_u[j] * s_qy[j] * Z < w;
-      } else {
-        for (int i = at + 1; i < j; ++i)
-          if (s_up[i] == at && s_tok[i] == y) w = 0;  // tried already
-        stays = (double)s_u[j] * Z < w;
-      }
-      if (stays) {
-        s_logp[len - 1] = (float)log(s_py[j]);
-        s_path[len++] = j;
-        at = j;
-        Z = 1.0;
-        a = 0.0;
-        tried = 0;
-        last = -1;
-      } else if (!argmax) {
-        ++tried;
-        last = j;
-        a += Z;  // (its Z: of the last one the sum is still to be formed, and not needed here)
-        Z = sampled ? s_left[j] : Z - w;
-      }
-    }
-    s_end.node = at;
-    s_end.len = len;
-    s_end.a = sampled && tried ? a : 0.0;
-    s_end.tried = tried;
-    s_end.last = last;
-    s_end.max = s_p[at].max;
-    s_end.sum = s_p[at].sum;
-    s_end.arg = s_p[at].usable ? s_p[at].arg : -1;
-    s_end.greedy = argmax;
-    if (chunk == 0) {
-      p.end[s] = s_end;
-      p.out_count[s] = len;
-    }
-  }
-  __syncthreads();
-  if (chunk == 0 && tid < d.nodes) {
-    const int len = s_end.len;
-    p.out_path[row0 + tid] = tid < len ? s_path[tid] : -1;
-    if (tid != len - 1) {  // (draft_sample writes the last)
-      p.out_tokens[row0 + tid] = tid < len - 1 ? s_tok[s_path[tid + 1]] : -1;
-      p.out_logp[row0 + tid] = tid < len - 1 ? s_logp[tid] : 0.f;
-    }
-  }
-  if (!(s_end.a > 0)) return;
-  const int at = s_end.node;
-  const double sum = residual_sum<T>(p, row0 + at, chunk, s_p[at], s_q[at], s_end.a, s_sum);
-  if (tid == 0) p.ends[(int64_t)s * d.chunks + chunk] = sum;
 }
 
 // The first lane whose running sum passes `want`, or the last that adds anything; `before`: the
 // sum ahead of it.  -1: no lane adds anything.  `upto`: the lane's running sum.
 __device__ __forceinline__ int pass_lane(double mine, double start, double want, int lane, double& before, bool& passed) {
-  double upto = mine;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const double y = __shfl_up(upto, off, 64);
-    if (lane >= off) upto += y;
-  }
-  upto += start;
+  const double upto = wave_scan_d(mine) + start;
   const uint64_t past = __ballot(upto > want && mine > 0), some = __ballot(mine > 0);
   passed = past != 0;
   const int who = past ? __ffsll((unsigned long long)past) - 1 : some ? 63 - __clzll((long long)some) : -1;
-  before = who > 0 ? __shfl(upto, who - 1, 64) : start;
+  before = who > 0 ? lane_d(upto, who - 1) : start;
   return who;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads) void draft_sample_kernel(DraftParams p) {
-  constexpr int VPC = kDraftChunk / kVec<T>, PER = VPC / 64;  // loads of a chunk, and a lane's
-  __shared__ double s_w[VPC];
-  __shared__ double s_want;
-  __shared__ int s_chunk, s_whole, s_gone[kTreeNodes], s_n_gone;
-  const DraftShape& d = p.shape;
-  const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
-  const DraftEnd e = p.end[s];
-  if (e.node < 0) return;
-  const int64_t row0 = (int64_t)s * d.nodes, row = row0 + e.node;
-  auto finish = [&](int64_t y, double logp) {
-    p.out_tokens[row0 + e.len - 1] = (int32_t)y;
-    p.out_logp[row0 + e.len - 1] = (float)logp;
-  };
-  const double it = inv_temp(p.temperature, s);
-  if (e.arg < 0) {
-    if (tid == 0) finish(-1, (double)__builtin_nanf(""));
-    return;
-  }
-  if (e.greedy) {
-    if (tid == 0) finish(e.arg, -log(e.sum));
-    return;
-  }
-  RowDist tp{};
-  tp.max = e.max;
-  tp.sum = e.sum;
-  tp.a = it;
-  tp.b = -(double)e.max * it;
-  bool residual = e.a > 0;
-  const DraftPart* part = p.part + row * d.chunks;
-  RowDist tq{};
-  if (residual) tq = row_dist(p.part + ((int64_t)d.n * d.nodes + row) * d.chunks, d.chunks, it, lane);
-  const T* target = (const T*)p.target + row * d.vocab;
-  if (tid < 64) {
-    // given drafts: the tokens of the children that were tried are gone, a lane each
-    double gone = 0;
-    int gone_at = -1, y = -1;
-    if (!residual && e.tried > 0) {
-      const TreeOf t = tree_of(d, p.parents, p.count, s, lane);
-      bool is = t.up == e.node && lane <= e.last;
-      y = is ? p.tokens[row0 + lane] : -1;
-      is = is && y >= 0 && y < d.vocab;
-      for (uint64_t m = __ballot(is); m; m &= m - 1) {
-        const int j = __ffsll((unsigned long long)m) - 1;
-        if (lane > j && __builtin_amdgcn_readlane(y, j) == y) is = false;  // the same again
-      }
-      if (is) {
-        const int ahead = (int)((reinterpret_cast<uintptr_t>(target) / sizeof(T)) % kVec<T>);
-        gone_at = (y + ahead) / kDraftChunk;
-        gone = tp.raw(to_float(target[y])) / tp.sum;
-      }
-    }
-    uint64_t takes = __ballot(gone_at >= 0);
-    auto share = [&](int c) {  // of chunk c in what is left
-      const bool is = c < d.chunks;
-      if (residual) return is ? p.ends[(int64_t)s * d.chunks + c] : 0.0;
-      double x = is && part[c].max > kNegInf ? part[c].sum * tp.raw(part[c].max) / tp.sum : 0.0;
-      for (uint64_t m = takes; m; m &= m - 1) {  // (all lanes: they read each other's)
-        const int j = __ffsll((unsigned long long)m) - 1;
-        const double off = __shfl(gone, j, 64);
-        if (__shfl(gone_at, j, 64) == c) x -= off;
-      }
-      return fmax(x, 0.0);
-    };
-    double total = 0;
-    for (int c0 = 0; c0 < d.chunks; c0 += 64) total += share(c0 + lane);
-    total = wave_sum_d(total);
-    if (!(total > 0)) {  // nothing is left: from p itself
-      residual = false;
-      takes = 0;
-      total = 0;
-      for (int c0 = 0; c0 < d.chunks; c0 += 64) total += share(c0 + lane);
-      total = wave_sum_d(total);
-    }
-    const double want = (double)p.u[row0] * total;
-    double start = 0, ahead = 0;
-    int pick = -1;
-    for (int c0 = 0; c0 < d.chunks; c0 += 64) {
-      const double x = share(c0 + lane);
-      double before;
-      bool passed;
-      const int who = pass_lane(x, start, want, lane, before, passed);
-      if (who >= 0) {  // (the last chunk that has any, should none pass)
-        pick = c0 + who;
-        ahead = before;
-      }
-      if (passed) break;
-      start += wave_sum_d(x);
-    }
-    const bool here = gone_at == pick && (takes >> lane & 1);
-    const uint64_t in_chunk = __ballot(here);
-    if (here) s_gone[__popcll(in_chunk & ((1ull << lane) - 1))] = y;
-    if (lane == 0) {
-      s_n_gone = __popcll(in_chunk);
-      s_chunk = pick;
-      s_want = want - ahead;
-      s_whole = !residual;
-    }
-  }
-  __syncthreads();
-  LeftOf<T> left;
-  left.init(p, row, s_chunk, tp, tq, s_whole ? 0.0 : e.a);
-  const int n_gone = s_n_gone;
+// Where to look for the next token: a chunk, what its running sum has to pass, and tokens in
+// it that are gone.
+struct PickOf {
+  double want;
+  int chunk, n_gone, gone[kTreeNodes];
+};
+struct Picked {
+  bool mine;  // the thread that has it
+  int64_t y;  // -1: nothing there
+  double logp;
+};
+// By the workgroup: the entry of the chunk at which the running sum of what is left passes; s_w:
+// room for the sums of the chunk's loads.
+template <typename T, int CH>
+__device__ __forceinline__ Picked pick_entry(const DraftParams& p, int64_t row, const RowDist& tp, const RowDist& tq, double a,
+                                             const PickOf& pick, double* s_w) {
+  constexpr int VPC = CH / kVec<T>, PER = VPC / 64, L = kLoads<T, CH>;  // loads of a chunk, a lane's, a thread's
+  const int tid = threadIdx.x, lane = tid & 63;
+  Picked out{false, -1, (double)__builtin_nanf("")};
+  LeftOf<T, CH> left;
+  left.init(p, row, pick.chunk, tp, tq, a);
+  const int n_gone = pick.n_gone;
   auto is_gone = [&](int64_t y) {
     for (int i = 0; i < n_gone; ++i)
-      if (s_gone[i] == y) return true;
+      if (pick.gone[i] == y) return true;
     return false;
   };
-  for (int u = 0; u < kLoads<T>; ++u) {
-    double w[kVec<T>], sum = 0;
-    left.load(u, w);
+  double sums[L] = {};
+  left.each([&](int u, int i, double w) { sums[u] += n_gone && is_gone(left.c.at(u) + i) ? 0.0 : w; });
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) sum += n_gone && is_gone(left.c.at(u) + i) ? 0.0 : w[i];
-    s_w[u * kThreads + tid] = sum;
-  }
+  for (int u = 0; u < L; ++u) s_w[u * kThreads + tid] = sums[u];
   __syncthreads();
-  if (tid >= 64) return;
+  if (tid >= 64) return out;
   // one wave: a lane's loads, then the load, then the entry
   double mine = 0, before;
   bool passed;
+#pragma unroll
   for (int i = 0; i < PER; ++i) mine += s_w[lane * PER + i];
-  const double want = s_want;
-  const int who = pass_lane(mine, 0.0, want, lane, before, passed);
+  const int who = pass_lane(mine, 0.0, pick.want, lane, before, passed);
   int load = 0;
   double ahead = before;
   if (who >= 0) {
@@ -669,19 +599,211 @@ __global__ __launch_bounds__(kThreads) void draft_sample_kernel(DraftParams p) {
         ahead = run;
       }
       run += w;
-      if (w > 0 && run > want) break;
+      if (w > 0 && run > pick.want) break;
     }
   }
   const int64_t y = left.c.first - (int64_t)tid * kVec<T> + (int64_t)load * kVec<T> + lane;  // (first: the thread's)
   double w = 0;
-  if (who >= 0 && lane < kVec<T> && y >= 0 && y < d.vocab && !(n_gone && is_gone(y)))
-    w = left.of(to_float(left.c.row[y]), left.q ? to_float(left.q[y]) : 0.f);
-  const int last = pass_lane(w, ahead, want, lane, before, passed);
-  if (last < 0) {
-    if (lane == 0) finish(-1, (double)__builtin_nanf(""));
-  } else if (lane == last) {
-    finish(y, fma((double)to_float(left.c.row[y]), tp.a, tp.b) * 0.6931471805599453 - log(tp.sum));
+  float x = 0.f;
+  if (who >= 0 && lane < kVec<T> && y >= 0 && y < p.shape.vocab && !(n_gone && is_gone(y))) {
+    x = to_float(left.c.row[y]);
+    w = left.of(x, left.q ? to_float(left.q[y]) : 0.f);
   }
+  const int last = pass_lane(w, ahead, pick.want, lane, before, passed);
+  out.mine = lane == max(last, 0);
+  if (lane == last) {
+    out.y = y;
+    out.logp = fma((double)x, tp.a, tp.b) * 0.6931471805599453 - log(tp.sum);
+  }
+  return out;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
+  __shared__ double s_w[kDraftChunk / kVec<T>], s_sum[kWavesD];
+  __shared__ PickOf s_pick;
+  __shared__ int s_whole, s_last;
+  const DraftShape& d = p.shape;
+  const int s = blockIdx.y, chunk = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const TreeOf t = tree_of(d, p.parents, p.count, s, lane);
+  const int n = t.count;
+  const int64_t row0 = (int64_t)s * d.nodes, rows = (int64_t)d.n * d.nodes;
+  if (n == 0) {
+    if (chunk == 0 && tid < d.nodes) {
+      p.out_tokens[row0 + tid] = p.out_path[row0 + tid] = -1;
+      p.out_logp[row0 + tid] = 0.f;
+    }
+    if (chunk == 0 && tid == 0) p.out_count[s] = 0;
+    return;
+  }
+  const bool argmax = greedy(p.temperature, s), sampled = p.draft != nullptr && !argmax;
+  const double it = inv_temp(p.temperature, s);
+  const EdgeOf e = edge_of(p, row0, lane, n);
+
+  // the walk, by every wave on its own
+  int at = 0, len = 1, order = lane == 0 ? 0 : -1;
+  double a = 0;
+  uint64_t gone = 0;  // children of `at` that were tried
+  for (bool moved = true; moved;) {
+    moved = false;
+    double Z = 1.0;
+    a = 0;
+    gone = 0;
+    const int p_arg = __builtin_amdgcn_readlane(e.p_arg, at);
+    const uint64_t kids = lane_u64(t.kids, at);
+    if (kids == 0 || p_arg < 0 || (sampled && __builtin_amdgcn_readlane(e.q_arg, at) < 0)) break;  // nothing to try
+    for (uint64_t m = kids; m; m &= m - 1) {
+      const int j = __ffsll((unsigned long long)m) - 1;
+      const int y = __builtin_amdgcn_readlane(e.tok, j);
+      const double u = (double)lane_f(e.u, j);
+      double w = lane_d(e.p, j);
+      bool stays;
+      if (argmax) {
+        stays = y == p_arg;
+      } else if (sampled) {
+        const double q = lane_d(e.q, j);
+        w = fmax(fma(-a, q, w), 0.0);
+        stays = u * q * Z < w;
+      } else {
+        if (__ballot((gone >> lane & 1) && e.tok == y)) w = 0;  // tried already
+        stays = u * Z < w;
+      }
+      if (stays) {
+        if (lane == j) order = len;
+        ++len;
+        at = j;
+        moved = true;
+        break;
+      }
+      if (argmax) continue;
+      gone |= 1ull << j;
+      a += Z;
+      if (!sampled) {
+        Z -= w;
+      } else if (m & (m - 1)) {  // (the last one's sum is still to be formed)
+        Z = left_after(p, row0 + j, lane);
+      }
+    }
+  }
+  bool residual = sampled && gone != 0;
+  if (!residual) a = 0;
+  if (chunk == 0 && tid < 64) {
+    if (order >= 0) {
+      p.out_path[row0 + order] = lane;
+      if (order > 0) {
+        p.out_tokens[row0 + order - 1] = e.tok;
+        p.out_logp[row0 + order - 1] = (float)log(e.p);
+      }
+    }
+    if (lane >= len && lane < d.nodes) {
+      p.out_path[row0 + lane] = p.out_tokens[row0 + lane] = -1;
+      p.out_logp[row0 + lane] = 0.f;
+    }
+    if (lane == 0) p.out_count[s] = len;
+  }
+  const int64_t row = row0 + at;
+  const RowDist tp = row_dist(p.row[row], it);
+  auto finish = [&](int64_t y, double logp) {
+    p.out_tokens[row0 + len - 1] = (int32_t)y;
+    p.out_logp[row0 + len - 1] = (float)logp;
+  };
+  if (!tp.usable || argmax) {
+    if (chunk == 0 && tid == 0) {
+      if (tp.usable) finish(tp.arg, -log(tp.sum));
+      else finish(-1, (double)__builtin_nanf(""));
+    }
+    return;
+  }
+  RowDist tq{};
+  if (residual) {
+    tq = row_dist(p.row[rows + row], it);
+    const double sum = residual_sum<T>(p, row, chunk, tp, tq, a, s_sum);
+    if (tid == 0) {
+      // written through to where all XCDs see it, and waited for, ahead of the count: a fence
+      // would write back the whole L2
+      __hip_atomic_store(p.ends + (int64_t)s * d.shorts + chunk, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      s_last = __hip_atomic_fetch_add(p.arrived + s, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == d.shorts - 1;
+    }
+    __syncthreads();
+    if (!s_last) return;
+  } else if (chunk != 0) {
+    return;
+  }
+
+  const DraftPart* part = p.part + row * d.chunks;
+  const T* target = (const T*)p.target + row * d.vocab;
+  if (tid < 64) {
+    // given drafts: the tokens of the children that were tried are gone, a lane each
+    double off = 0;
+    int off_at = -1;
+    if (!sampled && gone) {
+      bool is = (gone >> lane & 1) && e.tok >= 0 && e.tok < d.vocab;
+      for (uint64_t m = __ballot(is); m; m &= m - 1) {
+        const int j = __ffsll((unsigned long long)m) - 1;
+        if (lane > j && __builtin_amdgcn_readlane(e.tok, j) == e.tok) is = false;  // the same again
+      }
+      if (is) {
+        const int ahead = (int)((reinterpret_cast<uintptr_t>(target) / sizeof(T)) % kVec<T>);
+        off_at = (e.tok + ahead) / kDraftChunk;
+        off = e.p;
+      }
+    }
+    uint64_t takes = __ballot(off_at >= 0);
+    int chunks = residual ? d.shorts : d.chunks;
+    auto share = [&](int c) {  // of chunk c in what is left
+      const bool is = c < chunks;
+      if (residual) return is ? __hip_atomic_load(p.ends + (int64_t)s * d.shorts + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+      double x = is && part[c].max > kNegInf ? part[c].sum * tp.raw(part[c].max) / tp.sum : 0.0;
+      for (uint64_t m = takes; m; m &= m - 1) {  // (all lanes: they read each other's)
+        const int j = __ffsll((unsigned long long)m) - 1;
+        const double less = lane_d(off, j);
+        if (__builtin_amdgcn_readlane(off_at, j) == c) x -= less;
+      }
+      return fmax(x, 0.0);
+    };
+    auto whole_sum = [&]() {
+      double x = 0;
+      for (int c0 = 0; c0 < chunks; c0 += 64) x += share(c0 + lane);
+      return wave_sum_d(x);
+    };
+    double total = whole_sum();
+    if (!(total > 0)) {  // nothing is left: from p itself
+      residual = false;
+      chunks = d.chunks;
+      takes = 0;
+      total = whole_sum();
+    }
+    const double want = (double)p.u[row0] * total;
+    double start = 0, ahead = 0;
+    int pick = -1;
+    for (int c0 = 0; c0 < chunks; c0 += 64) {
+      const double x = share(c0 + lane);
+      double before;
+      bool passed;
+      const int who = pass_lane(x, start, want, lane, before, passed);
+      if (who >= 0) {  // (the last chunk that has any, should none pass)
+        pick = c0 + who;
+        ahead = before;
+      }
+      if (passed) break;
+      start += wave_sum_d(x);
+    }
+    const bool here = off_at == pick && (takes >> lane & 1);
+    const uint64_t in_chunk = __ballot(here);
+    if (here) s_pick.gone[__popcll(in_chunk & ((1ull << lane) - 1))] = e.tok;
+    if (lane == 0) {
+      s_pick.n_gone = __popcll(in_chunk);
+      s_pick.chunk = pick;
+      s_pick.want = want - ahead;
+      s_whole = !residual;
+    }
+  }
+  __syncthreads();
+  Picked got;
+  if (s_whole) got = pick_entry<T, kDraftChunk>(p, row, tp, tq, 0.0, s_pick, s_w);
+  else got = pick_entry<T, kDraftShort>(p, row, tp, tq, a, s_pick, s_w);
+  if (got.mine) finish(got.y, got.logp);
 }
 
 template <typename T>
@@ -693,18 +815,18 @@ hipError_t launch_draft_t(const DraftParams& p, hipStream_t s) {
     hipLaunchKernelGGL((draft_rows_kernel<T>), dim3(d.chunks, d.n * d.nodes, p.draft ? 2 : 1), dim3(kThreads), 0, s, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
+  {
+    TimingScope t("pp_verify_draft_edges", s);
+    hipLaunchKernelGGL((draft_edges_kernel<T>), dim3(d.n), dim3(kEdgeThreads), 0, s, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   for (int round = 0; p.draft && round + 1 < d.max_children; ++round) {
     TimingScope t("pp_verify_draft_residual", s);
-    hipLaunchKernelGGL((draft_residual_kernel<T>), dim3(d.chunks, d.n * d.nodes), dim3(kThreads), 0, s, p, round);
+    hipLaunchKernelGGL((draft_residual_kernel<T>), dim3(d.shorts, d.n), dim3(kThreads), 0, s, p, round);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  {
-    TimingScope t("pp_verify_draft_walk", s);
-    hipLaunchKernelGGL((draft_walk_kernel<T>), dim3(p.draft ? d.chunks : 1, d.n), dim3(kThreads), 0, s, p);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  TimingScope t("pp_verify_draft_sample", s);
-  hipLaunchKernelGGL((draft_sample_kernel<T>), dim3(d.n), dim3(kThreads), 0, s, p);
+  TimingScope t("pp_verify_draft_end", s);
+  hipLaunchKernelGGL((draft_end_kernel<T>), dim3(p.draft ? d.shorts : 1, d.n), dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }
 

@@ -155,9 +155,11 @@ struct TreeLaunch {
 hipError_t launch_tree_attn(const CacheView& c, const TreeLaunch& a, hipStream_t s);
 
 // Draft verification (pp_draft.hip).
-constexpr int kDraftChunk = 8192;  // entries of a row that a workgroup takes
+constexpr int kDraftChunk = 8192;  // entries of a row that a workgroup takes,
+constexpr int kDraftShort = 2048;  // and of what is left of one, where few rows are looked at
 struct DraftShape {
-  int n, nodes, vocab, chunks, max_children;
+  int n, nodes, vocab, max_children;
+  int chunks, shorts;  // of a row
 };
 // What a row's entries in one chunk hold: their maximum (NaN: a NaN or +inf among them), the
 // sum of e^((x - max) / T), and the first entry at the maximum.
@@ -166,17 +168,17 @@ struct DraftPart {
   float max;
   int32_t arg;
 };
-// Where a sequence's walk ends.
-struct DraftEnd {
-  double sum, a;   // of the node's row; the draft's factor in what is left of it (0: nothing taken off that way)
+// A row's distribution, joined from its chunks.
+struct DraftRow {
+  double sum;
   float max;
-  int32_t node;    // < 0: no such sequence
-  int32_t len;     // nodes kept
-  int32_t tried;   // children that were rejected
-  int32_t last;    // the last of them
-  int32_t arg;     // < 0: nothing to sample from
-  int32_t greedy;
-  int32_t pad;
+  int32_t arg;  // < 0: the row cannot be used
+};
+// Of a drafted token: its probabilities, and whether what is left after its rejection may be
+// asked for (first children).
+struct DraftEdge {
+  double p, q;
+  int32_t need, pad;
 };
 struct DraftParams {
   DraftShape shape;
@@ -192,9 +194,11 @@ struct DraftParams {
   int32_t* out_path;
   float* out_logp;
   DraftPart* part;  // [2, n, nodes, chunks]: of the target's rows, of the draft's
-  double* left;     // [n, nodes, chunks]: Z after a node is rejected
-  double* ends;     // [n, chunks]: Z where the walk ends
-  DraftEnd* end;    // [n]
+  double* left;     // [n, nodes, shorts]: Z after a node is rejected
+  DraftRow* row;    // [2, n, nodes]: the target's, the draft's (of nodes with children)
+  DraftEdge* edge;  // [n, nodes]
+  double* ends;     // [n, shorts]: Z where the walk ends
+  int32_t* arrived; // [n]: workgroups that have left theirs
 };
 hipError_t launch_verify_draft(const DraftParams& p, int dtype, hipStream_t s);
 

@@ -214,9 +214,11 @@ size_t carve_draft(DraftParams* p, void* ws) {
   const DraftShape& d = p->shape;
   const int64_t rows = (int64_t)d.n * d.nodes;
   p->part = at.take<DraftPart>(2 * rows * d.chunks);
-  p->left = at.take<double>(rows * d.chunks);
-  p->ends = at.take<double>((int64_t)d.n * d.chunks);
-  p->end = at.take<DraftEnd>(d.n);
+  p->left = at.take<double>(rows * d.shorts);
+  p->ends = at.take<double>((int64_t)d.n * d.shorts);
+  p->row = at.take<DraftRow>(2 * rows);
+  p->edge = at.take<DraftEdge>(rows);
+  p->arrived = at.take<int32_t>(d.n);
   return at.used;
 }
 
@@ -234,7 +236,9 @@ pp_status shape_draft(int n, int nodes, int vocab, int max_children, pp_dtype dt
   d->n = n;
   d->nodes = nodes;
   d->vocab = vocab;
-  d->chunks = (vocab + 16 / (dtype == PP_BF16 ? 2 : 4) - 1 + kDraftChunk - 1) / kDraftChunk;
+  const int reach = vocab + 16 / (dtype == PP_BF16 ? 2 : 4) - 1;  // from a 16-byte boundary on
+  d->chunks = (reach + kDraftChunk - 1) / kDraftChunk;
+  d->shorts = (reach + kDraftShort - 1) / kDraftShort;
   d->max_children = max_children < nodes ? max_children : nodes;
   return PP_OK;
 }
