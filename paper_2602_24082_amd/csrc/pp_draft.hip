@@ -12,7 +12,7 @@
 // drafts are given: y stays if u Z < w(y), else w(y) = 0.  From a node that none of its
 // children follow the next token is the first x at which the running sum of w passes u_0 Z.
 //
-//   draft_rows      a workgroup for 8192 entries of a row: maximum, sum, where the maximum is
+//   draft_rows      a wave for 2048 entries of a row: maximum, sum, where the maximum is
 //   draft_edges     a workgroup a sequence: rows' sums joined, p and q of every drafted token,
 //                   and which nodes can be reached at all: a first child's fate is known here
 //   draft_residual  Z after a rejected child that has siblings behind it and can be reached; one
@@ -39,8 +39,8 @@ constexpr int kWavesD = kThreads / 64;
 
 template <typename T>
 constexpr int kVec = 16 / sizeof(T);  // entries of a 16-byte load
-template <typename T, int CH>
-constexpr int kLoads = CH / (kThreads * kVec<T>);  // a thread's of a chunk
+template <typename T, int THREADS>
+constexpr int kLoads = kDraftChunk / (THREADS * kVec<T>);  // a thread's of a chunk
 
 __device__ __forceinline__ float to_float(uint16_t x) { return bf16_bits_to_f32(x); }
 __device__ __forceinline__ float to_float(float x) { return x; }
@@ -82,10 +82,10 @@ __device__ __forceinline__ double exp2_neg(double t) {
 template <typename T>
 using RawOf = T __attribute__((ext_vector_type(kVec<T>)));
 
-// A thread's entries of one chunk (CH entries) of a row: load u holds entries at(u) .. + kVec - 1, -inf
+// A thread's entries of one chunk of a row, of THREADS threads: load u holds entries at(u) .. + kVec - 1, -inf
 // outside the row.  Loads lie on the row's 16-byte boundaries; those that reach over an end of
 // the row are taken entry by entry.
-template <typename T, int CH>
+template <typename T, int THREADS>
 struct ChunkOf {
   using Raw = RawOf<T>;
   const T* row;
@@ -96,9 +96,9 @@ struct ChunkOf {
     row = r;
     vocab = v;
     const int ahead = (int)((reinterpret_cast<uintptr_t>(r) / sizeof(T)) % kVec<T>);
-    first = (int64_t)chunk * CH + thread * kVec<T> - ahead;
+    first = (int64_t)chunk * kDraftChunk + thread * kVec<T> - ahead;
   }
-  __device__ __forceinline__ int64_t at(int u) const { return first + (int64_t)u * kThreads * kVec<T>; }
+  __device__ __forceinline__ int64_t at(int u) const { return first + u * (THREADS * kVec<T>); }
   __device__ __forceinline__ Raw load(int u) const {
     const int64_t e = at(u);
     if (e >= 0 && e + kVec<T> <= vocab) return *reinterpret_cast<const Raw*>(row + e);
@@ -197,19 +197,17 @@ __device__ __forceinline__ double inv_temp(const float* temperature, int s) {
 }
 __device__ __forceinline__ bool greedy(const float* temperature, int s) { return temperature && !(temperature[s] > 0); }
 
+// A wave a chunk, without a barrier.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
-  __shared__ float s_m[kWavesD];
-  __shared__ int s_arg[kWavesD], s_bad[kWavesD];
-  __shared__ double s_sum[kWavesD];
-  constexpr int L = kLoads<T, kDraftChunk>;
+  constexpr int L = kLoads<T, 64>;
   const DraftShape& d = p.shape;
-  const int row = blockIdx.y, chunk = blockIdx.x, s = row / d.nodes, node = row - s * d.nodes;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = blockIdx.y, chunk = blockIdx.x * kWavesD + wave, s = row / d.nodes, node = row - s * d.nodes;
   const bool is_draft = blockIdx.z != 0, argmax = greedy(p.temperature, s);
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int n = max(0, min(p.count ? p.count[s] : d.nodes, d.nodes));
-  if (node == 0 && chunk == 0 && !is_draft && tid == 0) p.arrived[s] = 0;
-  if (node >= n) return;
+  if (node == 0 && chunk == 0 && !is_draft && lane == 0) p.arrived[s] = 0;
+  if (node >= n || chunk >= d.chunks) return;
   if (is_draft) {
     if (argmax) return;
     bool kid = false;  // only nodes with children have drafts
@@ -217,11 +215,12 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
       kid = kid || (p.parents ? p.parents[(int64_t)s * d.nodes + j] == node : j == node + 1);
     if (!__any(kid)) return;
   }
-  ChunkOf<T, kDraftChunk> c;
-  c.init((const T*)(is_draft ? p.draft : p.target) + (int64_t)row * d.vocab, d.vocab, chunk, tid);
+  ChunkOf<T, 64> c;
+  c.init((const T*)(is_draft ? p.draft : p.target) + (int64_t)row * d.vocab, d.vocab, chunk, lane);
   RawOf<T> x[L];
 #pragma unroll
   for (int u = 0; u < L; ++u) x[u] = c.load(u);
+  const double a = inv_temp(p.temperature, s);
   float m = kNegInf;
   typename BitsOf<T>::Type bits{};
 #pragma unroll
@@ -230,55 +229,32 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
 #pragma unroll
     for (int i = 0; i < kVec<T>; ++i) m = fmaxf(m, to_float(x[u][i]));
   }
-  m = wave_max(m);
-  const bool nan = __any(most_bits(bits) > kInfBits<T>);
-  if (lane == 0) {
-    s_m[wave] = m;
-    s_bad[wave] = nan;
-  }
-  __syncthreads();
-  float top = kNegInf;
-  bool bad = false;
-#pragma unroll
-  for (int w = 0; w < kWavesD; ++w) {
-    top = fmaxf(top, s_m[w]);
-    bad = bad || s_bad[w];
-  }
-  bad = bad || top == -kNegInf;
-  const double a = inv_temp(p.temperature, s), b = -(double)top * a;
-  double sum = 0;
-  int arg = 0x7fffffff;
+  const float top = wave_max(m);
+  const bool bad = __any(most_bits(bits) > kInfBits<T>) || top == -kNegInf;
+  DraftPart out;
+  out.sum = 0;
+  out.arg = 0x7fffffff;
+  out.max = bad ? __builtin_nanf("") : top > lowest<T>() ? top : kNegInf;
   if (top > lowest<T>() && !bad) {
+    const double b = -(double)top * a;
+    double sum = 0;
 #pragma unroll
     for (int u = 0; u < L; ++u)
 #pragma unroll
       for (int i = 0; i < kVec<T>; ++i) sum += exp2_neg(fma((double)to_float(x[u][i]), a, b));
-    sum = wave_sum_d(sum);
+    out.sum = wave_sum_d(sum);
     if (argmax) {
+      int arg = 0x7fffffff;
 #pragma unroll
       for (int u = 0; u < L; ++u)
 #pragma unroll
         for (int i = 0; i < kVec<T>; ++i)
           if (to_float(x[u][i]) == top) arg = min(arg, (int)(c.at(u) + i));
       for (int off = 32; off > 0; off >>= 1) arg = min(arg, __shfl_xor(arg, off, 64));
+      out.arg = arg;
     }
   }
-  if (lane == 0) {
-    s_sum[wave] = sum;
-    s_arg[wave] = arg;
-  }
-  __syncthreads();
-  if (tid == 0) {
-    DraftPart out;
-    out.sum = 0;
-    out.arg = 0x7fffffff;
-    for (int w = 0; w < kWavesD; ++w) {
-      out.sum += s_sum[w];
-      out.arg = min(out.arg, s_arg[w]);
-    }
-    out.max = bad ? __builtin_nanf("") : top > lowest<T>() ? top : kNegInf;
-    p.part[((int64_t)blockIdx.z * d.n * d.nodes + row) * d.chunks + chunk] = out;
-  }
+  if (lane == 0) p.part[((int64_t)blockIdx.z * d.n * d.nodes + row) * d.chunks + chunk] = out;
 }
 
 // A row's distribution, 2^(a x + b) / sum, a = log2(e) / T.
@@ -340,10 +316,10 @@ __device__ __forceinline__ RowDist row_dist(const DraftPart* part, int chunks, d
 }
 
 // What is left of a row's distribution: max(p - a q, 0), or p where there is no q.
-template <typename T, int CH>
+template <typename T>
 struct LeftOf {
-  static constexpr int L = kLoads<T, CH>;
-  ChunkOf<T, CH> c;  // the target's row
+  static constexpr int L = kLoads<T, kThreads>;
+  ChunkOf<T, kThreads> c;  // the target's row
   const T* q;     // or null
   RowDist tp, tq;
   double ip, iq;  // 1 / sum, a / sum
@@ -366,7 +342,7 @@ struct LeftOf {
   template <typename Use>
   __device__ __forceinline__ void each(Use&& use) const {
     RawOf<T> x[L], y[L];
-    ChunkOf<T, CH> cq = c;
+    ChunkOf<T, kThreads> cq = c;
     cq.row = q;
 #pragma unroll
     for (int u = 0; u < L; ++u) x[u] = c.load(u);
@@ -391,11 +367,11 @@ struct LeftOf {
   }
 };
 
-// Sum over a short chunk of max(p - a q, 0), valid in every thread.
+// Sum over a chunk of max(p - a q, 0), valid in every thread.
 template <typename T>
 __device__ __forceinline__ double residual_sum(const DraftParams& p, int64_t row, int chunk, const RowDist& tp, const RowDist& tq,
                                                double a, double* s_sum) {
-  LeftOf<T, kDraftShort> left;
+  LeftOf<T> left;
   left.init(p, row, chunk, tp, tq, a);
   double sum = 0;
   left.each([&](int, int, double w) { sum += w; });
@@ -433,7 +409,7 @@ __device__ __forceinline__ EdgeOf edge_of(const DraftParams& p, int64_t row0, in
 // Z after a node is rejected, by a wave.
 __device__ __forceinline__ double left_after(const DraftParams& p, int64_t node, int lane) {
   double z = 0;
-  for (int c = lane; c < p.shape.shorts; c += 64) z += p.left[node * p.shape.shorts + c];
+  for (int c = lane; c < p.shape.chunks; c += 64) z += p.left[node * p.shape.chunks + c];
   return wave_sum_d(z);
 }
 
@@ -500,7 +476,7 @@ __global__ __launch_bounds__(kEdgeThreads) void draft_edges_kernel(DraftParams p
   if (lane < n) p.edge[row0 + lane] = e;
 }
 
-// Z after a child of rank `round` is rejected that has a sibling behind it, a short chunk's
+// Z after a child of rank `round` is rejected that has a sibling behind it, a chunk's
 // share, for every node where it may be asked for.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void draft_residual_kernel(DraftParams p, int round) {
@@ -534,7 +510,7 @@ __global__ __launch_bounds__(kThreads) void draft_residual_kernel(DraftParams p,
     if (stays) continue;
     const RowDist tp = row_dist(p.row[row0 + up], it), tq = row_dist(p.row[rows + row0 + up], it);
     const double sum = residual_sum<T>(p, row0 + up, chunk, tp, tq, a, s_sum);
-    if (threadIdx.x == 0) p.left[(row0 + j) * d.shorts + chunk] = sum;
+    if (threadIdx.x == 0) p.left[(row0 + j) * d.chunks + chunk] = sum;
   }
 }
 
@@ -562,13 +538,13 @@ struct Picked {
 };
 // By the workgroup: the entry of the chunk at which the running sum of what is left passes; s_w:
 // room for the sums of the chunk's loads.
-template <typename T, int CH>
+template <typename T>
 __device__ __forceinline__ Picked pick_entry(const DraftParams& p, int64_t row, const RowDist& tp, const RowDist& tq, double a,
                                              const PickOf& pick, double* s_w) {
-  constexpr int VPC = CH / kVec<T>, PER = VPC / 64, L = kLoads<T, CH>;  // loads of a chunk, a lane's, a thread's
+  constexpr int VPC = kDraftChunk / kVec<T>, PER = VPC / 64, L = kLoads<T, kThreads>;  // loads of a chunk, a lane's, a thread's
   const int tid = threadIdx.x, lane = tid & 63;
   Picked out{false, -1, (double)__builtin_nanf("")};
-  LeftOf<T, CH> left;
+  LeftOf<T> left;
   left.init(p, row, pick.chunk, tp, tq, a);
   const int n_gone = pick.n_gone;
   auto is_gone = [&](int64_t y) {
@@ -721,9 +697,9 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
     if (tid == 0) {
       // written through to where all XCDs see it, and waited for, ahead of the count: a fence
       // would write back the whole L2
-      __hip_atomic_store(p.ends + (int64_t)s * d.shorts + chunk, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(p.ends + (int64_t)s * d.chunks + chunk, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      s_last = __hip_atomic_fetch_add(p.arrived + s, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == d.shorts - 1;
+      s_last = __hip_atomic_fetch_add(p.arrived + s, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == d.chunks - 1;
     }
     __syncthreads();
     if (!s_last) return;
@@ -750,10 +726,9 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
       }
     }
     uint64_t takes = __ballot(off_at >= 0);
-    int chunks = residual ? d.shorts : d.chunks;
     auto share = [&](int c) {  // of chunk c in what is left
-      const bool is = c < chunks;
-      if (residual) return is ? __hip_atomic_load(p.ends + (int64_t)s * d.shorts + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
+      const bool is = c < d.chunks;
+      if (residual) return is ? __hip_atomic_load(p.ends + (int64_t)s * d.chunks + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
       double x = is && part[c].max > kNegInf ? part[c].sum * tp.raw(part[c].max) / tp.sum : 0.0;
       for (uint64_t m = takes; m; m &= m - 1) {  // (all lanes: they read each other's)
         const int j = __ffsll((unsigned long long)m) - 1;
@@ -764,20 +739,19 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
     };
     auto whole_sum = [&]() {
       double x = 0;
-      for (int c0 = 0; c0 < chunks; c0 += 64) x += share(c0 + lane);
+      for (int c0 = 0; c0 < d.chunks; c0 += 64) x += share(c0 + lane);
       return wave_sum_d(x);
     };
     double total = whole_sum();
     if (!(total > 0)) {  // nothing is left: from p itself
       residual = false;
-      chunks = d.chunks;
       takes = 0;
       total = whole_sum();
     }
     const double want = (double)p.u[row0] * total;
     double start = 0, ahead = 0;
     int pick = -1;
-    for (int c0 = 0; c0 < chunks; c0 += 64) {
+    for (int c0 = 0; c0 < d.chunks; c0 += 64) {
       const double x = share(c0 + lane);
       double before;
       bool passed;
@@ -800,9 +774,7 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
     }
   }
   __syncthreads();
-  Picked got;
-  if (s_whole) got = pick_entry<T, kDraftChunk>(p, row, tp, tq, 0.0, s_pick, s_w);
-  else got = pick_entry<T, kDraftShort>(p, row, tp, tq, a, s_pick, s_w);
+  const Picked got = pick_entry<T>(p, row, tp, tq, s_whole ? 0.0 : a, s_pick, s_w);
   if (got.mine) finish(got.y, got.logp);
 }
 
@@ -812,7 +784,7 @@ hipError_t launch_draft_t(const DraftParams& p, hipStream_t s) {
   hipError_t e;
   {
     TimingScope t("pp_verify_draft_rows", s);
-    hipLaunchKernelGGL((draft_rows_kernel<T>), dim3(d.chunks, d.n * d.nodes, p.draft ? 2 : 1), dim3(kThreads), 0, s, p);
+    hipLaunchKernelGGL((draft_rows_kernel<T>), dim3((d.chunks + kWavesD - 1) / kWavesD, d.n * d.nodes, p.draft ? 2 : 1), dim3(kThreads), 0, s, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   {
@@ -822,11 +794,11 @@ hipError_t launch_draft_t(const DraftParams& p, hipStream_t s) {
   }
   for (int round = 0; p.draft && round + 1 < d.max_children; ++round) {
     TimingScope t("pp_verify_draft_residual", s);
-    hipLaunchKernelGGL((draft_residual_kernel<T>), dim3(d.shorts, d.n), dim3(kThreads), 0, s, p, round);
+    hipLaunchKernelGGL((draft_residual_kernel<T>), dim3(d.chunks, d.n), dim3(kThreads), 0, s, p, round);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   TimingScope t("pp_verify_draft_end", s);
-  hipLaunchKernelGGL((draft_end_kernel<T>), dim3(p.draft ? d.shorts : 1, d.n), dim3(kThreads), 0, s, p);
+  hipLaunchKernelGGL((draft_end_kernel<T>), dim3(p.draft ? d.chunks : 1, d.n), dim3(kThreads), 0, s, p);
   return hipGetLastError();
 }
 

@@ -155,11 +155,9 @@ struct TreeLaunch {
 hipError_t launch_tree_attn(const CacheView& c, const TreeLaunch& a, hipStream_t s);
 
 // Draft verification (pp_draft.hip).
-constexpr int kDraftChunk = 8192;  // entries of a row that a workgroup takes,
-constexpr int kDraftShort = 2048;  // and of what is left of one, where few rows are looked at
+constexpr int kDraftChunk = 2048;  // entries of a row that are looked at together
 struct DraftShape {
-  int n, nodes, vocab, max_children;
-  int chunks, shorts;  // of a row
+  int n, nodes, vocab, chunks, max_children;
 };
 // What a row's entries in one chunk hold: their maximum (NaN: a NaN or +inf among them), the
 // sum of e^((x - max) / T), and the first entry at the maximum.
@@ -194,10 +192,10 @@ struct DraftParams {
   int32_t* out_path;
   float* out_logp;
   DraftPart* part;  // [2, n, nodes, chunks]: of the target's rows, of the draft's
-  double* left;     // [n, nodes, shorts]: Z after a node is rejected
+  double* left;     // [n, nodes, chunks]: Z after a node is rejected
   DraftRow* row;    // [2, n, nodes]: the target's, the draft's (of nodes with children)
   DraftEdge* edge;  // [n, nodes]
-  double* ends;     // [n, shorts]: Z where the walk ends
+  double* ends;     // [n, chunks]: Z where the walk ends
   int32_t* arrived; // [n]: workgroups that have left theirs
 };
 hipError_t launch_verify_draft(const DraftParams& p, int dtype, hipStream_t s);

@@ -214,8 +214,8 @@ size_t carve_draft(DraftParams* p, void* ws) {
   const DraftShape& d = p->shape;
   const int64_t rows = (int64_t)d.n * d.nodes;
   p->part = at.take<DraftPart>(2 * rows * d.chunks);
-  p->left = at.take<double>(rows * d.shorts);
-  p->ends = at.take<double>((int64_t)d.n * d.shorts);
+  p->left = at.take<double>(rows * d.chunks);
+  p->ends = at.take<double>((int64_t)d.n * d.chunks);
   p->row = at.take<DraftRow>(2 * rows);
   p->edge = at.take<DraftEdge>(rows);
   p->arrived = at.take<int32_t>(d.n);
@@ -238,7 +238,6 @@ pp_status shape_draft(int n, int nodes, int vocab, int max_children, pp_dtype dt
   d->vocab = vocab;
   const int reach = vocab + 16 / (dtype == PP_BF16 ? 2 : 4) - 1;  // from a 16-byte boundary on
   d->chunks = (reach + kDraftChunk - 1) / kDraftChunk;
-  d->shorts = (reach + kDraftShort - 1) / kDraftShort;
   d->max_children = max_children < nodes ? max_children : nodes;
   return PP_OK;
 }
