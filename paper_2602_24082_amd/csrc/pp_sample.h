@@ -88,17 +88,29 @@ hipError_t launch_cache_shared(const CacheView& c, int groups, const int32_t* sl
 hipError_t launch_cache_append(const CacheView& c, const AppendParams& a, int n, int head_dim, int dtype, hipStream_t s);
 
 // Attention of drafted trees over the cache (pp_tree.hip).
+#ifndef PP_TEAM_CU
+#define PP_TEAM_CU 2
+#define PP_TEAM_KEYS 64
+#define PP_TEAM_STAGES 2
+#endif
 constexpr int kTreeSeqs = 2048;  // sequences a call
 constexpr int kTreeNodes = 64;   // nodes a sequence
 constexpr int kCus = 256;
 // Workgroups a compute unit: of one wave, each with a ring of two blocks of 32 keys and values
-// in LDS, and of a team of four waves, with two blocks of 64 (fp32: 32) between them.
+// in LDS, and of a team of four waves, with a ring between them.
 template <int D, typename T>
 constexpr int kTreeSolo = D * sizeof(T) > 256 ? 2 : D * sizeof(T) > 128 ? 4 : 8;
 template <int D, typename T>
-constexpr int kTreeTeam = sizeof(T) == 4 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : 2;
-template <typename T>
-constexpr int kTeamKeys = sizeof(T) == 2 ? 64 : 32;
+constexpr int kTreeTeam = sizeof(T) == 4 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : PP_TEAM_CU;
+template <int D, typename T>
+constexpr int kTeamKeys = sizeof(T) == 2 ? PP_TEAM_KEYS : 32;
+// Blocks that a team has room for: what a compute unit's LDS leaves each
+template <int D, typename T>
+constexpr int kTeamStages = sizeof(T) == 2 && D == 128 ? PP_TEAM_STAGES : D * sizeof(T) > 128 ? 4 : 3;
+#ifndef PP_TREE_START
+#define PP_TREE_START 4
+#endif
+constexpr int kTreeStart = PP_TREE_START;
 constexpr int kSoloKeys = 32, kSoloRows = 32, kTeamWaves = 4, kTeamRows = 128;
 
 // An item: rows against a range of keys; its units: a block of keys, for a tile of rows of one
@@ -110,14 +122,16 @@ struct TreeItem {
   int32_t seen;    // all rows see the keys below
   int32_t seq;     // the (first) sequence of its rows
   int32_t bad;     // nodes asked for of a sequence that is not sound
-  int32_t pad;
+  int32_t rows;    // for one kv-head: nodes in use x G
+  int32_t row0;    // a sequence's first node among its group's
+  int32_t pad[3];
 };
 // The two kinds of items: a group's shared keys, a sequence's own.
 struct TreeKind {
-  int rows;       // of an item, for one kv-head
+  int rows;       // of an item, for one kv-head, at most
   int team;       // more than 32: taken by teams
   int keys;       // of a block
-  int tiles;      // of rows; 0: no such items
+  int tiles;      // of rows, at most; 0: no such items
   int part_rows;  // of a partial result
   int64_t part0;  // row of the first one
 };
@@ -129,7 +143,7 @@ struct TreeShape {
 };
 struct TreePlan {
   TreeItem* items;         // [n + groups]
-  int32_t* live;           // [n]: nodes of a sequence
+  int32_t* nodes;          // [n * max_new]: a group's nodes in use, the rows of its shared keys
   int64_t* first[2];       // [n + groups]: units ahead of an item, of those that solo waves / teams take
   int64_t* head;           // [2][2]: units in all, units a worker
   int32_t* start_item[2];  // [workers]: where a worker starts

@@ -167,7 +167,7 @@ bool shape_tree(int n, int group, int nodes, int hq, int hkv, pp_dtype dtype, in
     x = TreeKind{};
     x.rows = k == 0 && (group == 1 || !shared) ? 0 : (int)rows;
     x.team = x.rows > kSoloRows;
-    x.keys = x.team ? (bf16 ? kTeamKeys<uint16_t> : kTeamKeys<float>) : kSoloKeys;
+    x.keys = !x.team ? kSoloKeys : bf16 ? kTeamKeys<128, uint16_t> : kTeamKeys<128, float>;
     const int tile = x.team ? kTeamRows : kSoloRows;
     x.tiles = (x.rows + tile - 1) / tile;
     x.part_rows = x.rows < tile ? x.rows : tile;
@@ -183,7 +183,7 @@ size_t carve_tree(const TreeShape& t, int d, void* ws, TreeLaunch* a) {
   Carve at(ws);
   const int items = t.n + t.groups;
   a->plan.items = at.take<TreeItem>(items);
-  a->plan.live = at.take<int32_t>(t.n);
+  a->plan.nodes = at.take<int32_t>((int64_t)t.n * t.nodes);
   a->plan.head = at.take<int64_t>(4);
   for (int c = 0; c < 2; ++c) {
     a->plan.first[c] = at.take<int64_t>(items);

@@ -54,88 +54,132 @@ __device__ __forceinline__ int64_t plan_scan64(int64_t x, int64_t* total) {
   return before + s - x;
 }
 
+// a / b for a >= 0, b > 0, short where both are
+__device__ __forceinline__ int64_t div_floor(int64_t a, int64_t b) {
+  if (((uint64_t)(a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
+  return a / b;
+}
+
+// What a tile of an item counts as where units are dealt out: its blocks, and what its start
+// costs (rows, pages and the first keys to fetch, a partial result to leave) in blocks.
+__device__ __forceinline__ int units_of(int blocks) { return blocks ? blocks + kTreeStart : 0; }
+__device__ __forceinline__ int rows_a_tile(const TreeKind& k) { return k.team ? kTeamRows : kSoloRows; }
+__device__ __forceinline__ int tiles_of(int rows, const TreeKind& k) { return (rows + rows_a_tile(k) - 1) / rows_a_tile(k); }
+
 // Items in the order of the groups: a group's shared keys, then its sequences' own.
 __global__ __launch_bounds__(kPlan) void tree_plan_kernel(CacheView c, TreeShape t, const int32_t* slots, const int32_t* count,
                                                           const int32_t* shared, TreePlan out) {
-  __shared__ int s_shared[kTreeSeqs], s_lead[kTreeSeqs], s_members[kTreeSeqs];
-  __shared__ int s_blocks[2 * kTreeSeqs];
+  __shared__ int s_shared[kTreeSeqs], s_lead[kTreeSeqs], s_nodes[kTreeSeqs + 1];
+  __shared__ int64_t s_units[2 * kTreeSeqs];
   __shared__ int64_t s_first[2 * kTreeSeqs];
+  constexpr int PER = kTreeSeqs / kPlan;  // sequences a thread, next to each other
   const int tid = threadIdx.x, items = t.n + t.groups;
-  for (int g = tid; g < t.groups; g += kPlan) {
-    s_shared[g] = s_lead[g] = 0x7fffffff;
-    s_members[g] = 0;
+  const bool share = t.kind[0].tiles > 0;
+  int slot_of[PER], len_of[PER], live_of[PER], bad_of[PER], lead = 0;
+  for (int g = tid; share && g < t.groups; g += kPlan) s_shared[g] = s_lead[g] = 0x7fffffff;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int i = tid * PER + u;
+    slot_of[u] = i < t.n ? slots[i] : -1;
+    bad_of[u] = slot_of[u] < 0 ? 0 : max(0, min(count ? count[i] : t.nodes, t.nodes));  // asked for
   }
-  __syncthreads();
-  auto look = [&](int i, int& len, int& live) {  // nodes asked for of a sequence that is not sound
-    const int slot = slots[i];
-    len = live = 0;
-    const int want = max(0, min(count ? count[i] : t.nodes, t.nodes));
-    if (slot < 0 || want == 0) return 0;
-    if (!c.has_slot(slot)) return want;
-    const int64_t n = c.seq_len[slot], held = c.held[slot];
-    if (!c.sound(n, held) || n + want > held << c.page_log2) return want;
-    len = (int)n;
-    live = want;
-    return 0;
-  };
-  for (int i = tid; i < t.n; i += kPlan) {
-    int len, live;
-    look(i, len, live);
-    out.live[i] = live;
-    if (!live || !t.kind[0].tiles) continue;
-    const int g = i / t.group;
-    atomicMin(&s_shared[g], len);
-    atomicMin(&s_lead[g], i);
-    atomicAdd(&s_members[g], 1);
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    len_of[u] = live_of[u] = 0;
+    if (bad_of[u] == 0 || !c.has_slot(slot_of[u])) continue;
+    const int64_t n = c.seq_len[slot_of[u]], held = c.held[slot_of[u]];
+    if (!c.sound(n, held) || n + bad_of[u] > held << c.page_log2) continue;
+    len_of[u] = (int)n;
+    live_of[u] = bad_of[u];
+    bad_of[u] = 0;
   }
-  __syncthreads();
-  for (int g = tid; g < t.groups; g += kPlan) {
-    TreeItem it{};
-    if (t.kind[0].tiles && s_members[g] > 1) {
-      const int pages = max(0, min(shared[g], s_shared[g] >> c.page_log2));
-      it.k1 = it.seen = pages << c.page_log2;
-      it.blocks = (it.k1 + t.kind[0].keys - 1) / t.kind[0].keys;
-      it.slot = slots[s_lead[g]];
-    }
-    it.seq = g * t.group;
-    s_shared[g] = it.k1;
-    out.items[g * (t.group + 1)] = it;
-    s_blocks[g * (t.group + 1)] = it.blocks;
-  }
-  __syncthreads();
-  for (int i = tid; i < t.n; i += kPlan) {
-    const int g = i / t.group, at = i + g + 1;
-    int len, live;
-    TreeItem it{};
-    it.bad = look(i, len, live);
-    it.seq = i;
-    if (live) {
-      it.slot = slots[i];
-      it.k0 = s_shared[g];
-      it.k1 = len + live;
-      it.seen = len;
-      it.blocks = (it.k1 - it.k0 + t.kind[1].keys - 1) / t.kind[1].keys;
-    }
-    out.items[at] = it;
-    s_blocks[at] = it.blocks;
-  }
-  for (int cls = 0; cls < 2; ++cls) {
-    const bool takes[2] = {t.kind[0].tiles > 0 && t.kind[0].team == cls, t.kind[1].team == cls};
-    if (!takes[0] && !takes[1]) continue;
-    __syncthreads();
-    constexpr int PER = 2 * kTreeSeqs / kPlan;
-    int64_t w[PER], sum = 0, total;
+  if (share) {
+    // the nodes in use, group by group, are the rows of the shared keys
+    int64_t sum = 0, total;
+#pragma unroll
+    for (int u = 0; u < PER; ++u) sum += live_of[u];
+    lead = (int)plan_scan64(sum, &total);  // (its barriers cover s_shared's start as well)
+    int at = lead;
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
-      const int at = tid * PER + u, own = at % (t.group + 1) != 0;
-      w[u] = at < items && takes[own] ? (int64_t)s_blocks[at] * t.kind[own].tiles * t.hkv : 0;
+      const int i = tid * PER + u;
+      if (i <= t.n) s_nodes[i] = at;
+      at += live_of[u];
+      if (!live_of[u]) continue;
+      atomicMin(&s_shared[i / t.group], len_of[u]);
+      atomicMin(&s_lead[i / t.group], i);
+    }
+    if (tid == 0) s_nodes[t.n] = (int)total;
+    __syncthreads();
+    for (int g = tid; g < t.groups; g += kPlan) {
+      TreeItem it{};
+      const int nodes = s_nodes[min(t.n, (g + 1) * t.group)] - s_nodes[g * t.group];
+      const int first = s_lead[g];
+      // with one sequence in use there is nobody to share with
+      if (nodes > 0 && first < t.n && s_nodes[first + 1] - s_nodes[first] < nodes) {
+        const int pages = max(0, min(shared[g], s_shared[g] >> c.page_log2));
+        it.k1 = it.seen = pages << c.page_log2;
+        it.blocks = (it.k1 + t.kind[0].keys - 1) / t.kind[0].keys;
+        it.slot = slots[first];
+        it.rows = nodes * t.G;
+      }
+      it.seq = g * t.group;
+      s_shared[g] = it.k1;
+      out.items[g * (t.group + 1)] = it;
+      s_units[g * (t.group + 1)] = (int64_t)tiles_of(it.rows, t.kind[0]) * units_of(it.blocks);
+    }
+    __syncthreads();
+  } else {
+    for (int g = tid; g < t.groups; g += kPlan) {
+      TreeItem it{};
+      it.seq = g * t.group;
+      out.items[g * (t.group + 1)] = it;
+      s_units[g * (t.group + 1)] = 0;
+    }
+  }
+  int at = lead;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int i = tid * PER + u;
+    if (i >= t.n) continue;
+    const int g = i / t.group;
+    TreeItem it{};
+    it.bad = bad_of[u];
+    it.seq = i;
+    if (share) {
+      const int base = s_nodes[g * t.group];
+      it.row0 = at - base;
+      for (int k = 0; k < live_of[u]; ++k) out.nodes[(int64_t)g * t.group * t.nodes + it.row0 + k] = i * t.nodes + k;
+      at += live_of[u];
+    }
+    if (live_of[u]) {
+      it.slot = slot_of[u];
+      it.k0 = share ? s_shared[g] : 0;
+      it.k1 = len_of[u] + live_of[u];
+      it.seen = len_of[u];
+      it.blocks = (it.k1 - it.k0 + t.kind[1].keys - 1) / t.kind[1].keys;
+      it.rows = live_of[u] * t.G;
+    }
+    out.items[i + g + 1] = it;
+    s_units[i + g + 1] = (int64_t)tiles_of(it.rows, t.kind[1]) * units_of(it.blocks);
+  }
+  for (int cls = 0; cls < 2; ++cls) {
+    const bool takes[2] = {share && t.kind[0].team == cls, t.kind[1].team == cls};
+    if (!takes[0] && !takes[1]) continue;
+    __syncthreads();
+    constexpr int PER_ITEM = 2 * kTreeSeqs / kPlan;
+    int64_t w[PER_ITEM], sum = 0, total;
+#pragma unroll
+    for (int u = 0; u < PER_ITEM; ++u) {
+      const int k = tid * PER_ITEM + u;
+      w[u] = k < items && takes[k % (t.group + 1) != 0] ? s_units[k] * t.hkv : 0;
       sum += w[u];
     }
     int64_t before = plan_scan64(sum, &total);
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int at = tid * PER + u;
-      if (at < items) s_first[at] = out.first[cls][at] = before;
+    for (int u = 0; u < PER_ITEM; ++u) {
+      const int k = tid * PER_ITEM + u;
+      if (k < items) s_first[k] = out.first[cls][k] = before;
       before += w[u];
     }
     __syncthreads();
@@ -201,7 +245,8 @@ struct TreeRun {
   TreeItem it;
   int own;         // which kind of item
   int g, tile;     // kv-head, tile of rows
-  int key, blocks; // from key on (a multiple of 16)
+  int key, blocks; // from key on (a multiple of 16); blocks 0: the run ends ahead of the first
+  int units;
   int64_t prow;    // row of its partial result
 };
 
@@ -217,13 +262,16 @@ __device__ __forceinline__ TreeRun tree_run(const TreeShape& sh, const TreePlan&
     if (kind.tiles == 0 || kind.team != cls) continue;
     r.it = load_uniform(plan.items + item);
     const int64_t rel = pos - plan.first[cls][item];
-    if (rel >= (int64_t)r.it.blocks * kind.tiles * sh.hkv) continue;  // none, or this one's end
-    const int j = (int)(rel / r.it.blocks), b0 = (int)(rel - (int64_t)j * r.it.blocks);
-    r.g = j / kind.tiles;
-    r.tile = j - r.g * kind.tiles;
+    const int units = units_of(r.it.blocks), tiles = tiles_of(r.it.rows, kind);
+    if (rel >= (int64_t)units * tiles * sh.hkv) continue;  // none, or this one's end
+    const int j = (int)div_floor(rel, units), u0 = (int)(rel - (int64_t)j * units);
+    r.g = j / tiles;
+    r.tile = j - r.g * tiles;
+    r.units = (int)min((int64_t)(units - u0), end - pos);
+    const int b0 = max(u0 - kTreeStart, 0);
+    r.blocks = max(u0 + r.units - kTreeStart, 0) - b0;
     r.key = r.it.k0 + kind.keys * b0;
-    r.blocks = (int)min((int64_t)(r.it.blocks - b0), end - pos);
-    const int64_t tile = (int64_t)(r.own ? r.it.seq : grp) * kind.tiles * sh.hkv + j;
+    const int64_t tile = (int64_t)((r.own ? r.it.seq : grp) * sh.hkv + r.g) * kind.tiles + r.tile;
     r.prow = kind.part0 + (tile + worker) * kind.part_rows;
     return r;
   }
@@ -239,10 +287,11 @@ template <int D, typename T>
 __device__ __forceinline__ TreeRow tree_row(const TreeShape& sh, const TreeParams<T>& p, const TreeRun& r, int row, uint64_t path,
                                             bool path_fine) {
   const int node_at = row / sh.G, head = r.g * sh.G + (row - node_at * sh.G);
-  const int m = r.own ? 0 : node_at / sh.nodes, node = node_at - m * sh.nodes, seq = r.it.seq + m;
-  const bool live = row < sh.kind[r.own].rows && node < p.plan.live[min(seq, sh.n - 1)];
+  const bool live = row < r.it.rows;
+  const int64_t tok = !live ? 0 : r.own ? (int64_t)r.it.seq * sh.nodes + node_at
+                                       : p.plan.nodes[(int64_t)r.it.seq * sh.nodes + node_at];
   TreeRow x;
-  x.q = live ? (((int64_t)seq * sh.nodes + node) * sh.hq + head) * D : -1;
+  x.q = live ? (tok * sh.hq + head) * D : -1;
   const uint64_t tree = __shfl(path, min(node_at, 63), 64);
   const int fine = __shfl((int)path_fine, min(node_at, 63), 64);
   x.tree = r.own ? tree : 0;
@@ -316,12 +365,12 @@ __device__ __forceinline__ void leave_partial(const TreeParams<T>& p, const RowS
   }
 }
 
-// Two stages of keys and values.  The DMA goes by byte addresses in LDS: a generic pointer,
+// Stages of keys and values.  The DMA goes by byte addresses in LDS: a generic pointer,
 // carried round the kernels' outer loops, is checked for null where it is turned back, in a
 // form that the compiler cannot encode.
-template <typename T, int N>
+template <typename T, int S, int N>
 struct TreeRing {
-  T kv[2][2][N];  // [stage][K / V]
+  T kv[S][2][N];  // [stage][K / V]
 };
 template <typename X>
 __device__ __forceinline__ __attribute__((address_space(3))) X* in_lds(X* x) {
@@ -347,7 +396,7 @@ __global__ __launch_bounds__(64, 2) void tree_solo_kernel(CacheView c, TreeShape
   using Frag = typename O::Frag;
   using Dma = RowDma<T, D, 16>;
   constexpr int NC = D / 16, KN = 2 * Dma::N;
-  __shared__ __attribute__((aligned(1024))) TreeRing<T, kSoloKeys * D> smem;
+  __shared__ __attribute__((aligned(1024))) TreeRing<T, 2, kSoloKeys * D> smem;
   auto* ring = in_lds(&smem);
   const int worker = blockIdx.x, lane = threadIdx.x & 63, ln = lane & 31, hf = lane >> 5;
   const int64_t total = p.plan.head[0], run_len = p.plan.head[1];
@@ -359,6 +408,7 @@ __global__ __launch_bounds__(64, 2) void tree_solo_kernel(CacheView c, TreeShape
   dma.init(0, (int64_t)D * (sizeof(T) / 2), lane);
   while (pos < end) {
     const TreeRun r = tree_run(sh, p.plan, 0, worker, pos, end, item);
+    if (r.blocks == 0) break;  // (the run's end)
     TreePages pages;
     pages.init(c, sh, r);
     struct Place {
@@ -437,7 +487,21 @@ __global__ __launch_bounds__(64, 2) void tree_solo_kernel(CacheView c, TreeShape
       if (i + 2 < n) issue(i + 2, 1, p.v, next);
     }
     leave_partial<D>(p, st, row, r.prow + ln, wave_any(pages.bad), hf);
-    pos += r.blocks;
+    pos += r.units;
+  }
+}
+
+// Waits until block t of n has landed, PER loads each, with S - 2 later ones in flight at most.
+template <int S, int PER>
+__device__ __forceinline__ void wait_block(int t, int n) {
+  if constexpr (S > 2) {
+    if (t + S - 2 < n) {
+      wait_vmem<(S - 2) * PER>();
+      return;
+    }
+    wait_block<S - 1, PER>(t, n);
+  } else {
+    wait_vmem<0>();
   }
 }
 
@@ -446,9 +510,9 @@ template <int D, typename T>
 __global__ __launch_bounds__(kTeamWaves * 64, (kTreeTeam<D, T>)) void tree_team_kernel(CacheView c, TreeShape sh, TreeParams<T> p) {
   using O = Ops<T>;
   using Frag = typename O::Frag;
-  constexpr int BN = kTeamKeys<T>, KB = BN / 32, RPW = BN / kTeamWaves, NC = D / 16, NI = KB * NC, PD = 3;
+  constexpr int BN = kTeamKeys<D, T>, S = kTeamStages<D, T>, KB = BN / 32, RPW = BN / kTeamWaves, NC = D / 16, NI = KB * NC, PD = 3;
   using Dma = RowDma<T, D, RPW>;
-  __shared__ __attribute__((aligned(1024))) TreeRing<T, BN * D> smem;
+  __shared__ __attribute__((aligned(1024))) TreeRing<T, S, BN * D> smem;
   auto* ring = in_lds(&smem);
   const int worker = blockIdx.x, tid = threadIdx.x, lane = tid & 63, ln = lane & 31, hf = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -461,20 +525,24 @@ __global__ __launch_bounds__(kTeamWaves * 64, (kTreeTeam<D, T>)) void tree_team_
   dma.init(wave * RPW, (int64_t)D * (sizeof(T) / 2), lane);
   for (bool first = true; pos < end; first = false) {
     const TreeRun r = tree_run(sh, p.plan, 1, worker, pos, end, item);
+    if (r.blocks == 0) break;  // (the run's end)
     TreePages pages;
     pages.init(c, sh, r);
-    auto issue = [&](int t) {
+    auto issue = [&](int t, int stage) {
       // this wave's rows of the block lie in one page; past the last key it fetches the block's first ones again
       const int key = r.key + BN * t, mine = key + wave * RPW;
       const int64_t at = pages.row(c, mine < r.it.k1 ? mine : key);
       const int rows = mine < r.it.k1 ? min(RPW, r.it.k1 - mine) : min(RPW, r.it.k1 - key);
       const int64_t base = (at - wave * RPW) * D;  // (the DMA adds the wave's first row)
-      const unsigned tile = (unsigned)(uintptr_t)&ring->kv[t & 1][0][wave * RPW * D];
+      const unsigned tile = (unsigned)(uintptr_t)&ring->kv[stage][0][wave * RPW * D];
       dma_rows_at<false>(dma, tile, p.k + base, wave * RPW + rows);
       dma_rows_at<false>(dma, tile + BN * D * sizeof(T), p.v + base, wave * RPW + rows);
     };
     if (!first) __syncthreads();  // the ring is free
-    issue(0);
+    const int n = r.blocks;
+#pragma unroll
+    for (int t = 0; t < S - 1; ++t)
+      if (t < n) issue(t, t);
     bool path_fine = true;
     uint64_t path = 0;
     if (r.own) path = tree_paths(p.parents ? p.parents + (int64_t)r.it.seq * sh.nodes : nullptr, sh.nodes, lane, path_fine);
@@ -485,15 +553,17 @@ __global__ __launch_bounds__(kTeamWaves * 64, (kTreeTeam<D, T>)) void tree_team_
     st.init();
 #pragma unroll
     for (int cc = 0; cc < NC; ++cc) qf[cc] = row.q >= 0 ? O::load(p.q + row.q + 16 * cc + 8 * hf) : Frag{};
-    const int n = r.blocks;
+    int stage = 0;
     for (int t = 0; t < n; ++t) {
-      wait_vmem<0>();
-      __syncthreads();  // block t has landed for every wave; the stage of block t - 1 is free
-      if (t + 1 < n) issue(t + 1);
+      if (t == 0) wait_vmem<0>();  // (Q's loads as well)
+      else wait_block<S, 2 * Dma::N>(t, n);
+      lds_barrier();  // block t has landed for every wave; the stage of block t - 1 is free
+      if (t + S - 1 < n) issue(t + S - 1, stage == 0 ? S - 1 : stage - 1);
+      const T* sK = (const T*)ring->kv[stage][0];
+      const T* sV = (const T*)ring->kv[stage][1];
+      stage = stage == S - 1 ? 0 : stage + 1;
       if (!some) continue;
       const int k0 = r.key + BN * t;
-      const T* sK = (const T*)ring->kv[t & 1][0];
-      const T* sV = (const T*)ring->kv[t & 1][1];
       f32x16 s[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) s[kb] = f32x16{};
@@ -529,61 +599,69 @@ __global__ __launch_bounds__(kTeamWaves * 64, (kTreeTeam<D, T>)) void tree_team_
     // a page that is none may be another wave's
     const bool bad = __syncthreads_or(pages.bad);
     leave_partial<D>(p, st, row, r.prow + wave * 32 + ln, bad, hf);
-    pos += r.blocks;
+    pos += r.units;
   }
 }
 
-// A row is D / 4 lanes, four partial results' loads in flight: first those of its group's
-// shared keys, then its own's.
+// Where a row's partial results of one item lie.
+struct TreeParts {
+  int64_t row, n, stride;
+};
+__device__ __forceinline__ TreeParts tree_parts(const TreeShape& sh, const TreePlan& plan, int kind_of, int item, const TreeItem& it,
+                                                int who, int g, int row) {
+  const TreeKind& kind = sh.kind[kind_of];
+  const int64_t run = plan.head[2 * kind.team + 1], first = plan.first[kind.team][item];
+  const int per = rows_a_tile(kind), tile = row / per, j = g * tiles_of(it.rows, kind) + tile;
+  const int64_t from = first + (int64_t)j * units_of(it.blocks) + kTreeStart, w0 = div_floor(from, run);
+  TreeParts p;
+  p.n = it.blocks ? div_floor(from + it.blocks - 1, run) - w0 + 1 : 0;
+  p.stride = kind.part_rows;
+  p.row = kind.part0 + ((int64_t)(who * sh.hkv + g) * kind.tiles + tile + w0) * kind.part_rows + row % per;
+  return p;
+}
+
+// A row is D / 4 lanes, four partial results' loads in flight: those of its group's shared
+// keys, then its own's.
 template <int D, typename T>
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeShape sh, TreeParams<T> p) {
   constexpr int LPR = D / 4, RPB = 256 / LPR, NP = 4;
   const int64_t out_row = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR;
   if (out_row >= (int64_t)sh.n * sh.nodes * sh.hq) return;
   const int col = (threadIdx.x % LPR) * 4;
-  const int head = (int)(out_row % sh.hq);
-  const int64_t tok = out_row / sh.hq;
-  const int seq = (int)(tok / sh.nodes), node = (int)(tok - (int64_t)seq * sh.nodes);
-  const int grp = seq / sh.group, member = seq - grp * sh.group;
+  const int tok = (int)(out_row / sh.hq), head = (int)(out_row - (int64_t)tok * sh.hq);
+  const int seq = tok / sh.nodes, node = tok - seq * sh.nodes, grp = seq / sh.group;
   const int g = head / sh.G, h = head - g * sh.G;
-  const int own = seq + grp + 1;
+  const int lead = grp * (sh.group + 1), own = seq + grp + 1;
+  const TreeItem mine = p.plan.items[own], all = p.plan.items[lead];
   f32x4 acc = f32x4{};
   float m = kNegInf, l = 0.f;
-  if (node < p.plan.live[seq]) {
-    auto join = [&](int item, const TreeKind& kind, int64_t tile0, int row) {
-      const int blocks = p.plan.items[item].blocks;
-      if (blocks == 0) return;
-      const int per = kind.team ? kTeamRows : kSoloRows;
-      const int j = g * kind.tiles + row / per;
-      const int64_t run = p.plan.head[2 * kind.team + 1], from = p.plan.first[kind.team][item] + (int64_t)j * blocks;
-      const int64_t w0 = from / run, parts = (from + blocks - 1) / run - w0 + 1;
-      int64_t prow = kind.part0 + (tile0 + j + w0) * kind.part_rows + row % per;
-      for (int64_t n0 = 0; n0 < parts; n0 += NP, prow += (int64_t)NP * kind.part_rows) {
-        f32x4 x[NP];
-        float pm[NP], pl[NP];
+  if (node * sh.G < mine.rows) {
+    TreeParts a{0, 0, 0};
+    if (all.blocks) a = tree_parts(sh, p.plan, 0, lead, all, grp, g, (mine.row0 + node) * sh.G + h);
+    const TreeParts b = tree_parts(sh, p.plan, 1, own, mine, seq, g, node * sh.G + h);
+    const int64_t parts = a.n + b.n;
+    for (int64_t n0 = 0; n0 < parts; n0 += NP) {
+      f32x4 x[NP];
+      float pm[NP], pl[NP];
 #pragma unroll
-        for (int n = 0; n < NP; ++n) {
-          const bool on = n0 + n < parts;
-          const int64_t r = prow + (on ? n : 0) * (int64_t)kind.part_rows;
-          x[n] = *reinterpret_cast<const f32x4*>(p.part + r * D + col);
-          pm[n] = p.part_ml[2 * r];
-          pl[n] = on ? p.part_ml[2 * r + 1] : 0.f;
-        }
-#pragma unroll
-        for (int n = 0; n < NP; ++n) {
-          if (pl[n] == 0.f) continue;  // a part without a visible key
-          const float mn = fmaxf(m, pm[n]);
-          const float a = m == kNegInf ? 0.f : fast_exp2(m - mn), b = fast_exp2(pm[n] - mn);
-          l = l * a + pl[n] * b;
-          acc = acc * a + x[n] * b;
-          m = mn;
-        }
+      for (int n = 0; n < NP; ++n) {
+        const int64_t k = n0 + n < parts ? n0 + n : 0;
+        const int64_t r = k < a.n ? a.row + k * a.stride : b.row + (k - a.n) * b.stride;
+        x[n] = *reinterpret_cast<const f32x4*>(p.part + r * D + col);
+        pm[n] = p.part_ml[2 * r];
+        pl[n] = n0 + n < parts ? p.part_ml[2 * r + 1] : 0.f;
       }
-    };
-    const TreeKind &ks = sh.kind[0], &ko = sh.kind[1];
-    if (ks.tiles) join(own - member - 1, ks, (int64_t)grp * ks.tiles * sh.hkv, (member * sh.nodes + node) * sh.G + h);
-    join(own, ko, (int64_t)seq * ko.tiles * sh.hkv, node * sh.G + h);
-  } else if (node < p.plan.items[own].bad) {
+#pragma unroll
+      for (int n = 0; n < NP; ++n) {
+        if (pl[n] == 0.f) continue;  // a part without a visible key
+        const float mn = fmaxf(m, pm[n]);
+        const float c = m == kNegInf ? 0.f : fast_exp2(m - mn), d = fast_exp2(pm[n] - mn);
+        l = l * c + pl[n] * d;
+        acc = acc * c + x[n] * d;
+        m = mn;
+      }
+    }
+  } else if (node < mine.bad) {
     l = __builtin_nanf("");
   }
   const bool some = l != 0.f;  // NaN: so is the row
