@@ -116,6 +116,7 @@ constexpr int kSoloKeys = 32, kSoloRows = 32, kTeamWaves = 4, kTeamRows = 128;
 // An item: rows against a range of keys; its units: a block of keys, for a tile of rows of one
 // kv-head.
 struct TreeItem {
+  int64_t first;   // units ahead of it, of those that solo waves / teams take
   int32_t blocks;  // of keys, for every tile of rows and head
   int32_t slot;    // whose pages
   int32_t k0, k1;  // keys [k0, k1)
@@ -124,7 +125,7 @@ struct TreeItem {
   int32_t bad;     // nodes asked for of a sequence that is not sound
   int32_t rows;    // for one kv-head: nodes in use x G
   int32_t row0;    // a sequence's first node among its group's
-  int32_t pad[3];
+  int32_t pad[5];
 };
 // The two kinds of items: a group's shared keys, a sequence's own.
 struct TreeKind {
@@ -144,7 +145,6 @@ struct TreeShape {
 struct TreePlan {
   TreeItem* items;         // [n + groups]
   int32_t* nodes;          // [n * max_new]: a group's nodes in use, the rows of its shared keys
-  int64_t* first[2];       // [n + groups]: units ahead of an item, of those that solo waves / teams take
   int64_t* head;           // [2][2]: units in all, units a worker
   int32_t* start_item[2];  // [workers]: where a worker starts
 };

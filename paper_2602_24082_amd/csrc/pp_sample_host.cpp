@@ -185,10 +185,7 @@ size_t carve_tree(const TreeShape& t, int d, void* ws, TreeLaunch* a) {
   a->plan.items = at.take<TreeItem>(items);
   a->plan.nodes = at.take<int32_t>((int64_t)t.n * t.nodes);
   a->plan.head = at.take<int64_t>(4);
-  for (int c = 0; c < 2; ++c) {
-    a->plan.first[c] = at.take<int64_t>(items);
-    a->plan.start_item[c] = at.take<int32_t>(t.workers[c]);
-  }
+  for (int c = 0; c < 2; ++c) a->plan.start_item[c] = at.take<int32_t>(t.workers[c]);
   const TreeKind& last = t.kind[1];
   const int64_t parts = last.part0 + ((int64_t)t.n * last.tiles * t.hkv + t.workers[last.team]) * last.part_rows;
   a->part_ml = at.take<float>(2 * parts);

@@ -32,23 +32,32 @@ namespace {
 
 constexpr int kPlan = 1024;
 
+// Exclusive sum of x over the workgroup's threads, and the whole; lanes by DPP (to the left by 1,
+// 2, 4, 8 within rows of 16, then the rows' last lanes).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t add_moved64(int64_t x) {
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(x >> 32), CTRL, ROWS, 0xf, false);
+  return x + (int64_t)((uint64_t)hi << 32 | lo);
+}
 __device__ __forceinline__ int64_t plan_scan64(int64_t x, int64_t* total) {
   __shared__ int64_t part[kPlan / 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t s = x;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int64_t y = __shfl_up(s, off, 64);
-    if (lane >= off) s += y;
-  }
+  int64_t s = add_moved64<0x111, 0xf>(x);
+  s = add_moved64<0x112, 0xf>(s);
+  s = add_moved64<0x114, 0xf>(s);
+  s = add_moved64<0x118, 0xf>(s);
+  s = add_moved64<0x142, 0xa>(s);
+  s = add_moved64<0x143, 0xc>(s);
   __syncthreads();
   if (lane == 63) part[wave] = s;
   __syncthreads();
   int64_t before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kPlan / 64; ++w) {
-    before += w < wave ? part[w] : 0;
-    all += part[w];
+    const int64_t y = part[w];
+    before += w < wave ? y : 0;
+    all += y;
   }
   *total = all;
   return before + s - x;
@@ -69,14 +78,21 @@ __device__ __forceinline__ int tiles_of(int rows, const TreeKind& k) { return (r
 // Items in the order of the groups: a group's shared keys, then its sequences' own.
 __global__ __launch_bounds__(kPlan) void tree_plan_kernel(CacheView c, TreeShape t, const int32_t* slots, const int32_t* count,
                                                           const int32_t* shared, TreePlan out) {
-  __shared__ int s_shared[kTreeSeqs], s_lead[kTreeSeqs], s_nodes[kTreeSeqs + 1];
+  __shared__ int s_shared[kTreeSeqs], s_lead[kTreeSeqs], s_nodes[kTreeSeqs + 1], s_slot[kTreeSeqs];
   __shared__ int64_t s_units[2 * kTreeSeqs];
   __shared__ int64_t s_first[2 * kTreeSeqs];
   constexpr int PER = kTreeSeqs / kPlan;  // sequences a thread, next to each other
   const int tid = threadIdx.x, items = t.n + t.groups;
   const bool share = t.kind[0].tiles > 0;
   int slot_of[PER], len_of[PER], live_of[PER], bad_of[PER], lead = 0;
-  for (int g = tid; share && g < t.groups; g += kPlan) s_shared[g] = s_lead[g] = 0x7fffffff;
+  int pages_of[PER];  // that groups tid, tid + kPlan .. share
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    const int g = tid + u * kPlan;
+    if (!share || g >= t.groups) continue;
+    s_shared[g] = s_lead[g] = 0x7fffffff;
+    pages_of[u] = shared[g];
+  }
 #pragma unroll
   for (int u = 0; u < PER; ++u) {
     const int i = tid * PER + u;
@@ -106,21 +122,25 @@ __global__ __launch_bounds__(kPlan) void tree_plan_kernel(CacheView c, TreeShape
       if (i <= t.n) s_nodes[i] = at;
       at += live_of[u];
       if (!live_of[u]) continue;
+      s_slot[i] = slot_of[u];
       atomicMin(&s_shared[i / t.group], len_of[u]);
       atomicMin(&s_lead[i / t.group], i);
     }
     if (tid == 0) s_nodes[t.n] = (int)total;
     __syncthreads();
-    for (int g = tid; g < t.groups; g += kPlan) {
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+      const int g = tid + u * kPlan;
+      if (g >= t.groups) continue;
       TreeItem it{};
       const int nodes = s_nodes[min(t.n, (g + 1) * t.group)] - s_nodes[g * t.group];
       const int first = s_lead[g];
       // with one sequence in use there is nobody to share with
       if (nodes > 0 && first < t.n && s_nodes[first + 1] - s_nodes[first] < nodes) {
-        const int pages = max(0, min(shared[g], s_shared[g] >> c.page_log2));
+        const int pages = max(0, min(pages_of[u], s_shared[g] >> c.page_log2));
         it.k1 = it.seen = pages << c.page_log2;
         it.blocks = (it.k1 + t.kind[0].keys - 1) / t.kind[0].keys;
-        it.slot = slots[first];
+        it.slot = s_slot[first];
         it.rows = nodes * t.G;
       }
       it.seq = g * t.group;
@@ -179,7 +199,10 @@ __global__ __launch_bounds__(kPlan) void tree_plan_kernel(CacheView c, TreeShape
 #pragma unroll
     for (int u = 0; u < PER_ITEM; ++u) {
       const int k = tid * PER_ITEM + u;
-      if (k < items) s_first[k] = out.first[cls][k] = before;
+      if (k < items) {
+        s_first[k] = before;
+        if (takes[k % (t.group + 1) != 0]) out.items[k].first = before;
+      }
       before += w[u];
     }
     __syncthreads();
@@ -261,7 +284,7 @@ __device__ __forceinline__ TreeRun tree_run(const TreeShape& sh, const TreePlan&
     const TreeKind& kind = sh.kind[r.own];
     if (kind.tiles == 0 || kind.team != cls) continue;
     r.it = load_uniform(plan.items + item);
-    const int64_t rel = pos - plan.first[cls][item];
+    const int64_t rel = pos - r.it.first;
     const int units = units_of(r.it.blocks), tiles = tiles_of(r.it.rows, kind);
     if (rel >= (int64_t)units * tiles * sh.hkv) continue;  // none, or this one's end
     const int j = (int)div_floor(rel, units), u0 = (int)(rel - (int64_t)j * units);
@@ -607,12 +630,11 @@ __global__ __launch_bounds__(kTeamWaves * 64, (kTreeTeam<D, T>)) void tree_team_
 struct TreeParts {
   int64_t row, n, stride;
 };
-__device__ __forceinline__ TreeParts tree_parts(const TreeShape& sh, const TreePlan& plan, int kind_of, int item, const TreeItem& it,
-                                                int who, int g, int row) {
+__device__ __forceinline__ TreeParts tree_parts(const TreeShape& sh, int64_t run, int kind_of, const TreeItem& it, int who, int g,
+                                                int row) {
   const TreeKind& kind = sh.kind[kind_of];
-  const int64_t run = plan.head[2 * kind.team + 1], first = plan.first[kind.team][item];
   const int per = rows_a_tile(kind), tile = row / per, j = g * tiles_of(it.rows, kind) + tile;
-  const int64_t from = first + (int64_t)j * units_of(it.blocks) + kTreeStart, w0 = div_floor(from, run);
+  const int64_t from = it.first + (int64_t)j * units_of(it.blocks) + kTreeStart, w0 = div_floor(from, run);
   TreeParts p;
   p.n = it.blocks ? div_floor(from + it.blocks - 1, run) - w0 + 1 : 0;
   p.stride = kind.part_rows;
@@ -633,12 +655,13 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeShape sh, TreePar
   const int g = head / sh.G, h = head - g * sh.G;
   const int lead = grp * (sh.group + 1), own = seq + grp + 1;
   const TreeItem mine = p.plan.items[own], all = p.plan.items[lead];
+  const int64_t run_all = p.plan.head[2 * sh.kind[0].team + 1], run_own = p.plan.head[2 * sh.kind[1].team + 1];
   f32x4 acc = f32x4{};
   float m = kNegInf, l = 0.f;
   if (node * sh.G < mine.rows) {
     TreeParts a{0, 0, 0};
-    if (all.blocks) a = tree_parts(sh, p.plan, 0, lead, all, grp, g, (mine.row0 + node) * sh.G + h);
-    const TreeParts b = tree_parts(sh, p.plan, 1, own, mine, seq, g, node * sh.G + h);
+    if (all.blocks) a = tree_parts(sh, run_all, 0, all, grp, g, (mine.row0 + node) * sh.G + h);
+    const TreeParts b = tree_parts(sh, run_own, 1, mine, seq, g, node * sh.G + h);
     const int64_t parts = a.n + b.n;
     for (int64_t n0 = 0; n0 < parts; n0 += NP) {
       f32x4 x[NP];
