@@ -30,24 +30,30 @@ namespace {
 constexpr int kPlan = 1024;  // threads of the kernels that plan, one workgroup each
 constexpr int kFreeRun = 8;  // pages a thread looks at in a row
 
-// Exclusive sum of x over the workgroup's threads, and the whole.
+// Exclusive sum of x over the workgroup's threads, and the whole; lanes by DPP (to the left by 1,
+// 2, 4, 8 within rows of 16, then the rows' last lanes).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int add_moved(int x) {
+  return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
 __device__ __forceinline__ int plan_scan(int x, int* total) {
   __shared__ int part[kPlan / 64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int s = x;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int y = __shfl_up(s, off, 64);
-    if (lane >= off) s += y;
-  }
+  int s = add_moved<0x111, 0xf>(x);
+  s = add_moved<0x112, 0xf>(s);
+  s = add_moved<0x114, 0xf>(s);
+  s = add_moved<0x118, 0xf>(s);
+  s = add_moved<0x142, 0xa>(s);
+  s = add_moved<0x143, 0xc>(s);
   __syncthreads();  // the previous call's reads of `part`
   if (lane == 63) part[wave] = s;
   __syncthreads();
   int before = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kPlan / 64; ++w) {
-    before += w < wave ? part[w] : 0;
-    all += part[w];
+    const int y = part[w];
+    before += w < wave ? y : 0;
+    all += y;
   }
   *total = all;
   return before + s - x;
@@ -87,19 +93,35 @@ __device__ __forceinline__ int list_pages(const CacheView& c, int most, int32_t*
   return found;
 }
 
-// mark[s] = the first of the call's entries that names slot s (a slot named again is left out).
-__device__ __forceinline__ void mark_slots(const CacheView& c, int n, const int32_t* slots, int32_t* mark) {
-  for (int e = threadIdx.x; e < n; e += kPlan)
-    if (c.has_slot(slots[e])) __hip_atomic_store(mark + slots[e], 0x7fffffff, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  __threadfence();
-  __syncthreads();
-  for (int e = threadIdx.x; e < n; e += kPlan)
-    if (c.has_slot(slots[e])) atomicMin(mark + slots[e], e);
-  __threadfence();
-  __syncthreads();
-}
-__device__ __forceinline__ bool marked(const int32_t* mark, int slot, int e) {
-  return __hip_atomic_load(mark + slot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == e;
+// Which of the call's entries names a slot first (a slot named again is left out), in LDS for
+// caches of up to kLdsSlots slots, else in the workspace.
+constexpr int kLdsSlots = 8192;
+struct Marks {
+  int* lds;
+  int32_t* ws;  // null: in LDS
+  __device__ __forceinline__ void mark(const CacheView& c, int n, const int32_t* slots) const {
+    for (int e = threadIdx.x; e < n; e += kPlan) {
+      const int s = slots[e];
+      if (!c.has_slot(s)) continue;
+      if (ws) __hip_atomic_store(ws + s, 0x7fffffff, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      else lds[s] = 0x7fffffff;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < n; e += kPlan) {
+      const int s = slots[e];
+      if (!c.has_slot(s)) continue;
+      if (ws) atomicMin(ws + s, e);
+      else atomicMin(lds + s, e);
+    }
+    __syncthreads();
+  }
+  __device__ __forceinline__ bool first(int slot, int e) const {
+    return (ws ? __hip_atomic_load(ws + slot, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : lds[slot]) == e;
+  }
+};
+__device__ __forceinline__ Marks marks_of(const CacheView& c, int32_t* ws) {
+  __shared__ int s_mark[kLdsSlots];
+  return Marks{s_mark, c.num_slots > kLdsSlots ? ws : nullptr};
 }
 
 // Adds a thread's refused entries up; valid in every thread.
@@ -115,8 +137,8 @@ struct Want {
   bool refused;
 };
 
-// Gives every entry the pages that `want` says: need_of(e) may be called twice.  `put(e, i,
-// page)` stores an entry's i-th new page.  All or nothing: false if pages are missing.
+// Gives every entry the need_of(e) pages that it asks for.  `put(e, i, page)` stores an entry's
+// i-th new page.  All or nothing: false if pages are missing.
 template <typename NeedOf, typename Put>
 __device__ __forceinline__ bool hand_out(const CacheView& c, int n, int32_t* first, int32_t* list, int32_t* status, int refused,
                                          NeedOf&& need_of, Put&& put) {
@@ -152,25 +174,35 @@ __device__ __forceinline__ bool hand_out(const CacheView& c, int n, int32_t* fir
 
 __global__ __launch_bounds__(kPlan) void cache_reserve_kernel(CacheView c, int n, const int32_t* slots, const int32_t* add,
                                                               int32_t* status, int32_t* mark, int32_t* first, int32_t* list) {
-  mark_slots(c, n, slots, mark);
+  const Marks marks = marks_of(c, mark);
+  // what a thread's first entry says is looked up once: most calls have no more of them
   auto want = [&](int e) {
     const int s = slots[e];
     if (s < 0) return Want{0, false};
-    if (!c.has_slot(s) || !marked(mark, s, e)) return Want{0, true};
+    if (!c.has_slot(s)) return Want{0, true};
     const int64_t len = c.seq_len[s], held = c.held[s], more = add[e];
     const int64_t pages = (len + more + c.page_size - 1) >> c.page_log2;
     if (more < 0 || !c.sound(len, held) || pages > c.max_pages) return Want{0, true};
     return Want{pages > held ? (int)(pages - held) : 0, false};
   };
+  const int mine = threadIdx.x;
+  Want my = mine < n ? want(mine) : Want{0, false};
+  marks.mark(c, n, slots);
+  auto settled = [&](int e) {
+    Want w = e == mine ? my : want(e);
+    if (c.has_slot(slots[e]) && !marks.first(slots[e], e)) w = Want{0, true};
+    return w;
+  };
+  if (mine < n) my = settled(mine);
   int bad = 0;
-  for (int e = threadIdx.x; e < n; e += kPlan) bad += want(e).refused;
+  for (int e = mine; e < n; e += kPlan) bad += e == mine ? my.refused : settled(e).refused;
   bad = plan_sum(bad);
-  const bool ok = hand_out(c, n, first, list, status, bad, [&](int e) { return want(e).need; },
+  const bool ok = hand_out(c, n, first, list, status, bad, [&](int e) { return e == mine ? my.need : settled(e).need; },
                            [&](int e, int i, int32_t page) { c.row(slots[e])[c.held[slots[e]] + i] = page; });
   __syncthreads();  // every read of held is done
   if (!ok) return;
-  for (int e = threadIdx.x; e < n; e += kPlan) {
-    const int need = want(e).need;
+  for (int e = mine; e < n; e += kPlan) {
+    const int need = e == mine ? my.need : settled(e).need;
     if (need) c.held[slots[e]] += need;
   }
 }
@@ -178,14 +210,15 @@ __global__ __launch_bounds__(kPlan) void cache_reserve_kernel(CacheView c, int n
 __global__ __launch_bounds__(kPlan) void cache_fork_plan_kernel(CacheView c, int n, const int32_t* src, const int32_t* dst,
                                                                 int32_t* status, int32_t* mark, int32_t* first, int32_t* list,
                                                                 ForkEntry* out) {
-  mark_slots(c, n, dst, mark);
+  const Marks marks = marks_of(c, mark);
+  marks.mark(c, n, dst);
   int bad = 0;
   for (int e = threadIdx.x; e < n; e += kPlan) {
     const int a = src[e], b = dst[e];
     ForkEntry f{};
     f.src = f.dst = f.old_page = f.new_page = -1;
     if (a >= 0 || b >= 0) {
-      bool fine = c.has_slot(a) && c.has_slot(b) && a != b && marked(mark, b, e) && c.held[b] == 0 && c.seq_len[b] == 0;
+      bool fine = c.has_slot(a) && c.has_slot(b) && a != b && marks.first(b, e) && c.held[b] == 0 && c.seq_len[b] == 0;
       if (fine) {
         const int64_t len = c.seq_len[a];
         fine = c.sound(len, c.held[a]);
@@ -215,7 +248,7 @@ __global__ __launch_bounds__(kPlan) void cache_fork_plan_kernel(CacheView c, int
     if (out[e].dst < 0) continue;
     if (ok) {
       c.held[out[e].dst] = out[e].whole + (out[e].rest != 0);
-      c.seq_len[out[e].dst] = c.seq_len[out[e].src];
+      c.seq_len[out[e].dst] = (out[e].whole << c.page_log2) + out[e].rest;  // (src may be another entry's dst)
     } else {
       out[e].dst = -1;
     }
@@ -324,32 +357,37 @@ __global__ __launch_bounds__(256) void cache_compact_kernel(CacheView c, CachePo
 __global__ __launch_bounds__(kPlan) void cache_accept_plan_kernel(CacheView c, int n, const int32_t* slots, int max_new,
                                                                   const int32_t* count, const int32_t* path, int32_t* status,
                                                                   int32_t* mark, AcceptEntry* out) {
-  mark_slots(c, n, slots, mark);
+  const Marks marks = marks_of(c, mark);
+  marks.mark(c, n, slots);
   int bad = 0;
-  for (int e = threadIdx.x; e < n; e += kPlan) {
+  // with a path an entry is a wave, a lane a node (64 at most)
+  const int lane = threadIdx.x & 63, lanes = path ? 64 : 1;
+  for (int e = threadIdx.x / lanes; e < n; e += kPlan / lanes) {
     const int s = slots[e], m = count[e];
     AcceptEntry a{-1, 0, 0, 0};
-    if (s >= 0 && m != 0) {
-      bool fine = c.has_slot(s) && marked(mark, s, e) && m > 0 && m <= max_new;
+    bool fine = true;
+    const bool any = s >= 0 && m != 0;
+    if (any) {
+      fine = c.has_slot(s) && marks.first(s, e) && m > 0 && m <= max_new;
       if (fine) {
         const int64_t len = c.seq_len[s], held = c.held[s];
-        int last = path ? -1 : m - 1;
-        if (path)
-          for (int j = 0; j < m; ++j) {
-            const int at = path[(int64_t)e * max_new + j];
-            fine = fine && at > last && at < max_new;
-            a.moved |= at != j;
-            last = at;
-          }
+        int last = m - 1;
+        if (path) {
+          const int at = lane < m ? path[(int64_t)e * max_new + lane] : 0;
+          const int ahead = __shfl_up(at, 1, 64);
+          fine = !__any(lane < m && (at <= (lane ? ahead : -1) || at >= max_new));
+          a.moved = __any(lane < m && at != lane);
+          last = __shfl(at, m - 1, 64);
+        }
         fine = fine && c.sound(len, held) && len + last < held << c.page_log2;
-        a.slot = s;
         a.len = (int)len;
         a.count = m;
       }
-      if (!fine) a.slot = -1;
-      bad += !fine;
+      if (fine) a.slot = s;
     }
-    if (out) out[e] = a;
+    if (threadIdx.x % lanes) continue;
+    bad += !fine;
+    out[e] = a;
     if (a.slot >= 0) c.seq_len[s] = a.len + m;
   }
   bad = plan_sum(bad);

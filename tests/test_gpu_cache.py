@@ -93,6 +93,35 @@ def test_fork_runs_out():
     same(c, k, v, b)
 
 
+def test_fork_of_what_the_same_call_fills():
+    """The state ahead of the call counts: a source that another entry fills is empty."""
+    for order in (1, -1):
+        c = pp.make_cache(400, 4, 900, 16, DEV)
+        k, v = pools(1, 900, 1, 16, 64, torch.bfloat16, 2)
+        pp.pp_cache_reserve(c, ints([0]), ints([40]))
+        pp.pp_cache_accept(c, ints([0]), ints([40]))
+        b = book_of(c, k, v)
+        src, dst = [0] + list(range(1, 300)), list(range(1, 301))
+        args = src[::order], dst[::order]
+        assert pp.pp_cache_fork(c, ints(args[0]), ints(args[1]), k, v).cpu().tolist() == b.fork(*args) == [0, 0]
+        same(c, k, v, b)
+
+
+def test_many_slots():
+    """More slots than a workgroup marks in LDS."""
+    n = 9000
+    c = pp.make_cache(n, 2, 400, 16, DEV)
+    k, v = pools(1, 400, 1, 16, 64, torch.bfloat16, 4)
+    b = book_of(c, k, v)
+    slots = [n - 1 - i for i in range(0, 1200, 7)] + [n - 1, 5, n]
+    add = [1 + i % 20 for i in range(len(slots))]
+    assert pp.pp_cache_reserve(c, ints(slots), ints(add), ws=junk_ws(c, len(slots))).cpu().tolist() == b.reserve(slots, add) == [0, 2]
+    assert pp.pp_cache_accept(c, ints(slots), ints(add)).cpu().tolist() == b.accept(slots, add) == [0, 2]
+    src = slots[:20]
+    assert pp.pp_cache_fork(c, ints(src), ints([i % 18 for i in range(20)]), k, v).cpu().tolist() == b.fork(src, [i % 18 for i in range(20)])
+    same(c, k, v, b)
+
+
 def test_large_pool():
     """More pages than one round of the search looks at, free ones far apart; many entries."""
     pages, n = 30011, 1500
