@@ -907,7 +907,7 @@ class Cache:
         _check_tensor("refs", refs, refs.shape, torch.int32, dev)
         _on_gpu(page_table)
         self.page_table, self.seq_len, self.held, self.refs = page_table, seq_len, held, refs
-        self.num_pages, self.page_size, self.device = refs.shape[0], int(page_size), dev
+        self.num_pages, self.page_size, self.device, self.index = refs.shape[0], int(page_size), dev, dev.index
         self._desc = _CacheDesc(slots, page_table.shape[1], refs.shape[0], self.page_size, page_table.data_ptr(),
                                 seq_len.data_ptr(), held.data_ptr(), refs.data_ptr())
         self.ref = ctypes.byref(self._desc)
@@ -932,36 +932,50 @@ def make_cache(num_slots: int, max_pages: int, num_pages: int, page_size: int, d
     return Cache(z(num_slots, max_pages), z(num_slots), z(num_slots), z(num_pages), page_size)
 
 
-def _ints_of(name: str, t: torch.Tensor, n: int, dev: torch.device):
-    return _check_tensor(name, t, (n,), torch.int32, dev)
+_Tensor, _int32 = torch.Tensor, torch.int32
 
 
-def _slots_of(name: str, t: torch.Tensor, dev: torch.device) -> int:
+def _fits(name: str, t: torch.Tensor, shape, dtype, dev: torch.device, index: int):
+    """_check_tensor, in the order in which a good tensor is told soonest (a decode step makes many small calls)."""
+    if type(t) is _Tensor and t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
+        return t
+    return _check_tensor(name, t, shape, dtype, dev)
+
+
+def _slots_of(name: str, t: torch.Tensor, cache: Cache) -> int:
     if not isinstance(t, torch.Tensor) or t.dim() != 1:
         raise ValueError(f"{name} must be a tensor [n]")
-    _check_tensor(name, t, t.shape, torch.int32, dev)
+    _fits(name, t, t.shape, _int32, cache.device, cache.index)
     return t.shape[0]
 
 
 def _pools(cache: Cache, k_pages: torch.Tensor, v_pages: torch.Tensor, layered: bool):
     """(dtype code, layers, hkv, head_dim) of the pools of keys and values, checked."""
-    want = 5 if layered else 4
-    if k_pages.dim() != want:
+    shape = k_pages.shape
+    if len(shape) != (5 if layered else 4):
         raise ValueError("k_pages must be [%spages, hkv, page_size, head_dim]" % ("layers, " if layered else ""))
-    hkv, d = k_pages.shape[-3], k_pages.shape[-1]
-    layers = k_pages.shape[0] if layered else 1
-    shape = ((layers,) if layered else ()) + (cache.num_pages, hkv, cache.page_size, d)
-    _check_tensor("k_pages", k_pages, shape, k_pages.dtype, cache.device)
-    _check_tensor("v_pages", v_pages, shape, k_pages.dtype, cache.device)
-    return _dtype_code(k_pages), layers, hkv, d
+    pages, hkv, size, d = shape[-4:]
+    dtype = k_pages.dtype
+    if pages != cache.num_pages or size != cache.page_size:
+        raise ValueError(f"k_pages has {pages} pages of {size} tokens, the cache {cache.num_pages} of {cache.page_size}")
+    _fits("k_pages", k_pages, shape, dtype, cache.device, cache.index)
+    _fits("v_pages", v_pages, shape, dtype, cache.device, cache.index)
+    return _dtype_code(k_pages), shape[0] if layered else 1, hkv, d
 
 
-def _cache_ws(cache: Cache, n: int, ws):
-    return _maybe_workspace(cache._ws_size("pp_cache_workspace_size", n), cache.device) if ws is None else ws
+def _scratch(nbytes: int, dev: torch.device, ws):
+    """(workspace, its address, its bytes): the caller's, checked, or a new one."""
+    if ws is None:
+        if not nbytes:
+            return None, None, 0
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
+        return ws, ws.data_ptr(), nbytes
+    return ws, ws.data_ptr(), _ws_bytes(ws, dev)
 
 
-def _new_ints(n, dev, out=None, name="status"):
-    return torch.empty(n, dtype=torch.int32, device=dev) if out is None else _ints_of(name, out, n, dev)
+def _new_ints(n, cache: Cache, out=None, name="status"):
+    return (torch.empty(n, dtype=_int32, device=cache.device) if out is None
+            else _fits(name, out, (n,), _int32, cache.device, cache.index))
 
 
 def pp_cache_workspace_size(cache: Cache, n: int) -> int:
@@ -971,11 +985,12 @@ def pp_cache_workspace_size(cache: Cache, n: int) -> int:
 def pp_cache_reserve(cache: Cache, slots: torch.Tensor, add: torch.Tensor, status=None, ws=None) -> torch.Tensor:
     """Room for add[i] more tokens in slots[i]; returns status [2]: pages missing (then nothing changed), entries refused."""
     dev = cache.device
-    n = _slots_of("slots", slots, dev)
-    _ints_of("add", add, n, dev)
-    status, ws = _new_ints(2, dev, status), _cache_ws(cache, n, ws)
+    n = _slots_of("slots", slots, cache)
+    _fits("add", add, (n,), _int32, dev, cache.index)
+    status = _new_ints(2, cache, status)
+    ws, at, nbytes = _scratch(cache._ws_size("pp_cache_workspace_size", n) if ws is None else 0, dev, ws)
     with _device_of(dev):
-        _check(lib().pp_cache_reserve(cache.ref, n, _addr(slots), _addr(add), _addr(status), _addr(ws), _ws_bytes(ws, dev),
+        _check(lib().pp_cache_reserve(cache.ref, n, slots.data_ptr(), add.data_ptr(), status.data_ptr(), at, nbytes,
                                       _raw_stream(dev)))
     return status
 
@@ -985,44 +1000,46 @@ def pp_cache_fork(cache: Cache, src: torch.Tensor, dst: torch.Tensor, k_pages: t
     """Makes the empty slots dst[i] copies of src[i]: whole pages shared, a partial last page copied in every layer of the
     pools [layers, pages, hkv, page_size, head_dim]; returns status [2] as pp_cache_reserve."""
     dev = cache.device
-    n = _slots_of("src", src, dev)
-    _ints_of("dst", dst, n, dev)
+    n = _slots_of("src", src, cache)
+    _fits("dst", dst, (n,), _int32, dev, cache.index)
     dt, layers, hkv, d = _pools(cache, k_pages, v_pages, True)
-    status, ws = _new_ints(2, dev, status), _cache_ws(cache, n, ws)
+    status = _new_ints(2, cache, status)
+    ws, at, nbytes = _scratch(cache._ws_size("pp_cache_workspace_size", n) if ws is None else 0, dev, ws)
     with _device_of(dev):
-        _check(lib().pp_cache_fork(cache.ref, n, _addr(src), _addr(dst), dt, layers, hkv, d, _addr(k_pages), _addr(v_pages),
-                                   _addr(status), _addr(ws), _ws_bytes(ws, dev), _raw_stream(dev)))
+        _check(lib().pp_cache_fork(cache.ref, n, src.data_ptr(), dst.data_ptr(), dt, layers, hkv, d, k_pages.data_ptr(),
+                                   v_pages.data_ptr(), status.data_ptr(), at, nbytes, _raw_stream(dev)))
     return status
 
 
 def pp_cache_free(cache: Cache, slots: torch.Tensor):
     """Empties slots."""
     dev = cache.device
-    n = _slots_of("slots", slots, dev)
+    n = _slots_of("slots", slots, cache)
     with _device_of(dev):
-        _check(lib().pp_cache_free(cache.ref, n, _addr(slots), _raw_stream(dev)))
+        _check(lib().pp_cache_free(cache.ref, n, slots.data_ptr(), _raw_stream(dev)))
 
 
 def pp_cache_compact(cache: Cache, k_pages: torch.Tensor, v_pages: torch.Tensor, live=None, ws=None) -> torch.Tensor:
     """Moves the live pages to the pool's front; returns their number [1]."""
     dev = cache.device
     dt, layers, hkv, d = _pools(cache, k_pages, v_pages, True)
-    live, ws = _new_ints(1, dev, live, "live"), _cache_ws(cache, 0, ws)
+    live = _new_ints(1, cache, live, "live")
+    ws, at, nbytes = _scratch(cache._ws_size("pp_cache_workspace_size", 0) if ws is None else 0, dev, ws)
     with _device_of(dev):
-        _check(lib().pp_cache_compact(cache.ref, dt, layers, hkv, d, _addr(k_pages), _addr(v_pages), _addr(live), _addr(ws),
-                                      _ws_bytes(ws, dev), _raw_stream(dev)))
+        _check(lib().pp_cache_compact(cache.ref, dt, layers, hkv, d, k_pages.data_ptr(), v_pages.data_ptr(), live.data_ptr(), at,
+                                      nbytes, _raw_stream(dev)))
     return live
 
 
 def pp_cache_shared(cache: Cache, slots: torch.Tensor, group: int, shared=None) -> torch.Tensor:
     """Leading whole pages that the sequences of each group have in common: [n / group]."""
     dev = cache.device
-    n = _slots_of("slots", slots, dev)
+    n = _slots_of("slots", slots, cache)
     if group < 1 or n % group:
         raise ValueError(f"{n} slots do not make groups of {group}")
-    shared = _new_ints(n // group, dev, shared, "shared")
+    shared = _new_ints(n // group, cache, shared, "shared")
     with _device_of(dev):
-        _check(lib().pp_cache_shared(cache.ref, n, _addr(slots), group, _addr(shared), _raw_stream(dev)))
+        _check(lib().pp_cache_shared(cache.ref, n, slots.data_ptr(), group, shared.data_ptr(), _raw_stream(dev)))
     return shared
 
 
@@ -1033,39 +1050,40 @@ def pp_cache_append(cache: Cache, slots: torch.Tensor, k: torch.Tensor, v: torch
     """Writes keys and values of new tokens into one layer's pages behind the cached ones, keys (and q) rotated if rope_base
     is not 0.  k, v [n, max_new, hkv, d], or [rows, hkv, d] with max_new (and start [n], the sequences' first rows); q
     alike.  Returns the rotated q (None without q)."""
-    dev = cache.device
-    n = _slots_of("slots", slots, dev)
+    dev, idx = cache.device, cache.index
+    n = _slots_of("slots", slots, cache)
     dt, _, hkv, d = _pools(cache, k_pages, v_pages, False)
-    if k.dim() not in (3, 4) or (k.dim() == 3 and max_new is None):
+    shape, dtype = k.shape, k_pages.dtype
+    if len(shape) == 4:
+        rows = n * shape[1]
+        if shape[0] != n or (max_new is not None and max_new != shape[1]):
+            raise ValueError(f"k is {tuple(shape)}, with {n} slots and max_new {max_new}")
+        max_new = shape[1]
+    elif len(shape) == 3 and max_new is not None:
+        rows = shape[0]
+    else:
         raise ValueError("k must be [n, max_new, hkv, head_dim], or [rows, hkv, head_dim] with max_new")
-    if k.dim() == 4:
-        if max_new is not None and max_new != k.shape[1]:
-            raise ValueError(f"max_new is {max_new}, k has {k.shape[1]} rows a sequence")
-        max_new = k.shape[1]
-        if k.shape[0] != n:
-            raise ValueError(f"k has {k.shape[0]} sequences, slots {n}")
-    lead = k.shape[:-2]
-    rows = k.shape[0] if k.dim() == 3 else n * max_new
-    _check_tensor("k", k, (*lead, hkv, d), k_pages.dtype, dev)
-    _check_tensor("v", v, (*lead, hkv, d), k_pages.dtype, dev)
+    if shape[-2] != hkv or shape[-1] != d:
+        raise ValueError(f"k is {tuple(shape)}, the pages have {hkv} heads of {d}")
+    _fits("k", k, shape, dtype, dev, idx)
+    _fits("v", v, shape, dtype, dev, idx)
     hq = 0
     if q is not None:
-        if q.dim() != k.dim():
-            raise ValueError("q must be shaped as k but for its heads")
-        hq = q.shape[-2]
-        _check_tensor("q", q, (*lead, hq, d), k_pages.dtype, dev)
-        q_rot = torch.empty_like(q) if q_rot is None else _check_tensor("q_rot", q_rot, q.shape, q.dtype, dev)
+        hq = q.shape[-2] if q.dim() > 1 else 0
+        _fits("q", q, (*shape[:-2], hq, d), dtype, dev, idx)
+        q_rot = torch.empty_like(q) if q_rot is None else _fits("q_rot", q_rot, q.shape, dtype, dev, idx)
     elif q_rot is not None:
         raise ValueError("q_rot without q")
-    for name, t in (("count", count), ("start", start)):
-        if t is not None:
-            _ints_of(name, t, n, dev)
+    if count is not None:
+        _fits("count", count, (n,), _int32, dev, idx)
+    if start is not None:
+        _fits("start", start, (n,), _int32, dev, idx)
     if parents is not None:
-        _check_tensor("parents", parents, (n, max_new), torch.int32, dev)
+        _fits("parents", parents, (n, max_new), _int32, dev, idx)
     with _device_of(dev):
-        _check(lib().pp_cache_append(cache.ref, n, _addr(slots), max_new, _addr(count), _addr(start), rows, _addr(parents), dt, hq,
-                                     hkv, d, float(rope_base), _addr(q), _addr(k), _addr(v), _addr(q_rot), _addr(k_pages),
-                                     _addr(v_pages), _raw_stream(dev)))
+        _check(lib().pp_cache_append(cache.ref, n, slots.data_ptr(), max_new, _addr(count), _addr(start), rows, _addr(parents), dt,
+                                     hq, hkv, d, rope_base, _addr(q), k.data_ptr(), v.data_ptr(), _addr(q_rot),
+                                     k_pages.data_ptr(), v_pages.data_ptr(), _raw_stream(dev)))
     return q_rot
 
 
@@ -1074,23 +1092,23 @@ def pp_cache_accept(cache: Cache, slots: torch.Tensor, count: torch.Tensor, path
                     status=None, ws=None) -> torch.Tensor:
     """Keeps count[i] of the tokens appended to slots[i]: the nodes path[i] ([n, max_new]) of a drafted tree, whose rows move
     together in every layer of the pools, or without path the first ones.  Returns status [2]: 0, entries refused."""
-    dev = cache.device
-    n = _slots_of("slots", slots, dev)
-    _ints_of("count", count, n, dev)
+    dev, idx = cache.device, cache.index
+    n = _slots_of("slots", slots, cache)
+    _fits("count", count, (n,), _int32, dev, idx)
     dt, layers, hkv, d = PP_BF16, 0, 1, 64
     if path is not None:
         if path.dim() != 2 or k_pages is None or v_pages is None:
             raise ValueError("path must be [n, max_new], and comes with k_pages and v_pages")
-        _check_tensor("path", path, (n, path.shape[1]), torch.int32, dev)
         max_new = path.shape[1]
+        _fits("path", path, (n, max_new), _int32, dev, idx)
         dt, layers, hkv, d = _pools(cache, k_pages, v_pages, True)
     elif max_new is None:
         max_new = 2**31 - 1
-    status, ws = _new_ints(2, dev, status), _cache_ws(cache, n, ws)
+    status = _new_ints(2, cache, status)
+    ws, at, nbytes = _scratch(cache._ws_size("pp_cache_workspace_size", n) if ws is None else 0, dev, ws)
     with _device_of(dev):
-        _check(lib().pp_cache_accept(cache.ref, n, _addr(slots), max_new, _addr(count), _addr(path), dt, layers, hkv, d,
-                                     _addr(k_pages), _addr(v_pages), _addr(status), _addr(ws), _ws_bytes(ws, dev),
-                                     _raw_stream(dev)))
+        _check(lib().pp_cache_accept(cache.ref, n, slots.data_ptr(), max_new, count.data_ptr(), _addr(path), dt, layers, hkv, d,
+                                     _addr(k_pages), _addr(v_pages), status.data_ptr(), at, nbytes, _raw_stream(dev)))
     return status
 
 
@@ -1105,32 +1123,32 @@ def pp_tree_attn_fwd(cache: Cache, slots: torch.Tensor, q: torch.Tensor, k_pages
     """Attention of new tokens q [n, max_new, hq, d] over the cache, each to its sequence's cached tokens and its path to the
     tree's root; returns (o like q, lse [hq, n * max_new] fp32).  planned: ws holds the plan of an earlier call of the same
     step (another layer's)."""
-    dev = cache.device
-    n = _slots_of("slots", slots, dev)
+    dev, idx = cache.device, cache.index
+    n = _slots_of("slots", slots, cache)
     dt, _, hkv, d = _pools(cache, k_pages, v_pages, False)
-    if q.dim() != 4:
-        raise ValueError("q must be [n, max_new, hq, head_dim]")
-    N, hq = q.shape[1], q.shape[2]
-    _check_tensor("q", q, (n, N, hq, d), k_pages.dtype, dev)
+    shape, dtype = q.shape, k_pages.dtype
+    if len(shape) != 4 or shape[0] != n or shape[3] != d:
+        raise ValueError(f"q must be [n, max_new, hq, head_dim], of {n} sequences and heads of {d}: got {tuple(shape)}")
+    N, hq = shape[1], shape[2]
+    _fits("q", q, shape, dtype, dev, idx)
     if parents is not None:
-        _check_tensor("parents", parents, (n, N), torch.int32, dev)
+        _fits("parents", parents, (n, N), _int32, dev, idx)
     if count is not None:
-        _ints_of("count", count, n, dev)
+        _fits("count", count, (n,), _int32, dev, idx)
     if group < 1 or n % group:
         raise ValueError(f"{n} sequences do not make groups of {group}")
     if shared is not None:
-        _ints_of("shared", shared, n // group, dev)
-    out = torch.empty_like(q) if out is None else _check_tensor("out", out, q.shape, q.dtype, dev)
+        _fits("shared", shared, (n // group,), _int32, dev, idx)
+    if ws is None and planned:
+        raise ValueError("planned comes with the ws that holds the plan")
+    out = torch.empty_like(q) if out is None else _fits("out", out, shape, dtype, dev, idx)
     lse = (torch.empty(hq, n * N, dtype=torch.float32, device=dev) if lse is None
-           else _check_tensor("lse", lse, (hq, n * N), torch.float32, dev))
-    if ws is None:
-        if planned:
-            raise ValueError("planned comes with the ws that holds the plan")
-        ws = _maybe_workspace(cache._ws_size("pp_tree_workspace_size", n, group, N, dt, hq, hkv, d), dev)
+           else _fits("lse", lse, (hq, n * N), torch.float32, dev, idx))
+    ws, at, nbytes = _scratch(cache._ws_size("pp_tree_workspace_size", n, group, N, dt, hq, hkv, d) if ws is None else 0, dev, ws)
     with _device_of(dev):
-        _check(lib().pp_tree_attn_fwd(cache.ref, n, _addr(slots), group, _addr(shared), N, _addr(count), _addr(parents), dt, hq, hkv,
-                                      d, float(scale), _addr(q), _addr(k_pages), _addr(v_pages), _addr(out), _addr(lse),
-                                      int(planned), _addr(ws), _ws_bytes(ws, dev), _raw_stream(dev)))
+        _check(lib().pp_tree_attn_fwd(cache.ref, n, slots.data_ptr(), group, _addr(shared), N, _addr(count), _addr(parents), dt, hq,
+                                      hkv, d, scale, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), out.data_ptr(),
+                                      lse.data_ptr(), planned, at, nbytes, _raw_stream(dev)))
     return out, lse
 
 
@@ -1157,29 +1175,28 @@ def pp_verify_draft(target: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor,
     token that follows.  Returns (count [n], new tokens [n, max_new], path [n, max_new], their log-probs [n, max_new])."""
     if target.dim() != 3:
         raise ValueError("target must be [n, max_new, vocab]")
-    (n, N, V), dev = target.shape, target.device
-    _check_tensor("target", target, target.shape, target.dtype, dev)
-    _check_tensor("tokens", tokens, (n, N), torch.int32, dev)
-    _check_tensor("u", u, (n, N), torch.float32, dev)
-    if draft is not None:
-        _check_tensor("draft", draft, target.shape, target.dtype, dev)
-    if parents is not None:
-        _check_tensor("parents", parents, (n, N), torch.int32, dev)
-    if count is not None:
-        _ints_of("count", count, n, dev)
-    if temperature is not None:
-        _check_tensor("temperature", temperature, (n,), torch.float32, dev)
+    (n, N, V), dev, dtype = target.shape, target.device, target.dtype
     dt = _dtype_code(target)
     _on_gpu(target)
-    out = torch.empty(2 * n * N + n, dtype=torch.int32, device=dev)
-    out_tokens, path, out_count = out[:n * N].view(n, N), out[n * N:2 * n * N].view(n, N), out[2 * n * N:]
-    logp = torch.empty(n, N, dtype=torch.float32, device=dev)
-    if ws is None:
-        ws = _maybe_workspace(pp_verify_workspace_size(n, N, V, dt), dev)
+    idx, each = dev.index, (n, N)
+    _fits("target", target, target.shape, dtype, dev, idx)
+    _fits("tokens", tokens, each, _int32, dev, idx)
+    _fits("u", u, each, torch.float32, dev, idx)
+    if draft is not None:
+        _fits("draft", draft, target.shape, dtype, dev, idx)
+    if parents is not None:
+        _fits("parents", parents, each, _int32, dev, idx)
+    if count is not None:
+        _fits("count", count, (n,), _int32, dev, idx)
+    if temperature is not None:
+        _fits("temperature", temperature, (n,), torch.float32, dev, idx)
+    new = lambda *shape: torch.empty(shape, dtype=_int32, device=dev)
+    out_count, out_tokens, path, logp = new(n), new(n, N), new(n, N), torch.empty(n, N, dtype=torch.float32, device=dev)
+    ws, at, nbytes = _scratch(pp_verify_workspace_size(n, N, V, dt) if ws is None else 0, dev, ws)
     with _device_of(dev):
-        _check(lib().pp_verify_draft(n, N, V, dt, max_children, _addr(count), _addr(parents), _addr(tokens), _addr(target),
-                                     _addr(draft), _addr(temperature), _addr(u), _addr(out_count), _addr(out_tokens), _addr(path),
-                                     _addr(logp), _addr(ws), _ws_bytes(ws, dev), _raw_stream(dev)))
+        _check(lib().pp_verify_draft(n, N, V, dt, max_children, _addr(count), _addr(parents), tokens.data_ptr(), target.data_ptr(),
+                                     _addr(draft), _addr(temperature), u.data_ptr(), out_count.data_ptr(), out_tokens.data_ptr(),
+                                     path.data_ptr(), logp.data_ptr(), at, nbytes, _raw_stream(dev)))
     return out_count, out_tokens, path, logp
 
 
