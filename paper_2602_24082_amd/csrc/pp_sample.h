@@ -88,29 +88,26 @@ hipError_t launch_cache_shared(const CacheView& c, int groups, const int32_t* sl
 hipError_t launch_cache_append(const CacheView& c, const AppendParams& a, int n, int head_dim, int dtype, hipStream_t s);
 
 // Attention of drafted trees over the cache (pp_tree.hip).
-#ifndef PP_TEAM_CU
-#define PP_TEAM_CU 2
-#define PP_TEAM_KEYS 64
-#define PP_TEAM_STAGES 2
-#endif
 constexpr int kTreeSeqs = 2048;  // sequences a call
 constexpr int kTreeNodes = 64;   // nodes a sequence
 constexpr int kCus = 256;
 // Workgroups a compute unit: of one wave, each with a ring of two blocks of 32 keys and values
-// in LDS, and of a team of four waves, with a ring between them.
+// in LDS, and of a team of four waves, with a ring between them.  bf16 of head size 128, a team:
+// 64 keys a block, two blocks, two teams a unit.  16 drafted nodes of each of four sequences of
+// 36 000 tokens, 64 heads over 8, take 127 us so, 130 with three or four blocks of 32 keys, 142
+// with one team of four blocks of 64, 147 with three teams.
 template <int D, typename T>
 constexpr int kTreeSolo = D * sizeof(T) > 256 ? 2 : D * sizeof(T) > 128 ? 4 : 8;
 template <int D, typename T>
-constexpr int kTreeTeam = sizeof(T) == 4 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : PP_TEAM_CU;
+constexpr int kTreeTeam = sizeof(T) == 4 ? (D == 64 ? 2 : 1) : D == 64 ? 3 : 2;
 template <int D, typename T>
-constexpr int kTeamKeys = sizeof(T) == 2 ? PP_TEAM_KEYS : 32;
+constexpr int kTeamKeys = sizeof(T) == 2 ? 64 : 32;
 // Blocks that a team has room for: what a compute unit's LDS leaves each
 template <int D, typename T>
-constexpr int kTeamStages = sizeof(T) == 2 && D == 128 ? PP_TEAM_STAGES : D * sizeof(T) > 128 ? 4 : 3;
-#ifndef PP_TREE_START
-#define PP_TREE_START 4
-#endif
-constexpr int kTreeStart = PP_TREE_START;
+constexpr int kTeamStages = sizeof(T) == 2 && D == 128 ? 2 : D * sizeof(T) > 128 ? 4 : 3;
+// An item's start in blocks of keys, where work is dealt out: single tokens of 16 groups of 16 over
+// 2048 shared and some 500 own tokens take 92 us with 0, 80 with 2, 79 with 4.
+constexpr int kTreeStart = 4;
 constexpr int kSoloKeys = 32, kSoloRows = 32, kTeamWaves = 4, kTeamRows = 128;
 
 // An item: rows against a range of keys; its units: a block of keys, for a tile of rows of one
