@@ -28,6 +28,8 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "pp_device.h"
 #include "pp_sample.h"
 
@@ -57,26 +59,39 @@ __device__ __forceinline__ float lowest<float>() {
 template <typename T>
 constexpr uint32_t kInfBits = sizeof(T) == 2 ? 0x7f80u : 0x7f800000u;
 
-// 2^t for t <= 0 in 64 bits: 2^n by the exponent's bits, 2^f, |f| <= 1/2, by the polynomial of
-// degree 9 through Chebyshev's points, good to 2e-14 of it (degree 14 of the series takes five
-// more multiplications).  n comes out of the low bits of t + 1.5 2^52.  Below 2^-1000, and for
-// -inf and NaN, 2^-1000.
+// 2^(i / 64), in LDS: entries are two banks each, so that a wave's lanes meet at most twice.
+// Their upper words are lower by i << 14: k << 14 on top makes entry k & 63 2^(k / 64).
+constexpr int kRoots = 64;
+__device__ __forceinline__ double* exp2_roots() {
+  __shared__ double roots[kRoots];
+  return roots;
+}
+__device__ __forceinline__ void fill_roots() {
+  if (threadIdx.x < kRoots) {
+    const double r = exp2((double)threadIdx.x / kRoots);
+    exp2_roots()[threadIdx.x] = __hiloint2double(__double2hiint(r) - (int)(threadIdx.x << 14), __double2loint(r));
+  }
+  lds_barrier();
+}
+// 2^t for t <= 0 in 64 bits: with k the whole number next to 64 t and f = t - k / 64,
+// |f| <= 1/128, 2^(k / 64) from the table, 2^f by the polynomial of degree 4 through 1 at 0 and
+// Chebyshev's points, good to 5e-15 of it.  k comes out of the low bits of t + 1.5 2^46.  Below
+// 2^-1000, and for -inf and NaN, 2^-1000; without CLAMP t has to be above.
 constexpr double kTiny = -1000.0;
+template <bool CLAMP = true>
 __device__ __forceinline__ double exp2_neg(double t) {
-  t = fmax(t, kTiny);
-  const double u = t + 6755399441055744.0;
-  const double f = t - (u - 6755399441055744.0);
-  double s = 1.0205757125041537e-07;
-  s = fma(s, f, 1.325968083523609e-06);
-  s = fma(s, f, 1.5252674538194317e-05);
-  s = fma(s, f, 0.00015403433618713555);
-  s = fma(s, f, 0.001333355819593412);
-  s = fma(s, f, 0.009618129194074796);
-  s = fma(s, f, 0.05550410866470368);
-  s = fma(s, f, 0.2402265069563986);
-  s = fma(s, f, 0.6931471805599446);
-  s = fma(s, f, 1.0000000000000135);
-  return __hiloint2double(__double2hiint(s) + (__double2loint(u) << 20), __double2loint(s));
+  constexpr double shift = 1.5 * (1ull << 46);
+  if (CLAMP) t = fmax(t, kTiny);
+  const double u = t + shift;
+  const int k = __double2loint(u);
+  const double base = exp2_roots()[k & (kRoots - 1)];
+  const double root = __hiloint2double(__double2hiint(base) + (k << 14), __double2loint(base));
+  const double f = t - (u - shift);
+  double s = 0.009618138509201629;
+  s = fma(s, f, 0.05550419004645178);
+  s = fma(s, f, 0.24022650695902897);
+  s = fma(s, f, 0.6931471805593244);
+  return fma(root, s * f, root);
 }
 
 template <typename T>
@@ -125,6 +140,10 @@ __device__ __forceinline__ uint32_t most_bits(const RawOf<uint16_t>& m) {
   return r;
 }
 __device__ __forceinline__ uint32_t most_bits(uint32_t m) { return m; }
+template <typename T>
+__device__ __forceinline__ float float_of_bits(uint32_t b) {
+  return __uint_as_float(sizeof(T) == 2 ? b << 16 : b);
+}
 template <typename T>
 struct BitsOf {
   using Type = uint32_t;
@@ -197,7 +216,7 @@ __device__ __forceinline__ double inv_temp(const float* temperature, int s) {
 }
 __device__ __forceinline__ bool greedy(const float* temperature, int s) { return temperature && !(temperature[s] > 0); }
 
-// A wave a chunk, without a barrier.
+// A wave a chunk.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
   constexpr int L = kLoads<T, 64>;
@@ -206,21 +225,23 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
   const int row = blockIdx.y, chunk = blockIdx.x * kWavesD + wave, s = row / d.nodes, node = row - s * d.nodes;
   const bool is_draft = blockIdx.z != 0, argmax = greedy(p.temperature, s);
   const int n = max(0, min(p.count ? p.count[s] : d.nodes, d.nodes));
+  const double a = inv_temp(p.temperature, s);
   if (node == 0 && chunk == 0 && !is_draft && lane == 0) p.arrived[s] = 0;
-  if (node >= n || chunk >= d.chunks) return;
+  if (node >= n) return;
   if (is_draft) {
     if (argmax) return;
-    bool kid = false;  // only nodes with children have drafts
-    for (int j = node + 1 + lane; j < n; j += 64)
-      kid = kid || (p.parents ? p.parents[(int64_t)s * d.nodes + j] == node : j == node + 1);
-    if (!__any(kid)) return;
+    // only nodes with children have drafts
+    const bool later = lane > node && lane < n;
+    const int up = !later ? -1 : p.parents ? p.parents[(int64_t)s * d.nodes + lane] : lane - 1;
+    if (!__any(up == node)) return;
   }
   ChunkOf<T, 64> c;
-  c.init((const T*)(is_draft ? p.draft : p.target) + (int64_t)row * d.vocab, d.vocab, chunk, lane);
+  c.init((const T*)(is_draft ? p.draft : p.target) + (int64_t)row * d.vocab, d.vocab, min(chunk, d.chunks - 1), lane);
   RawOf<T> x[L];
 #pragma unroll
   for (int u = 0; u < L; ++u) x[u] = c.load(u);
-  const double a = inv_temp(p.temperature, s);
+  fill_roots();
+  if (chunk >= d.chunks) return;
   float m = kNegInf;
   typename BitsOf<T>::Type bits{};
 #pragma unroll
@@ -230,7 +251,8 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
     for (int i = 0; i < kVec<T>; ++i) m = fmaxf(m, to_float(x[u][i]));
   }
   const float top = wave_max(m);
-  const bool bad = __any(most_bits(bits) > kInfBits<T>) || top == -kNegInf;
+  const uint32_t most = most_bits(bits);
+  const bool bad = __any(most > kInfBits<T>) || top == -kNegInf;
   DraftPart out;
   out.sum = 0;
   out.arg = 0x7fffffff;
@@ -238,10 +260,17 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
   if (top > lowest<T>() && !bad) {
     const double b = -(double)top * a;
     double sum = 0;
+    auto add_all = [&](auto clamp) {
 #pragma unroll
-    for (int u = 0; u < L; ++u)
+      for (int u = 0; u < L; ++u) {
+        asm volatile("" : "+v"(x[u]));
 #pragma unroll
-      for (int i = 0; i < kVec<T>; ++i) sum += exp2_neg(fma((double)to_float(x[u][i]), a, b));
+        for (int i = 0; i < kVec<T>; ++i) sum += exp2_neg<clamp.value>(fma((double)to_float(x[u][i]), a, b));
+      }
+    };
+    const double low = fma(-(double)float_of_bits<T>(most), a, b);  // no exponent is below
+    if (__any(!(low > kTiny))) add_all(std::true_type{});
+    else add_all(std::false_type{});
     out.sum = wave_sum_d(sum);
     if (argmax) {
       int arg = 0x7fffffff;
@@ -425,6 +454,7 @@ __global__ __launch_bounds__(kEdgeThreads) void draft_edges_kernel(DraftParams p
   const int64_t row0 = (int64_t)s * d.nodes, rows = (int64_t)d.n * d.nodes;
   const bool argmax = greedy(p.temperature, s), sampled = p.draft != nullptr && !argmax;
   const double it = inv_temp(p.temperature, s);
+  fill_roots();
   for (int i = wave; i < 2 * n; i += kEdgeThreads / 64) {
     const int node = i >> 1, is_q = i & 1;
     if (is_q && !(sampled && lane_u64(t.kids, node))) continue;
@@ -490,6 +520,7 @@ __global__ __launch_bounds__(kThreads) void draft_residual_kernel(DraftParams p,
   const TreeOf t = tree_of(d, p.parents, p.count, s, lane);
   const EdgeOf e = edge_of(p, row0, lane, n);
   const double it = inv_temp(p.temperature, s);
+  fill_roots();
   for (; need; need &= need - 1) {
     const int first = __ffsll((unsigned long long)need) - 1, up = __builtin_amdgcn_readlane(t.up, first);
     const uint64_t kids = lane_u64(t.kids, up);
@@ -614,6 +645,7 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
   }
   const bool argmax = greedy(p.temperature, s), sampled = p.draft != nullptr && !argmax;
   const double it = inv_temp(p.temperature, s);
+  fill_roots();
   const EdgeOf e = edge_of(p, row0, lane, n);
 
   // the walk, by every wave on its own
