@@ -308,16 +308,22 @@ __device__ __forceinline__ RowDist row_dist(const DraftRow& x, double it) {
   r.b = -(double)x.max * it;
   return r;
 }
+// The parts of a row's first 128 chunks, two a lane.
+struct RowParts {
+  DraftPart a, b;
+  __device__ __forceinline__ void load(const DraftPart* part, int chunks, int lane) {
+    a.sum = b.sum = 0;
+    a.max = b.max = kNegInf;
+    a.arg = b.arg = 0x7fffffff;
+    if (lane < chunks) a = part[lane];
+    if (lane + 64 < chunks) b = part[lane + 64];
+  }
+};
 // By a wave, from the parts of the row's chunks.
-__device__ __forceinline__ RowDist row_dist(const DraftPart* part, int chunks, double it, int lane) {
-  DraftPart mine;  // of the first 64 chunks
-  mine.sum = 0;
-  mine.max = kNegInf;
-  mine.arg = 0x7fffffff;
-  if (lane < chunks) mine = part[lane];
-  float m = mine.max;
-  bool bad = m != m;
-  for (int c = lane + 64; c < chunks; c += 64) {
+__device__ __forceinline__ RowDist row_dist(const RowParts& first, const DraftPart* part, int chunks, double it, int lane) {
+  float m = fmaxf(first.a.max, first.b.max);
+  bool bad = first.a.max != first.a.max || first.b.max != first.b.max;
+  for (int c = lane + 128; c < chunks; c += 64) {
     const float x = part[c].max;
     bad = bad || x != x;
     m = fmaxf(m, x);
@@ -336,8 +342,9 @@ __device__ __forceinline__ RowDist row_dist(const DraftPart* part, int chunks, d
     if (x.max > kNegInf) s = fma(x.sum, r.raw(x.max), s);
     if (x.max == r.max) arg = min(arg, x.arg);
   };
-  add(mine);
-  for (int c = lane + 64; c < chunks; c += 64) add(part[c]);
+  add(first.a);
+  add(first.b);
+  for (int c = lane + 128; c < chunks; c += 64) add(part[c]);
   r.sum = wave_sum_d(s);
   for (int off = 32; off > 0; off >>= 1) arg = min(arg, __shfl_xor(arg, off, 64));
   r.arg = arg;
@@ -413,26 +420,34 @@ __device__ __forceinline__ double residual_sum(const DraftParams& p, int64_t row
   return sum;
 }
 
-// Of a drafted token, a lane each.
+// Of a drafted token, a lane each, and the lane's own rows (lanes behind the count hold
+// anything).
 struct EdgeOf {
   double p, q;
   float u;
   int tok;
-  int p_arg, q_arg;  // of the lane's own rows
+  DraftRow rp, rq;
 };
-__device__ __forceinline__ EdgeOf edge_of(const DraftParams& p, int64_t row0, int lane, int n) {
+__device__ __forceinline__ EdgeOf edge_of(const DraftParams& p, int64_t row0, int lane) {
   EdgeOf e{};
   e.tok = -1;
-  if (lane < n) {
+  if (lane < p.shape.nodes) {
     const DraftEdge x = p.edge[row0 + lane];
+    e.rp = p.row[row0 + lane];
+    e.rq = p.row[(int64_t)p.shape.n * p.shape.nodes + row0 + lane];
     e.p = x.p;
     e.q = x.q;
     e.u = p.u[row0 + lane];
     e.tok = p.tokens[row0 + lane];
-    e.p_arg = p.row[row0 + lane].arg;
-    e.q_arg = p.row[(int64_t)p.shape.n * p.shape.nodes + row0 + lane].arg;
   }
   return e;
+}
+__device__ __forceinline__ DraftRow lane_row(const DraftRow& r, int lane) {
+  DraftRow x;
+  x.sum = lane_d(r.sum, lane);
+  x.max = lane_f(r.max, lane);
+  x.arg = __builtin_amdgcn_readlane(r.arg, lane);
+  return x;
 }
 
 // Z after a node is rejected, by a wave.
@@ -454,11 +469,30 @@ __global__ __launch_bounds__(kEdgeThreads) void draft_edges_kernel(DraftParams p
   const int64_t row0 = (int64_t)s * d.nodes, rows = (int64_t)d.n * d.nodes;
   const bool argmax = greedy(p.temperature, s), sampled = p.draft != nullptr && !argmax;
   const double it = inv_temp(p.temperature, s);
+  // the drafted tokens' logits
+  const int y = lane < n ? p.tokens[row0 + lane] : -1;
+  float xp = 0.f, xq = 0.f;
+  if (tid < 64 && t.up >= 0 && y >= 0 && y < d.vocab) {
+    const int64_t at = (row0 + t.up) * d.vocab + y;
+    xp = to_float(((const T*)p.target)[at]);
+    if (sampled) xq = to_float(((const T*)p.draft)[at]);
+  }
+  // the rows, each one's parts fetched ahead
+  auto part_of = [&](int i) { return p.part + ((i & 1) * rows + row0 + (i >> 1)) * d.chunks; };
+  auto next = [&](int i) {  // the wave's next row from i on that is looked at
+    while (i < 2 * n && (i & 1) && !(sampled && lane_u64(t.kids, i >> 1))) i += kEdgeThreads / 64;
+    return i;
+  };
+  int i = next(wave);
+  RowParts ahead;
+  if (i < 2 * n) ahead.load(part_of(i), d.chunks, lane);
   fill_roots();
-  for (int i = wave; i < 2 * n; i += kEdgeThreads / 64) {
-    const int node = i >> 1, is_q = i & 1;
-    if (is_q && !(sampled && lane_u64(t.kids, node))) continue;
-    const RowDist r = row_dist(p.part + (is_q * rows + row0 + node) * d.chunks, d.chunks, it, lane);
+  while (i < 2 * n) {
+    const int node = i >> 1, is_q = i & 1, then = next(i + kEdgeThreads / 64);
+    const RowParts mine = ahead;
+    if (then < 2 * n) ahead.load(part_of(then), d.chunks, lane);
+    const RowDist r = row_dist(mine, part_of(i), d.chunks, it, lane);
+    i = then;
     if (lane == 0) {
       DraftRow x;
       x.sum = r.sum;
@@ -473,13 +507,11 @@ __global__ __launch_bounds__(kEdgeThreads) void draft_edges_kernel(DraftParams p
   DraftEdge e{};
   bool tried = false, stays = false;  // as a first child
   if (lane < n && t.up >= 0) {
-    const int y = p.tokens[row0 + lane];
     const DraftRow rp = s_p[t.up], rq = sampled ? s_q[t.up] : rp;
     tried = rp.arg >= 0 && rq.arg >= 0;
     if (tried && y >= 0 && y < d.vocab) {
-      const int64_t at = (row0 + t.up) * d.vocab + y;
-      e.p = row_dist(rp, it).raw(to_float(((const T*)p.target)[at])) / rp.sum;
-      if (sampled) e.q = row_dist(rq, it).raw(to_float(((const T*)p.draft)[at])) / rq.sum;
+      e.p = row_dist(rp, it).raw(xp) / rp.sum;
+      if (sampled) e.q = row_dist(rq, it).raw(xq) / rq.sum;
     }
     const double u = (double)p.u[row0 + lane];
     stays = tried && (sampled ? u * e.q < e.p : argmax ? y == rp.arg : u < e.p);
@@ -513,12 +545,12 @@ __global__ __launch_bounds__(kThreads) void draft_residual_kernel(DraftParams p,
   __shared__ double s_sum[kWavesD];
   const DraftShape& d = p.shape;
   const int chunk = blockIdx.x, s = blockIdx.y, lane = threadIdx.x & 63;
-  const int64_t row0 = (int64_t)s * d.nodes, rows = (int64_t)d.n * d.nodes;
+  const int64_t row0 = (int64_t)s * d.nodes;
   const int n = max(0, min(p.count ? p.count[s] : d.nodes, d.nodes));
   uint64_t need = __ballot(lane < n && p.edge[row0 + lane].need);
   if (need == 0) return;
   const TreeOf t = tree_of(d, p.parents, p.count, s, lane);
-  const EdgeOf e = edge_of(p, row0, lane, n);
+  const EdgeOf e = edge_of(p, row0, lane);
   const double it = inv_temp(p.temperature, s);
   fill_roots();
   for (; need; need &= need - 1) {
@@ -539,7 +571,7 @@ __global__ __launch_bounds__(kThreads) void draft_residual_kernel(DraftParams p,
       Z = left_after(p, row0 + j, lane);
     }
     if (stays) continue;
-    const RowDist tp = row_dist(p.row[row0 + up], it), tq = row_dist(p.row[rows + row0 + up], it);
+    const RowDist tp = row_dist(lane_row(e.rp, up), it), tq = row_dist(lane_row(e.rq, up), it);
     const double sum = residual_sum<T>(p, row0 + up, chunk, tp, tq, a, s_sum);
     if (threadIdx.x == 0) p.left[(row0 + j) * d.chunks + chunk] = sum;
   }
@@ -567,11 +599,11 @@ struct Picked {
   int64_t y;  // -1: nothing there
   double logp;
 };
-// By the workgroup: the entry of the chunk at which the running sum of what is left passes; s_w:
-// room for the sums of the chunk's loads.
+// By the workgroup: the entry of the chunk at which the running sum of what is left passes; s_w,
+// s_sum: room for the entries' weights and the sums of the chunk's loads.
 template <typename T>
 __device__ __forceinline__ Picked pick_entry(const DraftParams& p, int64_t row, const RowDist& tp, const RowDist& tq, double a,
-                                             const PickOf& pick, double* s_w) {
+                                             const PickOf& pick, double* s_w, double* s_sum) {
   constexpr int VPC = kDraftChunk / kVec<T>, PER = VPC / 64, L = kLoads<T, kThreads>;  // loads of a chunk, a lane's, a thread's
   const int tid = threadIdx.x, lane = tid & 63;
   Picked out{false, -1, (double)__builtin_nanf("")};
@@ -584,23 +616,28 @@ __device__ __forceinline__ Picked pick_entry(const DraftParams& p, int64_t row, 
     return false;
   };
   double sums[L] = {};
-  left.each([&](int u, int i, double w) { sums[u] += n_gone && is_gone(left.c.at(u) + i) ? 0.0 : w; });
+  left.each([&](int u, int i, double w) {
+    if (n_gone && is_gone(left.c.at(u) + i)) w = 0.0;
+    const int at = (u * kThreads + tid) * kVec<T> + i;
+    s_w[at] = w;
+    sums[u] += w;
+  });
 #pragma unroll
-  for (int u = 0; u < L; ++u) s_w[u * kThreads + tid] = sums[u];
+  for (int u = 0; u < L; ++u) s_sum[u * kThreads + tid] = sums[u];
   __syncthreads();
   if (tid >= 64) return out;
   // one wave: a lane's loads, then the load, then the entry
   double mine = 0, before;
   bool passed;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) mine += s_w[lane * PER + i];
+  for (int i = 0; i < PER; ++i) mine += s_sum[lane * PER + i];
   const int who = pass_lane(mine, 0.0, pick.want, lane, before, passed);
   int load = 0;
   double ahead = before;
   if (who >= 0) {
     double run = before;
     for (int i = who * PER; i < who * PER + PER; ++i) {
-      const double w = s_w[i];
+      const double w = s_sum[i];
       if (w > 0) {  // (the last one that has any, should none pass)
         load = i;
         ahead = run;
@@ -610,12 +647,9 @@ __device__ __forceinline__ Picked pick_entry(const DraftParams& p, int64_t row, 
     }
   }
   const int64_t y = left.c.first - (int64_t)tid * kVec<T> + (int64_t)load * kVec<T> + lane;  // (first: the thread's)
-  double w = 0;
-  float x = 0.f;
-  if (who >= 0 && lane < kVec<T> && y >= 0 && y < p.shape.vocab && !(n_gone && is_gone(y))) {
-    x = to_float(left.c.row[y]);
-    w = left.of(x, left.q ? to_float(left.q[y]) : 0.f);
-  }
+  const bool entry = who >= 0 && lane < kVec<T>;
+  const double w = entry ? s_w[load * kVec<T> + lane] : 0.0;
+  const float x = entry && y >= 0 && y < p.shape.vocab ? to_float(left.c.row[y]) : 0.f;
   const int last = pass_lane(w, ahead, pick.want, lane, before, passed);
   out.mine = lane == max(last, 0);
   if (lane == last) {
@@ -627,14 +661,15 @@ __device__ __forceinline__ Picked pick_entry(const DraftParams& p, int64_t row, 
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
-  __shared__ double s_w[kDraftChunk / kVec<T>], s_sum[kWavesD];
+  __shared__ double s_w[kDraftChunk], s_sum[kDraftChunk / kVec<T>];
   __shared__ PickOf s_pick;
   __shared__ int s_whole, s_last;
   const DraftShape& d = p.shape;
   const int s = blockIdx.y, chunk = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+  const int64_t row0 = (int64_t)s * d.nodes;
+  const EdgeOf e = edge_of(p, row0, lane);
   const TreeOf t = tree_of(d, p.parents, p.count, s, lane);
   const int n = t.count;
-  const int64_t row0 = (int64_t)s * d.nodes, rows = (int64_t)d.n * d.nodes;
   if (n == 0) {
     if (chunk == 0 && tid < d.nodes) {
       p.out_tokens[row0 + tid] = p.out_path[row0 + tid] = -1;
@@ -646,7 +681,6 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
   const bool argmax = greedy(p.temperature, s), sampled = p.draft != nullptr && !argmax;
   const double it = inv_temp(p.temperature, s);
   fill_roots();
-  const EdgeOf e = edge_of(p, row0, lane, n);
 
   // the walk, by every wave on its own
   int at = 0, len = 1, order = lane == 0 ? 0 : -1;
@@ -657,9 +691,9 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
     double Z = 1.0;
     a = 0;
     gone = 0;
-    const int p_arg = __builtin_amdgcn_readlane(e.p_arg, at);
+    const int p_arg = __builtin_amdgcn_readlane(e.rp.arg, at);
     const uint64_t kids = lane_u64(t.kids, at);
-    if (kids == 0 || p_arg < 0 || (sampled && __builtin_amdgcn_readlane(e.q_arg, at) < 0)) break;  // nothing to try
+    if (kids == 0 || p_arg < 0 || (sampled && __builtin_amdgcn_readlane(e.rq.arg, at) < 0)) break;  // nothing to try
     for (uint64_t m = kids; m; m &= m - 1) {
       const int j = __ffsll((unsigned long long)m) - 1;
       const int y = __builtin_amdgcn_readlane(e.tok, j);
@@ -710,7 +744,7 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
     if (lane == 0) p.out_count[s] = len;
   }
   const int64_t row = row0 + at;
-  const RowDist tp = row_dist(p.row[row], it);
+  const RowDist tp = row_dist(lane_row(e.rp, at), it);
   auto finish = [&](int64_t y, double logp) {
     p.out_tokens[row0 + len - 1] = (int32_t)y;
     p.out_logp[row0 + len - 1] = (float)logp;
@@ -724,7 +758,7 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
   }
   RowDist tq{};
   if (residual) {
-    tq = row_dist(p.row[rows + row], it);
+    tq = row_dist(lane_row(e.rq, at), it);
     const double sum = residual_sum<T>(p, row, chunk, tp, tq, a, s_sum);
     if (tid == 0) {
       // written through to where all XCDs see it, and waited for, ahead of the count: a fence
@@ -806,7 +840,7 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
     }
   }
   __syncthreads();
-  const Picked got = pick_entry<T>(p, row, tp, tq, s_whole ? 0.0 : a, s_pick, s_w);
+  const Picked got = pick_entry<T>(p, row, tp, tq, s_whole ? 0.0 : a, s_pick, s_w, s_sum);
   if (got.mine) finish(got.y, got.logp);
 }
 
