@@ -642,35 +642,60 @@ __device__ __forceinline__ TreeParts tree_parts(const TreeShape& sh, int64_t run
   return p;
 }
 
-// A row is D / 4 lanes, four partial results' loads in flight: those of its group's shared
-// keys, then its own's.
-template <int D, typename T>
+// Rows a workgroup, PASS after PASS: where a row's partial results lie (its group's shared keys',
+// then its own's) takes a few divisions, which a thread of its own does ahead for each row; then a
+// row is D / 4 lanes, with four partial results' loads in flight.
+template <int D, typename T, int PASS>
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeShape sh, TreeParams<T> p) {
-  constexpr int LPR = D / 4, RPB = 256 / LPR, NP = 4;
-  const int64_t out_row = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR;
-  if (out_row >= (int64_t)sh.n * sh.nodes * sh.hq) return;
+  constexpr int LPR = D / 4, RPB = 256 / LPR, NP = 4, ROWS = RPB * PASS;
+  struct Row {
+    int64_t lse;  // where its lse goes; < 0: no such row
+    TreeParts a, b;
+    float l;      // NaN: a node of a bad sequence
+  };
+  __shared__ Row s_row[ROWS];
+  const int64_t row0 = (int64_t)blockIdx.x * ROWS, rows = (int64_t)sh.n * sh.nodes * sh.hq;
+  if (threadIdx.x < ROWS) {
+    Row x;
+    x.lse = -1;
+    x.l = 0.f;
+    x.a = x.b = TreeParts{0, 0, 0};
+    const int64_t out_row = row0 + threadIdx.x;
+    if (out_row < rows) {
+      const int tok = (int)div_floor(out_row, sh.hq), head = (int)(out_row - (int64_t)tok * sh.hq);
+      const int seq = tok / sh.nodes, node = tok - seq * sh.nodes, grp = seq / sh.group;
+      const int g = head / sh.G, h = head - g * sh.G;
+      const TreeItem mine = p.plan.items[seq + grp + 1], all = p.plan.items[grp * (sh.group + 1)];
+      const int64_t run_all = p.plan.head[2 * sh.kind[0].team + 1], run_own = p.plan.head[2 * sh.kind[1].team + 1];
+      x.lse = (int64_t)head * sh.n * sh.nodes + tok;
+      if (node * sh.G < mine.rows) {
+        if (all.blocks) x.a = tree_parts(sh, run_all, 0, all, grp, g, (mine.row0 + node) * sh.G + h);
+        x.b = tree_parts(sh, run_own, 1, mine, seq, g, node * sh.G + h);
+      } else if (node < mine.bad) {
+        x.l = __builtin_nanf("");
+      }
+    }
+    s_row[threadIdx.x] = x;
+  }
+  __syncthreads();
   const int col = (threadIdx.x % LPR) * 4;
-  const int tok = (int)(out_row / sh.hq), head = (int)(out_row - (int64_t)tok * sh.hq);
-  const int seq = tok / sh.nodes, node = tok - seq * sh.nodes, grp = seq / sh.group;
-  const int g = head / sh.G, h = head - g * sh.G;
-  const int lead = grp * (sh.group + 1), own = seq + grp + 1;
-  const TreeItem mine = p.plan.items[own], all = p.plan.items[lead];
-  const int64_t run_all = p.plan.head[2 * sh.kind[0].team + 1], run_own = p.plan.head[2 * sh.kind[1].team + 1];
-  f32x4 acc = f32x4{};
-  float m = kNegInf, l = 0.f;
-  if (node * sh.G < mine.rows) {
-    TreeParts a{0, 0, 0};
-    if (all.blocks) a = tree_parts(sh, run_all, 0, all, grp, g, (mine.row0 + node) * sh.G + h);
-    const TreeParts b = tree_parts(sh, run_own, 1, mine, seq, g, node * sh.G + h);
+#pragma unroll 1
+  for (int pass = 0; pass < PASS; ++pass) {
+    const int at = pass * RPB + threadIdx.x / LPR;
+    const Row& x = s_row[at];
+    if (x.lse < 0) return;
+    const TreeParts a = x.a, b = x.b;
+    f32x4 acc = f32x4{};
+    float m = kNegInf, l = x.l;
     const int64_t parts = a.n + b.n;
     for (int64_t n0 = 0; n0 < parts; n0 += NP) {
-      f32x4 x[NP];
+      f32x4 y[NP];
       float pm[NP], pl[NP];
 #pragma unroll
       for (int n = 0; n < NP; ++n) {
         const int64_t k = n0 + n < parts ? n0 + n : 0;
         const int64_t r = k < a.n ? a.row + k * a.stride : b.row + (k - a.n) * b.stride;
-        x[n] = *reinterpret_cast<const f32x4*>(p.part + r * D + col);
+        y[n] = *reinterpret_cast<const f32x4*>(p.part + r * D + col);
         pm[n] = p.part_ml[2 * r];
         pl[n] = n0 + n < parts ? p.part_ml[2 * r + 1] : 0.f;
       }
@@ -680,17 +705,15 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeShape sh, TreePar
         const float mn = fmaxf(m, pm[n]);
         const float c = m == kNegInf ? 0.f : fast_exp2(m - mn), d = fast_exp2(pm[n] - mn);
         l = l * c + pl[n] * d;
-        acc = acc * c + x[n] * d;
+        acc = acc * c + y[n] * d;
         m = mn;
       }
     }
-  } else if (node < mine.bad) {
-    l = __builtin_nanf("");
+    const bool some = l != 0.f;  // NaN: so is the row
+    const float inv = some ? 1.f / l : 0.f;
+    store4<T>(p.o + (row0 + at) * D + col, some ? acc * inv : f32x4{});
+    if (col == 0) p.lse[x.lse] = some ? (m + __log2f(l)) * (1.0f / kLog2e) : 0.f;
   }
-  const bool some = l != 0.f;  // NaN: so is the row
-  const float inv = some ? 1.f / l : 0.f;
-  store4<T>(p.o + out_row * D + col, some ? acc * inv : f32x4{});
-  if (col == 0) p.lse[(int64_t)head * sh.n * sh.nodes + tok] = some ? (m + __log2f(l)) * (1.0f / kLog2e) : 0.f;
 }
 
 template <int D, typename T>
@@ -723,9 +746,12 @@ hipError_t launch_tree_t(const CacheView& c, const TreeLaunch& a, hipStream_t s)
     if (e != hipSuccess) return e;
   }
   TimingScope t("pp_tree_attn_combine", s);
+  // four passes where that still leaves the compute units some workgroups each
   constexpr int RPB = 256 / (D / 4);
   const int64_t rows = (int64_t)sh.n * sh.nodes * sh.hq;
-  hipLaunchKernelGGL((tree_combine_kernel<D, T>), dim3((unsigned)((rows + RPB - 1) / RPB)), dim3(256), 0, s, sh, p);
+  auto grid = [&](int pass) { return dim3((unsigned)((rows + RPB * pass - 1) / (RPB * pass))); };
+  if (rows >= 4 * RPB * 4 * kCus) hipLaunchKernelGGL((tree_combine_kernel<D, T, 4>), grid(4), dim3(256), 0, s, sh, p);
+  else hipLaunchKernelGGL((tree_combine_kernel<D, T, 1>), grid(1), dim3(256), 0, s, sh, p);
   return hipGetLastError();
 }
 
