@@ -642,20 +642,21 @@ __device__ __forceinline__ TreeParts tree_parts(const TreeShape& sh, int64_t run
   return p;
 }
 
-// Rows a workgroup, PASS after PASS: where a row's partial results lie (its group's shared keys',
-// then its own's) takes a few divisions, which a thread of its own does ahead for each row; then a
-// row is D / 4 lanes, with four partial results' loads in flight.
-template <int D, typename T, int PASS>
+// Where a row's partial results lie (its group's shared keys', then its own's) takes a few
+// divisions, which one thread a row does ahead; then a row is D / 4 lanes, with four partial
+// results' loads in flight.  Bound by reading them: 32 768 rows of head size 128 with four or five
+// each, 80 MB, take 17 us.
+template <int D, typename T>
 __global__ __launch_bounds__(256) void tree_combine_kernel(TreeShape sh, TreeParams<T> p) {
-  constexpr int LPR = D / 4, RPB = 256 / LPR, NP = 4, ROWS = RPB * PASS;
+  constexpr int LPR = D / 4, RPB = 256 / LPR, NP = 4;
   struct Row {
     int64_t lse;  // where its lse goes; < 0: no such row
     TreeParts a, b;
     float l;      // NaN: a node of a bad sequence
   };
-  __shared__ Row s_row[ROWS];
-  const int64_t row0 = (int64_t)blockIdx.x * ROWS, rows = (int64_t)sh.n * sh.nodes * sh.hq;
-  if (threadIdx.x < ROWS) {
+  __shared__ Row s_row[RPB];
+  const int64_t row0 = (int64_t)blockIdx.x * RPB, rows = (int64_t)sh.n * sh.nodes * sh.hq;
+  if (threadIdx.x < RPB) {
     Row x;
     x.lse = -1;
     x.l = 0.f;
@@ -679,41 +680,38 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeShape sh, TreePar
   }
   __syncthreads();
   const int col = (threadIdx.x % LPR) * 4;
-#pragma unroll 1
-  for (int pass = 0; pass < PASS; ++pass) {
-    const int at = pass * RPB + threadIdx.x / LPR;
-    const Row& x = s_row[at];
-    if (x.lse < 0) return;
-    const TreeParts a = x.a, b = x.b;
-    f32x4 acc = f32x4{};
-    float m = kNegInf, l = x.l;
-    const int64_t parts = a.n + b.n;
-    for (int64_t n0 = 0; n0 < parts; n0 += NP) {
-      f32x4 y[NP];
-      float pm[NP], pl[NP];
+  const int at = threadIdx.x / LPR;
+  const Row& x = s_row[at];
+  if (x.lse < 0) return;
+  const TreeParts a = x.a, b = x.b;
+  f32x4 acc = f32x4{};
+  float m = kNegInf, l = x.l;
+  const int64_t parts = a.n + b.n;
+  for (int64_t n0 = 0; n0 < parts; n0 += NP) {
+    f32x4 y[NP];
+    float pm[NP], pl[NP];
 #pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        const int64_t k = n0 + n < parts ? n0 + n : 0;
-        const int64_t r = k < a.n ? a.row + k * a.stride : b.row + (k - a.n) * b.stride;
-        y[n] = *reinterpret_cast<const f32x4*>(p.part + r * D + col);
-        pm[n] = p.part_ml[2 * r];
-        pl[n] = n0 + n < parts ? p.part_ml[2 * r + 1] : 0.f;
-      }
-#pragma unroll
-      for (int n = 0; n < NP; ++n) {
-        if (pl[n] == 0.f) continue;  // a part without a visible key
-        const float mn = fmaxf(m, pm[n]);
-        const float c = m == kNegInf ? 0.f : fast_exp2(m - mn), d = fast_exp2(pm[n] - mn);
-        l = l * c + pl[n] * d;
-        acc = acc * c + y[n] * d;
-        m = mn;
-      }
+    for (int n = 0; n < NP; ++n) {
+      const int64_t k = n0 + n < parts ? n0 + n : 0;
+      const int64_t r = k < a.n ? a.row + k * a.stride : b.row + (k - a.n) * b.stride;
+      y[n] = *reinterpret_cast<const f32x4*>(p.part + r * D + col);
+      pm[n] = p.part_ml[2 * r];
+      pl[n] = n0 + n < parts ? p.part_ml[2 * r + 1] : 0.f;
     }
-    const bool some = l != 0.f;  // NaN: so is the row
-    const float inv = some ? 1.f / l : 0.f;
-    store4<T>(p.o + (row0 + at) * D + col, some ? acc * inv : f32x4{});
-    if (col == 0) p.lse[x.lse] = some ? (m + __log2f(l)) * (1.0f / kLog2e) : 0.f;
+#pragma unroll
+    for (int n = 0; n < NP; ++n) {
+      if (pl[n] == 0.f) continue;  // a part without a visible key
+      const float mn = fmaxf(m, pm[n]);
+      const float c = m == kNegInf ? 0.f : fast_exp2(m - mn), d = fast_exp2(pm[n] - mn);
+      l = l * c + pl[n] * d;
+      acc = acc * c + y[n] * d;
+      m = mn;
+    }
   }
+  const bool some = l != 0.f;  // NaN: so is the row
+  const float inv = some ? 1.f / l : 0.f;
+  store4<T>(p.o + (row0 + at) * D + col, some ? acc * inv : f32x4{});
+  if (col == 0) p.lse[x.lse] = some ? (m + __log2f(l)) * (1.0f / kLog2e) : 0.f;
 }
 
 template <int D, typename T>
@@ -746,12 +744,9 @@ hipError_t launch_tree_t(const CacheView& c, const TreeLaunch& a, hipStream_t s)
     if (e != hipSuccess) return e;
   }
   TimingScope t("pp_tree_attn_combine", s);
-  // four passes where that still leaves the compute units some workgroups each
   constexpr int RPB = 256 / (D / 4);
   const int64_t rows = (int64_t)sh.n * sh.nodes * sh.hq;
-  auto grid = [&](int pass) { return dim3((unsigned)((rows + RPB * pass - 1) / (RPB * pass))); };
-  if (rows >= 4 * RPB * 4 * kCus) hipLaunchKernelGGL((tree_combine_kernel<D, T, 4>), grid(4), dim3(256), 0, s, sh, p);
-  else hipLaunchKernelGGL((tree_combine_kernel<D, T, 1>), grid(1), dim3(256), 0, s, sh, p);
+  hipLaunchKernelGGL((tree_combine_kernel<D, T>), dim3((unsigned)((rows + RPB - 1) / RPB)), dim3(256), 0, s, sh, p);
   return hipGetLastError();
 }
 
