@@ -583,7 +583,7 @@ pp_status pp_cache_compact(const pp_cache* cache, pp_dtype dtype, int layers, in
 pp_status pp_cache_shared(const pp_cache* cache, int n, const int32_t* slots, int group, int32_t* shared, void* hip_stream);
 
 /* Writes one layer's keys and values of new tokens behind the sequences' cached ones:
- * token j < count[i] (dev; NULL: max_new) of slots[i] at place seq_len + j, which has to
+ * token j < count[i] (dev; NULL: max_new, at most 2^24) of slots[i] at place seq_len + j, which has to
  * have been reserved (a token without a page is not written); seq_len stays.
  * Its row in k, v (dev [rows, hkv, head_dim]) and q is start[i] + j (dev; a packed
  * batch's row_start, say), or i * max_new + j without start.
@@ -622,7 +622,8 @@ pp_status pp_cache_accept(const pp_cache* cache, int n, const int32_t* slots, in
  * sequence).  A sequence that names no slot, or whose nodes have not all been reserved,
  * and a node with a parent that is no earlier one, come out as NaN.
  * planned != 0: ws holds the plan of an earlier call with the same cache state and
- * arguments but q, the pools and the results, as for every layer after a step's first.
+ * arguments but q, the pools and the results, as for every layer after a step's first;
+ * with a plan of other sizes, or none, the results are NaN.
  * ws_bytes >= pp_tree_workspace_size's bytes. */
 pp_status pp_tree_workspace_size(const pp_cache* cache, int n, int group, int max_new, pp_dtype dtype, int hq, int hkv, int head_dim,
                                  size_t* bytes);
@@ -638,7 +639,7 @@ pp_status pp_tree_attn_fwd(const pp_cache* cache, int n, const int32_t* slots, i
  * the attention; a node without a parent is never reached).  target (dev [n, max_new,
  * vocab], dtype) are the model's logits at the nodes, p = softmax(target / T), draft (dev,
  * same shape) the drafter's from which the children of a node were drawn, q; T =
- * temperature[i] (dev; NULL: 1).
+ * temperature[i] (dev; NULL: 1; taken as at most 10^6).
  * From node 0 on, a node's children y are tried in order, at most max_children of them:
  *   w = p, Z = 1, a = 0 at first;  y follows if u[i][y's node] q(y) Z < w(y), else
  *   a += Z, w = max(p - a q, 0), Z = sum w
@@ -655,7 +656,8 @@ pp_status pp_tree_attn_fwd(const pp_cache* cache, int n, const int32_t* slots, i
  *   out_tokens dev int32 [n, max_new]: out_count new tokens, the last of them sampled, then -1
  *   out_logp   dev float [n, max_new]: their ln p (at T = 1 where T is not above 0),
  *              pp_policy_loss's logp_old; then 0
- * Probabilities and sums are 64 bits.  max_new <= 64, n * max_new <= 65535. */
+ * Probabilities and sums are 64 bits, exponentials good to 10^-14, those below 2^-999 are
+ * 0.  max_new <= 64, n * max_new <= 65535. */
 pp_status pp_verify_workspace_size(int n, int max_new, int vocab, pp_dtype dtype, size_t* bytes);
 pp_status pp_verify_draft(int n, int max_new, int vocab, pp_dtype dtype, int max_children, const int32_t* count,
                           const int32_t* parents, const int32_t* tokens, const void* target, const void* draft,

@@ -196,12 +196,12 @@ def tree_attn(book, layer, slots, q, parents=None, count=None, scale=None):
     return o, lse, size, score
 
 
-def _softmax(x, lowest):
-    """Probabilities of a row of logits, masked entries 0; None if it cannot be used."""
+def _softmax(x, lowest, T=1.0):
+    """Probabilities of a row of logits at temperature T, masked entries 0; None if it cannot be used."""
     x = np.where(x <= lowest, -np.inf, x)
     if np.isnan(x).any() or (x == np.inf).any() or not (x > -np.inf).any():
         return None
-    e = np.exp(x - x.max())
+    e = np.exp((x - x.max()) / T)
     return e / e.sum()
 
 
@@ -221,7 +221,7 @@ def verify(target, tokens, u, draft=None, parents=None, count=None, temperature=
         with np.errstate(invalid="ignore", over="ignore"):
             while True:
                 row = target[i, at].astype(np.float64)
-                p = _softmax(row if greedy else np.where(row <= lowest, -np.inf, row / T), lowest)
+                p = _softmax(row, lowest, 1.0 if greedy else T)
                 r = None if p is None else p.copy()
                 q = None
                 if p is not None and greedy:
@@ -229,8 +229,7 @@ def verify(target, tokens, u, draft=None, parents=None, count=None, temperature=
                     r[int(np.argmax(np.where(np.isnan(row) | (row <= lowest), -np.inf, row)))] = 1.0
                 usable = p is not None
                 if usable and draft is not None and not greedy:
-                    drow = draft[i, at].astype(np.float64)
-                    q = _softmax(np.where(drow <= lowest, -np.inf, drow / T), lowest)
+                    q = _softmax(draft[i, at].astype(np.float64), lowest, T)
                     usable = q is not None
                 step, tried = None, 0
                 for j in range(1, c):

@@ -599,7 +599,7 @@ hipError_t launch_cache_fork(const CacheView& c, const CachePools& p, int n, con
     TimingScope t("pp_cache_fork_plan", s);
     hipLaunchKernelGGL(cache_fork_plan_kernel, dim3(1), dim3(kPlan), 0, s, c, n, src, dst, status, w.mark, w.first, w.list, entries);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (e != hipSuccess || n == 0) return e;
   }
   TimingScope t("pp_cache_fork", s);
   hipLaunchKernelGGL(cache_fork_kernel, dim3(n, 1 + 2 * p.layers, p.layers ? p.hkv : 1), dim3(256), 0, s, c, p, entries);
@@ -634,7 +634,7 @@ hipError_t launch_cache_accept(const CacheView& c, const CachePools& p, int n, c
     hipLaunchKernelGGL(cache_accept_plan_kernel, dim3(1), dim3(kPlan), 0, s, c, n, slots, max_new, count, path, status, w.mark,
                        entries);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !path || p.layers == 0) return e;
+    if (e != hipSuccess || n == 0 || !path || p.layers == 0) return e;
   }
   TimingScope t("pp_cache_accept", s);
   hipLaunchKernelGGL(cache_accept_kernel, dim3(n, p.hkv, 2 * p.layers), dim3(256), 0, s, c, p, entries, max_new, path);

@@ -258,18 +258,23 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
   out.arg = 0x7fffffff;
   out.max = bad ? __builtin_nanf("") : top > lowest<T>() ? top : kNegInf;
   if (top > lowest<T>() && !bad) {
-    const double b = -(double)top * a;
     double sum = 0;
-    auto add_all = [&](auto clamp) {
+    // (x - top) a, as one operation where the rounding of top a is below 2^-45
+    const double b = -(double)top * a;
+    auto add_all = [&](auto careful) {
 #pragma unroll
       for (int u = 0; u < L; ++u) {
         asm volatile("" : "+v"(x[u]));
 #pragma unroll
-        for (int i = 0; i < kVec<T>; ++i) sum += exp2_neg<clamp.value>(fma((double)to_float(x[u][i]), a, b));
+          for (int i = 0; i < kVec<T>; ++i) {
+          const double y = (double)to_float(x[u][i]);
+          if constexpr (careful.value) sum += exp2_neg<true>((y - (double)top) * a);
+          else sum += exp2_neg<false>(fma(y, a, b));
+        }
       }
     };
     const double low = fma(-(double)float_of_bits<T>(most), a, b);  // no exponent is below
-    if (__any(!(low > kTiny))) add_all(std::true_type{});
+    if (__any(!(low > kTiny)) || !(fabs(b) < 256.0)) add_all(std::true_type{});
     else add_all(std::false_type{});
     out.sum = wave_sum_d(sum);
     if (argmax) {
@@ -286,16 +291,16 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
   if (lane == 0) p.part[((int64_t)blockIdx.z * d.n * d.nodes + row) * d.chunks + chunk] = out;
 }
 
-// A row's distribution, 2^(a x + b) / sum, a = log2(e) / T.
+// A row's distribution, 2^(a (x - max)) / sum, a = log2(e) / T.
 struct RowDist {
-  double a, b, sum;
+  double a, sum;
   float max;
   int arg;
   bool usable;
   // e^((x - max) / T); 0 where masked (or below 2^-999)
   __device__ __forceinline__ double raw(float x) const {
-    const double t = fma((double)x, a, b);
-    return t > kTiny + 1 ? exp2_neg(t) : 0.0;
+    const double t = ((double)x - (double)max) * a;
+    return t > kTiny + 1 ? exp2_neg<false>(t) : 0.0;
   }
 };
 __device__ __forceinline__ RowDist row_dist(const DraftRow& x, double it) {
@@ -305,7 +310,6 @@ __device__ __forceinline__ RowDist row_dist(const DraftRow& x, double it) {
   r.arg = x.arg;
   r.usable = x.arg >= 0;
   r.a = it;
-  r.b = -(double)x.max * it;
   return r;
 }
 // The parts of a row's first 128 chunks, two a lane.
@@ -332,7 +336,6 @@ __device__ __forceinline__ RowDist row_dist(const RowParts& first, const DraftPa
   r.max = wave_max(m);
   r.usable = !__any(bad) && r.max > kNegInf;
   r.a = it;
-  r.b = -(double)r.max * it;
   r.sum = 0;
   r.arg = 0x7fffffff;
   if (!r.usable) return r;
@@ -654,7 +657,7 @@ __device__ __forceinline__ Picked pick_entry(const DraftParams& p, int64_t row, 
   out.mine = lane == max(last, 0);
   if (lane == last) {
     out.y = y;
-    out.logp = fma((double)x, tp.a, tp.b) * 0.6931471805599453 - log(tp.sum);
+    out.logp = ((double)x - (double)tp.max) * tp.a * 0.6931471805599453 - log(tp.sum);
   }
   return out;
 }

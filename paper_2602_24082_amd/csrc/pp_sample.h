@@ -138,11 +138,12 @@ struct TreeShape {
   int hq, hkv, G;
   TreeKind kind[2];  // shared, own
   int workers[2];    // solo waves, teams
+  uint64_t key;      // of calls that can go by one plan
 };
 struct TreePlan {
   TreeItem* items;         // [n + groups]
   int32_t* nodes;          // [n * max_new]: a group's nodes in use, the rows of its shared keys
-  int64_t* head;           // [2][2]: units in all, units a worker
+  int64_t* head;           // [2][2]: units in all, units a worker; then the key
   int32_t* start_item[2];  // [workers]: where a worker starts
 };
 struct TreeLaunch {

@@ -59,6 +59,7 @@ pp_status check_cache(const pp_cache* c, CacheView* v) {
 }
 
 constexpr int kMostSeqs = 65535;  // a launch's second dimension
+constexpr int kMostNew = 1 << 24;  // tokens a sequence and call: a launch's first, in threads
 
 pp_status check_n(int n) {
   if (n < 0) return report_error(PP_ERR_INVALID_ARGUMENT, "n must be >= 0 (got %d)", n);
@@ -184,13 +185,23 @@ size_t carve_tree(const TreeShape& t, int d, void* ws, TreeLaunch* a) {
   const int items = t.n + t.groups;
   a->plan.items = at.take<TreeItem>(items);
   a->plan.nodes = at.take<int32_t>((int64_t)t.n * t.nodes);
-  a->plan.head = at.take<int64_t>(4);
+  a->plan.head = at.take<int64_t>(5);
   for (int c = 0; c < 2; ++c) a->plan.start_item[c] = at.take<int32_t>(t.workers[c]);
   const TreeKind& last = t.kind[1];
   const int64_t parts = last.part0 + ((int64_t)t.n * last.tiles * t.hkv + t.workers[last.team]) * last.part_rows;
   a->part_ml = at.take<float>(2 * parts);
   a->part = at.take<float>(parts * d);
   return at.used;
+}
+
+// Names the calls that can go by a plan: those of its sizes.
+uint64_t key_of(const TreeShape& t, const CacheView& c, int d, int dtype) {
+  uint64_t k = 0x9e3779b97f4a7c15ull;
+  for (const int x : {t.n, t.nodes, t.group, t.hq, t.hkv, t.kind[0].tiles, d, dtype, c.num_slots, c.max_pages, c.num_pages, c.page_size}) {
+    k = (k ^ (uint32_t)x) * 0xd6e8feb86659fd93ull;
+    k ^= k >> 32;
+  }
+  return k;
 }
 
 pp_status check_tree(int n, int group, int nodes, pp_dtype dtype, int hq, int hkv, int d) {
@@ -341,6 +352,8 @@ pp_status pp_cache_append(const pp_cache* cache, int n, const int32_t* slots, in
   if ((st = check_n(n)) != PP_OK) return st;
   if ((st = check_pools(c, dtype, 1, hkv, head_dim, k_pages, v_pages, &p)) != PP_OK) return st;
   if (max_new < 1) return report_error(PP_ERR_INVALID_ARGUMENT, "max_new must be >= 1");
+  if (max_new > kMostNew)
+    return report_error(PP_ERR_UNSUPPORTED, "a call appends at most %d tokens to a sequence (got %d)", kMostNew, max_new);
   if (q && (hq < 1 || hq % hkv || hq > 4096))
     return report_error(PP_ERR_INVALID_ARGUMENT, "hq (%d) must be a multiple of hkv (%d), at most 4096", hq, hkv);
   if (!q != !q_rot) return report_error(PP_ERR_INVALID_ARGUMENT, "q and q_rot must be given together");
@@ -424,6 +437,7 @@ pp_status pp_tree_attn_fwd(const pp_cache* cache, int n, const int32_t* slots, i
   a.scale = scale > 0.f ? scale : 1.0f / std::sqrt((float)head_dim);
   a.head_dim = head_dim;
   a.dtype = dtype == PP_BF16 ? kBF16 : kFP32;
+  a.shape.key = key_of(a.shape, c, head_dim, a.dtype);
   return launched(launch_tree_attn(c, a, (hipStream_t)hip_stream), "tree attention launch");
 }
 

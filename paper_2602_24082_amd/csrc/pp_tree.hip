@@ -208,6 +208,7 @@ __global__ __launch_bounds__(kPlan) void tree_plan_kernel(CacheView c, TreeShape
     __syncthreads();
     const int64_t run = max((int64_t)1, (total + t.workers[cls] - 1) / t.workers[cls]);
     if (tid == 0) {
+      out.head[4] = (int64_t)t.key;
       out.head[2 * cls] = total;
       out.head[2 * cls + 1] = run;
     }
@@ -261,6 +262,11 @@ __device__ __forceinline__ uint64_t tree_paths(const int32_t* parents, int nodes
   }
   fine = ok != 0;
   return m;
+}
+
+// Units in all that workers of a class take; none where ws holds no plan for this call.
+__device__ __forceinline__ int64_t tree_units(const TreeShape& sh, const TreePlan& plan, int cls) {
+  return (uint64_t)plan.head[4] == sh.key ? plan.head[2 * cls] : 0;
 }
 
 // A worker's run of units of one item, tile and head.
@@ -422,7 +428,7 @@ __global__ __launch_bounds__(64, 2) void tree_solo_kernel(CacheView c, TreeShape
   __shared__ __attribute__((aligned(1024))) TreeRing<T, 2, kSoloKeys * D> smem;
   auto* ring = in_lds(&smem);
   const int worker = blockIdx.x, lane = threadIdx.x & 63, ln = lane & 31, hf = lane >> 5;
-  const int64_t total = p.plan.head[0], run_len = p.plan.head[1];
+  const int64_t total = tree_units(sh, p.plan, 0), run_len = p.plan.head[1];
   int64_t pos = worker * run_len;
   const int64_t end = min(pos + run_len, total);
   if (pos >= end) return;
@@ -539,7 +545,7 @@ __global__ __launch_bounds__(kTeamWaves * 64, (kTreeTeam<D, T>)) void tree_team_
   auto* ring = in_lds(&smem);
   const int worker = blockIdx.x, tid = threadIdx.x, lane = tid & 63, ln = lane & 31, hf = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int64_t total = p.plan.head[2], run_len = p.plan.head[3];
+  const int64_t total = tree_units(sh, p.plan, 1), run_len = p.plan.head[3];
   int64_t pos = worker * run_len;
   const int64_t end = min(pos + run_len, total);
   if (pos >= end) return;
@@ -669,7 +675,9 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeShape sh, TreePar
       const TreeItem mine = p.plan.items[seq + grp + 1], all = p.plan.items[grp * (sh.group + 1)];
       const int64_t run_all = p.plan.head[2 * sh.kind[0].team + 1], run_own = p.plan.head[2 * sh.kind[1].team + 1];
       x.lse = (int64_t)head * sh.n * sh.nodes + tok;
-      if (node * sh.G < mine.rows) {
+      if ((uint64_t)p.plan.head[4] != sh.key) {
+        x.l = __builtin_nanf("");
+      } else if (node * sh.G < mine.rows) {
         if (all.blocks) x.a = tree_parts(sh, run_all, 0, all, grp, g, (mine.row0 + node) * sh.G + h);
         x.b = tree_parts(sh, run_own, 1, mine, seq, g, node * sh.G + h);
       } else if (node < mine.bad) {

@@ -293,6 +293,21 @@ def test_unsound_lengths_are_refused():
     same(c, kp, vp, b)
 
 
+def test_no_entries():
+    """Calls of no sequences: the statuses say so and nothing changes."""
+    c, kp, vp = _append_case(torch.bfloat16, 16, 2, 64)
+    b, none = book_of(c, kp, vp), ints([])
+    assert pp.pp_cache_reserve(c, none, none).tolist() == [0, 0]
+    assert pp.pp_cache_fork(c, none, none, kp, vp).tolist() == [0, 0]
+    assert pp.pp_cache_accept(c, none, none).tolist() == [0, 0]
+    assert pp.pp_cache_accept(c, none, none, ints(np.zeros((0, 4))), kp, vp).tolist() == [0, 0]
+    pp.pp_cache_free(c, none)
+    x = torch.ones(0, 4, 2, 64, dtype=torch.bfloat16, device=DEV)
+    pp.pp_cache_append(c, none, x, x, kp[0], vp[0])
+    assert pp.pp_cache_shared(c, none, 3).tolist() == []
+    same(c, kp, vp, b)
+
+
 def test_binding_refuses():
     c, kp, vp = _append_case(torch.bfloat16, 16, 2, 64)
     x = torch.ones(1, 3, 2, 64, dtype=torch.bfloat16, device=DEV)

@@ -135,6 +135,17 @@ def test_masks_and_rows_that_cannot_be_used(dtype):
         check(target, tokens, u, None, temperature=temp)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("offset", [0.0, 300.0])
+def test_hot_and_cold(dtype, offset):
+    """Temperatures from the smallest number to the largest that is told apart, also far from zero."""
+    temps = [1e-45, 1e-38, 1e-20, 1e-9, 1e-6, 1e-4, 1e-3, 0.01, 0.1, 10.0, 1e3, 1e5, 1e6]
+    target, tokens, u, draft, parents = case(len(temps), 4, 5000, dtype, 41, near=0.3)
+    target, draft = ((x.float() + offset).to(dtype) for x in (target, draft))
+    check(target, tokens, u, draft, parents, temperature=temps, max_children=2)
+    check(target, tokens, u, None, parents, temperature=temps, max_children=2)
+
+
 def test_greedy_takes_the_first_largest():
     target, tokens, u, draft, _ = case(6, 4, 20000, torch.bfloat16, 31, width=1)
     for i in range(6):

@@ -240,6 +240,22 @@ def test_planned_calls_and_streams():
         pp.pp_tree_attn_fwd(a.cache, slots, q, k, v, planned=True, **kw)
 
 
+def test_a_plan_of_another_call_is_refused():
+    """planned with a workspace that holds no plan, or one of other sizes: NaN, and nothing is read by it."""
+    a = Case(torch.bfloat16, 4, 2, 64, 16, [100, 7, 64, 65], nodes=3, seed=10)
+    b = Case(torch.bfloat16, 4, 2, 64, 16, [5, 9], nodes=2, seed=11)
+    size = max(pp.pp_tree_workspace_size(a.cache, 4, 1, 3, 4, 2, 64), pp.pp_tree_workspace_size(b.cache, 2, 1, 2, 4, 2, 64))
+    ws = torch.zeros(size, dtype=torch.uint8, device=DEV)
+    run = lambda x, planned: pp.pp_tree_attn_fwd(x.cache, ints(x.slots), x.q.to(DEV), x.k.to(DEV), x.v.to(DEV), parents=ints(x.parents),
+                                                 count=ints(x.count), planned=planned, ws=ws)
+    for planned in (lambda: None, lambda: run(b, False)):
+        planned()
+        o, lse = run(a, True)
+        assert torch.isnan(o).all() and torch.isnan(lse).all()
+    want = run(a, False)
+    assert all(torch.equal(x, y) for x, y in zip(want, run(a, True))) and not torch.isnan(want[0]).any()
+
+
 def test_a_pool_past_2_31_elements():
     """Pages whose rows lie past 2^31 elements of the pool."""
     pages, hkv, ps, d = 70000, 2, 256, 64

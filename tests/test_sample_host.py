@@ -160,6 +160,7 @@ def test_cache_call_refusals():
     assert app(qr=None) == 1 and app(k=None) == 1 and app(k=OFF4) == 1 and app(kp=None) == 1 and app(s=None) == 1
     assert app(base=-1.0) == 1 and app(base=float("inf")) == 1 and app(base=float("nan")) == 1 and app(dt=7) == 1
     assert app(d=80) == 3 and app(N=65, rows=200, par=OK) == 3
+    assert app(N=2**31 - 1, rows=4, start=OK) == 3 and app(N=2**24 + 1, rows=4, start=OK) == 3
 
 
 def test_tree_and_verify_refusals():
