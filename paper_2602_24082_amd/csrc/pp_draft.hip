@@ -226,7 +226,7 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
   const bool is_draft = blockIdx.z != 0, argmax = greedy(p.temperature, s);
   const int n = max(0, min(p.count ? p.count[s] : d.nodes, d.nodes));
   const double a = inv_temp(p.temperature, s);
-  if (node == 0 && chunk == 0 && !is_draft && lane == 0) p.arrived[s] = 0;
+  if (node == 0 && chunk == 0 && !is_draft && lane == 0) p.arrived[s * kOwnLine] = 0;
   if (node >= n) return;
   if (is_draft) {
     if (argmax) return;
@@ -768,7 +768,7 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
       // would write back the whole L2
       __hip_atomic_store(p.ends + (int64_t)s * d.chunks + chunk, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      s_last = __hip_atomic_fetch_add(p.arrived + s, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == d.chunks - 1;
+      s_last = __hip_atomic_fetch_add(p.arrived + s * kOwnLine, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == d.chunks - 1;
     }
     __syncthreads();
     if (!s_last) return;

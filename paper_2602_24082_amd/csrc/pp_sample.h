@@ -167,6 +167,7 @@ struct TreeLaunch {
 hipError_t launch_tree_attn(const CacheView& c, const TreeLaunch& a, hipStream_t s);
 
 // Draft verification (pp_draft.hip).
+constexpr int kOwnLine = 32;       // int32 counters of different sequences are a line of 128 bytes apart
 constexpr int kDraftChunk = 2048;  // entries of a row that are looked at together
 struct DraftShape {
   int n, nodes, vocab, chunks, max_children;
@@ -208,7 +209,7 @@ struct DraftParams {
   DraftRow* row;    // [2, n, nodes]: the target's, the draft's (of nodes with children)
   DraftEdge* edge;  // [n, nodes]
   double* ends;     // [n, chunks]: Z where the walk ends
-  int32_t* arrived; // [n]: workgroups that have left theirs
+  int32_t* arrived; // [n * kOwnLine]: workgroups that have left theirs
 };
 hipError_t launch_verify_draft(const DraftParams& p, int dtype, hipStream_t s);
 

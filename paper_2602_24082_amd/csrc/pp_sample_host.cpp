@@ -226,7 +226,7 @@ size_t carve_draft(DraftParams* p, void* ws) {
   p->ends = at.take<double>((int64_t)d.n * d.chunks);
   p->row = at.take<DraftRow>(2 * rows);
   p->edge = at.take<DraftEdge>(rows);
-  p->arrived = at.take<int32_t>(d.n);
+  p->arrived = at.take<int32_t>((int64_t)d.n * kOwnLine);
   return at.used;
 }
 
