@@ -197,11 +197,13 @@ def tree_attn(book, layer, slots, q, parents=None, count=None, scale=None):
 
 
 def _softmax(x, lowest, T=1.0):
-    """Probabilities of a row of logits at temperature T, masked entries 0; None if it cannot be used."""
+    """Probabilities of a row of logits at temperature T, masked entries and those below 2^-999 of the largest 0; None if it
+    cannot be used."""
     x = np.where(x <= lowest, -np.inf, x)
     if np.isnan(x).any() or (x == np.inf).any() or not (x > -np.inf).any():
         return None
     e = np.exp((x - x.max()) / T)
+    e[e <= 2.0 ** -999] = 0.0
     return e / e.sum()
 
 

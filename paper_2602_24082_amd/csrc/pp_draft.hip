@@ -56,8 +56,6 @@ template <>
 __device__ __forceinline__ float lowest<float>() {
   return -3.4028234663852886e38f;
 }
-template <typename T>
-constexpr uint32_t kInfBits = sizeof(T) == 2 ? 0x7f80u : 0x7f800000u;
 
 // 2^(i / 64), in LDS: entries are two banks each, so that a wave's lanes meet at most twice.
 // Their upper words are lower by i << 14: k << 14 on top makes entry k & 63 2^(k / 64).
@@ -76,12 +74,12 @@ __device__ __forceinline__ void fill_roots() {
 // 2^t for t <= 0 in 64 bits: with k the whole number next to 64 t and f = t - k / 64,
 // |f| <= 1/128, 2^(k / 64) from the table, 2^f by the polynomial of degree 4 through 1 at 0 and
 // Chebyshev's points, good to 5e-15 of it.  k comes out of the low bits of t + 1.5 2^46.  Below
-// 2^-1000, and for -inf and NaN, 2^-1000; without CLAMP t has to be above.
+// 2^-1000, and for -inf, 2^-1000; without CLAMP t has to be above.  NaN stays.
 constexpr double kTiny = -1000.0;
 template <bool CLAMP = true>
 __device__ __forceinline__ double exp2_neg(double t) {
   constexpr double shift = 1.5 * (1ull << 46);
-  if (CLAMP) t = fmax(t, kTiny);
+  if (CLAMP && t < kTiny) t = kTiny;
   const double u = t + shift;
   const int k = __double2loint(u);
   const double base = exp2_roots()[k & (kRoots - 1)];
@@ -105,15 +103,21 @@ struct ChunkOf {
   using Raw = RawOf<T>;
   const T* row;
   int64_t first;  // entry of the thread's first load
-  int vocab;
+  int vocab, ahead;  // ahead: of the row, from a 16-byte boundary on
 
   __device__ __forceinline__ void init(const T* r, int v, int chunk, int thread) {
     row = r;
     vocab = v;
-    const int ahead = (int)((reinterpret_cast<uintptr_t>(r) / sizeof(T)) % kVec<T>);
+    ahead = (int)((reinterpret_cast<uintptr_t>(r) / sizeof(T)) % kVec<T>);
     first = (int64_t)chunk * kDraftChunk + thread * kVec<T> - ahead;
   }
   __device__ __forceinline__ int64_t at(int u) const { return first + u * (THREADS * kVec<T>); }
+  // the whole chunk lies in the row
+  __device__ __forceinline__ bool inside(int chunk) const {
+    const int64_t e = (int64_t)chunk * kDraftChunk - ahead;
+    return e >= 0 && e + kDraftChunk <= vocab;
+  }
+  __device__ __forceinline__ Raw load_inside(int u) const { return *reinterpret_cast<const Raw*>(row + at(u)); }
   __device__ __forceinline__ Raw load(int u) const {
     const int64_t e = at(u);
     if (e >= 0 && e + kVec<T> <= vocab) return *reinterpret_cast<const Raw*>(row + e);
@@ -123,34 +127,6 @@ struct ChunkOf {
     for (int i = 0; i < kVec<T>; ++i) x[i] = e + i >= 0 && e + i < vocab ? row[e + i] : none;
     return x;
   }
-};
-
-// The largest of the entries' bits without their signs: NaN and infinities lie at the top.
-__device__ __forceinline__ void track_bits(RawOf<uint16_t>& most, const RawOf<uint16_t>& x) {
-  most = __builtin_elementwise_max(most, x & (uint16_t)0x7fff);
-}
-__device__ __forceinline__ void track_bits(uint32_t& most, const RawOf<float>& x) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
-}
-__device__ __forceinline__ uint32_t most_bits(const RawOf<uint16_t>& m) {
-  uint32_t r = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) r = max(r, (uint32_t)m[i]);
-  return r;
-}
-__device__ __forceinline__ uint32_t most_bits(uint32_t m) { return m; }
-template <typename T>
-__device__ __forceinline__ float float_of_bits(uint32_t b) {
-  return __uint_as_float(sizeof(T) == 2 ? b << 16 : b);
-}
-template <typename T>
-struct BitsOf {
-  using Type = uint32_t;
-};
-template <>
-struct BitsOf<uint16_t> {
-  using Type = RawOf<uint16_t>;
 };
 
 __device__ __forceinline__ double lane_d(double x, int lane) {
@@ -238,57 +214,68 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
   ChunkOf<T, 64> c;
   c.init((const T*)(is_draft ? p.draft : p.target) + (int64_t)row * d.vocab, d.vocab, min(chunk, d.chunks - 1), lane);
   RawOf<T> x[L];
+  if (c.inside(chunk)) {
 #pragma unroll
-  for (int u = 0; u < L; ++u) x[u] = c.load(u);
+    for (int u = 0; u < L; ++u) x[u] = c.load_inside(u);
+  } else {
+#pragma unroll
+    for (int u = 0; u < L; ++u) x[u] = c.load(u);
+  }
   fill_roots();
   if (chunk >= d.chunks) return;
-  float m = kNegInf;
-  typename BitsOf<T>::Type bits{};
+  float m = kNegInf, low = -kNegInf;
 #pragma unroll
-  for (int u = 0; u < L; ++u) {
-    track_bits(bits, x[u]);
+  for (int u = 0; u < L; ++u)
 #pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) m = fmaxf(m, to_float(x[u][i]));
-  }
+    for (int i = 0; i < kVec<T>; ++i) {
+      const float y = to_float(x[u][i]);
+      m = fmaxf(m, y);
+      low = fminf(low, y);
+    }
   const float top = wave_max(m);
-  const uint32_t most = most_bits(bits);
-  const bool bad = __any(most > kInfBits<T>) || top == -kNegInf;
-  DraftPart out;
-  out.sum = 0;
-  out.arg = 0x7fffffff;
-  out.max = bad ? __builtin_nanf("") : top > lowest<T>() ? top : kNegInf;
+  bool bad = top == -kNegInf;  // or a NaN among them
+  double sum = 0;
+  int arg = 0x7fffffff;
   if (top > lowest<T>() && !bad) {
-    double sum = 0;
     // (x - top) a, as one operation where the rounding of top a is below 2^-45
     const double b = -(double)top * a;
     auto add_all = [&](auto careful) {
 #pragma unroll
       for (int u = 0; u < L; ++u) {
-        asm volatile("" : "+v"(x[u]));
+        asm volatile("" : "+v"(x[u]));  // (else both loops' numbers are made ahead of them, in registers)
 #pragma unroll
-          for (int i = 0; i < kVec<T>; ++i) {
+        for (int i = 0; i < kVec<T>; ++i) {
           const double y = (double)to_float(x[u][i]);
           if constexpr (careful.value) sum += exp2_neg<true>((y - (double)top) * a);
           else sum += exp2_neg<false>(fma(y, a, b));
         }
       }
     };
-    const double low = fma(-(double)float_of_bits<T>(most), a, b);  // no exponent is below
-    if (__any(!(low > kTiny)) || !(fabs(b) < 256.0)) add_all(std::true_type{});
+    if (__any(!(fma((double)low, a, b) > kTiny)) || !(fabs(b) < 256.0)) add_all(std::true_type{});
     else add_all(std::false_type{});
-    out.sum = wave_sum_d(sum);
+    sum = wave_sum_d(sum);
+    bad = sum != sum;
     if (argmax) {
-      int arg = 0x7fffffff;
 #pragma unroll
       for (int u = 0; u < L; ++u)
 #pragma unroll
         for (int i = 0; i < kVec<T>; ++i)
           if (to_float(x[u][i]) == top) arg = min(arg, (int)(c.at(u) + i));
       for (int off = 32; off > 0; off >>= 1) arg = min(arg, __shfl_xor(arg, off, 64));
-      out.arg = arg;
     }
+  } else {
+#pragma unroll
+    for (int u = 0; u < L; ++u)
+#pragma unroll
+      for (int i = 0; i < kVec<T>; ++i) bad = bad || to_float(x[u][i]) != to_float(x[u][i]);
+    bad = __any(bad);
   }
-  if (lane == 0) p.part[((int64_t)blockIdx.z * d.n * d.nodes + row) * d.chunks + chunk] = out;
+  if (lane) return;
+  DraftPart out;
+  out.sum = sum;
+  out.arg = arg;
+  out.max = bad ? __builtin_nanf("") : top > lowest<T>() ? top : kNegInf;
+  p.part[((int64_t)blockIdx.z * d.n * d.nodes + row) * d.chunks + chunk] = out;
 }
 
 // A row's distribution, 2^(a (x - max)) / sum, a = log2(e) / T.

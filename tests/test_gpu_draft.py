@@ -136,6 +136,24 @@ def test_masks_and_rows_that_cannot_be_used(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+def test_nan_anywhere_in_a_row(dtype):
+    """A NaN beside ordinary logits, among masked ones, among logits far below the largest; also at low temperatures."""
+    target, tokens, u, draft, _ = case(10, 2, 9001, dtype, 27, width=1)
+    low = torch.finfo(dtype).min
+    for i, (node, at, around) in enumerate([(0, 0, None), (0, 9000, None), (0, 5000, -np.inf), (0, 5000, low), (1, 3000, -np.inf),
+                                            (0, 5000, float("nan")), (0, 5000, -3e4), (1, 8999, -3e4)]):
+        for x in (target, draft) if i % 2 else (target,):
+            if around is not None:
+                x[i, node, 2048 * (at // 2048):2048 * (at // 2048) + 2048] = around
+            x[i, node, at] = float("nan")
+    draft[8, 0, 77] = float("nan")
+    for temp in (None, [0.01] * 10, [0.0] * 10):
+        for d in (draft, None):
+            out = check(target, tokens, u, d, temperature=temp)
+    assert np.isnan(out[3]).any()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("offset", [0.0, 300.0])
 def test_hot_and_cold(dtype, offset):
     """Temperatures from the smallest number to the largest that is told apart, also far from zero."""
