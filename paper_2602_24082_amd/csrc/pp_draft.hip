@@ -781,17 +781,50 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
         off = e.p;
       }
     }
-    uint64_t takes = __ballot(off_at >= 0);
+    uint64_t takes = __ballot(off_at >= 0), firsts = 0;
+    auto part_share = [&](int c) { return part[c].max > kNegInf ? part[c].sum * tp.raw(part[c].max) / tp.sum : 0.0; };
+    // A chunk's share without them (the first such lane holds it) is its own less theirs; where that is all
+    // but nothing it is summed from the entries, since a rest of mere rounding would end the search in a
+    // chunk that has no entry left.
+    double rest = 0;
+    for (uint64_t todo = takes; todo;) {
+      const int j = __ffsll((unsigned long long)todo) - 1, c = __builtin_amdgcn_readlane(off_at, j);
+      const uint64_t same = __ballot(off_at == c);
+      todo &= ~same;
+      firsts |= 1ull << j;
+      const double whole = part_share(c);
+      double x = whole;
+      for (uint64_t m = same; m; m &= m - 1) x -= lane_d(off, __ffsll((unsigned long long)m) - 1);
+      if (x < whole * 0x1p-20) {
+        ChunkOf<T, 64> entries;
+        entries.init(target, d.vocab, c, lane);
+        const double ip = 1.0 / tp.sum;
+        x = 0;
+#pragma unroll 1
+        for (int u = 0; u < kLoads<T, 64>; ++u) {
+          const RawOf<T> v = entries.load(u);
+#pragma unroll
+          for (int i = 0; i < kVec<T>; ++i) {
+            bool is_gone = false;
+            for (uint64_t m = same; m; m &= m - 1)
+              is_gone = is_gone || entries.at(u) + i == __builtin_amdgcn_readlane(e.tok, __ffsll((unsigned long long)m) - 1);
+            if (!is_gone) x += tp.raw(to_float(v[i])) * ip;
+          }
+        }
+        x = wave_sum_d(x);
+      }
+      if (lane == j) rest = x;
+    }
     auto share = [&](int c) {  // of chunk c in what is left
       const bool is = c < d.chunks;
       if (residual) return is ? __hip_atomic_load(p.ends + (int64_t)s * d.chunks + c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0;
-      double x = is && part[c].max > kNegInf ? part[c].sum * tp.raw(part[c].max) / tp.sum : 0.0;
-      for (uint64_t m = takes; m; m &= m - 1) {  // (all lanes: they read each other's)
+      double x = is ? part_share(c) : 0.0;
+      for (uint64_t m = firsts; m; m &= m - 1) {  // (all lanes: they read each other's)
         const int j = __ffsll((unsigned long long)m) - 1;
-        const double less = lane_d(off, j);
-        if (__builtin_amdgcn_readlane(off_at, j) == c) x -= less;
+        const double left = lane_d(rest, j);
+        if (__builtin_amdgcn_readlane(off_at, j) == c) x = left;
       }
-      return fmax(x, 0.0);
+      return x;
     };
     auto whole_sum = [&]() {
       double x = 0;
@@ -801,7 +834,7 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
     double total = whole_sum();
     if (!(total > 0)) {  // nothing is left: from p itself
       residual = false;
-      takes = 0;
+      takes = firsts = 0;
       total = whole_sum();
     }
     const double want = (double)p.u[row0] * total;

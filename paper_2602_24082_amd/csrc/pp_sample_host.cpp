@@ -40,7 +40,8 @@ pp_status check_cache(const pp_cache* c, CacheView* v) {
   const int ps = c->page_size;
   if (ps < 16 || ps > 256 || (ps & (ps - 1)))
     return report_error(PP_ERR_UNSUPPORTED, "page_size %d not supported (16, 32, 64, 128 or 256)", ps);
-  if ((int64_t)c->max_pages * ps > INT32_MAX || (int64_t)c->num_pages * ps > INT32_MAX)
+  // places of tokens are counted in 32 bits, up to two blocks of keys past a sequence's last
+  if ((int64_t)c->max_pages * ps > INT32_MAX - 1024 || (int64_t)c->num_pages * ps > INT32_MAX)
     return report_error(PP_ERR_UNSUPPORTED, "a sequence or pool of 2^31 tokens or more is too large");
   if (!c->page_table || !c->seq_len || !c->held || !c->refs)
     return report_error(PP_ERR_INVALID_ARGUMENT, "page_table, seq_len, held and refs must be non-NULL");
@@ -59,6 +60,7 @@ pp_status check_cache(const pp_cache* c, CacheView* v) {
 }
 
 constexpr int kMostSeqs = 65535;  // a launch's second dimension
+constexpr int64_t kMostRows = 1 << 27;  // query rows of the attention: the join's launch has 32 threads a row at most
 constexpr int kMostNew = 1 << 24;  // tokens a sequence and call: a launch's first, in threads
 
 pp_status check_n(int n) {
@@ -156,6 +158,7 @@ bool shape_tree(int n, int group, int nodes, int hq, int hkv, pp_dtype dtype, in
   t->hkv = hkv;
   t->G = hq / hkv;
   const bool bf16 = dtype == PP_BF16;
+  if ((int64_t)n * nodes * hq >= kMostRows) return false;
   t->workers[0] = kCus * (bf16 ? (d == 128 ? kTreeSolo<128, uint16_t> : kTreeSolo<64, uint16_t>)
                                : (d == 128 ? kTreeSolo<128, float> : kTreeSolo<64, float>));
   t->workers[1] = kCus * (bf16 ? (d == 128 ? kTreeTeam<128, uint16_t> : kTreeTeam<64, uint16_t>)

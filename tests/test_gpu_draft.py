@@ -111,6 +111,26 @@ def test_the_same_token_twice_among_siblings(dtype):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("faint", [False, True])
+def test_given_drafts_that_are_all_of_a_stretch(dtype, faint):
+    """The rejected drafts hold all, or all but 10^-20, of the vocabulary's first entries: the smallest u still finds an entry
+    that is left, the faint one or else the first behind them."""
+    rng, n, V = np.random.default_rng(5), 96, 9000
+    target = torch.full((n, 4, V), -float("inf"), dtype=dtype)
+    target[:, :, 6000:6050] = torch.tensor(rng.normal(0, 1, (n, 4, 50)), dtype=dtype)
+    tokens = np.zeros((n, 4), int)
+    for i in range(n):
+        tokens[i, 1:] = rng.choice(np.arange(10, 1500), size=3, replace=False)
+        target[i, :, torch.tensor(tokens[i, 1:])] = torch.tensor(rng.normal(2.5, 1, 3), dtype=dtype)
+    if faint:
+        target[:, :, 1700] = -46.0
+    u = np.full((n, 4), 0.9995, np.float32)
+    u[:, 0] = 0
+    count, out, _, _ = check(target, tokens, u, None, [[-1, 0, 0, 0]] * n, max_children=3)
+    assert (count == 1).all() and (out[:, 0] == (1700 if faint else 6000)).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
 def test_masks_and_rows_that_cannot_be_used(dtype):
     target, tokens, u, draft, _ = case(14, 3, 9000, dtype, 21, width=1)
     low = torch.finfo(dtype).min

@@ -171,6 +171,7 @@ def test_tree_and_verify_refusals():
     assert tree(group=3) == 1 and tree(group=0) == 1 and tree(N=0) == 1 and tree(hq=3) == 1 and tree(hkv=0) == 1 and tree(dt=2) == 1
     assert tree(N=65) == 3 and tree(n=2050) == 3 and tree(d=256) == 3 and tree(hq=8192) == 3 and tree(b=64) == 4 and tree(ws=None) == 1
     assert tree(n=0) == 0
+    assert tree(n=2048, N=64, hq=1024, hkv=1) == 3 and tree(n=2048, N=64, hq=1023, hkv=1, b=64) == 4  # 2^27 rows
     assert L.pp_tree_workspace_size(_desc(), 4, 2, 3, 0, 4, 2, 64, ctypes.byref(n)) == 0 and n.value > 0
     assert L.pp_tree_workspace_size(_desc(), 4, 2, 3, 0, 4, 2, 64, None) == 1
     ver = lambda n=4, N=3, V=100, dt=0, kids=1, tok=OK, t=OK, dr=None, temp=None, u=OK, oc=OK, b=big: L.pp_verify_draft(
