@@ -311,7 +311,7 @@ struct RowParts {
   }
 };
 // By a wave, from the parts of the row's chunks.
-__device__ __forceinline__ RowDist row_dist(const RowParts& first, const DraftPart* part, int chunks, double it, int lane) {
+__device__ __forceinline__ RowDist row_dist(const RowParts& first, const DraftPart* part, int chunks, double it, bool argmax, int lane) {
   float m = fmaxf(first.a.max, first.b.max);
   bool bad = first.a.max != first.a.max || first.b.max != first.b.max;
   for (int c = lane + 128; c < chunks; c += 64) {
@@ -336,8 +336,11 @@ __device__ __forceinline__ RowDist row_dist(const RowParts& first, const DraftPa
   add(first.b);
   for (int c = lane + 128; c < chunks; c += 64) add(part[c]);
   r.sum = wave_sum_d(s);
-  for (int off = 32; off > 0; off >>= 1) arg = min(arg, __shfl_xor(arg, off, 64));
-  r.arg = arg;
+  r.arg = 0;
+  if (argmax) {
+    for (int off = 32; off > 0; off >>= 1) arg = min(arg, __shfl_xor(arg, off, 64));
+    r.arg = arg;
+  }
   return r;
 }
 
@@ -481,7 +484,7 @@ __global__ __launch_bounds__(kEdgeThreads) void draft_edges_kernel(DraftParams p
     const int node = i >> 1, is_q = i & 1, then = next(i + kEdgeThreads / 64);
     const RowParts mine = ahead;
     if (then < 2 * n) ahead.load(part_of(then), d.chunks, lane);
-    const RowDist r = row_dist(mine, part_of(i), d.chunks, it, lane);
+    const RowDist r = row_dist(mine, part_of(i), d.chunks, it, argmax, lane);
     i = then;
     if (lane == 0) {
       DraftRow x;
@@ -826,9 +829,13 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
       }
       return x;
     };
+    double near[2];  // the first 128 chunks' shares, looked up once
+    auto share_from = [&](int c0) { return c0 < 128 ? c0 ? near[1] : near[0] : share(c0 + lane); };
     auto whole_sum = [&]() {
+      near[0] = share(lane);
+      near[1] = share(64 + lane);
       double x = 0;
-      for (int c0 = 0; c0 < d.chunks; c0 += 64) x += share(c0 + lane);
+      for (int c0 = 0; c0 < d.chunks; c0 += 64) x += share_from(c0);
       return wave_sum_d(x);
     };
     double total = whole_sum();
@@ -841,7 +848,7 @@ __global__ __launch_bounds__(kThreads) void draft_end_kernel(DraftParams p) {
     double start = 0, ahead = 0;
     int pick = -1;
     for (int c0 = 0; c0 < d.chunks; c0 += 64) {
-      const double x = share(c0 + lane);
+      const double x = share_from(c0);
       double before;
       bool passed;
       const int who = pass_lane(x, start, want, lane, before, passed);

@@ -94,8 +94,8 @@ constexpr int kCus = 256;
 // Workgroups a compute unit: of one wave, each with a ring of two blocks of 32 keys and values
 // in LDS, and of a team of four waves, with a ring between them.  bf16 of head size 128, a team:
 // 64 keys a block, two blocks, two teams a unit.  16 drafted nodes of each of four sequences of
-// 36 000 tokens, 64 heads over 8, take 127 us so, 130 with three or four blocks of 32 keys, 142
-// with one team of four blocks of 64, 147 with three teams.
+// 36 000 tokens, 64 heads over 8, take 124 us so, 127 with four blocks of 32 keys, 143 with one
+// team of four blocks of 64.
 template <int D, typename T>
 constexpr int kTreeSolo = D * sizeof(T) > 256 ? 2 : D * sizeof(T) > 128 ? 4 : 8;
 template <int D, typename T>

@@ -273,7 +273,7 @@ __device__ __forceinline__ int64_t tree_units(const TreeShape& sh, const TreePla
 struct TreeRun {
   TreeItem it;
   int own;         // which kind of item
-  int g, tile;     // kv-head, tile of rows
+  int g, tile, tiles;  // kv-head, tile of rows, of how many
   int key, blocks; // from key on (a multiple of 16); blocks 0: the run ends ahead of the first
   int units;
   int64_t prow;    // row of its partial result
@@ -292,6 +292,7 @@ __device__ __forceinline__ TreeRun tree_run(const TreeShape& sh, const TreePlan&
     r.it = load_uniform(plan.items + item);
     const int64_t rel = pos - r.it.first;
     const int units = units_of(r.it.blocks), tiles = tiles_of(r.it.rows, kind);
+    r.tiles = tiles;
     if (rel >= (int64_t)units * tiles * sh.hkv) continue;  // none, or this one's end
     const int j = (int)div_floor(rel, units), u0 = (int)(rel - (int64_t)j * units);
     r.g = j / tiles;
@@ -543,9 +544,17 @@ __global__ __launch_bounds__(kTeamWaves * 64, (kTreeTeam<D, T>)) void tree_team_
   using Dma = RowDma<T, D, RPW>;
   __shared__ __attribute__((aligned(1024))) TreeRing<T, S, BN * D> smem;
   auto* ring = in_lds(&smem);
-  const int worker = blockIdx.x, tid = threadIdx.x, lane = tid & 63, ln = lane & 31, hf = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, ln = lane & 31, hf = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t total = tree_units(sh, p.plan, 1), run_len = p.plan.head[3];
+  if (total == 0) return;
+  // Workgroups go round the 8 XCDs: where an item may have several tiles an XCD takes a stretch of
+  // workers, so that tiles, which walk the same keys at about the same time, meet in one L2 (groups of
+  // eight sequences with eight nodes: 143 -> 141 us; alone, long trees would lose 1 us).
+  const bool meet = max(sh.kind[0].team ? sh.kind[0].tiles : 0, sh.kind[1].team ? sh.kind[1].tiles : 0) > 1;
+  const int stretch = (__builtin_amdgcn_readfirstlane((int)div_floor(total + run_len - 1, run_len)) + 7) >> 3;
+  if (meet && (int)(blockIdx.x >> 3) >= stretch) return;
+  const int worker = meet ? (int)(blockIdx.x & 7) * stretch + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
   int64_t pos = worker * run_len;
   const int64_t end = min(pos + run_len, total);
   if (pos >= end) return;
@@ -564,8 +573,13 @@ __global__ __launch_bounds__(kTeamWaves * 64, (kTreeTeam<D, T>)) void tree_team_
       const int rows = mine < r.it.k1 ? min(RPW, r.it.k1 - mine) : min(RPW, r.it.k1 - key);
       const int64_t base = (at - wave * RPW) * D;  // (the DMA adds the wave's first row)
       const unsigned tile = (unsigned)(uintptr_t)&ring->kv[stage][0][wave * RPW * D];
-      dma_rows_at<false>(dma, tile, p.k + base, wave * RPW + rows);
-      dma_rows_at<false>(dma, tile + BN * D * sizeof(T), p.v + base, wave * RPW + rows);
+      if (r.tiles == 1) {  // nobody else reads them: past the L2 (long trees 139 -> 124 us, groups 141 -> 133)
+        dma_rows_at<true>(dma, tile, p.k + base, wave * RPW + rows);
+        dma_rows_at<true>(dma, tile + BN * D * sizeof(T), p.v + base, wave * RPW + rows);
+      } else {
+        dma_rows_at<false>(dma, tile, p.k + base, wave * RPW + rows);
+        dma_rows_at<false>(dma, tile + BN * D * sizeof(T), p.v + base, wave * RPW + rows);
+      }
     };
     if (!first) __syncthreads();  // the ring is free
     const int n = r.blocks;
