@@ -57,39 +57,56 @@ __device__ __forceinline__ float lowest<float>() {
   return -3.4028234663852886e38f;
 }
 
-// 2^(i / 64), in LDS: entries are two banks each, so that a wave's lanes meet at most twice.
-// Their upper words are lower by i << 14: k << 14 on top makes entry k & 63 2^(k / 64).
-constexpr int kRoots = 64;
+// 2^(i / 256), in LDS.  Their upper words are lower by i << 12: k << 12 on top makes entry k & 255
+// 2^(k / 256).
+constexpr int kRoots = 256;
+struct RootTable {
+  double of[kRoots];
+};
+constexpr RootTable root_table() {
+  RootTable t{};
+  for (int i = 0; i < kRoots; ++i) {
+    const double x = i * (0.6931471805599453 / kRoots);
+    double sum = 0.0;
+    for (int n = 18; n > 0; --n) sum = (1.0 + sum) * x / n;  // e^x - 1
+    t.of[i] = __builtin_bit_cast(double, __builtin_bit_cast(uint64_t, 1.0 + sum) - ((uint64_t)i << 44));
+  }
+  return t;
+}
+__device__ const RootTable kRootTable = root_table();
 __device__ __forceinline__ double* exp2_roots() {
   __shared__ double roots[kRoots];
   return roots;
 }
 __device__ __forceinline__ void fill_roots() {
-  if (threadIdx.x < kRoots) {
-    const double r = exp2((double)threadIdx.x / kRoots);
-    exp2_roots()[threadIdx.x] = __hiloint2double(__double2hiint(r) - (int)(threadIdx.x << 14), __double2loint(r));
-  }
+  if (threadIdx.x < kRoots) exp2_roots()[threadIdx.x] = kRootTable.of[threadIdx.x];
   lds_barrier();
 }
-// 2^t for t <= 0 in 64 bits: with k the whole number next to 64 t and f = t - k / 64,
-// |f| <= 1/128, 2^(k / 64) from the table, 2^f by the polynomial of degree 4 through 1 at 0 and
-// Chebyshev's points, good to 5e-15 of it.  k comes out of the low bits of t + 1.5 2^46.  Below
+// 2^t for t <= 0 in 64 bits: with k the whole number next to 256 t and f = t - k / 256,
+// |f| <= 1/512, 2^(k / 256) from the table, 2^f by the polynomial of degree 3 through 1 at 0 and
+// Chebyshev's points, good to 3.5e-14 of it.  k comes out of the low bits of t + 1.5 2^44.  Below
 // 2^-1000, and for -inf, 2^-1000; without CLAMP t has to be above.  NaN stays.
 constexpr double kTiny = -1000.0;
+struct Exp2 {
+  double root, p;  // whose product it is
+};
 template <bool CLAMP = true>
-__device__ __forceinline__ double exp2_neg(double t) {
-  constexpr double shift = 1.5 * (1ull << 46);
+__device__ __forceinline__ Exp2 exp2_parts(double t) {
+  constexpr double shift = 1.5 * (1ull << 44);
   if (CLAMP && t < kTiny) t = kTiny;
   const double u = t + shift;
   const int k = __double2loint(u);
   const double base = exp2_roots()[k & (kRoots - 1)];
-  const double root = __hiloint2double(__double2hiint(base) + (k << 14), __double2loint(base));
   const double f = t - (u - shift);
-  double s = 0.009618138509201629;
-  s = fma(s, f, 0.05550419004645178);
-  s = fma(s, f, 0.24022650695902897);
-  s = fma(s, f, 0.6931471805593244);
-  return fma(root, s * f, root);
+  Exp2 x;
+  x.root = __hiloint2double(__double2hiint(base) + (k << 12), __double2loint(base));
+  x.p = fma(fma(fma(0.05550411247958329, f, 0.24022653447679007), f, 0.6931471805599453), f, 1.0);
+  return x;
+}
+template <bool CLAMP = true>
+__device__ __forceinline__ double exp2_neg(double t) {
+  const Exp2 x = exp2_parts<CLAMP>(t);
+  return x.root * x.p;
 }
 
 template <typename T>
@@ -155,6 +172,19 @@ __device__ __forceinline__ double wave_scan_d(double x) {
   x = add_moved<0x142, 0xa>(x);
   return add_moved<0x143, 0xc>(x);
 }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float max_moved(float x) {
+  const int own = (int)__float_as_uint(x);
+  return fmaxf(x, __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(own, own, CTRL, ROWS, 0xf, false)));
+}
+__device__ __forceinline__ float wave_max_f(float x) {
+  x = max_moved<0x111, 0xf>(x);
+  x = max_moved<0x112, 0xf>(x);
+  x = max_moved<0x114, 0xf>(x);
+  x = max_moved<0x118, 0xf>(x);
+  x = max_moved<0x142, 0xa>(x);
+  return lane_f(max_moved<0x143, 0xc>(x), 63);
+}
 __device__ __forceinline__ double wave_sum_d(double x) { return lane_d(wave_scan_d(x), 63); }
 
 // A sequence's tree: lane l of a wave looks at node l.
@@ -192,6 +222,51 @@ __device__ __forceinline__ double inv_temp(const float* temperature, int s) {
 }
 __device__ __forceinline__ bool greedy(const float* temperature, int s) { return temperature && !(temperature[s] > 0); }
 
+// The greatest of a wave's entries (NaN left out), and a number that none of the lane's is below.
+// As whole numbers bf16 ones rise where they are positive and fall where they are negative, so two
+// entries at a time can be compared: with sign the greatest of those that have none, if there is one, and
+// without it the lowest of those that have one.
+__device__ __forceinline__ float extremes(const RawOf<uint16_t> (&x)[4], float& low) {
+  typedef int16_t Signed __attribute__((ext_vector_type(8)));
+  typedef int16_t Two __attribute__((ext_vector_type(2)));
+  typedef uint16_t UTwo __attribute__((ext_vector_type(2)));
+  typedef uint16_t UFour __attribute__((ext_vector_type(4)));
+  typedef int16_t Four __attribute__((ext_vector_type(4)));
+  Signed hi = __builtin_bit_cast(Signed, x[0]);
+  RawOf<uint16_t> lo = x[0];
+#pragma unroll
+  for (int u = 1; u < 4; ++u) {
+    hi = __builtin_elementwise_max(hi, __builtin_bit_cast(Signed, x[u]));
+    lo = __builtin_elementwise_max(lo, x[u]);
+  }
+  const Four h4 = __builtin_elementwise_max(hi.lo, hi.hi);
+  const UFour l4 = __builtin_elementwise_max(lo.lo, lo.hi);
+  const Two h2 = __builtin_elementwise_max(h4.lo, h4.hi);
+  const UTwo l2 = __builtin_elementwise_max(l4.lo, l4.hi);
+  const int h = max((int)h2.x, (int)h2.y);
+  const uint32_t l = max((uint32_t)l2.x, (uint32_t)l2.y);
+  low = l & 0x8000u ? bf16_bits_to_f32((uint16_t)l) : 0.f;
+  if (wave_any(h >= 0)) return wave_max_f(h >= 0 ? bf16_bits_to_f32((uint16_t)h) : kNegInf);
+  uint32_t least = 0xffffu;  // all have a sign (or are NaN)
+#pragma unroll
+  for (int u = 0; u < 4; ++u)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) least = min(least, (uint32_t)x[u][i]);
+  return wave_max_f(least & 0x8000u ? bf16_bits_to_f32((uint16_t)least) : kNegInf);
+}
+__device__ __forceinline__ float extremes(const RawOf<float> (&x)[8], float& low) {
+  float m = kNegInf;
+  low = -kNegInf;
+#pragma unroll
+  for (int u = 0; u < 8; ++u)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m = fmaxf(m, x[u][i]);
+      low = fminf(low, x[u][i]);
+    }
+  return wave_max_f(m);
+}
+
 // A wave a chunk.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
@@ -223,16 +298,8 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
   }
   fill_roots();
   if (chunk >= d.chunks) return;
-  float m = kNegInf, low = -kNegInf;
-#pragma unroll
-  for (int u = 0; u < L; ++u)
-#pragma unroll
-    for (int i = 0; i < kVec<T>; ++i) {
-      const float y = to_float(x[u][i]);
-      m = fmaxf(m, y);
-      low = fminf(low, y);
-    }
-  const float top = wave_max(m);
+  float low;  // none of the thread's entries is below
+  const float top = extremes(x, low);
   bool bad = top == -kNegInf;  // or a NaN among them
   double sum = 0;
   int arg = 0x7fffffff;
@@ -246,8 +313,8 @@ __global__ __launch_bounds__(kThreads) void draft_rows_kernel(DraftParams p) {
 #pragma unroll
         for (int i = 0; i < kVec<T>; ++i) {
           const double y = (double)to_float(x[u][i]);
-          if constexpr (careful.value) sum += exp2_neg<true>((y - (double)top) * a);
-          else sum += exp2_neg<false>(fma(y, a, b));
+          const Exp2 e = careful.value ? exp2_parts<true>((y - (double)top) * a) : exp2_parts<false>(fma(y, a, b));
+          sum = fma(e.root, e.p, sum);
         }
       }
     };
@@ -320,7 +387,7 @@ __device__ __forceinline__ RowDist row_dist(const RowParts& first, const DraftPa
     m = fmaxf(m, x);
   }
   RowDist r;
-  r.max = wave_max(m);
+  r.max = wave_max_f(m);
   r.usable = !__any(bad) && r.max > kNegInf;
   r.a = it;
   r.sum = 0;
