@@ -195,9 +195,9 @@ struct TreeOf {
 };
 __device__ __forceinline__ TreeOf tree_of(const DraftShape& d, const int32_t* parents, const int32_t* count, int s, int lane) {
   TreeOf t;
+  int up = !parents ? lane - 1 : lane < d.nodes ? parents[(int64_t)s * d.nodes + lane] : -1;  // (on its way with the count)
   t.count = max(0, min(count ? count[s] : d.nodes, d.nodes));
-  int up = lane > 0 && lane < t.count ? (parents ? parents[(int64_t)s * d.nodes + lane] : lane - 1) : -1;
-  if (up >= lane) up = -1;
+  if (lane == 0 || lane >= t.count || up >= lane) up = -1;
   t.kids = 0;
   t.rank = 0;
   for (int j = 1; j < t.count; ++j) {
@@ -524,13 +524,19 @@ __global__ __launch_bounds__(kEdgeThreads) void draft_edges_kernel(DraftParams p
   __shared__ DraftRow s_p[kTreeNodes], s_q[kTreeNodes];
   const DraftShape& d = p.shape;
   const int s = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t row0 = (int64_t)s * d.nodes, rows = (int64_t)d.n * d.nodes;
+  // what does not wait for anything else: tokens, numbers, the parts of the wave's first row
+  auto part_of = [&](int i) { return p.part + ((i & 1) * rows + row0 + (i >> 1)) * d.chunks; };
+  int y = lane < d.nodes ? p.tokens[row0 + lane] : -1;
+  const float u32 = lane < d.nodes ? p.u[row0 + lane] : 0.f;
+  RowParts ahead;
+  if (wave < 2 * d.nodes) ahead.load(part_of(wave), d.chunks, lane);
   const TreeOf t = tree_of(d, p.parents, p.count, s, lane);
   const int n = t.count;
-  const int64_t row0 = (int64_t)s * d.nodes, rows = (int64_t)d.n * d.nodes;
+  if (lane >= n) y = -1;
   const bool argmax = greedy(p.temperature, s), sampled = p.draft != nullptr && !argmax;
   const double it = inv_temp(p.temperature, s);
   // the drafted tokens' logits
-  const int y = lane < n ? p.tokens[row0 + lane] : -1;
   float xp = 0.f, xq = 0.f;
   if (tid < 64 && t.up >= 0 && y >= 0 && y < d.vocab) {
     const int64_t at = (row0 + t.up) * d.vocab + y;
@@ -538,14 +544,12 @@ __global__ __launch_bounds__(kEdgeThreads) void draft_edges_kernel(DraftParams p
     if (sampled) xq = to_float(((const T*)p.draft)[at]);
   }
   // the rows, each one's parts fetched ahead
-  auto part_of = [&](int i) { return p.part + ((i & 1) * rows + row0 + (i >> 1)) * d.chunks; };
   auto next = [&](int i) {  // the wave's next row from i on that is looked at
     while (i < 2 * n && (i & 1) && !(sampled && lane_u64(t.kids, i >> 1))) i += kEdgeThreads / 64;
     return i;
   };
   int i = next(wave);
-  RowParts ahead;
-  if (i < 2 * n) ahead.load(part_of(i), d.chunks, lane);
+  if (i != wave && i < 2 * n) ahead.load(part_of(i), d.chunks, lane);
   fill_roots();
   while (i < 2 * n) {
     const int node = i >> 1, is_q = i & 1, then = next(i + kEdgeThreads / 64);
@@ -573,7 +577,7 @@ __global__ __launch_bounds__(kEdgeThreads) void draft_edges_kernel(DraftParams p
       e.p = row_dist(rp, it).raw(xp) / rp.sum;
       if (sampled) e.q = row_dist(rq, it).raw(xq) / rq.sum;
     }
-    const double u = (double)p.u[row0 + lane];
+    const double u = (double)u32;
     stays = tried && (sampled ? u * e.q < e.p : argmax ? y == rp.arg : u < e.p);
   }
   // a node can be reached if its edge can be taken, and its parent's, ..: a first child's if it
