@@ -622,7 +622,8 @@ pp_status pp_cache_accept(const pp_cache* cache, int n, const int32_t* slots, in
  * sequence).  A sequence that names no slot, or whose nodes have not all been reserved,
  * and a node with a parent that is no earlier one, come out as NaN.
  * planned != 0: ws holds the plan of an earlier call with the same cache state and
- * arguments but q, the pools and the results, as for every layer after a step's first;
+ * arguments but q, the pools and the results, as for every layer after a step's first,
+ * and only such calls have used ws since;
  * with a plan of other sizes, or none, the results are NaN.
  * ws_bytes >= pp_tree_workspace_size's bytes. */
 pp_status pp_tree_workspace_size(const pp_cache* cache, int n, int group, int max_new, pp_dtype dtype, int hq, int hkv, int head_dim,

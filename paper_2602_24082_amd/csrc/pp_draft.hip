@@ -23,7 +23,8 @@
 //
 // Probabilities are 64 bits throughout: numbers are compared with given ones, and a running
 // sum over 10^5 entries in 32 bits passes a number u elsewhere in one case of some hundred.
-// Bound by reading the rows once.
+// Bound by their arithmetic: an entry's exponential and its place in the sum are nine 64-bit and three
+// other operations (33 million of them, 66 MB of logits, 24 us).
 
 #include <hip/hip_runtime.h>
 #include <math.h>

@@ -285,6 +285,8 @@ __device__ __forceinline__ TreeRun tree_run(const TreeShape& sh, const TreePlan&
                                             int& item) {
   TreeRun r;
   for (;; ++item) {
+    r.blocks = 0;
+    if (item >= sh.n + sh.groups) return r;  // (never by a plan that is whole)
     const int grp = item / (sh.group + 1), member = item - grp * (sh.group + 1) - 1;
     r.own = member >= 0;
     const TreeKind& kind = sh.kind[r.own];
