@@ -184,6 +184,30 @@ def test_hot_and_cold(dtype, offset):
     check(target, tokens, u, None, parents, temperature=temps, max_children=2)
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("offset", [-300.0, -12.0, 12.0])
+def test_logits_of_one_sign(dtype, offset):
+    """Rows whose entries are all negative (as log-probs are) or all positive, stretches of them among others, masks beside
+    them, zeros of both signs as the largest, NaN with a sign."""
+    target, tokens, u, draft, parents = case(9, 4, 7001, dtype, 43, near=0.3)
+    target, draft = ((x.float() + offset).to(dtype) for x in (target, draft))
+    for x in (target, draft):
+        x[1, :, 2000:5000] = -float("inf")
+        x[2, :, 4096:6144] = torch.finfo(dtype).min
+        x[3, :, 2048:4096] -= 2 * offset  # a stretch of the other sign
+    for i, zeros in ((4, (-0.0, 0.0)), (5, (0.0, -0.0)), (6, (-0.0, -0.0))):
+        target[i] = -target[i].abs() - 1
+        target[i, :, 1111], target[i, :, 6666] = zeros
+    sign = torch.tensor(-1, dtype=torch.int16 if dtype == torch.bfloat16 else torch.int32).view(dtype)  # a NaN
+    target[7, 0, 4321] = sign
+    draft[8, 0, 6999] = sign
+    assert torch.isnan(target[7, 0, 4321]) and torch.isnan(draft[8, 0, 6999])
+    for temp in (None, [0.7] * 9, [0.0] * 9):
+        for d in (draft, None):
+            out = check(target, tokens, u, d, parents, temperature=temp, max_children=2)
+    assert [out[1][i, out[0][i] - 1] for i in (4, 5, 6)] == [1111] * 3 and np.isnan(out[3][7]).any()
+
+
 def test_greedy_takes_the_first_largest():
     target, tokens, u, draft, _ = case(6, 4, 20000, torch.bfloat16, 31, width=1)
     for i in range(6):
