@@ -432,6 +432,7 @@ __global__ __launch_bounds__(64, 2) void tree_solo_kernel(CacheView c, TreeShape
   auto* ring = in_lds(&smem);
   const int worker = blockIdx.x, lane = threadIdx.x & 63, ln = lane & 31, hf = lane >> 5;
   const int64_t total = tree_units(sh, p.plan, 0), run_len = p.plan.head[1];
+  if (total == 0) return;  // (without a plan the run's length is anything)
   int64_t pos = worker * run_len;
   const int64_t end = min(pos + run_len, total);
   if (pos >= end) return;

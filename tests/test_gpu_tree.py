@@ -256,6 +256,17 @@ def test_a_plan_of_another_call_is_refused():
     assert all(torch.equal(x, y) for x, y in zip(want, run(a, True))) and not torch.isnan(want[0]).any()
 
 
+@pytest.mark.parametrize("nodes", [3, 40])
+def test_numbers_that_are_no_plan(nodes):
+    """A workspace of large numbers whose products leave 64 bits, for waves and for teams: NaN."""
+    a = Case(torch.bfloat16, 4, 2, 64, 16, [100, 7, 64, 65], nodes=nodes, seed=12)
+    ws = torch.zeros(pp.pp_tree_workspace_size(a.cache, 4, 1, nodes, 4, 2, 64) // 8, dtype=torch.int64, device=DEV)
+    for x in (0x2000000000000001, 0x7fffffffffffffff, -1):
+        ws.fill_(x)
+        o, lse = pp.pp_tree_attn_fwd(a.cache, ints(a.slots), a.q.to(DEV), a.k.to(DEV), a.v.to(DEV), planned=True, ws=ws)
+        assert torch.isnan(o).all() and torch.isnan(lse).all()
+
+
 def test_a_pool_past_2_31_elements():
     """Pages whose rows lie past 2^31 elements of the pool."""
     pages, hkv, ps, d = 70000, 2, 256, 64
