@@ -894,8 +894,9 @@ def pp_policy_loss(pack: Pack, logp: torch.Tensor, adv: torch.Tensor, logp_old: 
 
 class Cache:
     """A paged cache's bookkeeping (struct pp_cache): page_table [slots, max_pages], seq_len and held [slots], refs [pages],
-    int32 on the GPU, all zeros when empty.  The tensors stay the caller's to read; keys and values lie in pools
-    [layers, pages, hkv, page_size, head_dim] that go to each call."""
+    int32 on the GPU, all zeros when empty.  The tensors stay the caller's to read, and to change in place: calls go to their
+    memory, so another tensor in an attribute's place is refused.  Keys and values lie in pools [layers, pages, hkv, page_size,
+    head_dim] that go to each call."""
 
     def __init__(self, page_table: torch.Tensor, seq_len: torch.Tensor, held: torch.Tensor, refs: torch.Tensor, page_size: int):
         if not isinstance(page_table, torch.Tensor) or page_table.dim() != 2 or not isinstance(refs, torch.Tensor) or refs.dim() != 1:
@@ -912,6 +913,15 @@ class Cache:
                                 seq_len.data_ptr(), held.data_ptr(), refs.data_ptr())
         self.ref = ctypes.byref(self._desc)
         self._sizes = {}
+
+    def __setattr__(self, name, value):
+        # (`cache.seq_len += 1` sets the same tensor again)
+        if name in self.__dict__ and self.__dict__[name] is not value:
+            raise AttributeError(f"a Cache's {name} cannot be replaced (tensors can be changed in place: {name}.copy_(..))")
+        object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        raise AttributeError(f"a Cache's {name} cannot be deleted")
 
     def _ws_size(self, name: str, *args) -> int:
         """Workspace bytes, kept (they follow from the sizes)."""
