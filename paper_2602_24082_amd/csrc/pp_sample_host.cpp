@@ -60,7 +60,9 @@ pp_status check_cache(const pp_cache* c, CacheView* v) {
 }
 
 constexpr int kMostSeqs = 65535;  // a launch's second dimension
-constexpr int64_t kMostRows = 1 << 27;  // query rows of the attention: the join's launch has 32 threads a row at most
+// query rows of the attention: the join takes 8 a workgroup of 256 threads at head size 128, and a launch
+// has fewer than 2^32 threads
+constexpr int64_t kMostRows = 8 * ((int64_t)UINT32_MAX / 256);
 constexpr int kMostNew = 1 << 24;  // tokens a sequence and call: a launch's first, in threads
 
 pp_status check_n(int n) {
@@ -158,7 +160,7 @@ bool shape_tree(int n, int group, int nodes, int hq, int hkv, pp_dtype dtype, in
   t->hkv = hkv;
   t->G = hq / hkv;
   const bool bf16 = dtype == PP_BF16;
-  if ((int64_t)n * nodes * hq >= kMostRows) return false;
+  if ((int64_t)n * nodes * hq > kMostRows) return false;
   t->workers[0] = kCus * (bf16 ? (d == 128 ? kTreeSolo<128, uint16_t> : kTreeSolo<64, uint16_t>)
                                : (d == 128 ? kTreeSolo<128, float> : kTreeSolo<64, float>));
   t->workers[1] = kCus * (bf16 ? (d == 128 ? kTreeTeam<128, uint16_t> : kTreeTeam<64, uint16_t>)
