@@ -1179,16 +1179,20 @@ def pp_verify_workspace_size(n: int, max_new: int, vocab: int, dtype: int = PP_B
 
 def pp_verify_draft(target: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor, draft: Optional[torch.Tensor] = None,
                     parents: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
-                    temperature: Optional[torch.Tensor] = None, max_children: int = 1, ws=None):
+                    temperature: Optional[torch.Tensor] = None, max_children: Optional[int] = None, ws=None):
     """Verifies drafted tokens [n, max_new] (node 0 the last token) against the model's logits target [n, max_new, vocab]
     with the numbers u [n, max_new], draft [n, max_new, vocab] the drafter's logits (None: given drafts), and samples the
-    token that follows.  Returns (count [n], new tokens [n, max_new], path [n, max_new], their log-probs [n, max_new])."""
+    token that follows.  max_children: a node's children from there on are not tried (None: all are); with draft logits
+    each costs a launch, so trees of a known width do well to name it.  Returns (count [n], new tokens [n, max_new],
+    path [n, max_new], their log-probs [n, max_new])."""
     if target.dim() != 3:
         raise ValueError("target must be [n, max_new, vocab]")
     (n, N, V), dev, dtype = target.shape, target.device, target.dtype
     dt = _dtype_code(target)
     _on_gpu(target)
     idx, each = dev.index, (n, N)
+    if max_children is None:
+        max_children = 1 if parents is None else N
     _fits("target", target, target.shape, dtype, dev, idx)
     _fits("tokens", tokens, each, _int32, dev, idx)
     _fits("u", u, each, torch.float32, dev, idx)

@@ -1,4 +1,6 @@
 """CPU tests of what the binding of the sampling operators keeps and refuses by itself."""
+import contextlib
+
 import pytest
 import torch
 
@@ -42,3 +44,23 @@ def test_a_cache_keeps_its_sizes(monkeypatch, name, value):
     c = _cache(monkeypatch)
     with pytest.raises(AttributeError):
         setattr(c, name, value)
+
+
+@pytest.mark.parametrize("given,want", [({}, 1), ({"parents": True}, 6), ({"parents": True, "max_children": 2}, 2), ({"max_children": 3}, 3)])
+def test_children_of_a_tree_are_all_tried_unless_said_otherwise(monkeypatch, given, want):
+    seen = []
+
+    class Library:
+        def pp_verify_draft(self, *args):
+            seen.append(args)
+            return 0
+
+    monkeypatch.setattr(pp, "lib", Library)
+    monkeypatch.setattr(pp, "_on_gpu", lambda t: None)
+    monkeypatch.setattr(pp, "_raw_stream", lambda dev: None)
+    monkeypatch.setattr(pp, "_device_of", lambda dev: contextlib.nullcontext())
+    monkeypatch.setattr(pp, "pp_verify_workspace_size", lambda *a: 256)
+    z = lambda dtype: torch.zeros(2, 6, dtype=dtype)
+    kw = dict(given, parents=z(torch.int32)) if "parents" in given else given
+    pp.pp_verify_draft(torch.zeros(2, 6, 10), z(torch.int32), z(torch.float32), **kw)
+    assert seen[0][:5] == (2, 6, 10, pp.PP_FP32, want)
