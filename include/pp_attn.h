@@ -617,10 +617,11 @@ pp_status pp_cache_accept(const pp_cache* cache, int n, const int32_t* slots, in
  * [n / group]; pp_cache_shared's) pages, whose keys are then read once for all of
  * them; NULL: nothing is shared.  More than whole pages of the shortest count as those.
  * PP_BF16: probabilities are rounded to bf16 for the second product, sums are fp32;
- * PP_FP32: as exact as fp32 products (as pp_cross_attn_fwd, also where infinities and
- * NaN are concerned: a node that is not finite may reach the other nodes of its
- * sequence).  A sequence that names no slot, or whose nodes have not all been reserved,
- * and a node with a parent that is no earlier one, come out as NaN.
+ * PP_FP32: as exact as fp32 products (as pp_cross_attn_fwd).  A node that is not finite
+ * reaches those that see it and no other; of what a node sees infinities may come out as
+ * NaN (for PP_FP32 also elements above bf16's 3.39e38).  A sequence that names no slot, or
+ * whose nodes have not all been reserved, and a node with a parent that is no earlier one,
+ * come out as NaN.
  * planned != 0: ws holds the plan of an earlier call with the same cache state and
  * arguments but q, the pools and the results, as for every layer after a step's first,
  * and only such calls have used ws since;

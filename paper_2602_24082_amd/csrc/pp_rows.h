@@ -32,6 +32,14 @@ struct Ops<__bf16> {
   static __device__ __forceinline__ Frag tr8(const __bf16* tile, int row16, int col0, int lane) {
     return lds_tr8<D>(tile, row16, col0, lane);
   }
+  // elements col .. col + 3 of row r (col a multiple of 4)
+  template <int D>
+  static __device__ __forceinline__ f32x4 four(const __bf16* tile, int r, int col) {
+    return __builtin_convertvector(*reinterpret_cast<const bf16x4*>(tile + r * D + (((col >> 3) ^ swz<D>(r)) << 3) + (col & 7)), f32x4);
+  }
+  // what the products take is below; in a word's magnitudes the rest carries into the sign's place
+  static constexpr float kLimit = __builtin_inff();
+  static constexpr uint32_t kMagnitude = 0x7fff7fffu, kCarry = 0x00800080u, kSign = 0x80008000u;
 };
 
 // fp32 on the bf16 matrix units: x = h + m + l, three bf16 numbers that hold all 24 bits
@@ -93,6 +101,12 @@ struct Ops<float> {
     }
     return split3(f);
   }
+  template <int D>
+  static __device__ __forceinline__ f32x4 four(const float* tile, int r, int col) {
+    return *reinterpret_cast<const f32x4*>(tile + r * D + (((col >> 2) ^ swz<2 * D>(r)) << 2));
+  }
+  static constexpr float kLimit = 0x1.ffp127f;  // rounds to infinity as bf16
+  static constexpr uint32_t kMagnitude = 0x7fffffffu, kCarry = 0x00808000u, kSign = 0x80000000u;
 };
 
 // Wave-cooperative DMA of NR rows of D elements of T (see TileDma).
@@ -130,7 +144,7 @@ struct RowState {
     const bool raise = mx > m_ref + kRescaleSlack;
     if (wave_any(raise)) {
       const float m_new = raise ? mx : m_ref;
-      const float alpha = (m_ref == kNegInf) ? 0.f : fast_exp2(m_ref - m_new);  // nothing seen yet: O = l = 0
+      const float alpha = (m_ref == kNegInf) ? 1.f : fast_exp2(m_ref - m_new);  // nothing seen yet: l and O's finite elements are 0
       l *= alpha;
 #pragma unroll
       for (int m = 0; m < D / 32; ++m)

@@ -379,6 +379,49 @@ __device__ __forceinline__ void tree_mask(f32x16& s, int k0, int seen, uint64_t 
   for (int r = 0; r < 16; ++r) s[r] = keep_or_neginf(s[r], word, 8 * (r >> 2) + (r & 3));
 }
 
+// A probability of 0 keeps a number out of P V, but no infinity and no NaN.  So where a row does not see
+// all keys of a block, values that are not finite (or not so as bf16) leave it ahead of the product, and
+// a row that sees one adds infinity or NaN, whatever its probability.
+//
+// Whether N elements at `tile` have one, by a wave.
+template <int N, typename T>
+__device__ __forceinline__ bool not_finite(const T* tile, int lane) {
+  typedef uint32_t Words __attribute__((ext_vector_type(4)));
+  using O = Ops<T>;
+  const Words* at = reinterpret_cast<const Words*>(tile) + lane;
+  uint32_t carry = 0;
+#pragma unroll
+  for (int i = 0; i < (int)(N * sizeof(T) / 1024); ++i) {
+    const Words w = at[64 * i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) carry |= (w[e] & O::kMagnitude) + O::kCarry;
+  }
+  return wave_any((carry & O::kSign) != 0);
+}
+// Adds what the row sees of them among KEYS keys from k0 on.
+template <int D, int KEYS, typename T>
+__device__ __forceinline__ void add_not_finite(RowState<D>& st, const T* sV, int k0, int seen, uint64_t tree, int hf) {
+#pragma unroll 1
+  for (int k = 0; k < KEYS; ++k) {
+    const int node = k0 + k - seen;
+    const bool sees = node < 0 || (node < 64 && (tree >> node & 1));
+#pragma unroll
+    for (int m = 0; m < D / 32; ++m)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const f32x4 v = Ops<T>::template four<D>(sV, k, 32 * m + 8 * r4 + 4 * hf);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) st.o[m][4 * r4 + e] += sees && !(fabsf(v[e]) < Ops<T>::kLimit) ? v[e] * __builtin_inff() : 0.f;
+      }
+  }
+}
+// Makes them 0.
+template <int N, typename T>
+__device__ __forceinline__ void drop_not_finite(T* tile, int lane) {
+  for (int i = lane; i < N; i += 64)
+    if (!(fabsf((float)tile[i]) < Ops<T>::kLimit)) tile[i] = (T)0.f;
+}
+
 template <int D, typename T>
 __device__ __forceinline__ void leave_partial(const TreeParams<T>& p, const RowState<D>& st, const TreeRow& row, int64_t at, bool bad,
                                               int hf) {
@@ -421,8 +464,9 @@ __device__ __forceinline__ void dma_rows_at(const TileDma<RD, NR>& d, unsigned t
   }
 }
 
-// Up to 32 rows, row ln in lanes ln and ln + 32.
-template <int D, typename T>
+// Up to 32 rows, row ln in lanes ln and ln + 32.  BRANCH: sequences have several nodes, so that one
+// row may see a key that another does not (the look at values takes single tokens from 22.4 to 23.1 us).
+template <int D, typename T, bool BRANCH>
 __global__ __launch_bounds__(64, 2) void tree_solo_kernel(CacheView c, TreeShape sh, TreeParams<T> p) {
   using O = Ops<T>;
   using Frag = typename O::Frag;
@@ -495,7 +539,7 @@ __global__ __launch_bounds__(64, 2) void tree_solo_kernel(CacheView c, TreeShape
       asm volatile("" ::: "memory");
       const int k0 = r.key + kSoloKeys * i;
       const T* sK = (const T*)ring->kv[i & 1][0];
-      const T* sV = (const T*)ring->kv[i & 1][1];
+      T* sV = (T*)ring->kv[i & 1][1];
       f32x16 s[1] = {f32x16{}};
 #pragma unroll
       for (int cc = 0; cc < NC; ++cc) s[0] = O::mma(O::use(O::template row8<D>(sK, ln, 2 * cc + hf)), qf[cc], s[0]);
@@ -504,12 +548,19 @@ __global__ __launch_bounds__(64, 2) void tree_solo_kernel(CacheView c, TreeShape
         next = place(i + 2);
         issue(i + 2, 0, p.k, next);
       }
-      if (k0 + kSoloKeys > r.it.seen) tree_mask(s[0], k0, r.it.seen, row.tree, hf);
+      const bool masked = k0 + kSoloKeys > r.it.seen;
+      if (masked) tree_mask(s[0], k0, r.it.seen, row.tree, hf);
       st.probabilities(s, p.scale_log2);
       if (i + 2 < n) wait_vmem<3 * KN>();  // behind V(i): K and V of i + 1, K of i + 2
       else if (i + 1 < n) wait_vmem<2 * KN>();
       else wait_vmem<0>();
       asm volatile("" ::: "memory");
+      if constexpr (BRANCH) {
+        if (masked && r.own && not_finite<kSoloKeys * D>(sV, lane)) {
+          add_not_finite<D, kSoloKeys>(st, sV, k0, r.it.seen, row.tree, hf);
+          drop_not_finite<kSoloKeys * D>(sV, lane);
+        }
+      }
 #pragma unroll
       for (int ch = 0; ch < 2; ++ch) {
         const Frag pb = O::from_acc(s[0], ch);
@@ -539,7 +590,7 @@ __device__ __forceinline__ void wait_block(int t, int n) {
 }
 
 // Tiles of 128 rows: four waves of 32, which fetch a quarter of every block each.
-template <int D, typename T>
+template <int D, typename T, bool BRANCH>
 __global__ __launch_bounds__(kTeamWaves * 64, (kTreeTeam<D, T>)) void tree_team_kernel(CacheView c, TreeShape sh, TreeParams<T> p) {
   using O = Ops<T>;
   using Frag = typename O::Frag;
@@ -606,10 +657,19 @@ __global__ __launch_bounds__(kTeamWaves * 64, (kTreeTeam<D, T>)) void tree_team_
       lds_barrier();  // block t has landed for every wave; the stage of block t - 1 is free
       if (t + S - 1 < n) issue(t + S - 1, stage == 0 ? S - 1 : stage - 1);
       const T* sK = (const T*)ring->kv[stage][0];
-      const T* sV = (const T*)ring->kv[stage][1];
+      T* sV = (T*)ring->kv[stage][1];
       stage = stage == S - 1 ? 0 : stage + 1;
-      if (!some) continue;
       const int k0 = r.key + BN * t;
+      const bool masked = k0 + BN > r.it.seen;
+      if constexpr (BRANCH) {
+        if (masked && r.own && __syncthreads_or(not_finite<RPW * D>(sV + wave * RPW * D, lane))) {
+          if (some) add_not_finite<D, BN>(st, sV, k0, r.it.seen, row.tree, hf);
+          __syncthreads();
+          drop_not_finite<RPW * D>(sV + wave * RPW * D, lane);
+          __syncthreads();
+        }
+      }
+      if (!some) continue;
       f32x16 s[KB];
 #pragma unroll
       for (int kb = 0; kb < KB; ++kb) s[kb] = f32x16{};
@@ -630,7 +690,7 @@ __global__ __launch_bounds__(kTeamWaves * 64, (kTreeTeam<D, T>)) void tree_team_
           __builtin_amdgcn_sched_group_barrier(kSchedMfma, 1, 0);
         }
       }
-      if (k0 + BN > r.it.seen) {
+      if (masked) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) tree_mask(s[kb], k0 + 32 * kb, r.it.seen, row.tree, hf);
       }
@@ -739,7 +799,7 @@ __global__ __launch_bounds__(256) void tree_combine_kernel(TreeShape sh, TreePar
   if (col == 0) p.lse[x.lse] = some ? (m + __log2f(l)) * (1.0f / kLog2e) : 0.f;
 }
 
-template <int D, typename T>
+template <int D, typename T, bool BRANCH>
 hipError_t launch_tree_t(const CacheView& c, const TreeLaunch& a, hipStream_t s) {
   const TreeShape& sh = a.shape;
   TreeParams<T> p{};
@@ -758,13 +818,13 @@ hipError_t launch_tree_t(const CacheView& c, const TreeLaunch& a, hipStream_t s)
     if (k.tiles) takes[k.team] = true;
   if (takes[1]) {
     TimingScope t("pp_tree_attn_team", s);
-    hipLaunchKernelGGL((tree_team_kernel<D, T>), dim3(sh.workers[1]), dim3(kTeamWaves * 64), 0, s, c, sh, p);
+    hipLaunchKernelGGL((tree_team_kernel<D, T, BRANCH>), dim3(sh.workers[1]), dim3(kTeamWaves * 64), 0, s, c, sh, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (takes[0]) {
     TimingScope t("pp_tree_attn_solo", s);
-    hipLaunchKernelGGL((tree_solo_kernel<D, T>), dim3(sh.workers[0]), dim3(64), 0, s, c, sh, p);
+    hipLaunchKernelGGL((tree_solo_kernel<D, T, BRANCH>), dim3(sh.workers[0]), dim3(64), 0, s, c, sh, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -773,6 +833,11 @@ hipError_t launch_tree_t(const CacheView& c, const TreeLaunch& a, hipStream_t s)
   const int64_t rows = (int64_t)sh.n * sh.nodes * sh.hq;
   hipLaunchKernelGGL((tree_combine_kernel<D, T>), dim3((unsigned)((rows + RPB - 1) / RPB)), dim3(256), 0, s, sh, p);
   return hipGetLastError();
+}
+
+template <int D, typename T>
+hipError_t launch_tree_d(const CacheView& c, const TreeLaunch& a, hipStream_t s) {
+  return a.shape.nodes > 1 ? launch_tree_t<D, T, true>(c, a, s) : launch_tree_t<D, T, false>(c, a, s);
 }
 
 }  // namespace
@@ -784,8 +849,8 @@ hipError_t launch_tree_attn(const CacheView& c, const TreeLaunch& a, hipStream_t
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (a.dtype == kBF16) return a.head_dim == 128 ? launch_tree_t<128, __bf16>(c, a, s) : launch_tree_t<64, __bf16>(c, a, s);
-  return a.head_dim == 128 ? launch_tree_t<128, float>(c, a, s) : launch_tree_t<64, float>(c, a, s);
+  if (a.dtype == kBF16) return a.head_dim == 128 ? launch_tree_d<128, __bf16>(c, a, s) : launch_tree_d<64, __bf16>(c, a, s);
+  return a.head_dim == 128 ? launch_tree_d<128, float>(c, a, s) : launch_tree_d<64, float>(c, a, s);
 }
 
 }  // namespace pp
