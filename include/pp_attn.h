@@ -658,8 +658,8 @@ pp_status pp_tree_attn_fwd(const pp_cache* cache, int n, const int32_t* slots, i
  *   out_tokens dev int32 [n, max_new]: out_count new tokens, the last of them sampled, then -1
  *   out_logp   dev float [n, max_new]: their ln p (at T = 1 where T is not above 0),
  *              pp_policy_loss's logp_old; then 0
- * Probabilities and sums are 64 bits, exponentials good to 4 10^-14, those below 2^-999 are
- * 0.  max_new <= 64, n * max_new <= 65535. */
+ * Probabilities and sums are 64 bits; exponentials e^x, x = (logit - largest) / T, are good to
+ * 5 10^-14 + 4 10^-16 |x| of themselves, those below 2^-999 are 0.  max_new <= 64, n * max_new <= 65535. */
 pp_status pp_verify_workspace_size(int n, int max_new, int vocab, pp_dtype dtype, size_t* bytes);
 pp_status pp_verify_draft(int n, int max_new, int vocab, pp_dtype dtype, int max_children, const int32_t* count,
                           const int32_t* parents, const int32_t* tokens, const void* target, const void* draft,
