@@ -591,7 +591,8 @@ pp_status pp_cache_shared(const pp_cache* cache, int n, const int32_t* slots, in
  * position seq_len + (nodes between the token and the tree's root): parents (dev
  * [n, max_new], max_new <= 64) gives every node's parent, an earlier node or -1 for
  * the root; NULL: token j follows j - 1.  q_rot (dev [rows, hq, head_dim]) may be q;
- * without start its rows that hold no token are written as 0. */
+ * without start its rows that hold no token are written as 0, with start rows of no
+ * entry's token are left as they were. */
 pp_status pp_cache_append(const pp_cache* cache, int n, const int32_t* slots, int max_new, const int32_t* count, const int32_t* start,
                           int64_t rows, const int32_t* parents, pp_dtype dtype, int hq, int hkv, int head_dim, float rope_base,
                           const void* q, const void* k, const void* v, void* q_rot, void* k_pages, void* v_pages, void* hip_stream);
@@ -645,9 +646,15 @@ pp_status pp_tree_attn_fwd(const pp_cache* cache, int n, const int32_t* slots, i
  * From node 0 on, a node's children y are tried in order, at most max_children of them:
  *   w = p, Z = 1, a = 0 at first;  y follows if u[i][y's node] q(y) Z < w(y), else
  *   a += Z, w = max(p - a q, 0), Z = sum w
- * so that what comes out is distributed as p.  draft NULL: the drafts are given, y
- * follows if u Z < w(y), else w(y) = 0 and Z = sum w.  From the node that none of its
- * children follow, the next token is the first x with w(0) + .. + w(x) > u[i][0] Z.
+ * so that what comes out is distributed as p, if a node's children were each drawn from
+ * q by itself, the same one again where it comes out again (the k likeliest tokens of q,
+ * or draws without repeats, are no such children: they are given drafts).  A token outside
+ * the vocabulary never follows; with draft logits it counts as a rejected draw all the same,
+ * so leave it out by count or parents.
+ * draft NULL: the drafts are given, y follows if u Z < w(y), else w(y) = 0 and Z = sum w;
+ * what comes out is distributed as p however they were chosen ahead of u.  From the node
+ * that none of its children follow, the next token is the first x with
+ * w(0) + .. + w(x) > u[i][0] Z (of p where nothing is left of w).
  * T not above 0: y follows if it is the first largest logit, which is also the next token.
  * u dev float [n, max_new] in [0, 1).  Entries of -inf or of the type's lowest value are
  * masked ones, p = 0.  A row that holds a NaN or +inf or nothing else than masks gives no
@@ -659,7 +666,9 @@ pp_status pp_tree_attn_fwd(const pp_cache* cache, int n, const int32_t* slots, i
  *   out_logp   dev float [n, max_new]: their ln p (at T = 1 where T is not above 0),
  *              pp_policy_loss's logp_old; then 0
  * Probabilities and sums are 64 bits; exponentials e^x, x = (logit - largest) / T, are good to
- * 5 10^-14 + 4 10^-16 |x| of themselves, those below 2^-999 are 0.  max_new <= 64, n * max_new <= 65535. */
+ * 5 10^-14 + 4 10^-16 |x| of themselves, those below 2^-999 are 0.  max_new <= 64,
+ * n * max_new <= 65535: sequences are verified each by itself, so that more of them go in
+ * several calls. */
 pp_status pp_verify_workspace_size(int n, int max_new, int vocab, pp_dtype dtype, size_t* bytes);
 pp_status pp_verify_draft(int n, int max_new, int vocab, pp_dtype dtype, int max_children, const int32_t* count,
                           const int32_t* parents, const int32_t* tokens, const void* target, const void* draft,

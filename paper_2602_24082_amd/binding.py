@@ -1059,7 +1059,8 @@ def pp_cache_append(cache: Cache, slots: torch.Tensor, k: torch.Tensor, v: torch
                     rope_base: float = 0.0, q_rot=None) -> Optional[torch.Tensor]:
     """Writes keys and values of new tokens into one layer's pages behind the cached ones, keys (and q) rotated if rope_base
     is not 0.  k, v [n, max_new, hkv, d], or [rows, hkv, d] with max_new (and start [n], the sequences' first rows); q
-    alike.  Returns the rotated q (None without q)."""
+    alike.  Returns the rotated q (None without q): without start rows that hold no token are 0; with start rows of no
+    entry's token are not written, so they hold anything in a new q_rot, and what they held in a given one (q itself, say)."""
     dev, idx = cache.device, cache.index
     n = _slots_of("slots", slots, cache)
     dt, _, hkv, d = _pools(cache, k_pages, v_pages, False)
@@ -1182,7 +1183,8 @@ def pp_verify_draft(target: torch.Tensor, tokens: torch.Tensor, u: torch.Tensor,
                     temperature: Optional[torch.Tensor] = None, max_children: Optional[int] = None, ws=None):
     """Verifies drafted tokens [n, max_new] (node 0 the last token) against the model's logits target [n, max_new, vocab]
     with the numbers u [n, max_new], draft [n, max_new, vocab] the drafter's logits (None: given drafts), and samples the
-    token that follows.  max_children: a node's children from there on are not tried (None: all are); with draft logits
+    token that follows.  With draft logits the children of a node have to be draws from them, each by itself; drafts chosen in
+    another way are given ones.  max_children: a node's children from there on are not tried (None: all are); with draft logits
     each costs a launch, so trees of a known width do well to name it.  Returns (count [n], new tokens [n, max_new],
     path [n, max_new], their log-probs [n, max_new])."""
     if target.dim() != 3:

@@ -85,8 +85,9 @@ __device__ __forceinline__ void fill_roots() {
 }
 // 2^t for t <= 0 in 64 bits: with k the whole number next to 256 t and f = t - k / 256,
 // |f| <= 1/512, 2^(k / 256) from the table, 2^f by the polynomial of degree 3 through 1 at 0 and
-// Chebyshev's points, good to 3.5e-14 of it (and to ln 2 times what t is off by).  k comes out of the low bits of t + 1.5 2^44.  Below
-// 2^-1000, and for -inf, 2^-1000; without CLAMP t has to be above.  NaN stays.
+// Chebyshev's points, good to 3.5e-14 of it (and to ln 2 times what t is off by).  k comes out of the
+// low bits of t + 1.5 2^44.  Below 2^-1000, and for -inf, 2^-1000; without CLAMP t has to be above.
+// NaN stays.
 constexpr double kTiny = -1000.0;
 struct Exp2 {
   double root, p;  // whose product it is
