@@ -23,8 +23,9 @@
 //
 // Probabilities are 64 bits throughout: numbers are compared with given ones, and a running
 // sum over 10^5 entries in 32 bits passes a number u elsewhere in one case of some hundred.
-// Bound by their arithmetic: an entry's exponential and its place in the sum are nine 64-bit and three
-// other operations (33 million of them, 66 MB of logits, 24 us).
+// Bound by vector issue: 19 instructions an entry, nine 64-bit and three others of them for its exponential
+// and the sum.  33 million entries, 66 MB of logits, take 24 to 27 us: the compute units hold waves for some
+// 20 of them, and their vector units are busy for 81% of that (LDS, with its conflicts, for 28%).
 
 #include <hip/hip_runtime.h>
 #include <math.h>
