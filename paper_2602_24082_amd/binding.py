@@ -914,14 +914,18 @@ class Cache:
         self.ref = ctypes.byref(self._desc)
         self._sizes = {}
 
+    _FIXED = frozenset(("page_table", "seq_len", "held", "refs", "num_pages", "page_size", "device", "index", "_desc", "ref"))
+
     def __setattr__(self, name, value):
         # (`cache.seq_len += 1` sets the same tensor again)
-        if name in self.__dict__ and self.__dict__[name] is not value:
+        if name in self._FIXED and self.__dict__.get(name, value) is not value:
             raise AttributeError(f"a Cache's {name} cannot be replaced (tensors can be changed in place: {name}.copy_(..))")
         object.__setattr__(self, name, value)
 
     def __delattr__(self, name):
-        raise AttributeError(f"a Cache's {name} cannot be deleted")
+        if name in self._FIXED:
+            raise AttributeError(f"a Cache's {name} cannot be deleted")
+        object.__delattr__(self, name)
 
     def _ws_size(self, name: str, *args) -> int:
         """Workspace bytes, kept (they follow from the sizes)."""

@@ -46,6 +46,14 @@ def test_a_cache_keeps_its_sizes(monkeypatch, name, value):
         setattr(c, name, value)
 
 
+def test_a_cache_takes_a_callers_own_attributes(monkeypatch):
+    c = _cache(monkeypatch)
+    c.step = 1
+    c.step = 2
+    del c.step
+    assert not hasattr(c, "step")
+
+
 @pytest.mark.parametrize("given,want", [({}, 1), ({"parents": True}, 6), ({"parents": True, "max_children": 2}, 2), ({"max_children": 3}, 3)])
 def test_children_of_a_tree_are_all_tried_unless_said_otherwise(monkeypatch, given, want):
     seen = []
