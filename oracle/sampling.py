@@ -125,8 +125,10 @@ class Book:
 
     def accept(self, slots, count, path=None, max_new=1 << 30):
         bad = 0
-        for i, s, fine in self._entries([s if count[i] else -1 for i, s in enumerate(slots)]):
+        for i, s, fine in self._entries(slots):
             m = int(count[i])
+            if m == 0:  # (also the entry by which a slot counts that is named again)
+                continue
             fine = fine and 0 < m <= max_new and self.sound(s)
             nodes = [int(x) for x in path[i][:m]] if fine and path is not None else list(range(m))
             fine = fine and all(b > a for a, b in zip([-1] + nodes, nodes)) and max(nodes) < max_new

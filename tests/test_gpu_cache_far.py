@@ -42,3 +42,12 @@ def test_positions_past_2_20(d, length):
             # cos and sin to 2^-23 (an angle rounded to fp32, a series in it), products and their sum
             assert (np.abs(got - want) <= size * (angle + 6 * 2.0 ** -24) + 2.0 ** -24 * np.abs(want)).all(), (j, np.abs(got - want).max())
         np.testing.assert_array_equal(vp[page, :, row].cpu().numpy(), v[0, j].numpy())
+
+
+def test_accept_goes_by_a_slots_first_entry():
+    """Also where that one keeps nothing."""
+    c = pp.Cache(ints(np.zeros((3, 2))), ints([4, 4, 4]), ints([1, 1, 1]), ints(np.zeros(4)), 16)
+    slots, count = [0, 0, 1, 9, -1], [0, 3, 2, 0, 5]
+    b = smp.Book(np.zeros((3, 2)), [4, 4, 4], [1, 1, 1], np.zeros(4), 16)
+    assert pp.pp_cache_accept(c, ints(slots), ints(count)).tolist() == b.accept(slots, count) == [0, 1]
+    assert c.seq_len.tolist() == b.len.tolist() == [4, 6, 4]

@@ -1,8 +1,11 @@
-"""CPU tests of the sampling operators' largest sizes: what no launch can take is refused ahead of the first."""
+"""CPU tests of the sampling operators' largest sizes: what no launch can take is refused ahead of the first; and of which entry of
+a call counts."""
 import ctypes
 
+import numpy as np
 import pytest
 
+from oracle import sampling as smp
 from paper_2602_24082_amd import binding as pp
 
 OK = ctypes.c_void_p(4096)
@@ -27,3 +30,10 @@ def test_rows_that_the_join_cannot_launch(d, n, nodes, hq, status):
     assert _tree(n, nodes, hq, d) == status
     size = ctypes.c_size_t(0)
     assert pp.lib().pp_tree_workspace_size(ctypes.byref(DESC), n, 1, nodes, pp.PP_BF16, hq, 1, d, ctypes.byref(size)) == (3 if status == 3 else 0)
+
+
+def test_oracle_accepts_by_a_slots_first_entry():
+    """A slot named twice counts by its first entry, also where that one keeps nothing."""
+    b = smp.Book(np.zeros((3, 2)), [4, 4, 4], [1, 1, 1], np.zeros(4), 16)
+    assert b.accept([0, 0, 1, 9, -1], [0, 3, 2, 0, 5]) == [0, 1]
+    assert b.len.tolist() == [4, 6, 4]

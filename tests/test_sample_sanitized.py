@@ -21,4 +21,4 @@ def test_sampling_host_tests_pass_under_asan_and_ubsan(tmp_path):
                        env=env, capture_output=True, text=True, cwd=ROOT, timeout=900)
     out = r.stdout[-4000:] + r.stderr[-4000:]
     assert r.returncode == 0, out
-    assert "9 passed" in r.stdout and "runtime error" not in out and "AddressSanitizer" not in out, out
+    assert "10 passed" in r.stdout and "runtime error" not in out and "AddressSanitizer" not in out, out
