@@ -639,7 +639,7 @@ pp_status pp_tree_attn_fwd(const pp_cache* cache, int n, const int32_t* slots, i
  * samples the token that follows; with max_new 1 it is plain sampling.
  * Of a sequence's count[i] (dev; NULL: max_new; 0: left out) nodes node 0 is its last token
  * and the others, tokens (dev int32 [n, max_new]), were drafted as a tree (parents as for
- * the attention; a node without a parent is never reached).  target (dev [n, max_new,
+ * the attention; a node whose parent is no earlier node is never reached).  target (dev [n, max_new,
  * vocab], dtype) are the model's logits at the nodes, p = softmax(target / T), draft (dev,
  * same shape) the drafter's from which the children of a node were drawn, q; T =
  * temperature[i] (dev; NULL: 1; taken as at most 10^6).

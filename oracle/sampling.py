@@ -238,7 +238,7 @@ def verify(target, tokens, u, draft=None, parents=None, count=None, temperature=
                 step, tried = None, 0
                 for j in range(1, c):
                     up = j - 1 if parents is None else int(parents[i][j])
-                    if up != at or not usable or tried >= max_children:
+                    if up != at or up >= j or not usable or tried >= max_children:
                         continue
                     tried += 1
                     y = int(tokens[i, j])

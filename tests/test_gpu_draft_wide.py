@@ -120,3 +120,18 @@ def test_all_children_of_a_tree_by_default(drafted):
     got, want = pp.pp_verify_draft(*args), pp.pp_verify_draft(*args, max_children=4)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     assert not drafted or (got[2][:, 1] > 1).any()  # a later child follows
+
+
+@pytest.mark.parametrize("drafted", [True, False])
+def test_nodes_whose_parent_is_no_earlier_one(drafted):
+    """They are never reached, nor what hangs from them; the others are as they would be without."""
+    target, tokens, u, draft, _ = case(30, 6, 60, torch.float32, 31, drafted, near=0.3)
+    u[:, 1:] = 0.01
+    for parents in ([-1, 0, 4, 2, 0, 3], [-1, 1, 0, 0, 9, 2], [5, 0, 1, -7, 3, 2**31 - 1], [-1, -1, 0, 3, 2, 4]):
+        out = check(target, tokens, u, draft, [parents] * 30, max_children=5)
+        kept = set(out[2].ravel().tolist()) - {-1}
+        reach = {0}
+        for j in range(1, 6):
+            if 0 <= parents[j] < j and parents[j] in reach:
+                reach.add(j)
+        assert kept <= reach and (not drafted or len(kept) > 1)
